@@ -258,7 +258,7 @@ def _plain_scan(s):
     out = {"y": h.to(dt), "last": last}
     if case["mode"] == "forward":
         return out
-    g = s["dy"].float()
+    g = s["dy"].float().clone()
     g[end] += s["dlast"][full]
     a = torch.cat([f[1:], torch.zeros_like(f[:1])])  # the gate between a row and the next one
     a[end] = 0
