@@ -491,6 +491,140 @@ int tbe_plan_placement(const tbe_place_table *tables, int32_t num_tables, const 
                        int32_t num_mems, int64_t max_nodes, int32_t *h_memory_of_table, double *h_time,
                        int32_t *h_optimal);
 
+/*
+ * ---- Operators beside the embedding path ----
+ *
+ * What a model needs that trains on histories of looked-up rows: a pooling that keeps the order of a bag's rows
+ * (tbe_scan_*), a learned table looked up by the bucket of a distance between two rows of a history (tbe_bias_*), and
+ * the step of the dense weights (tbe_adamw_*).  The conventions above hold: pointers d_* are device memory of the
+ * caller's, h_* host memory; a call enqueues on the stream it is given (which may be capturing a graph) and returns
+ * without waiting (the *_create, *_destroy and tbe_scan_check calls wait); scratch memory is the handle's, allocated in
+ * *_create, so calls of one handle on several streams, and replays of graphs that hold some, have to be ordered by the caller;
+ * errors are returned as codes, their text is tbe_last_error(NULL).  A handle is used from one host thread at a time and on
+ * the GPU it was created on (TBE_EORDER).  Rows and scores may be TBE_FP32, TBE_FP16 or TBE_BF16; sums, states and
+ * statistics are fp32, and what is stored in 16 bits is rounded to nearest even, once.  Strides are in elements.
+ */
+#define TBE_BF16 2 /* rows, scores, parameters and gradients of the operators below (not of embedding tables) */
+
+/*
+ * Gated linear recurrence over the rows of every bag.  With f = 1 / (1 + exp(-u)), element by element,
+ *   h_t = f_t h_{t-1} + (1 - f_t) x_t   (coupled = 1)   or   h_t = f_t h_{t-1} + x_t   (coupled = 0)
+ * for the rows t = offsets[b] .. offsets[b+1]-1 of bag b in turn, from h = d_h0[b] (null: zero).
+ * dim: elements of a row, 1 .. 65536; max_bags, max_rows: what a call may bring at most.
+ */
+typedef struct tbe_scan_t *tbe_scan_handle;
+int tbe_scan_create(tbe_scan_handle *out, int32_t dim, int32_t dtype, int32_t coupled, int64_t max_bags,
+                    int64_t max_rows);
+int tbe_scan_destroy(tbe_scan_handle s);
+
+/* fp32 numbers that tbe_scan_forward leaves in d_saved for the backward of `rows` rows (a negative code on error) */
+int64_t tbe_scan_saved_floats(tbe_scan_handle s, int64_t rows);
+
+/*
+ * d_x, d_u: rows of dim elements, x_stride / u_stride apart; d_offsets[bags + 1] ascending from 0 to rows; d_h0: fp32
+ * rows h0_stride apart (0: one row for all bags) or null.  Writes, each unless null: d_y (h of every row), d_last (fp32
+ * [bags, dim], h after a bag's last row; that of an empty bag is where it starts), d_saved (for tbe_scan_backward).
+ */
+int tbe_scan_forward(tbe_scan_handle s, const void *d_x, int64_t x_stride, const void *d_u, int64_t u_stride,
+                     const int64_t *d_offsets, int64_t bags, int64_t rows, const float *d_h0, int64_t h0_stride, void *d_y,
+                     int64_t y_stride, float *d_last, float *d_saved, void *stream);
+
+/*
+ * The gradient of the same call: d_dy (rows' gradient) and d_dlast (fp32 [bags, dim]), either may be null = zero, to d_dx, d_du and,
+ * unless null, d_dh0 (fp32 [bags, dim]: a bag's own, also where d_h0 is one row for all).  d_saved: what that forward wrote.
+ *   g_t = dy_t + f_{t+1} g_{t+1} (the last row of a bag: dy_t + dlast_b),  dx_t = (1 - f_t) g_t  or  g_t,
+ *   du_t = f_t (1 - f_t) g_t (h_{t-1} - x_t)  or  f_t (1 - f_t) g_t h_{t-1},  dh0_b = f_first g_first.
+ */
+int tbe_scan_backward(tbe_scan_handle s, const void *d_x, int64_t x_stride, const void *d_u, int64_t u_stride,
+                      const int64_t *d_offsets, int64_t bags, int64_t rows, const float *d_h0, int64_t h0_stride,
+                      const float *d_saved, const void *d_dy, int64_t dy_stride, const float *d_dlast, void *d_dx,
+                      int64_t dx_stride, void *d_du, int64_t du_stride, float *d_dh0, void *stream);
+
+/*
+ * One more row for `rows` of the `slots` states d_state (fp32 rows of dim elements, state_stride apart), in place:
+ *   state[d_slots[i]] = f_i state[d_slots[i]] + ...  (as above),  y_i = the new state  (d_y may be null).
+ * d_slots null: row i belongs to state i.  A negative slot leaves its row out (y_i = 0).  A slot twice in one call: undefined
+ * which of its rows the state keeps.
+ */
+int tbe_scan_step(tbe_scan_handle s, float *d_state, int64_t state_stride, int64_t slots, const int64_t *d_slots,
+                  const void *d_x, int64_t x_stride, const void *d_u, int64_t u_stride, int64_t rows, void *d_y,
+                  int64_t y_stride, void *stream);
+
+/* Waits for the stream and returns TBE_EINVAL if a call since the last check had offsets that do not ascend from 0 to
+ * rows, TBE_ERANGE if a slot was not below `slots` (its row was left out).  Outputs of such a call are undefined, memory outside them is not touched. */
+int tbe_scan_check(tbe_scan_handle s, void *stream);
+
+/*
+ * Learned bias by the bucket of a distance.  For a query at position q and a key at position k the distance is
+ *   bidirectional = 0:  max(q - k, 0);    bidirectional = 1:  |q - k|, keys with k > q counted apart,
+ * its bucket is the number of h_thresholds (ascending, from 1 up) that it reaches, plus num_thresholds + 1 where counted
+ * apart.  A table holds a row of `heads` numbers for each of the (num_thresholds + 1) * (1 or 2) buckets.
+ * num_thresholds: 0 .. 127; heads 1 .. 4096.
+ */
+typedef struct tbe_bias_t *tbe_bias_handle;
+int tbe_bias_create(tbe_bias_handle *out, int32_t heads, const int64_t *h_thresholds, int32_t num_thresholds,
+                    int32_t bidirectional);
+int tbe_bias_destroy(tbe_bias_handle s);
+
+/* Scores [batch, heads, queries, keys]: the keys of a query side by side, the other strides free. */
+typedef struct {
+  int64_t batch, queries, keys;
+  int64_t query_offset;          /* query i is at position query_offset + i, key j at j, unless given by: */
+  const int64_t *d_query_pos;    /* [batch, queries], samples query_pos_stride apart (0: one for all), or null */
+  const int64_t *d_key_pos;      /* [batch, keys], samples key_pos_stride apart (0: one for all), or null */
+  int64_t query_pos_stride, key_pos_stride;
+  const int64_t *d_key_lengths;  /* [batch]: keys from this index on are masked, or null */
+  int32_t causal;                /* 1: keys at later positions than the query are masked */
+  int32_t dtype;                 /* of scores, output and gradient */
+} tbe_bias_shape;
+typedef struct {
+  int64_t sample, head, query;
+} tbe_bias_strides;
+
+/* d_out = d_scores * scale + table[bucket] (d_scores null: the table's value alone), mask_value where masked whatever the
+ * scores hold there.  d_table: [buckets, heads] of table_dtype.  d_out may be d_scores. */
+int tbe_bias_forward(tbe_bias_handle s, const tbe_bias_shape *shape, const void *d_table, int32_t table_dtype,
+                     const void *d_scores, const tbe_bias_strides *scores_strides, float scale, float mask_value, void *d_out,
+                     const tbe_bias_strides *out_strides, void *stream);
+
+/* d_dtable (fp32 [buckets, heads], or null) = sums of d_dout over everything unmasked, by bucket and head; the same inputs give the
+ * same bits.  d_dscores (or null) = d_dout * scale, 0 where masked; it may be d_dout.  What d_dout holds at masked places has
+ * no influence. */
+int tbe_bias_backward(tbe_bias_handle s, const tbe_bias_shape *shape, const void *d_dout,
+                      const tbe_bias_strides *dout_strides, float *d_dtable, float scale, void *d_dscores,
+                      const tbe_bias_strides *dscores_strides, void *stream);
+
+/*
+ * AdamW step of many tensors in one launch (one for every 256 tensors).  For every element, with g = gradient * grad_scale,
+ *   m = beta1 m + (1 - beta1) g,   v = beta2 v + (1 - beta2) g g,
+ *   w = w (1 - lr weight_decay) - lr / (1 - beta1^step) * m / (sqrt(v) / sqrt(1 - beta2^step) + eps)
+ * where w is the fp32 master copy if there is one, and the parameter is w rounded to its type.
+ * state_bits 32: m, v are fp32.  state_bits 8: m and sqrt(v) are 8-bit numbers (E4M3: 4 exponent bits, 3 mantissa bits,
+ * largest 448) times a scale for each TBE_ADAMW_BLOCK elements, the block's largest / 448.  Between two codes the upper is taken
+ * with the probability that keeps the expected value, by 16 bits of a hash of (seed, step, tensor, element), so the same call
+ * gives the same bits and moving averages do not stick between codes.  sqrt(v) above zero never becomes zero.  A block that holds an
+ * infinity or a NaN reads back as NaN.
+ */
+#define TBE_ADAMW_BLOCK 256
+typedef struct {
+  void *d_param;          /* numel elements of param_dtype, contiguous */
+  float *d_master;        /* fp32 copy of the parameter, or null */
+  void *d_m, *d_v;        /* states: fp32, or bytes for state_bits 8 */
+  float *d_m_scale, *d_v_scale; /* state_bits 8: a scale for each TBE_ADAMW_BLOCK elements, the last block may be short */
+  int64_t numel;
+  int32_t param_dtype, grad_dtype;
+  double weight_decay;
+} tbe_adamw_tensor;
+typedef struct tbe_adamw_t *tbe_adamw_handle;
+int tbe_adamw_create(tbe_adamw_handle *out, const tbe_adamw_tensor *h_tensors, int32_t num_tensors, int32_t state_bits);
+int tbe_adamw_destroy(tbe_adamw_handle s);
+
+/* h_grads: HOST array of num_tensors device pointers (null: that tensor is left as it is).  step: 1 for the first one.
+ * d_grad_scale: one fp32 number in device memory that all gradients are multiplied by (a clipping factor, one over a loss
+ * scale), or null. */
+int tbe_adamw_step(tbe_adamw_handle s, const void *const *h_grads, int64_t step, double lr, double beta1, double beta2,
+                   double eps, uint32_t seed, const float *d_grad_scale, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

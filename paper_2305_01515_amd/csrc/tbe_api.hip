@@ -11,6 +11,7 @@
 #include <vector>
 
 #include "../../include/tbe.h"
+#include "tbe_dense.h"
 #include "tbe_internal.h"
 
 using namespace tbe;
@@ -543,6 +544,14 @@ int do_prefetch(tbe_ctx *h, const int64_t *d_indices, const int64_t *d_offsets, 
 }
 
 }  // namespace
+
+int tbe::report(int code, const char *text) noexcept {
+  try {
+    g_create_error = text;
+  } catch (...) {  // no memory for the text: the code is told all the same
+  }
+  return code;
+}
 
 extern "C" {
 

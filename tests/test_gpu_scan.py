@@ -1,0 +1,322 @@
+"""The gated recurrence over bags against its formula in 64 bits, row by row.
+
+Bars.  eps = 2^-24.  A gate is off by (|u| + 8) eps of itself at most: the rounding of u log2(e) is |u| eps of exp(u), the
+exponential, the sum and the quotient some ulps each.  One row adds twice that (the products and sums of whatever order the
+rows are joined in) of f |h| + i |x| to the error of h, and carries the error before it on by f: the bar follows the same
+recurrence.  So does that of g with |dy|.  A result stored in 16 bits adds half an ulp of its own."""
+import numpy as np
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+EPS = 2.0 ** -24
+TYPES = {"f32": (torch.float32, EPS), "f16": (torch.float16, 2.0 ** -11), "bf16": (torch.bfloat16, 2.0 ** -8)}
+
+
+def reference(x, u, lengths, h0, dy, dlast, coupled):
+    """numpy float64; every result with its bar (before the rounding to the type of the rows)"""
+    n, d = x.shape
+    f, i = 1 / (1 + np.exp(-u)), 1 / (1 + np.exp(u))
+    w = i if coupled else np.ones_like(i)
+    c = 2 * (np.abs(u) + 8) * EPS
+    h, eh, g, eg = (np.zeros((n, d)) for _ in range(4))
+    before, eb = np.zeros((n, d)), np.zeros((n, d))
+    bags = len(lengths)
+    last, el, dh0, e0 = (np.zeros((bags, d)) for _ in range(4))
+    off = np.concatenate([[0], np.cumsum(lengths)])
+    for b in range(bags):
+        s, e = h0[b].copy(), np.zeros(d)
+        for t in range(off[b], off[b + 1]):
+            before[t], eb[t] = s, e
+            s, e = f[t] * s + w[t] * x[t], f[t] * e + c[t] * (f[t] * np.abs(s) + w[t] * np.abs(x[t]))
+            h[t], eh[t] = s, e
+        last[b], el[b] = s, e
+        s, m, e = dlast[b].copy(), np.abs(dlast[b]), np.zeros(d)  # what the row before gets, its magnitude, its error
+        for t in range(off[b + 1] - 1, off[b] - 1, -1):
+            g[t], eg[t] = dy[t] + s, e + EPS * (np.abs(dy[t]) + m)
+            m = f[t] * (np.abs(dy[t]) + m)
+            s, e = f[t] * g[t], f[t] * eg[t] + c[t] * m
+        dh0[b], e0[b] = s, e
+    diff = before - x if coupled else before
+    ed = eb + EPS * (np.abs(before) + np.abs(x))
+    out = {"y": (h, eh), "last": (last, el), "dx": (w * g, w * (eg + c * np.abs(g))),
+           "du": (g * diff * f * i, f * i * (eg * np.abs(diff) + np.abs(g) * ed + 3 * c * np.abs(g * diff))), "dh0": (dh0, e0)}
+    return out
+
+
+def near(name, got, want, half_ulp, tiny):
+    value, bar = want
+    off = np.abs(got.double().cpu().numpy() - value)
+    limit = bar + half_ulp * (np.abs(value) + bar) + tiny
+    assert (off <= limit).all(), f"{name}: {np.max(off / limit):.3g} of its bar at {np.unravel_index(np.argmax(off / limit), off.shape)}"
+
+
+def inputs(lengths, dim, dtype, h0, seed, spread=2.0):
+    g = torch.Generator().manual_seed(seed)
+    n, bags, dt = int(sum(lengths)), len(lengths), TYPES[dtype][0]
+    x, u, dy = (torch.randn(n, dim, generator=g).to(dt) for _ in range(3))
+    u = (u.float() * spread + 1.5).to(dt)
+    start = {"none": None, "own": torch.randn(bags, dim, generator=g), "one": torch.randn(1, dim, generator=g).expand(bags, dim)}[h0]
+    off = torch.tensor(np.concatenate([[0], np.cumsum(lengths)]), dtype=torch.int64)
+    return x, u, dy, torch.randn(bags, dim, generator=g), start, off
+
+
+def f64(t):
+    return t.double().numpy()
+
+
+def run_and_compare(lengths, dim, dtype, coupled, h0="none", seed=0, layout="plain", spread=2.0):
+    from paper_2305_01515_amd.dense import Scan
+    x, u, dy, dlast, start, off = inputs(lengths, dim, dtype, h0, seed, spread)
+    n, bags = x.shape[0], len(lengths)
+    want = reference(f64(x), f64(u), lengths, f64(start) if start is not None else np.zeros((bags, dim)), f64(dy), f64(dlast), coupled)
+    cu = lambda t: None if t is None else t.cuda()  # noqa: E731
+    xs, us, dys = cu(x), cu(u), cu(dy)
+    if layout == "halves":  # gates and rows as the two halves of one projection
+        both = torch.cat([us, xs], 1)
+        us, xs = both[:, :dim], both[:, dim:]
+    if layout == "shifted":  # rows that begin one element after an aligned address
+        def shift(t):
+            wide = torch.zeros(n * (dim + 1) + 1, dtype=t.dtype, device="cuda")
+            v = wide[1:].view(n, dim + 1)[:, :dim]
+            v.copy_(t)
+            return v
+        xs, us, dys = shift(xs), shift(us), shift(dys)
+    s0 = None if start is None else start[:1].cuda().expand(bags, dim) if h0 == "one" else start.cuda()
+    plan = Scan(dim, x.dtype, max_bags=bags, max_rows=n, coupled=coupled)
+    o = off.cuda()
+    y, last, saved = plan.forward(xs, us, o, s0, save=True)
+    dx, du, dh0 = plan.backward(xs, us, o, saved, dys, dlast.cuda(), s0)
+    plan.check()
+    half = TYPES[dtype][1] if dtype != "f32" else 0.0
+    tiny = {"f32": 0.0, "f16": 2.0 ** -25, "bf16": 0.0}[dtype] + 1e-37
+    for name, got in (("y", y), ("dx", dx), ("du", du)):
+        near(name, got, want[name], half, tiny)
+    near("last", last, want["last"], 0.0, 1e-37)
+    if s0 is not None:
+        near("dh0", dh0, want["dh0"], 0.0, 1e-37)
+    else:
+        assert dh0 is None
+    return plan, (xs, us, o, s0, dys, dlast.cuda()), (y, last, saved, dx, du, dh0)
+
+
+RAGGED = [0, 1, 3, 0, 0, 17, 64, 63, 65, 2, 127, 128, 129, 0, 31, 255, 257, 1, 1, 0]
+
+
+@pytest.mark.parametrize("coupled", [True, False])
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("dim,layout,h0", [(64, "plain", "own"), (128, "halves", "none"), (100, "plain", "one"), (7, "plain", "own"), (1, "plain", "none"),
+                                           (33, "halves", "own"), (16, "shifted", "one"), (320, "plain", "none"), (8, "plain", "own")])
+def test_ragged_bags(dim, layout, h0, dtype, coupled):
+    run_and_compare(RAGGED, dim, dtype, coupled, h0, seed=dim, layout=layout)
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("lengths", [[5000], [1], [0], [0, 0, 0], [1] * 700, [0] * 600 + [3] + [0] * 600, [1500, 0, 2500, 1], [2048, 2048], [256] * 9,
+                                     [1, 4095], [4095, 1], [700, 1, 700, 1, 700]], ids=lambda v: f"{len(v)}x{max(v)}")
+def test_lengths(lengths, dtype):
+    run_and_compare(lengths, 24, dtype, True, "own", seed=len(lengths))
+    run_and_compare(lengths, 40, dtype, False, "none", seed=len(lengths) + 1)
+
+
+@pytest.mark.parametrize("coupled", [True, False])
+def test_gates_that_never_forget_or_remember(coupled):
+    """u far out: f is 1 or 0 to the last bit, exp(-u) beyond the range of fp32"""
+    from paper_2305_01515_amd.dense import Scan
+    n, d = 600, 32
+    g = torch.Generator().manual_seed(3)
+    x = torch.randn(n, d, generator=g)
+    for value, f in ((200.0, 1.0), (-200.0, 0.0), (float("inf"), 1.0), (float("-inf"), 0.0)):
+        plan = Scan(d, torch.float32, 1, n, coupled=coupled)
+        u, off, h0 = torch.full((n, d), value).cuda(), torch.tensor([0, n]).cuda(), torch.ones(1, d).cuda()
+        y, last, saved = plan.forward(x.cuda(), u, off, h0, save=True)
+        dx, du, dh0 = plan.backward(x.cuda(), u, off, saved, torch.ones(n, d).cuda(), None, h0)
+        w = (1 - f) if coupled else 1.0
+        want = torch.ones(n, d) * f + w * (x.double().cumsum(0) if f else x.double())
+        assert torch.allclose(y.cpu().double(), want, rtol=0, atol=n * 2 * EPS * float(x.double().cumsum(0).abs().max() + 1))
+        assert torch.equal(du.cpu(), torch.zeros(n, d))
+        assert torch.equal(dx.cpu(), (torch.arange(n, 0, -1.0)[:, None].expand(n, d) if f else torch.ones(n, d)) * w)
+        assert torch.equal(dh0.cpu(), torch.full((1, d), n * f))
+
+
+def test_optional_outputs_and_inputs():
+    """no y, no gradient of y, none of the last rows: what is left is as with them"""
+    plan, (x, u, off, h0, dy, dlast), (y, last, saved, *_rest) = run_and_compare(RAGGED, 64, "bf16", True, "own", seed=9)
+    y2, last2, none = plan.forward(x, u, off, h0, want_y=False)
+    assert y2 is None and none is None and torch.equal(last, last2)
+    only_y = plan.backward(x, u, off, saved, dy, None, h0)
+    with_zero = plan.backward(x, u, off, saved, dy, torch.zeros_like(dlast), h0)
+    only_last = plan.backward(x, u, off, saved, None, dlast, h0)
+    zero_y = plan.backward(x, u, off, saved, torch.zeros_like(dy), dlast, h0)
+    for a, b in zip(only_y + only_last, with_zero + zero_y):
+        assert torch.equal(a, b)
+
+
+def test_same_bits_again_and_on_another_stream():
+    lengths = [3000, 1, 0, 4000, 17]
+    plan, (x, u, off, h0, dy, dlast), outs = run_and_compare(lengths, 72, "f32", False, "own", seed=4)
+    for k in range(4):
+        side = torch.cuda.Stream() if k % 2 else torch.cuda.current_stream()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            y, last, saved = plan.forward(x, u, off, h0, save=True)
+            grads = plan.backward(x, u, off, saved, dy, dlast, h0)
+        torch.cuda.current_stream().wait_stream(side)
+        for a, b in zip(outs, (y, last, saved, *grads)):
+            assert torch.equal(a, b)
+
+
+def test_gradient_against_differences():
+    """d(loss) along a random direction of x, u and h0 against central differences of the forward in fp32: step 2^-6, so that
+    the third derivative's share is below 1e-3 of the gradient here and fp32's rounding below 1e-4"""
+    from paper_2305_01515_amd.dense import Scan
+    lengths, d = [5, 0, 40, 9], 16
+    x, u, dy, dlast, h0, off = inputs(lengths, d, "f32", "own", seed=11, spread=1.0)
+    plan = Scan(d, torch.float32, len(lengths), sum(lengths))
+    ps = [t.cuda().requires_grad_() for t in (x, u, h0)]
+    loss = lambda a, b, c: sum((o.double() * w.cuda().double()).sum() for o, w in zip(plan(a, b, off.cuda(), c), (dy, dlast)))  # noqa: E731
+    loss(*ps).backward()
+    for k, p in enumerate(ps):
+        way = torch.randn(p.shape, generator=torch.Generator().manual_seed(k)).cuda()
+        with torch.no_grad():
+            args = lambda s: [q + s * way if j == k else q for j, q in enumerate(ps)]  # noqa: E731
+            diff = (loss(*args(2.0 ** -6)) - loss(*args(-2.0 ** -6))) / 2.0 ** -5
+        want = (p.grad.double() * way.double()).sum()
+        scale = (p.grad.double() * way.double()).norm() + want.abs()
+        assert abs(float(diff - want)) < 2e-3 * float(scale)
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("dim,rows,slots", [(64, 7, 64), (1, 1, 1), (100, 33, 40), (256, 1000, 1500), (37, 5, 9)])
+@pytest.mark.parametrize("coupled", [True, False])
+def test_step(dim, rows, slots, dtype, coupled):
+    from paper_2305_01515_amd.dense import Scan
+    g = torch.Generator().manual_seed(dim)
+    dt, half = TYPES[dtype]
+    x, u, state = torch.randn(rows, dim, generator=g).to(dt), (torch.randn(rows, dim, generator=g) * 2).to(dt), torch.randn(slots, dim, generator=g)
+    slot = torch.randperm(slots, generator=g)[:rows]
+    slot[::5] = -1
+    want, bar = f64(state).copy(), np.zeros((slots, dim))
+    y, ey = np.zeros((rows, dim)), np.zeros((rows, dim))
+    for r in range(rows):
+        if slot[r] < 0:
+            continue
+        a, b, s = f64(u)[r], f64(x)[r], want[slot[r]].copy()
+        f, i = 1 / (1 + np.exp(-a)), 1 / (1 + np.exp(a)) if coupled else np.ones(dim)
+        y[r] = want[slot[r]] = f * s + i * b
+        ey[r] = bar[slot[r]] = 2 * (np.abs(a) + 8) * EPS * (f * np.abs(s) + i * np.abs(b))
+    plan = Scan(dim, dt, rows, rows, coupled=coupled)
+    st = state.cuda()
+    got = plan.step(st, x.cuda(), u.cuda(), slot.cuda())
+    near("state", st, (want, bar), 0.0, 1e-37)
+    near("y", got, (y, ey), half if dtype != "f32" else 0.0, 2.0 ** -25 if dtype == "f16" else 1e-37)
+    st2 = state.cuda()
+    every = plan.step(st2, x.cuda(), u.cuda())  # the first states, in order
+    again, last, _ = Scan(dim, dt, rows, rows, coupled=coupled).forward(x.cuda(), u.cuda(), torch.arange(rows + 1).cuda(), state[:rows].cuda())
+    assert (every.float() - again.float()).abs().max() <= 2 * half * again.float().abs().max() + 1e-6
+    assert torch.equal(st2[rows:].cpu(), state[rows:])
+    plan.check()
+
+
+def test_step_continues_a_forward():
+    from paper_2305_01515_amd.dense import Scan
+    x, u, *_ = inputs([40], 48, "bf16", "none", seed=2)
+    plan = Scan(48, torch.bfloat16, 1, 40)
+    whole, last, _ = plan.forward(x.cuda(), u.cuda(), torch.tensor([0, 40]).cuda())
+    _, state, _ = plan.forward(x[:37].cuda(), u[:37].cuda(), torch.tensor([0, 37]).cuda())
+    for t in range(37, 40):
+        y = plan.step(state, x[t:t + 1].cuda(), u[t:t + 1].cuda())
+    assert (y.float() - whole[-1:].float()).abs().max() <= 2.0 ** -7 * whole[-1:].float().abs().max()
+    assert torch.allclose(state, last, rtol=1e-5, atol=1e-6)
+
+
+def test_graph_replays():
+    """captured once, replayed with other inputs in the same buffers, each time equal to the eager call"""
+    from paper_2305_01515_amd.dense import Scan
+    lengths, d = [900, 1, 0, 1400, 30], 64
+    plan = Scan(d, torch.float32, len(lengths), sum(lengths))
+    x, u, dy, dlast, h0, off = [t.cuda() for t in inputs(lengths, d, "f32", "own", seed=1)]
+
+    def both():
+        y, last, saved = plan.forward(x, u, off, h0, save=True)
+        return (y, last, *plan.backward(x, u, off, saved, dy, dlast, h0))
+    both()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        outs = both()
+    for k in range(4):
+        for t, new in zip((x, u, dy, dlast, h0), inputs(lengths, d, "f32", "own", seed=20 + k)):
+            t.copy_(new)
+        graph.replay()
+        torch.cuda.synchronize()
+        kept = [t.clone() for t in outs]
+        for a, b in zip(kept, both()):
+            assert torch.equal(a, b)
+
+
+def test_refusals():
+    from paper_2305_01515_amd.dense import Scan
+    from paper_2305_01515_amd.tbe import TbeError
+    plan = Scan(8, torch.float32, 2, 10)
+    x, off = torch.zeros(10, 8).cuda(), torch.tensor([0, 4, 10]).cuda()
+    with pytest.raises(ValueError):
+        Scan(8, torch.float64, 2, 10)
+    for bad in (dict(dim=0), dict(dim=70000), dict(max_bags=-1), dict(max_rows=-1)):
+        with pytest.raises(TbeError) as e:
+            Scan(**dict(dict(dim=8, dtype=torch.float32, max_bags=2, max_rows=10), **bad))
+        assert e.value.code == -1
+    with pytest.raises(ValueError):
+        plan.forward(x.half(), x, off)
+    with pytest.raises(ValueError):
+        plan.forward(x, x[:9], off)
+    with pytest.raises(ValueError):
+        plan.forward(x, x.t().contiguous().t(), off)
+    with pytest.raises(ValueError):
+        plan.forward(x, x, off.int())
+    with pytest.raises(TbeError) as e:  # more rows than the plan was made for
+        plan.forward(torch.zeros(11, 8).cuda(), torch.zeros(11, 8).cuda(), torch.tensor([0, 11]).cuda())
+    assert e.value.code == -5
+    with pytest.raises(TbeError) as e:
+        plan.forward(x[:1].expand(10, 8), x, off)
+    assert e.value.code == -1
+    with pytest.raises(ValueError):
+        plan.step(torch.zeros(4, 8).cuda(), x[:2], x[:2], torch.zeros(3, dtype=torch.int64).cuda())
+
+
+@pytest.mark.parametrize("offsets", [[0, 5, 3, 10], [1, 5, 7, 10], [0, 5, 7, 9], [0, 5, 7, 11], [0, -3, 7, 10], [0, 1 << 40, 7, 10]])
+def test_offsets_that_do_not_ascend_are_reported(offsets):
+    """memory outside the outputs stays as it is, the next call is as if nothing had been"""
+    from paper_2305_01515_amd.dense import Scan
+    from paper_2305_01515_amd.tbe import TbeError
+    x = torch.randn(10, 8, generator=torch.Generator().manual_seed(0)).cuda()
+    plan = Scan(8, torch.float32, 3, 10)
+    good = torch.tensor([0, 5, 7, 10]).cuda()
+    y, last, saved = plan.forward(x, x, good, save=True)
+    plan.check()
+    room = torch.full((30, 8), 7.0, device="cuda")
+    bad = torch.tensor(offsets).cuda()
+    plan.forward(x, x, bad, y=room[10:20])
+    with pytest.raises(TbeError) as e:
+        plan.check()
+    assert e.value.code == -1
+    plan.backward(x, x, bad, saved, x, None)
+    with pytest.raises(TbeError):
+        plan.check()
+    assert bool((room[:10] == 7).all()) and bool((room[20:] == 7).all())
+    y2, last2, _ = plan.forward(x, x, good)
+    plan.check()
+    assert torch.equal(y, y2) and torch.equal(last, last2)
+
+
+def test_slots_out_of_range_are_reported():
+    from paper_2305_01515_amd.dense import Scan
+    from paper_2305_01515_amd.tbe import TbeError
+    plan, x = Scan(8, torch.float32, 2, 10), torch.ones(3, 8).cuda()
+    room = torch.zeros(6, 8, device="cuda")
+    y = plan.step(room[:4], x, x, torch.tensor([1, 4, 1 << 33]).cuda())
+    with pytest.raises(TbeError) as e:
+        plan.check()
+    assert e.value.code == -2
+    assert bool((room[4:] == 0).all()) and bool((y[1:] == 0).all()) and bool((room[1] != 0).all())
+    plan.check()
