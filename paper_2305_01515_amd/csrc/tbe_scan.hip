@@ -1,5 +1,18 @@
 // Gated linear recurrence over the rows of every bag: forward, backward, one row for each of many states.
 // Contract: include/tbe.h.
+//
+// A row maps the state h to a h + b, element by element, with a = f and b = (1 - f) x (or x); where a bag starts the state
+// before does not count: a = 0, b = f h0 + ....  Two such maps, one after the other, are one again, (a2 a1, a2 b1 + b2), so the
+// rows of all bags are cut into chunks of equal length wherever the bags begin, and no bag's length matters:
+//   sum    every chunk's map, from the rows after the last start in it                       (scan_sum_kernel)
+//   join   the states before the chunks, by a scan over the chunks' maps                     (scan_join_kernel)
+//   apply  every chunk's rows from the state before it                                       (scan_apply_kernel, scan_grad_kernel)
+// One chunk needs the last one only.  The gradient runs the other way with c_t = f_t g_t = f_t (dy_t + c_{t+1}), reset where a bag
+// ends, beside the forward's states again from those before the chunks, which the forward saved.
+//
+// A row lies on L lanes of V elements (16 bytes; one element where dim is no multiple of that), a lane has R rows in a row in
+// registers, 32 elements of each input.  The maps of a wavefront's 64 / L lane groups are joined by exchange between lanes, those of
+// the workgroup's wavefronts through LDS.
 #include <cmath>
 #include <new>
 
@@ -7,75 +20,504 @@
 
 using namespace tbe;
 
-struct tbe_scan_t : DenseBase {
-  int dim = 0, dtype = 0;
-  bool coupled = false;
-  int64_t max_bags = 0, max_rows = 0;
-  int32_t *err = nullptr;  // device: 1 = bad offsets, 2 = slot out of range
-};
-
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 256, kWaves = kThreads / 64;
+constexpr int kJoinChannels = 16, kJoinSegments = 64;
 
-struct Gate {
-  float f, i;  // 1 / (1 + exp(-u)) and one less it
+// How the rows of a handle are cut: a function of dim and the type alone, because the backward uses what the forward saved.
+struct Cut {
+  int V, R, L;  // elements and rows of a lane, lanes of a row (a power of two)
+  int tiles;    // parts of L * V elements that a row has
+  int rows;     // rows of a chunk
 };
-__device__ inline Gate gate(float u) {
-  const float e = __expf(-fabsf(u)), big = 1.0f / (1.0f + e), small = e * big;
-  return u >= 0.0f ? Gate{big, small} : Gate{small, big};
+
+Cut cut_of(int dim, int dtype) {
+  Cut c;
+  const int wide = 16 / elem_bytes(dtype);
+  c.V = dim % wide ? 1 : wide;
+  c.R = 32 / c.V;
+  const int lanes = dim / c.V;
+  c.L = c.V == 1 ? 2 : 1;  // at least 2 for single elements: a chunk has 4096 rows at most
+  while (c.L < lanes && c.L < 64) c.L *= 2;
+  c.tiles = (lanes + c.L - 1) / c.L;
+  c.rows = kThreads / c.L * c.R;
+  return c;
 }
 
-// offsets ascend from 0 to rows: bags outside that are left out, and the call is reported by tbe_scan_check
-__device__ inline bool bag_rows(const int64_t *off, int64_t b, int64_t rows, int64_t &lo, int64_t &hi) {
-  lo = off[b];
-  hi = off[b + 1];
-  return lo >= 0 && lo <= hi && hi <= rows;
+// A map that does not depend on the state before it has a = -0: products with gates keep the sign, and joining maps leaves out what is
+// before (0 times an infinity or a NaN of another bag would be a NaN).
+constexpr float kReset = -0.0f;
+__device__ inline void join(float pa, float ph, float &a, float &h) {  // (pa, ph) first, then (a, h)
+  const bool reset = signbit(a);
+  h = reset ? h : a * ph + h;
+  a = reset ? a : a * pa;
 }
+__device__ inline float go(float a, float h, float s) { return signbit(a) ? h : a * s + h; }
+
+// The two gates f = 1 / (1 + exp(-u)) and 1 - f in one number: the smaller one, negative where that is 1 - f.  Each is then exact to
+// its own last bits (1 - f from a rounded f near one would not be).
+__device__ inline float gate(float u) {
+  const float e = __builtin_amdgcn_exp2f(fabsf(u) * -1.44269504f), s = e * __builtin_amdgcn_rcpf(1.0f + e);
+  return u >= 0.0f ? -s : s;
+}
+__device__ inline float keep_of(float q) { return signbit(q) ? 1.0f + q : q; }
+__device__ inline float take_of(float q) { return signbit(q) ? -q : 1.0f - q; }
 
 template <int DT>
-__global__ __launch_bounds__(kThreads) void scan_forward_kernel(const typename Elem<DT>::type *x, int64_t xs, const typename Elem<DT>::type *u,
-                                                                int64_t us, const int64_t *off, int64_t bags, int64_t rows, int dim, bool coupled,
-                                                                const float *h0, int64_t h0s, typename Elem<DT>::type *y, int64_t ys, float *last,
-                                                                float *saved, int32_t *err) {
-  const int64_t id = (int64_t)blockIdx.x * kThreads + threadIdx.x, b = id / dim;
-  const int d = (int)(id % dim);
-  if (b >= bags) return;
-  int64_t lo, hi;
-  if ((b == 0 && off[0] != 0) || (b == bags - 1 && off[bags] != rows)) *err = 1;
-  if (!bag_rows(off, b, rows, lo, hi)) { *err = 1; return; }
-  float h = h0 ? h0[b * h0s + d] : 0.0f;
-  for (int64_t t = lo; t < hi; t++) {
-    const Gate g = gate((float)u[t * us + d]);
-    h = g.f * h + (coupled ? g.i : 1.0f) * (float)x[t * xs + d];
-    if (y) y[t * ys + d] = (typename Elem<DT>::type)h;
-    if (saved) saved[t * dim + d] = h;
+struct Rows {
+  using E = typename Elem<DT>::type;
+  const E *x, *u, *dy;
+  E *y, *dx, *du;
+  int64_t xs, us, dys, ys, dxs, dus;
+  const int64_t *off;
+  const float *h0, *dlast;
+  float *last, *dh0;
+  float *maps;          // [chunks][2][dim]: a and b of the chunks
+  float *before;        // [chunks][dim]: states before the chunks
+  float *behind;        // [chunks][dim]: c behind the chunks
+  int64_t h0s, bags, rows;
+  int32_t *bag_of, *err;  // bag_of[chunks]: first bag that a chunk looks at
+  int dim, L, tiles, chunk_rows, chunks;
+  bool coupled;
+};
+
+template <class E, int V, bool ALIGNED>
+__device__ inline Pack<E, V> load_pack(const E *p) {
+  Pack<E, V> r;
+  if constexpr (ALIGNED) {
+    r = *(const Pack<E, V> *)p;
+  } else {
+#pragma unroll
+    for (int v = 0; v < V; v++) r.e[v] = p[v];
   }
-  if (last) last[b * dim + d] = h;
+  return r;
+}
+template <class E, int V, bool ALIGNED>
+__device__ inline void store_pack(E *p, const Pack<E, V> &r) {
+  if constexpr (ALIGNED) {
+    *(Pack<E, V> *)p = r;
+  } else {
+#pragma unroll
+    for (int v = 0; v < V; v++) p[v] = r.e[v];
+  }
 }
 
-template <int DT>
-__global__ __launch_bounds__(kThreads) void scan_backward_kernel(const typename Elem<DT>::type *x, int64_t xs, const typename Elem<DT>::type *u,
-                                                                 int64_t us, const int64_t *off, int64_t bags, int64_t rows, int dim, bool coupled,
-                                                                 const float *h0, int64_t h0s, const float *saved, const typename Elem<DT>::type *dy,
-                                                                 int64_t dys, const float *dlast, typename Elem<DT>::type *dx, int64_t dxs,
-                                                                 typename Elem<DT>::type *du, int64_t dus, float *dh0, int32_t *err) {
-  const int64_t id = (int64_t)blockIdx.x * kThreads + threadIdx.x, b = id / dim;
-  const int d = (int)(id % dim);
-  if (b >= bags) return;
-  int64_t lo, hi;
-  if ((b == 0 && off[0] != 0) || (b == bags - 1 && off[bags] != rows)) *err = 1;
-  if (!bag_rows(off, b, rows, lo, hi)) { *err = 1; return; }
-  float c = dlast ? dlast[b * dim + d] : 0.0f;
-  for (int64_t t = hi - 1; t >= lo; t--) {
-    const Gate g = gate((float)u[t * us + d]);
-    const float xv = (float)x[t * xs + d], before = t > lo ? saved[(t - 1) * dim + d] : h0 ? h0[b * h0s + d] : 0.0f;
-    const float gt = (dy ? (float)dy[t * dys + d] : 0.0f) + c;
-    dx[t * dxs + d] = (typename Elem<DT>::type)(coupled ? g.i * gt : gt);
-    du[t * dus + d] = (typename Elem<DT>::type)(gt * (coupled ? before - xv : before) * g.f * g.i);
-    c = g.f * gt;
+// first bag that ends at `row` or behind it (bags if none): every wavefront for itself, 64 places at a time
+__device__ inline int64_t first_bag(const int64_t *off, int64_t bags, int64_t row) {
+  const int lane = threadIdx.x & 63;
+  int64_t lo = 0, hi = bags;  // it is one of lo .. hi
+  while (lo < hi) {
+    const int64_t step = (hi - lo + 63) / 64, p = lo + (lane + 1) * step - 1;
+    const uint64_t there = __ballot(p >= hi || off[p + 1] >= row);
+    if (!there) return hi;
+    const int64_t k = __ffsll((unsigned long long)there) - 1;
+    hi = min(hi, lo + (k + 1) * step - 1);
+    lo += k * step;
   }
-  if (dh0) dh0[b * dim + d] = c;
+  return lo;
+}
+
+// Where the chunk's bags start and end: marks[2 r] is 1 + the bag that starts at row r of the chunk, marks[2 r + 1] 1 + the bag whose last
+// row that is; edge[0] is the last row with a start (0 if none), edge[1] the first with an end (the last row if none).  `empty` gets
+// the empty bags that lie in the chunk (those behind all rows: in the last chunk), a lane group each.
+template <class A, class F>
+__device__ inline void mark_bags(const A &a, int chunk, int64_t row0, int64_t from, int32_t *marks, int32_t *edge, F empty) {
+  for (int k = threadIdx.x; k < 2 * a.chunk_rows; k += kThreads) marks[k] = 0;
+  if (threadIdx.x == 0) { edge[0] = 0; edge[1] = a.chunk_rows - 1; }
+  __syncthreads();
+  const int64_t end = min(row0 + a.chunk_rows, a.rows);
+  const bool very_last = chunk == a.chunks - 1;
+  const int group = threadIdx.x / a.L, groups = kThreads / a.L, l = threadIdx.x & (a.L - 1);
+  for (int64_t b = from + group; b < a.bags; b += groups) {
+    const int64_t s = a.off[b], e = a.off[b + 1];
+    if (s >= end && !very_last) break;
+    if (s < 0 || s > e || e > a.rows) continue;  // check_offsets reports it
+    if (s == e) {
+      if (s >= row0 && (s < end || very_last)) empty(b);
+    } else if (l == 0) {
+      if (s >= row0 && s < end) {
+        marks[2 * (int)(s - row0)] = (int32_t)b + 1;
+        atomicMax(&edge[0], (int32_t)(s - row0));
+      }
+      if (e > row0 && e <= end) {
+        marks[2 * (int)(e - 1 - row0) + 1] = (int32_t)b + 1;
+        atomicMin(&edge[1], (int32_t)(e - 1 - row0));
+      }
+    }
+  }
+  __syncthreads();
+}
+
+// all offsets, once in a call
+template <class A>
+__device__ inline void check_offsets(const A &a) {
+  const int64_t id = (int64_t)blockIdx.x * kThreads + threadIdx.x, n = (int64_t)gridDim.x * kThreads;
+  for (int64_t b = id; b < a.bags; b += n)
+    if (a.off[b] > a.off[b + 1] || (b == 0 && a.off[0] != 0) || (b == a.bags - 1 && a.off[a.bags] != a.rows)) *a.err = 1;
+}
+
+// (A, H) becomes the map of all lane groups of the wavefront up to this one (BACK: from the last one down to it)
+template <int V, bool BACK>
+__device__ inline void scan_wave(float (&A)[V], float (&H)[V], int L) {
+  const int lane = threadIdx.x & 63;
+  for (int k = L; k < 64; k *= 2) {
+    const bool has = BACK ? lane + k < 64 : lane >= k;
+#pragma unroll
+    for (int v = 0; v < V; v++) {
+      const float pa = BACK ? __shfl_down(A[v], k) : __shfl_up(A[v], k), ph = BACK ? __shfl_down(H[v], k) : __shfl_up(H[v], k);
+      if (has) join(pa, ph, A[v], H[v]);
+    }
+  }
+}
+
+// The wavefronts' maps go to LDS (tot: [kWaves][2][C]); join_waves, a lane for an element, leaves there the states before (behind)
+// the wavefronts and returns that after all of them; start_of_lane goes on from there to that before (behind) the lane's rows.
+template <int V, bool BACK>
+__device__ inline void tell_wave(const float (&A)[V], const float (&H)[V], int L, float *tot) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, C = L * V, c = (lane & (L - 1)) * V;
+  if (BACK ? lane < L : lane >= 64 - L)
+#pragma unroll
+    for (int v = 0; v < V; v++) {
+      tot[(wave * 2) * C + c + v] = A[v];
+      tot[(wave * 2 + 1) * C + c + v] = H[v];
+    }
+}
+template <bool BACK>
+__device__ inline void join_waves(float *tot, int C, int c, float &A, float &s) {
+#pragma unroll
+  for (int k = 0; k < kWaves; k++) {
+    const int w = BACK ? kWaves - 1 - k : k;
+    const float wa = tot[(w * 2) * C + c], wh = tot[(w * 2 + 1) * C + c];
+    tot[(w * 2) * C + c] = s;
+    s = go(wa, wh, s);
+    A = signbit(wa) ? wa : wa * A;
+  }
+}
+template <int V, bool BACK>
+__device__ inline void start_of_lane(const float (&A)[V], const float (&H)[V], int L, const float *tot, float (&s)[V]) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, C = L * V, c = (lane & (L - 1)) * V;
+  const bool first = BACK ? lane >= 64 - L : lane < L;
+#pragma unroll
+  for (int v = 0; v < V; v++) {
+    const float w = tot[(wave * 2) * C + c + v];
+    const float pa = BACK ? __shfl_down(A[v], L) : __shfl_up(A[v], L), ph = BACK ? __shfl_down(H[v], L) : __shfl_up(H[v], L);
+    s[v] = first ? w : go(pa, ph, w);
+  }
+}
+
+// Rows behind the last one are taken for rows of zeros: nothing comes after them, and the gradient's way back from them ends at the
+// last row, where a bag ends.
+
+// Maps of the chunks: of h from x and u, BACK: of c from dy and u.
+template <int DT, int V, bool ALIGNED, bool BACK>
+__global__ __launch_bounds__(kThreads) void scan_sum_kernel(Rows<DT> a) {
+  using E = typename Elem<DT>::type;
+  constexpr int R = 32 / V;
+  extern __shared__ float lds[];
+  __shared__ int32_t edge[2];
+  const int chunk = blockIdx.x / a.tiles, tile = blockIdx.x % a.tiles, C = a.L * V;
+  int32_t *marks = (int32_t *)(lds + kWaves * 2 * C);
+  const int64_t row0 = (int64_t)chunk * a.chunk_rows, from = first_bag(a.off, a.bags, row0);
+  if (threadIdx.x == 0) a.bag_of[chunk] = (int32_t)from;  // the same from every tile
+  check_offsets(a);
+  mark_bags(a, chunk, row0, from, marks, edge, [](int64_t) {});
+  const int group = threadIdx.x / a.L, l = threadIdx.x & (a.L - 1), c0 = (tile * a.L + l) * V, r0 = group * R;
+  const int rows = (int)min((int64_t)a.chunk_rows, a.rows - row0), lo = BACK ? 0 : edge[0], hi = BACK ? min(edge[1], rows - 1) : rows - 1;
+  const E *in = BACK ? a.dy : a.x;
+  const int64_t stride = BACK ? a.dys : a.xs;
+  Pack<E, V> xv[R], uv[R];
+#pragma unroll
+  for (int j = 0; j < R; j++) {
+    const bool on = r0 + j >= lo && r0 + j <= hi && c0 < a.dim;
+    xv[j] = {};
+    uv[j] = {};
+    if (on) {
+      uv[j] = load_pack<E, V, ALIGNED>(a.u + (row0 + r0 + j) * a.us + c0);
+      if (in) xv[j] = load_pack<E, V, ALIGNED>(in + (row0 + r0 + j) * stride + c0);
+    }
+  }
+  float A[V], H[V];
+#pragma unroll
+  for (int v = 0; v < V; v++) { A[v] = 1.0f; H[v] = 0.0f; }
+#pragma unroll
+  for (int k = 0; k < R; k++) {
+    const int j = BACK ? R - 1 - k : k;
+    const int32_t bag = marks[2 * (r0 + j) + (BACK ? 1 : 0)];
+    if (bag) {
+      const float *s = BACK ? a.dlast : a.h0;
+      const int64_t at = (int64_t)(bag - 1) * (BACK ? a.dim : a.h0s) + c0;
+#pragma unroll
+      for (int v = 0; v < V; v++) {
+        A[v] = kReset;
+        H[v] = s ? s[at + v] : 0.0f;
+      }
+    }
+#pragma unroll
+    for (int v = 0; v < V; v++) {
+      const float q = gate((float)uv[j].e[v]), f = keep_of(q), x = (float)xv[j].e[v];
+      H[v] = BACK ? f * (H[v] + x) : f * H[v] + (a.coupled ? take_of(q) * x : x);
+      A[v] *= f;
+    }
+  }
+  scan_wave<V, BACK>(A, H, a.L);
+  tell_wave<V, BACK>(A, H, a.L, lds);
+  __syncthreads();
+  for (int c = threadIdx.x; c < C && tile * C + c < a.dim; c += kThreads) {
+    float A1 = 1.0f, s = 0.0f;
+    join_waves<BACK>(lds, C, c, A1, s);
+    a.maps[(int64_t)chunk * 2 * a.dim + tile * C + c] = A1;
+    a.maps[((int64_t)chunk * 2 + 1) * a.dim + tile * C + c] = s;
+  }
+}
+
+// States before the chunks (BACK: behind them) from their maps.  A workgroup has 16 elements; its lanes take 64 segments of the chunks
+// each, whose maps one wavefront for each element joins by exchange between lanes.
+template <bool BACK>
+__global__ __launch_bounds__(kJoinChannels *kJoinSegments) void scan_join_kernel(const float *maps, float *state, int chunks, int dim) {
+  __shared__ float tot[2][kJoinChannels][kJoinSegments + 1];
+  const int c = threadIdx.x % kJoinChannels, seg = threadIdx.x / kJoinChannels, d = blockIdx.x * kJoinChannels + c;
+  const int per = (chunks + kJoinSegments - 1) / kJoinSegments, k0 = min(seg * per, chunks), k1 = min(k0 + per, chunks);
+  const bool on = d < dim;
+  float A = 1.0f, H = 0.0f;
+#pragma unroll 8
+  for (int k = k0; k < k1; k++) {
+    const int64_t at = (int64_t)(BACK ? chunks - 1 - k : k) * 2 * dim + d;
+    const float a = on ? maps[at] : 1.0f, h = on ? maps[at + dim] : 0.0f;
+    H = go(a, h, H);
+    A = signbit(a) ? a : a * A;
+  }
+  tot[0][c][seg] = A;
+  tot[1][c][seg] = H;
+  __syncthreads();
+  {
+    const int w = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    float a = tot[0][w][lane], h = tot[1][w][lane];
+#pragma unroll
+    for (int k = 1; k < 64; k *= 2) {
+      const float pa = __shfl_up(a, k), ph = __shfl_up(h, k);
+      if (lane >= k) join(pa, ph, a, h);
+    }
+    const float s = __shfl_up(h, 1);
+    tot[1][w][lane] = lane ? s : 0.0f;
+  }
+  __syncthreads();
+  float s = tot[1][c][seg];
+  if (!on) return;
+#pragma unroll 8
+  for (int k = k0; k < k1; k++) {
+    const int64_t chunk = BACK ? chunks - 1 - k : k, at = chunk * 2 * dim + d;
+    state[chunk * dim + d] = s;
+    s = go(maps[at], maps[at + dim], s);
+  }
+}
+
+template <int DT, int V, bool ALIGNED>
+__global__ __launch_bounds__(kThreads) void scan_apply_kernel(Rows<DT> a) {
+  using E = typename Elem<DT>::type;
+  constexpr int R = 32 / V;
+  extern __shared__ float lds[];
+  __shared__ int32_t edge[2];
+  const int chunk = blockIdx.x / a.tiles, tile = blockIdx.x % a.tiles, C = a.L * V;
+  int32_t *marks = (int32_t *)(lds + kWaves * 2 * C);
+  const int64_t row0 = (int64_t)chunk * a.chunk_rows;
+  const int group = threadIdx.x / a.L, l = threadIdx.x & (a.L - 1), c0 = (tile * a.L + l) * V, r0 = group * R;
+  const int rows = (int)min((int64_t)a.chunk_rows, a.rows - row0);
+  const bool on = c0 < a.dim;
+  Pack<E, V> xv[R], uv[R];
+#pragma unroll
+  for (int j = 0; j < R; j++) {
+    xv[j] = {};
+    uv[j] = {};
+    if (on && r0 + j < rows) {
+      uv[j] = load_pack<E, V, ALIGNED>(a.u + (row0 + r0 + j) * a.us + c0);
+      xv[j] = load_pack<E, V, ALIGNED>(a.x + (row0 + r0 + j) * a.xs + c0);
+    }
+  }
+  if (a.chunks == 1) check_offsets(a);
+  mark_bags(a, chunk, row0, a.chunks > 1 ? a.bag_of[chunk] : 0, marks, edge, [&](int64_t b) {
+    if (a.last && on)
+#pragma unroll
+      for (int v = 0; v < V; v++) a.last[b * a.dim + c0 + v] = a.h0 ? a.h0[b * a.h0s + c0 + v] : 0.0f;
+  });
+  float q[R][V], A[V], H[V];
+#pragma unroll
+  for (int v = 0; v < V; v++) { A[v] = 1.0f; H[v] = 0.0f; }
+#pragma unroll
+  for (int j = 0; j < R; j++) {
+    const int32_t bag = marks[2 * (r0 + j)];
+    if (bag)
+#pragma unroll
+      for (int v = 0; v < V; v++) {
+        A[v] = kReset;
+        H[v] = a.h0 && on ? a.h0[(int64_t)(bag - 1) * a.h0s + c0 + v] : 0.0f;
+      }
+#pragma unroll
+    for (int v = 0; v < V; v++) {
+      q[j][v] = gate((float)uv[j].e[v]);
+      const float f = keep_of(q[j][v]), x = (float)xv[j].e[v];
+      H[v] = f * H[v] + (a.coupled ? take_of(q[j][v]) * x : x);
+      A[v] *= f;
+    }
+  }
+  scan_wave<V, false>(A, H, a.L);
+  tell_wave<V, false>(A, H, a.L, lds);
+  __syncthreads();
+  for (int c = threadIdx.x; c < C; c += kThreads) {
+    float A1 = 1.0f, s = a.chunks > 1 && tile * C + c < a.dim ? a.before[(int64_t)chunk * a.dim + tile * C + c] : 0.0f;
+    join_waves<false>(lds, C, c, A1, s);
+  }
+  __syncthreads();
+  float h[V];
+  start_of_lane<V, false>(A, H, a.L, lds, h);
+  if (!on) return;
+#pragma unroll
+  for (int j = 0; j < R; j++) {
+    const int32_t bag = marks[2 * (r0 + j)], ended = marks[2 * (r0 + j) + 1];
+    if (bag)
+#pragma unroll
+      for (int v = 0; v < V; v++) h[v] = a.h0 ? a.h0[(int64_t)(bag - 1) * a.h0s + c0 + v] : 0.0f;
+    Pack<E, V> out;
+#pragma unroll
+    for (int v = 0; v < V; v++) {
+      const float x = (float)xv[j].e[v];
+      h[v] = keep_of(q[j][v]) * h[v] + (a.coupled ? take_of(q[j][v]) * x : x);
+      out.e[v] = (E)h[v];
+    }
+    if (a.y && r0 + j < rows) store_pack<E, V, ALIGNED>(a.y + (row0 + r0 + j) * a.ys + c0, out);
+    if (ended && a.last)
+#pragma unroll
+      for (int v = 0; v < V; v++) a.last[(int64_t)(ended - 1) * a.dim + c0 + v] = h[v];
+  }
+}
+
+template <int DT, int V, bool ALIGNED>
+__global__ __launch_bounds__(kThreads) void scan_grad_kernel(Rows<DT> a) {
+  using E = typename Elem<DT>::type;
+  constexpr int R = 32 / V;
+  extern __shared__ float lds[];
+  __shared__ int32_t edge[2];
+  const int chunk = blockIdx.x / a.tiles, tile = blockIdx.x % a.tiles, C = a.L * V;
+  float *back = lds + kWaves * 2 * C;
+  int32_t *marks = (int32_t *)(back + kWaves * 2 * C);
+  const int64_t row0 = (int64_t)chunk * a.chunk_rows;
+  const int group = threadIdx.x / a.L, l = threadIdx.x & (a.L - 1), c0 = (tile * a.L + l) * V, r0 = group * R;
+  const int rows = (int)min((int64_t)a.chunk_rows, a.rows - row0);
+  const bool on = c0 < a.dim;
+  Pack<E, V> xv[R], uv[R], gv[R];
+#pragma unroll
+  for (int j = 0; j < R; j++) {
+    xv[j] = {};
+    uv[j] = {};
+    gv[j] = {};
+    if (on && r0 + j < rows) {
+      uv[j] = load_pack<E, V, ALIGNED>(a.u + (row0 + r0 + j) * a.us + c0);
+      xv[j] = load_pack<E, V, ALIGNED>(a.x + (row0 + r0 + j) * a.xs + c0);
+      if (a.dy) gv[j] = load_pack<E, V, ALIGNED>(a.dy + (row0 + r0 + j) * a.dys + c0);
+    }
+  }
+  if (a.chunks == 1) check_offsets(a);
+  mark_bags(a, chunk, row0, a.chunks > 1 ? a.bag_of[chunk] : 0, marks, edge, [&](int64_t b) {
+    if (a.dh0 && on)
+#pragma unroll
+      for (int v = 0; v < V; v++) a.dh0[b * a.dim + c0 + v] = a.dlast ? a.dlast[b * a.dim + c0 + v] : 0.0f;
+  });
+  float q[R][V], A[V], H[V], B[V], G[V];
+#pragma unroll
+  for (int v = 0; v < V; v++) { A[v] = B[v] = 1.0f; H[v] = G[v] = 0.0f; }
+#pragma unroll
+  for (int j = 0; j < R; j++) {
+    const int32_t bag = marks[2 * (r0 + j)];
+    if (bag)
+#pragma unroll
+      for (int v = 0; v < V; v++) {
+        A[v] = kReset;
+        H[v] = a.h0 && on ? a.h0[(int64_t)(bag - 1) * a.h0s + c0 + v] : 0.0f;
+      }
+#pragma unroll
+    for (int v = 0; v < V; v++) {
+      q[j][v] = gate((float)uv[j].e[v]);
+      const float f = keep_of(q[j][v]), x = (float)xv[j].e[v];
+      H[v] = f * H[v] + (a.coupled ? take_of(q[j][v]) * x : x);
+      A[v] *= f;
+    }
+  }
+#pragma unroll
+  for (int j = R - 1; j >= 0; j--) {
+    const int32_t ended = marks[2 * (r0 + j) + 1];
+    if (ended)
+#pragma unroll
+      for (int v = 0; v < V; v++) {
+        B[v] = kReset;
+        G[v] = a.dlast && on ? a.dlast[(int64_t)(ended - 1) * a.dim + c0 + v] : 0.0f;
+      }
+#pragma unroll
+    for (int v = 0; v < V; v++) {
+      const float f = keep_of(q[j][v]);
+      G[v] = f * (G[v] + (float)gv[j].e[v]);
+      B[v] *= f;
+    }
+  }
+  scan_wave<V, false>(A, H, a.L);
+  tell_wave<V, false>(A, H, a.L, lds);
+  scan_wave<V, true>(B, G, a.L);
+  tell_wave<V, true>(B, G, a.L, back);
+  __syncthreads();
+  for (int c = threadIdx.x; c < C; c += kThreads) {
+    const bool in = a.chunks > 1 && tile * C + c < a.dim;
+    float A1 = 1.0f, s = in ? a.before[(int64_t)chunk * a.dim + tile * C + c] : 0.0f;
+    join_waves<false>(lds, C, c, A1, s);
+    s = in ? a.behind[(int64_t)chunk * a.dim + tile * C + c] : 0.0f;
+    join_waves<true>(back, C, c, A1, s);
+  }
+  __syncthreads();
+  float h[R][V], s[V];
+  start_of_lane<V, false>(A, H, a.L, lds, s);
+#pragma unroll
+  for (int j = 0; j < R; j++) {
+    const int32_t bag = marks[2 * (r0 + j)];
+    if (bag)
+#pragma unroll
+      for (int v = 0; v < V; v++) s[v] = a.h0 && on ? a.h0[(int64_t)(bag - 1) * a.h0s + c0 + v] : 0.0f;
+#pragma unroll
+    for (int v = 0; v < V; v++) {
+      const float x = (float)xv[j].e[v];
+      h[j][v] = a.coupled ? s[v] - x : s[v];
+      s[v] = keep_of(q[j][v]) * s[v] + (a.coupled ? take_of(q[j][v]) * x : x);
+    }
+  }
+  start_of_lane<V, true>(B, G, a.L, back, s);
+  if (!on) return;
+#pragma unroll
+  for (int j = R - 1; j >= 0; j--) {
+    const int32_t bag = marks[2 * (r0 + j)], ended = marks[2 * (r0 + j) + 1];
+    if (ended)
+#pragma unroll
+      for (int v = 0; v < V; v++) s[v] = a.dlast ? a.dlast[(int64_t)(ended - 1) * a.dim + c0 + v] : 0.0f;
+    Pack<E, V> dx, du;
+#pragma unroll
+    for (int v = 0; v < V; v++) {
+      const float f = keep_of(q[j][v]), i = take_of(q[j][v]), g = (float)gv[j].e[v] + s[v];
+      dx.e[v] = (E)(a.coupled ? i * g : g);
+      du.e[v] = (E)(g * h[j][v] * (f * i));
+      s[v] = f * g;
+    }
+    if (r0 + j < rows) {
+      store_pack<E, V, ALIGNED>(a.dx + (row0 + r0 + j) * a.dxs + c0, dx);
+      store_pack<E, V, ALIGNED>(a.du + (row0 + r0 + j) * a.dus + c0, du);
+    }
+    if (bag && a.dh0)
+#pragma unroll
+      for (int v = 0; v < V; v++) a.dh0[(int64_t)(bag - 1) * a.dim + c0 + v] = s[v];
+  }
+}
+
+// Bags without any row in the whole call: where they start is where they end.
+__global__ __launch_bounds__(kThreads) void scan_empty_kernel(const int64_t *off, int64_t bags, int dim, const float *from, int64_t stride, float *to,
+                                                              int32_t *err) {
+  const int64_t id = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+  if (id <= bags && off[id] != 0) *err = 1;
+  for (int64_t k = id; k < bags * dim; k += (int64_t)gridDim.x * kThreads) to[k] = from ? from[k / dim * stride + k % dim] : 0.0f;
 }
 
 template <int DT>
@@ -89,12 +531,27 @@ __global__ __launch_bounds__(kThreads) void scan_step_kernel(float *state, int64
   if (slot >= slots) *err = 2;
   float h = 0.0f;
   if (slot >= 0 && slot < slots) {
-    const Gate g = gate((float)u[r * us + d]);
-    h = g.f * state[slot * ss + d] + (coupled ? g.i : 1.0f) * (float)x[r * xs + d];
+    const float q = gate((float)u[r * us + d]);
+    h = keep_of(q) * state[slot * ss + d] + (coupled ? take_of(q) : 1.0f) * (float)x[r * xs + d];
     state[slot * ss + d] = h;
   }
   if (y) y[r * ys + d] = (typename Elem<DT>::type)h;
 }
+
+}  // namespace
+
+struct tbe_scan_t : DenseBase {
+  int dim = 0, dtype = 0;
+  bool coupled = false;
+  int64_t max_bags = 0, max_rows = 0;
+  Cut cut{};
+  int32_t *err = nullptr;    // device: 1 = bad offsets, 2 = slot out of range
+  float *maps = nullptr;     // device [chunks][2][dim]
+  float *states = nullptr;   // device [chunks][dim]: before the chunks where the caller saves none, behind them in the backward
+  int32_t *bag_of = nullptr; // device [chunks]
+};
+
+namespace {
 
 int check_batch(tbe_scan_t *s, const void *x, int64_t xs, const void *u, int64_t us, const int64_t *off, int64_t bags, int64_t rows, const float *h0,
                 int64_t h0s) noexcept {
@@ -111,6 +568,99 @@ int check_batch(tbe_scan_t *s, const void *x, int64_t xs, const void *u, int64_t
 
 dim3 grid_of(int64_t n) { return dim3((unsigned)((n + kThreads - 1) / kThreads)); }
 
+int64_t chunks_of(const tbe_scan_t *s, int64_t rows) { return (rows + s->cut.rows - 1) / s->cut.rows; }
+
+template <int DT, int V, bool ALIGNED>
+int run(const tbe_scan_t *s, const Rows<DT> &a, bool grad, hipStream_t stream) noexcept {
+  const dim3 grid((unsigned)(a.chunks * a.tiles)), joins((unsigned)((a.dim + kJoinChannels - 1) / kJoinChannels));
+  const size_t tot = (size_t)kWaves * 2 * a.L * V * sizeof(float), marks = (size_t)a.chunk_rows * 2 * sizeof(int32_t);
+  if (!grad) {
+    if (a.chunks > 1) {
+      scan_sum_kernel<DT, V, ALIGNED, false><<<grid, kThreads, tot + marks, stream>>>(a);
+      scan_join_kernel<false><<<joins, kJoinChannels * kJoinSegments, 0, stream>>>(a.maps, a.before, a.chunks, a.dim);
+    }
+    scan_apply_kernel<DT, V, ALIGNED><<<grid, kThreads, tot + marks, stream>>>(a);
+  } else {
+    if (a.chunks > 1) {
+      scan_sum_kernel<DT, V, ALIGNED, true><<<grid, kThreads, tot + marks, stream>>>(a);
+      scan_join_kernel<true><<<joins, kJoinChannels * kJoinSegments, 0, stream>>>(a.maps, a.behind, a.chunks, a.dim);
+    }
+    scan_grad_kernel<DT, V, ALIGNED><<<grid, kThreads, 2 * tot + marks, stream>>>(a);
+  }
+  return check_launch();
+}
+
+bool aligned16(const void *p, int64_t stride, int es) { return ((uintptr_t)p | (uint64_t)(stride * es)) % 16 == 0; }
+
+template <int DT>
+int run_type(const tbe_scan_t *s, Rows<DT> a, bool grad, hipStream_t stream) noexcept {
+  constexpr int wide = 16 / (int)sizeof(typename Elem<DT>::type), es = sizeof(typename Elem<DT>::type);
+  if (s->cut.V == 1) return run<DT, 1, true>(s, a, grad, stream);
+  const bool al = aligned16(a.x, a.xs, es) && aligned16(a.u, a.us, es) && (!a.y || aligned16(a.y, a.ys, es)) && (!a.dy || aligned16(a.dy, a.dys, es)) &&
+                  (!grad || (aligned16(a.dx, a.dxs, es) && aligned16(a.du, a.dus, es)));
+  return al ? run<DT, wide, true>(s, a, grad, stream) : run<DT, wide, false>(s, a, grad, stream);
+}
+
+template <int DT>
+Rows<DT> rows_of(const tbe_scan_t *s, const void *x, int64_t xs, const void *u, int64_t us, const int64_t *off, int64_t bags, int64_t rows,
+                 const float *h0, int64_t h0s) {
+  using E = typename Elem<DT>::type;
+  Rows<DT> a = {};
+  a.x = (const E *)x;
+  a.u = (const E *)u;
+  a.xs = xs;
+  a.us = us;
+  a.off = off;
+  a.bags = bags;
+  a.rows = rows;
+  a.h0 = h0;
+  a.h0s = h0s;
+  a.maps = s->maps;
+  a.bag_of = s->bag_of;
+  a.err = s->err;
+  a.dim = s->dim;
+  a.L = s->cut.L;
+  a.tiles = s->cut.tiles;
+  a.chunk_rows = s->cut.rows;
+  a.chunks = (int)chunks_of(s, rows);
+  a.coupled = s->coupled;
+  return a;
+}
+
+template <int DT>
+int forward(const tbe_scan_t *s, Rows<DT> a, void *y, int64_t ys, float *last, float *saved, hipStream_t stream) noexcept {
+  a.y = (typename Elem<DT>::type *)y;
+  a.ys = ys;
+  a.last = last;
+  a.before = saved ? saved : s->states;
+  return run_type<DT>(s, a, false, stream);
+}
+
+template <int DT>
+int backward(const tbe_scan_t *s, Rows<DT> a, const float *saved, const void *dy, int64_t dys, const float *dlast, void *dx, int64_t dxs, void *du,
+             int64_t dus, float *dh0, hipStream_t stream) noexcept {
+  using E = typename Elem<DT>::type;
+  a.before = const_cast<float *>(saved);
+  a.behind = s->states;
+  a.dy = (const E *)dy;
+  a.dys = dys;
+  a.dlast = dlast;
+  a.dx = (E *)dx;
+  a.dxs = dxs;
+  a.du = (E *)du;
+  a.dus = dus;
+  a.dh0 = dh0;
+  return run_type<DT>(s, a, true, stream);
+}
+
+int only_empty(const tbe_scan_t *s, const int64_t *off, int64_t bags, const float *from, int64_t stride, float *to, hipStream_t stream) noexcept {
+  const int64_t n = to ? bags * s->dim : 0, most = n > bags + 1 ? n : bags + 1;
+  const int64_t blocks = (most + kThreads - 1) / kThreads;
+  scan_empty_kernel<<<dim3((unsigned)(blocks > bags / kThreads + 4096 ? bags / kThreads + 4096 : blocks)), kThreads, 0, stream>>>(
+      off, bags, to ? s->dim : 0, from, stride, to, s->err);
+  return check_launch();
+}
+
 }  // namespace
 
 extern "C" {
@@ -121,7 +671,8 @@ int tbe_scan_create(tbe_scan_handle *out, int32_t dim, int32_t dtype, int32_t co
   if (dim < 1 || dim > 65536) return report(TBE_EINVAL, "dim outside 1 .. 65536");
   if (!known_dtype(dtype)) return report(TBE_EINVAL, "unknown dtype");
   if (max_bags < 0 || max_rows < 0) return report(TBE_EINVAL, "negative number of bags or rows");
-  if (max_bags > (1ll << 38) / dim || max_rows > (1ll << 38) / dim) return report(TBE_ELIMIT, "more than 2^38 elements");
+  if (max_bags > (1ll << 38) / dim || max_rows > (1ll << 38) / dim || max_bags >= INT32_MAX)
+    return report(TBE_ELIMIT, "more than 2^38 elements, or 2^31 bags");
   tbe_scan_t *s = new (std::nothrow) tbe_scan_t;
   if (!s) return report(TBE_ENOMEM, "no memory for the handle");
   s->dim = dim;
@@ -129,14 +680,27 @@ int tbe_scan_create(tbe_scan_handle *out, int32_t dim, int32_t dtype, int32_t co
   s->coupled = coupled != 0;
   s->max_bags = max_bags;
   s->max_rows = max_rows;
+  s->cut = cut_of(dim, dtype);
+  const int64_t chunks = chunks_of(s, max_rows);
+  if (chunks * s->cut.tiles > INT32_MAX / kThreads) {
+    delete s;
+    return report(TBE_ELIMIT, "more rows than one launch can take");
+  }
+  // one block: [err][bag_of][maps][states]
+  const size_t bag_bytes = ((size_t)chunks * sizeof(int32_t) + 255) & ~(size_t)255, floats = (size_t)chunks * dim;
+  char *block = nullptr;
   hipError_t e = hipGetDevice(&s->device);
-  if (e == hipSuccess) e = hipMalloc((void **)&s->err, 256);
-  if (e == hipSuccess) e = hipMemset(s->err, 0, 256);
+  if (e == hipSuccess) e = hipMalloc((void **)&block, 256 + bag_bytes + floats * 3 * sizeof(float));
+  if (e == hipSuccess) e = hipMemset(block, 0, 256);
   if (e != hipSuccess) {
-    (void)hipFree(s->err);
+    (void)hipFree(block);
     delete s;
     return report_hip(e);
   }
+  s->err = (int32_t *)block;
+  s->bag_of = (int32_t *)(block + 256);
+  s->maps = (float *)(block + 256 + bag_bytes);
+  s->states = s->maps + floats * 2;
   *out = s;
   return TBE_OK;
 }
@@ -150,7 +714,7 @@ int tbe_scan_destroy(tbe_scan_handle s) {
 
 int64_t tbe_scan_saved_floats(tbe_scan_handle s, int64_t rows) {
   if (!s || rows < 0) return report(TBE_EINVAL, "null handle or a negative number of rows");
-  return rows * s->dim;
+  return chunks_of(s, rows) * s->dim;
 }
 
 int tbe_scan_forward(tbe_scan_handle s, const void *d_x, int64_t x_stride, const void *d_u, int64_t u_stride, const int64_t *d_offsets, int64_t bags,
@@ -159,16 +723,12 @@ int tbe_scan_forward(tbe_scan_handle s, const void *d_x, int64_t x_stride, const
   if (int rc = check_batch(s, d_x, x_stride, d_u, u_stride, d_offsets, bags, rows, d_h0, h0_stride)) return rc;
   if (d_y && y_stride < s->dim) return report(TBE_EINVAL, "a stride below dim");
   if (bags == 0) return TBE_OK;
-  const dim3 grid = grid_of(bags * s->dim);
-#define LAUNCH(DT)                                                                                                                            \
-  scan_forward_kernel<DT><<<grid, kThreads, 0, (hipStream_t)stream>>>((const Elem<DT>::type *)d_x, x_stride, (const Elem<DT>::type *)d_u, u_stride, d_offsets, \
-                                                            bags, rows, s->dim, s->coupled, d_h0, h0_stride, (Elem<DT>::type *)d_y, y_stride, \
-                                                            d_last, d_saved, s->err)
-  if (s->dtype == TBE_FP32) LAUNCH(TBE_FP32);
-  else if (s->dtype == TBE_FP16) LAUNCH(TBE_FP16);
-  else LAUNCH(TBE_BF16);
-#undef LAUNCH
-  return check_launch();
+  hipStream_t st = (hipStream_t)stream;
+  if (rows == 0) return only_empty(s, d_offsets, bags, d_h0, h0_stride, d_last, st);
+#define ROWS(DT) rows_of<DT>(s, d_x, x_stride, d_u, u_stride, d_offsets, bags, rows, d_h0, h0_stride)
+  if (s->dtype == TBE_FP32) return forward<TBE_FP32>(s, ROWS(TBE_FP32), d_y, y_stride, d_last, d_saved, st);
+  if (s->dtype == TBE_FP16) return forward<TBE_FP16>(s, ROWS(TBE_FP16), d_y, y_stride, d_last, d_saved, st);
+  return forward<TBE_BF16>(s, ROWS(TBE_BF16), d_y, y_stride, d_last, d_saved, st);
 }
 
 int tbe_scan_backward(tbe_scan_handle s, const void *d_x, int64_t x_stride, const void *d_u, int64_t u_stride, const int64_t *d_offsets, int64_t bags,
@@ -179,17 +739,14 @@ int tbe_scan_backward(tbe_scan_handle s, const void *d_x, int64_t x_stride, cons
   if (rows > 0 && (!d_saved || !d_dx || !d_du)) return report(TBE_EINVAL, "null pointer for what the forward saved or for a gradient");
   if ((d_dy && dy_stride < s->dim) || dx_stride < s->dim || du_stride < s->dim) return report(TBE_EINVAL, "a stride below dim");
   if (bags == 0) return TBE_OK;
-  const dim3 grid = grid_of(bags * s->dim);
-#define LAUNCH(DT)                                                                                                                             \
-  scan_backward_kernel<DT><<<grid, kThreads, 0, (hipStream_t)stream>>>((const Elem<DT>::type *)d_x, x_stride, (const Elem<DT>::type *)d_u, u_stride, d_offsets, \
-                                                             bags, rows, s->dim, s->coupled, d_h0, h0_stride, d_saved, (const Elem<DT>::type *)d_dy, \
-                                                             dy_stride, d_dlast, (Elem<DT>::type *)d_dx, dx_stride, (Elem<DT>::type *)d_du, du_stride, \
-                                                             d_dh0, s->err)
-  if (s->dtype == TBE_FP32) LAUNCH(TBE_FP32);
-  else if (s->dtype == TBE_FP16) LAUNCH(TBE_FP16);
-  else LAUNCH(TBE_BF16);
-#undef LAUNCH
-  return check_launch();
+  hipStream_t st = (hipStream_t)stream;
+  if (rows == 0) return only_empty(s, d_offsets, bags, d_dlast, s->dim, d_dh0, st);
+#define BACKWARD(DT) backward<DT>(s, ROWS(DT), d_saved, d_dy, dy_stride, d_dlast, d_dx, dx_stride, d_du, du_stride, d_dh0, st)
+  if (s->dtype == TBE_FP32) return BACKWARD(TBE_FP32);
+  if (s->dtype == TBE_FP16) return BACKWARD(TBE_FP16);
+  return BACKWARD(TBE_BF16);
+#undef BACKWARD
+#undef ROWS
 }
 
 int tbe_scan_step(tbe_scan_handle s, float *d_state, int64_t state_stride, int64_t slots, const int64_t *d_slots, const void *d_x, int64_t x_stride,

@@ -139,6 +139,34 @@ def test_gates_that_never_forget_or_remember(coupled):
         assert torch.equal(dh0.cpu(), torch.full((1, d), n * f))
 
 
+@pytest.mark.parametrize("dtype", list(TYPES))
+def test_bags_do_not_touch_each_other(dtype):
+    """an infinity or a NaN among the rows, gates or states of a bag: every other bag's results have the same bits as without it"""
+    from paper_2305_01515_amd.dense import Scan
+    lengths = RAGGED + [400, 1, 700, 2]
+    x, u, dy, dlast, h0, off = [t.cuda() for t in inputs(lengths, 24, dtype, "own", seed=12)]
+    plan = Scan(24, x.dtype, len(lengths), x.shape[0])
+
+    def everything(x, u, h0, dy, dlast):
+        y, last, saved = plan.forward(x, u, off, h0, save=True)
+        return (y, last, *plan.backward(x, u, off, saved, dy, dlast, h0))
+    clean = everything(x, u, h0, dy, dlast)
+    o = off.tolist()
+    for bag in (1, 6, 14, len(lengths) - 2, len(lengths) - 4):
+        for value in (float("nan"), float("inf"), float("-inf")):
+            for k in range(5):
+                args = [t.clone() for t in (x, u, h0, dy, dlast)]
+                rows = slice(o[bag], o[bag + 1])
+                if k in (0, 1, 3):
+                    args[k][(o[bag] + o[bag + 1]) // 2 if k != 3 else o[bag + 1] - 1] = value
+                else:
+                    args[k][bag] = value
+                for name, a, b in zip(("y", "last", "dx", "du", "dh0"), everything(*args), clean):
+                    keep = torch.ones(a.shape[0], dtype=torch.bool, device="cuda")
+                    keep[rows if name in ("y", "dx", "du") else bag] = False
+                    assert torch.equal(a[keep], b[keep]), (bag, value, k, name)
+
+
 def test_optional_outputs_and_inputs():
     """no y, no gradient of y, none of the last rows: what is left is as with them"""
     plan, (x, u, off, h0, dy, dlast), (y, last, saved, *_rest) = run_and_compare(RAGGED, 64, "bf16", True, "own", seed=9)
