@@ -3,8 +3,8 @@
 //
 // The bucket of a (query, key) pair is the same for all heads, so a lane finds those of V neighbouring keys (16 bytes of scores) once
 // and goes through the heads with them.  A bucket is found in two looks at LDS: the distance's exponent and 6 bits of its
-// mantissa name a cell, the cell the number of thresholds that everything in it reaches, and one comparison decides about the next
-// one.  (Where a cell holds more thresholds than one, as many comparisons as it takes.)
+// mantissa name a cell, the cell the number of thresholds that everything in it reaches, and a comparison decides about the next
+// one.  (As many comparisons as there are thresholds in the cell that has the most: one, unless thresholds beyond 128 are dense.)
 #include <cmath>
 #include <new>
 
@@ -19,7 +19,8 @@ constexpr int kThreads = 256, kWaves = kThreads / 64;
 constexpr int kMaxThresholds = 127;
 constexpr int kCells = 4096;                 // 64 an octave up to 2^63, and one for distance zero
 constexpr int kTableFloats = 8192;           // of the table in LDS: heads of a workgroup times buckets
-constexpr int kSums = 4096;                  // numbers of a wavefront's sums in LDS (gradient)
+constexpr int kSums = 2048;                  // numbers of a wavefront's sums of heads in LDS (gradient)
+constexpr int kFill = 2048;                  // wavefronts that the gradient wants at least
 constexpr int kMaxParts = 1024;              // workgroups whose sums of a head are added up
 
 struct Buckets {  // in device memory
@@ -30,7 +31,8 @@ struct Buckets {  // in device memory
 struct Shape {
   tbe_bias_shape s;
   int heads, thresholds, buckets;  // buckets of the whole table
-  bool both, dense;                // dense: a cell holds several thresholds
+  bool both;
+  int steps;                       // thresholds that a cell holds at most (1 at least)
   const Buckets *map;              // device
   uint32_t packs;                  // of a row
   unsigned long long packs_magic;
@@ -43,7 +45,7 @@ struct Finder {  // in LDS
 
 __device__ inline void load_finder(const Shape &p, Finder &f) {
   static_assert(sizeof(Finder) == sizeof(Buckets) && sizeof(Finder) % 16 == 0, "copied as it is");
-  for (int k = threadIdx.x; k < (int)(sizeof(Finder) / 16); k += kThreads) ((uint4 *)&f)[k] = ((const uint4 *)p.map)[k];
+  for (int k = threadIdx.x; k < (int)(sizeof(Finder) / 16); k += blockDim.x) ((uint4 *)&f)[k] = ((const uint4 *)p.map)[k];
 }
 
 // cell of a distance: monotone, and exact at the cells' borders below 2^22 (above, a distance just below a border may count as on it,
@@ -56,14 +58,12 @@ __host__ __device__ inline int cell_of(uint64_t a) {
   return c > 0 ? c : 0;
 }
 
-// bucket of a key `ahead` positions after the query
-__device__ inline int bucket_of(const Shape &p, const Finder &f, int64_t ahead) {
-  const int64_t d = min(ahead < 0 ? -ahead : (p.both ? ahead : 0), INT64_MAX - 1);  // below the number behind the last threshold
-  int b = f.reached[cell_of((uint64_t)d)];
-  b += d >= f.threshold[b];
-  if (p.dense)
-    while (d >= f.threshold[b]) b++;
-  return b + (p.both && ahead > 0 ? p.thresholds + 1 : 0);
+// the least number of a cell > 0
+inline double border_of(int c) {
+  const uint32_t bits = (uint32_t)(c + 127 * 64 - 1) << 17;
+  float f;
+  __builtin_memcpy(&f, &bits, 4);
+  return f;
 }
 
 __device__ inline float table_value(const void *table, int dtype, int64_t i) {
@@ -72,38 +72,54 @@ __device__ inline float table_value(const void *table, int dtype, int64_t i) {
   return (float)((const __bf16 *)table)[i];
 }
 
-// V keys of a query: their buckets, and which of them are masked
+// V keys of a query: their buckets, and which of them are masked.  The last pack of a row is moved back to end where the row does; the
+// keys that the pack before it has already are marked in `twice`.  (A row shorter than a pack has places without a key: n < V.)
 template <int V>
 struct Keys {
   int64_t i, j;
-  int n;               // keys that there are
+  int n;
   int bucket[V];
-  uint32_t masked;     // bits
+  uint32_t masked, twice;  // bits
 };
 
 template <int V>
-__device__ inline void find_keys(const Shape &p, const Finder &f, int64_t b, int64_t item, Keys<V> &k) {
-  k.i = (int64_t)div_by((uint32_t)item, p.packs_magic);
-  k.j = (item - k.i * p.packs) * V;
-  k.n = (int)min((int64_t)V, p.s.keys - k.j);
-  const int64_t q = p.s.d_query_pos ? p.s.d_query_pos[b * p.s.query_pos_stride + k.i] : p.s.query_offset + k.i;
+__device__ inline void find_keys(const Shape &p, const Finder &f, int64_t b, uint32_t item, Keys<V> &k) {
+  const uint32_t i = div_by(item, p.packs_magic), j = (item - i * p.packs) * V, keys = (uint32_t)p.s.keys;
+  const uint32_t from = keys >= V && j + V > keys ? keys - V : j;
+  k.i = i;
+  k.j = from;
+  k.n = (int)min((uint32_t)V, keys - from);
+  k.twice = (1u << (j - from)) - 1;
+  const int64_t q = p.s.d_query_pos ? p.s.d_query_pos[b * p.s.query_pos_stride + i] : p.s.query_offset + i;
   const int64_t len = p.s.d_key_lengths ? p.s.d_key_lengths[b] : p.s.keys;
-  int64_t ahead[V];
+  int64_t d[V];  // first keys' positions after the query, then distances
   if (p.s.d_key_pos) {
-    const int64_t *kp = p.s.d_key_pos + b * p.s.key_pos_stride + k.j;
+    const int64_t *kp = p.s.d_key_pos + b * p.s.key_pos_stride + from;
 #pragma unroll
-    for (int v = 0; v < V; v++) ahead[v] = kp[min(v, k.n - 1)] - q;
+    for (int v = 0; v < V; v++) d[v] = kp[min(v, k.n - 1)] - q;
   } else {
 #pragma unroll
-    for (int v = 0; v < V; v++) ahead[v] = k.j + v - q;
+    for (int v = 0; v < V; v++) d[v] = (int64_t)from + v - q;
   }
-  k.masked = 0;
+  uint32_t after = 0;
 #pragma unroll
   for (int v = 0; v < V; v++) {
-    k.bucket[v] = bucket_of(p, f, ahead[v]);
-    const bool later = p.s.causal && ahead[v] > 0, beyond = k.j + v >= len;
-    k.masked |= (later | beyond) ? 1u << v : 0u;
+    after |= d[v] > 0 ? 1u << v : 0u;
+    const int64_t back = -d[v];
+    d[v] = d[v] > 0 ? (p.both ? d[v] : 0) : back;
+    d[v] = min(d[v], INT64_MAX - 1);  // below the number behind the last threshold
+    k.bucket[v] = f.reached[cell_of((uint64_t)d[v])];
   }
+  for (int s = 0; s < p.steps; s++)
+#pragma unroll
+    for (int v = 0; v < V; v++) k.bucket[v] += d[v] >= f.threshold[k.bucket[v]];
+  const int apart = p.both ? p.thresholds + 1 : 0;
+  k.masked = p.s.causal ? after : 0u;
+  const int64_t left = len - (int64_t)from;  // keys from here that are not masked
+  k.masked |= left >= V ? 0u : left <= 0 ? ~0u : ~0u << left;
+  k.masked &= (1u << V) - 1;
+#pragma unroll
+  for (int v = 0; v < V; v++) k.bucket[v] += after >> v & 1 ? apart : 0;
 }
 
 template <class E, int V>
@@ -122,7 +138,7 @@ __device__ inline void write_pack(E *p, const Pack<E, V> &r) {
 template <int DT, bool SCORES>
 __global__ __launch_bounds__(kThreads) void bias_forward_kernel(Shape p, int group, const void *table, int table_dtype, const typename Elem<DT>::type *scores,
                                                                 tbe_bias_strides ss, float scale, float mask, typename Elem<DT>::type *out,
-                                                                tbe_bias_strides os) {
+                                                                tbe_bias_strides os, bool in_place) {
   using E = typename Elem<DT>::type;
   constexpr int V = 16 / sizeof(E);
   __shared__ __align__(16) Finder find;
@@ -137,15 +153,16 @@ __global__ __launch_bounds__(kThreads) void bias_forward_kernel(Shape p, int gro
     const int64_t b = w / blocks, item = (w - b * blocks) * kThreads + threadIdx.x;
     if (item >= items) continue;
     Keys<V> k;
-    find_keys<V>(p, find, b, item, k);
+    find_keys<V>(p, find, b, (uint32_t)item, k);
     const E *in = SCORES ? scores + b * ss.sample + h0 * ss.head + k.i * ss.query + k.j : nullptr;
     E *to = out + b * os.sample + h0 * os.head + k.i * os.query + k.j;
-    const bool whole = k.n == V, blank = k.masked == (1u << V) - 1;
+    const bool blank = k.masked == (1u << V) - 1;
+    const bool whole = k.n == V && !(in_place && k.twice);  // in place: what the pack before it has is not written again
 #pragma unroll 4
     for (int h = 0; h < heads; h++) {
       Pack<E, V> x = {}, y;
       if (SCORES && !blank) {
-        if (whole) x = read_pack<E, V>(in + h * ss.head);
+        if (k.n == V) x = read_pack<E, V>(in + h * ss.head);
         else
 #pragma unroll
           for (int v = 0; v < V; v++) x.e[v] = in[h * ss.head + min(v, k.n - 1)];
@@ -160,64 +177,127 @@ __global__ __launch_bounds__(kThreads) void bias_forward_kernel(Shape p, int gro
       else
 #pragma unroll
         for (int v = 0; v < V; v++)
-          if (v < k.n) to[h * os.head + v] = y.e[v];
+          if (v < k.n && !(k.twice >> v & 1)) to[h * os.head + v] = y.e[v];
     }
   }
 }
 
-// Gradient of the table.  A wavefront has sums of its own in LDS, [heads of the group][buckets][slots], a lane adds to slot lane % slots:
-// one wavefront's additions come in one order, so the sums do not depend on how the wavefronts run.
+// Gradient of the table.  A wavefront takes tiles of 64 * kTile packs of keys, leaves their buckets in LDS and goes through the heads with them:
+// every lane adds to sums of its own in LDS, [buckets + 1][64 lanes] (no two lanes on one bank; the row more takes what is masked), the 64
+// lanes' sums of a head are then added up into the wavefront's [heads][buckets].  One lane, one order: the same bits each time.
+// (Additions by LDS atomics into fewer slots took several times as long: 711 us for the gradient of 16 x 8 x 1024 x 1024.)
+constexpr int kTile = 8, kAhead = 4;  // packs of a lane in a tile, and on their way at once
+
+// LDS of a wavefront, in floats
+__host__ __device__ inline int grad_floats(int buckets, int group, int V) { return (buckets + 1) * 64 + kTile * 64 * V / 2 + ((group * buckets + 3) & ~3); }
+
+// where a pack's keys lie (as find_keys has them)
+template <int V>
+__device__ inline void place_of(const Shape &p, uint32_t item, uint32_t &i, uint32_t &from, uint32_t &mine) {
+  const uint32_t keys = (uint32_t)p.s.keys;
+  i = div_by(item, p.packs_magic);
+  const uint32_t j = (item - i * p.packs) * V;
+  from = keys >= V && j + V > keys ? keys - V : j;
+  mine = ~((1u << (j - from)) - 1) & ((1u << min((uint32_t)V, keys - from)) - 1);
+}
+
 template <int DT, bool SCORES>
-__global__ __launch_bounds__(kThreads) void bias_grad_kernel(Shape p, int group, int slots, const typename Elem<DT>::type *dout, tbe_bias_strides ds,
-                                                             float *part, float scale, typename Elem<DT>::type *dscores, tbe_bias_strides es) {
+__global__ __launch_bounds__(kThreads) void bias_grad_kernel(Shape p, int group, const typename Elem<DT>::type *dout, tbe_bias_strides ds, float *part,
+                                                             float scale, typename Elem<DT>::type *dscores, tbe_bias_strides es) {
   using E = typename Elem<DT>::type;
   constexpr int V = 16 / sizeof(E);
+  using Codes = Pack<uint16_t, V>;
   __shared__ __align__(16) Finder find;
-  extern __shared__ float sums[];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, h0 = blockIdx.y * group, heads = min(group, p.heads - h0);
-  const int head_floats = p.buckets * slots, own = group * head_floats;
-  float *sum = sums + wave * own + (lane & (slots - 1));
+  extern __shared__ __align__(16) float lds[];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x / 64, h0 = blockIdx.y * group, heads = min(group, p.heads - h0);
+  const int rows = p.buckets + 1, own = grad_floats(p.buckets, group, V);
+  float *lanes = lds + wave * own, *sum = lanes + rows * 64 + kTile * 64 * V / 2;
+  Codes *codes = (Codes *)(lanes + rows * 64) + lane;
   load_finder(p, find);
-  for (int k = threadIdx.x; k < kWaves * own; k += kThreads) sums[k] = 0.0f;
+  for (int k = threadIdx.x; k < waves * own; k += blockDim.x) lds[k] = 0.0f;
   __syncthreads();
-  const int64_t items = p.s.queries * p.packs, blocks = (items + kThreads - 1) / kThreads;
-  for (int64_t w = blockIdx.x; w < blocks * p.s.batch; w += gridDim.x) {
-    const int64_t b = w / blocks, item = (w - b * blocks) * kThreads + threadIdx.x;
-    if (item >= items) continue;
-    Keys<V> k;
-    find_keys<V>(p, find, b, item, k);
-    const E *in = dout + b * ds.sample + h0 * ds.head + k.i * ds.query + k.j;
-    const bool whole = k.n == V, blank = k.masked == (1u << V) - 1;
-#pragma unroll 4
+  const uint32_t items = (uint32_t)(p.s.queries * p.packs), tiles = (items + 64 * kTile - 1) / (64 * kTile);
+  const uint32_t none = (uint32_t)p.buckets | (uint32_t)p.buckets << 16;
+  const bool short_row = p.s.keys < V;
+  // a row of lanes' sums is added up by 64 / width lanes
+  int width = 1;
+  while (width < p.buckets && width < 64) width *= 2;
+  for (int64_t w = (int64_t)blockIdx.x * waves + wave; w < tiles * p.s.batch; w += (int64_t)gridDim.x * waves) {
+    const int64_t b = w / tiles;
+    const uint32_t first = (uint32_t)(w - b * tiles) * (64 * kTile) + lane;
+#pragma unroll 1
+    for (int r = 0; r < kTile; r++) {
+      const uint32_t item = first + r * 64;
+      Keys<V> k;
+      find_keys<V>(p, find, b, min(item, items - 1), k);
+      const uint32_t out = item < items ? k.masked | k.twice | ~((1u << k.n) - 1) : ~0u;
+      Codes c;
+#pragma unroll
+      for (int v = 0; v < V; v++) c.e[v] = (uint16_t)(out >> v & 1 ? p.buckets : k.bucket[v]);
+      codes[r * 64] = c;
+    }
+#pragma unroll 1
     for (int h = 0; h < heads; h++) {
-      Pack<E, V> x = {};
-      if (!blank) {
-        if (whole) x = read_pack<E, V>(in + h * ds.head);
-        else
+      const E *in = dout + b * ds.sample + (h0 + h) * ds.head;
+#pragma unroll 1
+      for (int r0 = 0; r0 < kTile; r0 += kAhead) {
+        Pack<E, V> x[kAhead];
+        uint32_t c[kAhead][V / 2];
 #pragma unroll
-          for (int v = 0; v < V; v++) x.e[v] = in[h * ds.head + min(v, k.n - 1)];
+        for (int r = 0; r < kAhead; r++) {
+          uint32_t i, j, mine;
+          place_of<V>(p, min(first + (r0 + r) * 64, items - 1), i, j, mine);
+          const E *from = in + i * ds.query + j;
+          __builtin_memcpy(c[r], &codes[(r0 + r) * 64], sizeof c[r]);
+          bool any = false;
+#pragma unroll
+          for (int v = 0; v < V / 2; v++) any |= c[r][v] != none;
+          x[r] = {};
+          if (any) {
+            if (!short_row) x[r] = read_pack<E, V>(from);
+            else
+              for (int v = 0; v < V; v++) x[r].e[v] = from[min(v, (int)p.s.keys - 1)];
+          }
+        }
+#pragma unroll
+        for (int r = 0; r < kAhead; r++) {
+#pragma unroll
+          for (int v = 0; v < V; v++) lanes[(v % 2 ? c[r][v / 2] >> 16 : c[r][v / 2] & 0xFFFFu) * 64 + lane] += (float)x[r].e[v];
+          if (SCORES) {
+            uint32_t i, j, mine;
+            place_of<V>(p, min(first + (r0 + r) * 64, items - 1), i, j, mine);
+            if (first + (r0 + r) * 64 >= items) mine = 0;
+            E *to = dscores + b * es.sample + (h0 + h) * es.head + i * es.query + j;
+#pragma unroll
+            for (int v = 0; v < V; v++)
+              x[r].e[v] = (E)((int)(v % 2 ? c[r][v / 2] >> 16 : c[r][v / 2] & 0xFFFFu) == p.buckets ? 0.0f : (float)x[r].e[v] * scale);
+            if (mine == (1u << V) - 1) write_pack<E, V>(to, x[r]);
+            else
+              for (int v = 0; v < V; v++)
+                if (mine >> v & 1) to[v] = x[r].e[v];
+          }
+        }
       }
-#pragma unroll
-      for (int v = 0; v < V; v++) {
-        const bool on = !(k.masked >> v & 1) && v < k.n;
-        if (on) unsafeAtomicAdd(sum + h * head_floats + k.bucket[v] * slots, (float)x.e[v]);
-        if (SCORES) x.e[v] = (E)(on ? (float)x.e[v] * scale : 0.0f);
-      }
-      if (SCORES) {
-        E *to = dscores + b * es.sample + (h0 + h) * es.head + k.i * es.query + k.j;
-        if (whole) write_pack<E, V>(to, x);
-        else
-#pragma unroll
-          for (int v = 0; v < V; v++)
-            if (v < k.n) to[v] = x.e[v];
+      // lanes' sums of this head, and zeros for the next one's (the row of what is masked may hold anything)
+      for (int c0 = 0; c0 < p.buckets; c0 += width) {
+        const int c = c0 + (lane & (width - 1));
+        float v = 0.0f;
+        if (c < p.buckets)
+#pragma unroll 8
+          for (int k = lane / width; k < 64; k += 64 / width) {
+            float *q = lanes + c * 64 + ((k + c) & 63);
+            v += *q;
+            *q = 0.0f;
+          }
+        for (int k = width; k < 64; k *= 2) v += __shfl_xor(v, k);
+        if (c < p.buckets && lane < width) sum[h * p.buckets + c] += v;
       }
     }
   }
   __syncthreads();
-  for (int k = threadIdx.x; k < heads * p.buckets; k += kThreads) {
+  for (int k = threadIdx.x; k < heads * p.buckets; k += blockDim.x) {
     float v = 0.0f;
-    for (int w = 0; w < kWaves; w++)
-      for (int s = 0; s < slots; s++) v += sums[w * own + k * slots + ((s + lane) & (slots - 1))];
+    for (int w = 0; w < waves; w++) v += lds[(w + 1) * own - ((group * p.buckets + 3) & ~3) + k];
     part[((int64_t)blockIdx.x * p.heads + h0) * p.buckets + k] = v;
   }
 }
@@ -237,7 +317,8 @@ __global__ __launch_bounds__(kThreads) void bias_join_kernel(const float *part, 
 
 struct tbe_bias_t : DenseBase {
   int heads = 0, thresholds = 0, buckets = 0;
-  bool both = false, dense = false;
+  int steps = 1;
+  bool both = false;
   Buckets *map = nullptr;  // device
   float *part = nullptr;   // device [kMaxParts, heads, buckets]
 };
@@ -257,7 +338,7 @@ int check_shape(tbe_bias_t *s, const tbe_bias_shape *p, Shape *out) noexcept {
       (p->d_key_pos && p->key_pos_stride != 0 && p->key_pos_stride < p->keys))
     return report(TBE_EINVAL, "a stride of positions that is neither 0 nor as long as a sample's");
   const uint32_t packs = (uint32_t)((p->keys + V - 1) / V);
-  *out = {*p, s->heads, s->thresholds, s->buckets, s->both, s->dense, s->map, packs, div_magic(packs)};
+  *out = {*p, s->heads, s->thresholds, s->buckets, s->both, s->steps, s->map, packs, div_magic(packs)};
   return TBE_OK;
 }
 
@@ -292,21 +373,18 @@ int tbe_bias_create(tbe_bias_handle *out, int32_t heads, const int64_t *h_thresh
   s->buckets = (num_thresholds + 1) * (s->both ? 2 : 1);
   Buckets map;
   for (int k = 0; k <= kMaxThresholds; k++) map.threshold[k] = k < num_thresholds ? h_thresholds[k] : INT64_MAX;
+  int all = 0, some = 0;                // thresholds up to lo and hi
   for (int c = 0; c < kCells; c++) {  // distances lo .. hi can lie in the cell; the next cell's border is hi + 1
     int64_t lo = 0, hi = 0;
     if (c > 0) {
-      const double from = std::ldexp(1.0 + ((c - 1) % 64) / 64.0, (c - 1) / 64), to = std::ldexp(1.0 + (c - 1) % 64 / 64.0 + 1.0 / 64.0, (c - 1) / 64);
-      const double below = from >= 4194304.0 ? from * (1.0 - 0x1p-22) : from;
+      const double from = border_of(c), to = border_of(c + 1), below = from >= 4194304.0 ? from * (1.0 - 0x1p-22) : from;
       lo = below >= 0x1p63 ? INT64_MAX - 1 : (int64_t)std::ceil(below);
       hi = to >= 0x1p63 ? INT64_MAX - 1 : (int64_t)std::ceil(to) - 1;
     }
-    int all = 0, some = 0;
-    for (int k = 0; k < num_thresholds; k++) {
-      all += h_thresholds[k] <= lo;
-      some += h_thresholds[k] <= hi;
-    }
+    while (all < num_thresholds && h_thresholds[all] <= lo) all++;
+    while (some < num_thresholds && h_thresholds[some] <= hi) some++;
     map.reached[c] = (uint8_t)all;
-    s->dense |= some - all > 1;
+    if (some - all > s->steps) s->steps = some - all;
   }
   hipError_t e = hipGetDevice(&s->device);
   if (e == hipSuccess) e = hipMalloc((void **)&s->map, sizeof(Buckets));
@@ -335,7 +413,7 @@ int tbe_bias_forward(tbe_bias_handle s, const tbe_bias_shape *shape, const void 
   const size_t lds = (size_t)group * p.buckets * sizeof(float);
 #define LAUNCH(DT, SCORES)                                                                                                              \
   bias_forward_kernel<DT, SCORES><<<grid, kThreads, lds, (hipStream_t)stream>>>(p, group, d_table, table_dtype, (const Elem<DT>::type *)d_scores, ss, \
-                                                                                scale, mask_value, (Elem<DT>::type *)d_out, *out_strides)
+                                                                                scale, mask_value, (Elem<DT>::type *)d_out, *out_strides, d_out == d_scores)
 #define LAUNCH2(DT) (d_scores ? LAUNCH(DT, true) : LAUNCH(DT, false))
   if (p.s.dtype == TBE_FP32) LAUNCH2(TBE_FP32);
   else if (p.s.dtype == TBE_FP16) LAUNCH2(TBE_FP16);
@@ -354,18 +432,17 @@ int tbe_bias_backward(tbe_bias_handle s, const tbe_bias_shape *shape, const void
   const tbe_bias_strides es = d_dscores ? *dscores_strides : tbe_bias_strides{0, 0, 0};
   int parts = 0;
   if (any) {
-    int group = 1, slots = 64;
-    while (slots > 1 && p.buckets * slots > kSums) slots /= 2;
-    while (group < p.heads && group < 16 && (2 * group * p.buckets * slots <= kSums || (slots > 16 && 2 * group * p.buckets * 16 <= kSums))) {
-      group *= 2;
-      while (slots > 16 && group * p.buckets * slots > kSums) slots /= 2;
-    }
-    const int64_t blocks = blocks_of(p);
-    parts = (int)(blocks < kMaxParts ? blocks : kMaxParts);
+    // heads of a workgroup: all, unless their sums take more than 8 KB of a wavefront, or the tiles are too few to fill the GPU
+    const int64_t tiles = (p.s.queries * p.packs + 64 * kTile - 1) / (64 * kTile) * p.s.batch;
+    int group = p.heads;
+    while (group > 1 && group * p.buckets > kSums) group = (group + 1) / 2;
+    while (group > 1 && tiles * ((p.heads + group - 1) / group) < kFill) group = (group + 1) / 2;
+    const int waves = p.buckets <= 128 ? 4 : 2;
+    parts = (int)((tiles + waves - 1) / waves < kMaxParts ? (tiles + waves - 1) / waves : kMaxParts);
     const dim3 grid((unsigned)parts, (unsigned)((p.heads + group - 1) / group));
-    const size_t lds = (size_t)kWaves * group * p.buckets * slots * sizeof(float);
+    const size_t lds = (size_t)waves * grad_floats(p.buckets, group, 16 / elem_bytes(p.s.dtype)) * sizeof(float);
 #define LAUNCH(DT, SCORES)                                                                                                                 \
-  bias_grad_kernel<DT, SCORES><<<grid, kThreads, lds, (hipStream_t)stream>>>(p, group, slots, (const Elem<DT>::type *)d_dout, *dout_strides, s->part, \
+  bias_grad_kernel<DT, SCORES><<<grid, 64 * waves, lds, (hipStream_t)stream>>>(p, group, (const Elem<DT>::type *)d_dout, *dout_strides, s->part, \
                                                                              scale, (Elem<DT>::type *)d_dscores, es)
 #define LAUNCH2(DT) (d_dscores ? LAUNCH(DT, true) : LAUNCH(DT, false))
     if (p.s.dtype == TBE_FP32) LAUNCH2(TBE_FP32);
