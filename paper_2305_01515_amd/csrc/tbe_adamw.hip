@@ -1,6 +1,12 @@
 // AdamW over many tensors in one launch, states in 32 or 8 bits.  Contract: include/tbe.h.
-// The arithmetic is written operation by operation, each rounded to fp32 (no contraction), so that a plain form in fp32
-// gives the same bits: with states in 8 bits a last bit that differs now and then makes another code.
+//
+// Bound by memory: 28 bytes an element with fp32 everywhere, 16 with states in 8 bits (fp32 weights and gradients, or 16-bit ones with an
+// fp32 copy).  A wavefront has a block of TBE_ADAMW_BLOCK elements, 4 side by side a lane, so that the largest of a block is an exchange
+// between lanes and every load is 4 elements of its type; a lane's loads of kBlocks blocks are on their way at once.  The types are
+// the tensor's: one kernel has a body for each combination and takes the one that its workgroup's tensor asks for.
+//
+// Moving averages and their codes are computed operation by operation, each rounded to fp32 (no contraction), so that a plain form in fp32
+// gives the same bits: a last bit that differs makes another code now and then, and a code is a sixteenth of its value.
 #include <cmath>
 #include <new>
 
@@ -11,8 +17,8 @@ using namespace tbe;
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kWaveBlocks = 4;                                  // blocks of TBE_ADAMW_BLOCK elements of a workgroup: one a wavefront
-constexpr int kChunk = kWaveBlocks * TBE_ADAMW_BLOCK;
+constexpr int kBlocks = 2;                                      // blocks of a wavefront
+constexpr int kChunk = kThreads / 64 * kBlocks * TBE_ADAMW_BLOCK;
 constexpr int kMaxGrads = 256;                                  // tensors of a launch: their gradients' addresses are kernel arguments
 
 struct Tensor {
@@ -43,26 +49,61 @@ __host__ __device__ inline uint32_t mix(uint32_t x) {  // multiplications by odd
   return x ^ (x >> 16);
 }
 
-__device__ inline float load(const void *p, int dtype, int64_t i) {
-  if (dtype == TBE_FP32) return ((const float *)p)[i];
-  if (dtype == TBE_FP16) return (float)((const _Float16 *)p)[i];
-  return (float)((const __bf16 *)p)[i];
+// 4 elements side by side, at any address that an element may have; `n` of them where the tensor ends
+template <int DT>
+__device__ inline Pack<typename Elem<DT>::type, 4> load4(const void *p, int64_t i, int n) {
+  using E = typename Elem<DT>::type;
+  Pack<E, 4> r = {};
+  if (n >= 4) __builtin_memcpy(&r, (const E *)p + i, sizeof r);
+  else
+#pragma unroll
+    for (int k = 0; k < 3; k++)
+      if (k < n) r.e[k] = ((const E *)p)[i + k];
+  return r;
 }
-__device__ inline void store(void *p, int dtype, int64_t i, float v) {
-  if (dtype == TBE_FP32) ((float *)p)[i] = v;
-  else if (dtype == TBE_FP16) ((_Float16 *)p)[i] = (_Float16)v;
-  else ((__bf16 *)p)[i] = (__bf16)v;
+template <int DT>
+__device__ inline void store4(void *p, int64_t i, int n, const float (&v)[4]) {
+  using E = typename Elem<DT>::type;
+  Pack<E, 4> r;
+#pragma unroll
+  for (int k = 0; k < 4; k++) r.e[k] = (E)v[k];
+  if (n >= 4) __builtin_memcpy((E *)p + i, &r, sizeof r);
+  else
+#pragma unroll
+    for (int k = 0; k < 3; k++)
+      if (k < n) ((E *)p)[i + k] = r.e[k];
+}
+__device__ inline uint32_t load_codes(const void *p, int64_t i, int n) {
+  uint32_t r = 0;
+  if (n >= 4) __builtin_memcpy(&r, (const uint8_t *)p + i, 4);
+  else
+#pragma unroll
+    for (int k = 0; k < 3; k++)
+      if (k < n) r |= (uint32_t)((const uint8_t *)p)[i + k] << (8 * k);
+  return r;
+}
+__device__ inline void store_codes(void *p, int64_t i, int n, uint32_t c) {
+  if (n >= 4) __builtin_memcpy((uint8_t *)p + i, &c, 4);
+  else
+#pragma unroll
+    for (int k = 0; k < 3; k++)
+      if (k < n) ((uint8_t *)p)[i + k] = (uint8_t)(c >> (8 * k));
 }
 
-__device__ inline float from_code(uint32_t c) {  // E4M3
-  const uint32_t e = (c >> 3) & 15u, m = c & 7u;
-  const float v = e ? __uint_as_float((e + 120u) << 23 | m << 20) : (float)m * 0x1p-9f;
-  return c & 128u ? -v : v;
+typedef float float2v __attribute__((ext_vector_type(2)));
+__device__ inline void from_codes(uint32_t c, float (&v)[4]) {  // E4M3, exact
+  const float2v lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)c, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)c, true);
+  v[0] = lo.x;
+  v[1] = lo.y;
+  v[2] = hi.x;
+  v[3] = hi.y;
 }
-__device__ inline uint32_t to_code(float q, uint32_t random) {  // 0 <= q <= 448
+// 0 <= q <= 448 to a code: the upper of two where the 16 random bits, as a share of their distance, reach beyond it
+__device__ inline uint32_t to_code(float q, uint32_t random) {
 #pragma clang fp contract(off)
-  if (q < 0x1p-6f) return (uint32_t)floorf(q * 512.0f + (float)random * (1.0f / 65536.0f));
-  return min(((__float_as_uint(q) + (random << 4)) >> 20) - 960u, 126u);
+  const uint32_t normal = ((__float_as_uint(q) + (random << 4)) >> 20) - 960u;
+  const uint32_t small = (uint32_t)(q * 512.0f + (float)random * (1.0f / 65536.0f));
+  return min(q < 0x1p-6f ? small : normal, 126u);
 }
 
 // the largest magnitude of a wavefront; a NaN is larger than an infinity, and that than any number
@@ -71,69 +112,117 @@ __device__ inline uint32_t wave_top(uint32_t bits) {
   return bits;
 }
 
+template <bool EIGHT, int PT, int GT, bool MASTER>
+__device__ inline void step_blocks(const Tensor &ts, const void *gp, uint32_t key, int64_t first, const Step &st, const float *grad_scale) {
+#pragma clang fp contract(off)
+  constexpr int WT = MASTER ? (int)TBE_FP32 : PT;  // what the weight is held in
+  const int lane = threadIdx.x & 63;
+  const float keep = (float)(1.0 - st.lr * ts.weight_decay), gs = grad_scale ? *grad_scale : 1.0f;
+  Pack<typename Elem<GT>::type, 4> g[kBlocks];
+  Pack<typename Elem<WT>::type, 4> w[kBlocks];
+  Pack<float, 4> m32[kBlocks], v32[kBlocks];
+  uint32_t mc[kBlocks], vc[kBlocks];
+  float ms[kBlocks], vs[kBlocks];
+#pragma unroll
+  for (int b = 0; b < kBlocks; b++) {
+    const int64_t block = first + b, i = block * TBE_ADAMW_BLOCK + lane * 4;
+    const int n = (int)min((int64_t)4, ts.numel - i);
+    g[b] = load4<GT>(gp, i, n);
+    w[b] = load4<WT>(MASTER ? (const void *)ts.master : ts.param, i, n);
+    if (EIGHT) {
+      mc[b] = load_codes(ts.m, i, n);
+      vc[b] = load_codes(ts.v, i, n);
+      const bool there = block * TBE_ADAMW_BLOCK < ts.numel;
+      ms[b] = there ? ts.m_scale[block] : 0.0f;
+      vs[b] = there ? ts.v_scale[block] : 0.0f;
+    } else {
+      m32[b] = load4<TBE_FP32>(ts.m, i, n);
+      v32[b] = load4<TBE_FP32>(ts.v, i, n);
+    }
+  }
+#pragma unroll
+  for (int b = 0; b < kBlocks; b++) {
+    const int64_t block = first + b, i = block * TBE_ADAMW_BLOCK + lane * 4;
+    if (block * TBE_ADAMW_BLOCK >= ts.numel) return;  // the same in all lanes
+    const int n = (int)min((int64_t)4, ts.numel - i);
+    float m[4], v[4], r[4], x[4];
+    if (EIGHT) {
+      from_codes(mc[b], m);
+      from_codes(vc[b], v);
+    }
+#pragma unroll
+    for (int k = 0; k < 4; k++) {
+      float gk = (float)g[b].e[k];
+      if (grad_scale) gk = gk * gs;
+      if (EIGHT) {
+        m[k] = m[k] * ms[b];
+        v[k] = v[k] * vs[b];
+        v[k] = v[k] * v[k];
+      } else {
+        m[k] = m32[b].e[k];
+        v[k] = v32[b].e[k];
+      }
+      m[k] = m[k] * st.beta1 + gk * st.one_minus_beta1;
+      v[k] = v[k] * st.beta2 + (gk * gk) * st.one_minus_beta2;
+      r[k] = sqrtf(v[k]);
+      // the quotient by a reciprocal of an ulp: an error far below that of the weight it changes
+      x[k] = (float)w[b].e[k] * keep - (m[k] * st.rate) * __builtin_amdgcn_rcpf(r[k] * st.root + st.eps);
+    }
+    if (MASTER) store4<TBE_FP32>(ts.master, i, n, x);
+    store4<PT>(ts.param, i, n, x);
+    if (!EIGHT) {
+      store4<TBE_FP32>(ts.m, i, n, m);
+      store4<TBE_FP32>(ts.v, i, n, v);
+      continue;
+    }
+    uint32_t m_top = 0, v_top = 0;
+#pragma unroll
+    for (int k = 0; k < 4; k++)
+      if (k < n) {  // zeros behind the end would not count, but what a NaN grad_scale makes of them would
+        m_top = max(m_top, __float_as_uint(fabsf(m[k])));
+        v_top = max(v_top, __float_as_uint(r[k]));
+      }
+    const float mt = __uint_as_float(wave_top(m_top)), vt = __uint_as_float(wave_top(v_top));
+    const bool mu = mt > 0.0f && mt < INFINITY, vu = vt > 0.0f && vt < INFINITY;
+    const float mi = (1.0f / mt) * 448.0f, vi = (1.0f / vt) * 448.0f;
+    uint32_t mw = 0, vw = 0;
+#pragma unroll
+    for (int k = 0; k < 4; k++) {
+      const uint32_t random = mix((uint32_t)(i + k) * 0x9E3779B9u + key);
+      const uint32_t a = to_code(fminf(fabsf(m[k]) * mi, 448.0f), random >> 16) | (__float_as_uint(m[k]) >> 24 & 128u);
+      const uint32_t c = max(to_code(fminf(r[k] * vi, 448.0f), random & 0xFFFFu), 1u);  // above zero: never zero
+      mw |= (m[k] != 0.0f ? a : 0u) << (8 * k);
+      vw |= (r[k] > 0.0f ? c : 0u) << (8 * k);
+    }
+    store_codes(ts.m, i, n, mu ? mw : 0u);
+    store_codes(ts.v, i, n, vu ? vw : 0u);
+    if (lane == 0) {
+      ts.m_scale[block] = mt * (1.0f / 448.0f);
+      ts.v_scale[block] = vt * (1.0f / 448.0f);
+    }
+  }
+}
+
 template <bool EIGHT>
 __global__ __launch_bounds__(kThreads) void adamw_kernel(const Tensor *tensors, const int64_t *chunk_of, int first_tensor, Grads grads, Step st,
                                                          const float *grad_scale) {
-#pragma clang fp contract(off)
   const int64_t word = chunk_of[blockIdx.x];
   const int t = (int)(word >> 40);
   const void *gp = grads.p[t - first_tensor];
   if (!gp) return;
   const Tensor ts = tensors[t];
-  const int lane = threadIdx.x & 63;
-  const int64_t block = (word & ((1ll << 40) - 1)) * kWaveBlocks + (threadIdx.x >> 6);
-  if (block * TBE_ADAMW_BLOCK >= ts.numel) return;
-  const float keep = (float)(1.0 - st.lr * ts.weight_decay), gs = grad_scale ? *grad_scale : 1.0f;
   const uint32_t key = mix(st.key ^ (uint32_t)t);
-  float m[4], r[4], v[4], ms = 0.0f, vs = 0.0f;
-  if (EIGHT) { ms = ts.m_scale[block]; vs = ts.v_scale[block]; }
-  uint32_t m_top = 0, v_top = 0;
-  for (int k = 0; k < 4; k++) {
-    const int64_t i = block * TBE_ADAMW_BLOCK + k * 64 + lane;
-    m[k] = r[k] = v[k] = 0.0f;
-    if (i >= ts.numel) continue;
-    float g = load(gp, ts.grad_dtype, i);
-    if (grad_scale) g = g * gs;
-    float w = ts.master ? ts.master[i] : load(ts.param, ts.param_dtype, i);
-    if (EIGHT) {
-      m[k] = from_code(((const uint8_t *)ts.m)[i]) * ms;
-      const float old = from_code(((const uint8_t *)ts.v)[i]) * vs;
-      v[k] = old * old;
-    } else {
-      m[k] = ((const float *)ts.m)[i];
-      v[k] = ((const float *)ts.v)[i];
-    }
-    m[k] = m[k] * st.beta1 + g * st.one_minus_beta1;
-    v[k] = v[k] * st.beta2 + (g * g) * st.one_minus_beta2;
-    r[k] = sqrtf(v[k]);
-    w = w * keep - (m[k] * st.rate) / (r[k] * st.root + st.eps);
-    if (ts.master) ts.master[i] = w;
-    store(ts.param, ts.param_dtype, i, w);
-    if (!EIGHT) {
-      ((float *)ts.m)[i] = m[k];
-      ((float *)ts.v)[i] = v[k];
-    }
-    m_top = max(m_top, __float_as_uint(fabsf(m[k])));
-    v_top = max(v_top, __float_as_uint(fabsf(r[k])));
+  const int64_t first = ((word & ((1ll << 40) - 1)) * (kThreads / 64) + (threadIdx.x >> 6)) * kBlocks;
+  const int kind = ts.param_dtype * 3 + ts.grad_dtype;
+#define BODY(PT, GT)                                                                          \
+  case PT * 3 + GT:                                                                           \
+    if (ts.master) step_blocks<EIGHT, PT, GT, true>(ts, gp, key, first, st, grad_scale);      \
+    else step_blocks<EIGHT, PT, GT, false>(ts, gp, key, first, st, grad_scale);               \
+    return;
+  switch (kind) {
+    BODY(0, 0) BODY(0, 1) BODY(0, 2) BODY(1, 0) BODY(1, 1) BODY(1, 2) BODY(2, 0) BODY(2, 1) BODY(2, 2)
   }
-  if (!EIGHT) return;
-  const float mt = __uint_as_float(wave_top(m_top)), vt = __uint_as_float(wave_top(v_top));
-  const bool mu = mt > 0.0f && mt < INFINITY, vu = vt > 0.0f && vt < INFINITY;
-  const float mi = (1.0f / mt) * 448.0f, vi = (1.0f / vt) * 448.0f;
-  for (int k = 0; k < 4; k++) {
-    const int64_t i = block * TBE_ADAMW_BLOCK + k * 64 + lane;
-    if (i >= ts.numel) continue;
-    const uint32_t random = mix((uint32_t)i * 0x9E3779B9u + key);
-    uint32_t mc = 0, vc = 0;
-    if (mu) mc = to_code(fminf(fabsf(m[k]) * mi, 448.0f), random >> 16) + (m[k] < 0.0f ? 128u : 0u);
-    if (vu && r[k] > 0.0f) vc = max(to_code(fminf(r[k] * vi, 448.0f), random & 0xFFFFu), 1u);
-    ((uint8_t *)ts.m)[i] = (uint8_t)mc;
-    ((uint8_t *)ts.v)[i] = (uint8_t)vc;
-  }
-  if (lane == 0) {
-    ts.m_scale[block] = mt * (1.0f / 448.0f);
-    ts.v_scale[block] = vt * (1.0f / 448.0f);
-  }
+#undef BODY
 }
 
 }  // namespace
