@@ -17,8 +17,8 @@ using namespace tbe;
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kBlocks = 2;                                      // blocks of a wavefront
-constexpr int kChunk = kThreads / 64 * kBlocks * TBE_ADAMW_BLOCK;
+constexpr int blocks_of(bool eight) { return eight ? 2 : 1; }    // blocks of a wavefront
+constexpr int chunk_of(bool eight) { return kThreads / 64 * blocks_of(eight) * TBE_ADAMW_BLOCK; }
 constexpr int kMaxGrads = 256;                                  // tensors of a launch: their gradients' addresses are kernel arguments
 
 struct Tensor {
@@ -115,6 +115,7 @@ __device__ inline uint32_t wave_top(uint32_t bits) {
 template <bool EIGHT, int PT, int GT, bool MASTER>
 __device__ inline void step_blocks(const Tensor &ts, const void *gp, uint32_t key, int64_t first, const Step &st, const float *grad_scale) {
 #pragma clang fp contract(off)
+  constexpr int kBlocks = blocks_of(EIGHT);
   constexpr int WT = MASTER ? (int)TBE_FP32 : PT;  // what the weight is held in
   const int lane = threadIdx.x & 63;
   const float keep = (float)(1.0 - st.lr * ts.weight_decay), gs = grad_scale ? *grad_scale : 1.0f;
@@ -204,15 +205,15 @@ __device__ inline void step_blocks(const Tensor &ts, const void *gp, uint32_t ke
 }
 
 template <bool EIGHT>
-__global__ __launch_bounds__(kThreads) void adamw_kernel(const Tensor *tensors, const int64_t *chunk_of, int first_tensor, Grads grads, Step st,
+__global__ __launch_bounds__(kThreads) void adamw_kernel(const Tensor *tensors, const int64_t *chunk_list, int first_tensor, Grads grads, Step st,
                                                          const float *grad_scale) {
-  const int64_t word = chunk_of[blockIdx.x];
+  const int64_t word = chunk_list[blockIdx.x];
   const int t = (int)(word >> 40);
   const void *gp = grads.p[t - first_tensor];
   if (!gp) return;
   const Tensor ts = tensors[t];
   const uint32_t key = mix(st.key ^ (uint32_t)t);
-  const int64_t first = ((word & ((1ll << 40) - 1)) * (kThreads / 64) + (threadIdx.x >> 6)) * kBlocks;
+  const int64_t first = ((word & ((1ll << 40) - 1)) * (kThreads / 64) + (threadIdx.x >> 6)) * blocks_of(EIGHT);
   const int kind = ts.param_dtype * 3 + ts.grad_dtype;
 #define BODY(PT, GT)                                                                          \
   case PT * 3 + GT:                                                                           \
@@ -230,7 +231,7 @@ __global__ __launch_bounds__(kThreads) void adamw_kernel(const Tensor *tensors, 
 struct tbe_adamw_t : DenseBase {
   int bits = 32, n = 0;
   Tensor *tensors = nullptr;   // device [n]
-  int64_t *chunk_of = nullptr; // device: tensor << 40 | chunk of it, for every workgroup
+  int64_t *chunk_list = nullptr; // device: tensor << 40 | chunk of it, for every workgroup
   int64_t *first = nullptr;    // host [n + 1]: first workgroup of a tensor
 };
 
@@ -239,7 +240,7 @@ extern "C" {
 int tbe_adamw_destroy(tbe_adamw_handle s) {
   if (!s) return TBE_OK;
   (void)hipFree(s->tensors);
-  (void)hipFree(s->chunk_of);
+  (void)hipFree(s->chunk_list);
   delete[] s->first;
   delete s;
   return TBE_OK;
@@ -251,6 +252,7 @@ int tbe_adamw_create(tbe_adamw_handle *out, const tbe_adamw_tensor *h_tensors, i
   if (!h_tensors || num_tensors < 1) return report(TBE_EINVAL, "no tensors");
   if (state_bits != 32 && state_bits != 8) return report(TBE_EINVAL, "states have 32 or 8 bits");
   if (num_tensors > 1 << 20) return report(TBE_ELIMIT, "more than 2^20 tensors");
+  const int64_t chunk = chunk_of(state_bits == 8);
   int64_t chunks = 0;
   for (int t = 0; t < num_tensors; t++) {
     const tbe_adamw_tensor &a = h_tensors[t];
@@ -260,15 +262,15 @@ int tbe_adamw_create(tbe_adamw_handle *out, const tbe_adamw_tensor *h_tensors, i
     if (a.numel && (!a.d_param || !a.d_m || !a.d_v || (state_bits == 8 && (!a.d_m_scale || !a.d_v_scale))))
       return report(TBE_EINVAL, "null parameter or state");
     if (!std::isfinite(a.weight_decay)) return report(TBE_EINVAL, "weight_decay is not finite");
-    chunks += (a.numel + kChunk - 1) / kChunk;
+    chunks += (a.numel + chunk - 1) / chunk;
   }
   if (chunks > INT32_MAX) return report(TBE_ELIMIT, "more elements than one launch can take");
   tbe_adamw_t *s = new (std::nothrow) tbe_adamw_t;
   Tensor *host = new (std::nothrow) Tensor[num_tensors];
-  int64_t *chunk_of = new (std::nothrow) int64_t[chunks + 1];
+  int64_t *list = new (std::nothrow) int64_t[chunks + 1];
   int rc = TBE_OK;
   if (s) s->first = new (std::nothrow) int64_t[num_tensors + 1];
-  if (!s || !host || !chunk_of || !s->first) {
+  if (!s || !host || !list || !s->first) {
     rc = report(TBE_ENOMEM, "no memory for the handle");
   } else {
     s->bits = state_bits;
@@ -278,18 +280,18 @@ int tbe_adamw_create(tbe_adamw_handle *out, const tbe_adamw_tensor *h_tensors, i
       const tbe_adamw_tensor &a = h_tensors[t];
       host[t] = {a.d_param, a.d_master, a.d_m, a.d_v, a.d_m_scale, a.d_v_scale, a.numel, a.weight_decay, a.param_dtype, a.grad_dtype};
       s->first[t] = at;
-      for (int64_t c = 0; c < (a.numel + kChunk - 1) / kChunk; c++) chunk_of[at++] = (int64_t)t << 40 | c;
+      for (int64_t c = 0; c < (a.numel + chunk - 1) / chunk; c++) list[at++] = (int64_t)t << 40 | c;
     }
     s->first[num_tensors] = at;
     hipError_t e = hipGetDevice(&s->device);
     if (e == hipSuccess) e = hipMalloc((void **)&s->tensors, num_tensors * sizeof(Tensor));
-    if (e == hipSuccess) e = hipMalloc((void **)&s->chunk_of, (chunks + 1) * sizeof(int64_t));
+    if (e == hipSuccess) e = hipMalloc((void **)&s->chunk_list, (chunks + 1) * sizeof(int64_t));
     if (e == hipSuccess) e = hipMemcpy(s->tensors, host, num_tensors * sizeof(Tensor), hipMemcpyHostToDevice);
-    if (e == hipSuccess) e = hipMemcpy(s->chunk_of, chunk_of, chunks * sizeof(int64_t), hipMemcpyHostToDevice);
+    if (e == hipSuccess) e = hipMemcpy(s->chunk_list, list, chunks * sizeof(int64_t), hipMemcpyHostToDevice);
     if (e != hipSuccess) rc = report_hip(e);
   }
   delete[] host;
-  delete[] chunk_of;
+  delete[] list;
   if (rc) {
     (void)tbe_adamw_destroy(s);
     return rc;
@@ -321,8 +323,8 @@ int tbe_adamw_step(tbe_adamw_handle s, const void *const *h_grads, int64_t step,
     if (count == 0) continue;
     Grads g = {};
     for (int t = t0; t < t1; t++) g.p[t - t0] = h_grads[t];
-    if (s->bits == 8) adamw_kernel<true><<<dim3((unsigned)count), kThreads, 0, (hipStream_t)stream>>>(s->tensors, s->chunk_of + first, t0, g, st, d_grad_scale);
-    else adamw_kernel<false><<<dim3((unsigned)count), kThreads, 0, (hipStream_t)stream>>>(s->tensors, s->chunk_of + first, t0, g, st, d_grad_scale);
+    if (s->bits == 8) adamw_kernel<true><<<dim3((unsigned)count), kThreads, 0, (hipStream_t)stream>>>(s->tensors, s->chunk_list + first, t0, g, st, d_grad_scale);
+    else adamw_kernel<false><<<dim3((unsigned)count), kThreads, 0, (hipStream_t)stream>>>(s->tensors, s->chunk_list + first, t0, g, st, d_grad_scale);
   }
   return check_launch();
 }
