@@ -20,6 +20,7 @@ constexpr int kMaxThresholds = 127;
 constexpr int kCells = 4096;                 // 64 an octave up to 2^63, and one for distance zero
 constexpr int kTableFloats = 8192;           // of the table in LDS: heads of a workgroup times buckets
 constexpr int kSums = 2048;                  // numbers of a wavefront's sums of heads in LDS (gradient)
+constexpr int kHeads = 4;                    // packs of scores on their way at once: as many heads
 constexpr int kFill = 2048;                  // wavefronts that the gradient wants at least
 constexpr int kMaxParts = 1024;              // workgroups whose sums of a head are added up
 
@@ -64,6 +65,14 @@ inline double border_of(int c) {
   float f;
   __builtin_memcpy(&f, &bits, 4);
   return f;
+}
+
+// bucket of a key `ahead` positions after the query
+__device__ inline int bucket_of(const Shape &p, const Finder &f, int64_t ahead) {
+  const int64_t back = -ahead, d = min(ahead > 0 ? (p.both ? ahead : 0) : back, INT64_MAX - 1);
+  int b = f.reached[cell_of((uint64_t)d)];
+  for (int s = 0; s < p.steps; s++) b += d >= f.threshold[b];
+  return b + (p.both && ahead > 0 ? p.thresholds + 1 : 0);
 }
 
 __device__ inline float table_value(const void *table, int dtype, int64_t i) {
@@ -148,6 +157,7 @@ __global__ __launch_bounds__(kThreads) void bias_forward_kernel(Shape p, int gro
   for (int k = threadIdx.x; k < heads * p.buckets; k += kThreads)
     value[k] = table_value(table, table_dtype, (int64_t)(k % p.buckets) * p.heads + h0 + k / p.buckets);
   __syncthreads();
+  const bool short_row = p.s.keys < V;
   const int64_t items = p.s.queries * p.packs, blocks = (items + kThreads - 1) / kThreads;
   for (int64_t w = blockIdx.x; w < blocks * p.s.batch; w += gridDim.x) {
     const int64_t b = w / blocks, item = (w - b * blocks) * kThreads + threadIdx.x;
@@ -158,26 +168,37 @@ __global__ __launch_bounds__(kThreads) void bias_forward_kernel(Shape p, int gro
     E *to = out + b * os.sample + h0 * os.head + k.i * os.query + k.j;
     const bool blank = k.masked == (1u << V) - 1;
     const bool whole = k.n == V && !(in_place && k.twice);  // in place: what the pack before it has is not written again
-#pragma unroll 4
-    for (int h = 0; h < heads; h++) {
-      Pack<E, V> x = {}, y;
-      if (SCORES && !blank) {
-        if (k.n == V) x = read_pack<E, V>(in + h * ss.head);
+    if (SCORES && blank && !short_row) in = scores;         // lanes that want nothing read one place, and need no branch
+    const int64_t step = SCORES && blank && !short_row ? 0 : ss.head;
+    for (int h = 0; h < heads; h += kHeads) {
+      Pack<E, V> x[kHeads];
+      if (SCORES) {
+        if (!short_row) {
+#pragma unroll
+          for (int g = 0; g < kHeads; g++) x[g] = read_pack<E, V>(in + min(h + g, heads - 1) * step);
+        } else {
+#pragma unroll
+          for (int g = 0; g < kHeads; g++)
+#pragma unroll
+            for (int v = 0; v < V; v++) x[g].e[v] = in[min(h + g, heads - 1) * step + min(v, k.n - 1)];
+        }
+      }
+#pragma unroll
+      for (int g = 0; g < kHeads; g++) {
+        if (h + g >= heads) break;
+        Pack<E, V> y;
+#pragma unroll
+        for (int v = 0; v < V; v++) {
+          float r = value[(h + g) * p.buckets + k.bucket[v]];
+          if (SCORES) r += (float)x[g].e[v] * scale;
+          y.e[v] = (E)(k.masked >> v & 1 ? mask : r);
+        }
+        if (whole) write_pack<E, V>(to + (h + g) * os.head, y);
         else
 #pragma unroll
-          for (int v = 0; v < V; v++) x.e[v] = in[h * ss.head + min(v, k.n - 1)];
+          for (int v = 0; v < V; v++)
+            if (v < k.n && !(k.twice >> v & 1)) to[(h + g) * os.head + v] = y.e[v];
       }
-#pragma unroll
-      for (int v = 0; v < V; v++) {
-        float r = value[h * p.buckets + k.bucket[v]];
-        if (SCORES) r += (float)x.e[v] * scale;
-        y.e[v] = (E)(k.masked >> v & 1 ? mask : r);
-      }
-      if (whole) write_pack<E, V>(to + h * os.head, y);
-      else
-#pragma unroll
-        for (int v = 0; v < V; v++)
-          if (v < k.n && !(k.twice >> v & 1)) to[h * os.head + v] = y.e[v];
     }
   }
 }
@@ -243,21 +264,25 @@ __global__ __launch_bounds__(kThreads) void bias_grad_kernel(Shape p, int group,
       for (int r0 = 0; r0 < kTile; r0 += kAhead) {
         Pack<E, V> x[kAhead];
         uint32_t c[kAhead][V / 2];
+        const E *from[kAhead];
 #pragma unroll
         for (int r = 0; r < kAhead; r++) {
           uint32_t i, j, mine;
           place_of<V>(p, min(first + (r0 + r) * 64, items - 1), i, j, mine);
-          const E *from = in + i * ds.query + j;
           __builtin_memcpy(c[r], &codes[(r0 + r) * 64], sizeof c[r]);
           bool any = false;
 #pragma unroll
           for (int v = 0; v < V / 2; v++) any |= c[r][v] != none;
-          x[r] = {};
-          if (any) {
-            if (!short_row) x[r] = read_pack<E, V>(from);
-            else
-              for (int v = 0; v < V; v++) x[r].e[v] = from[min(v, (int)p.s.keys - 1)];
-          }
+          from[r] = in + (any ? i * ds.query + j : 0);  // lanes that want nothing read one place, and need no branch
+        }
+        if (!short_row) {
+#pragma unroll
+          for (int r = 0; r < kAhead; r++) x[r] = read_pack<E, V>(from[r]);
+        } else {
+#pragma unroll
+          for (int r = 0; r < kAhead; r++)
+#pragma unroll
+            for (int v = 0; v < V; v++) x[r].e[v] = from[r][min(v, (int)p.s.keys - 1)];
         }
 #pragma unroll
         for (int r = 0; r < kAhead; r++) {
@@ -299,6 +324,136 @@ __global__ __launch_bounds__(kThreads) void bias_grad_kernel(Shape p, int group,
     float v = 0.0f;
     for (int w = 0; w < waves; w++) v += lds[(w + 1) * own - ((group * p.buckets + 3) & ~3) + k];
     part[((int64_t)blockIdx.x * p.heads + h0) * p.buckets + k] = v;
+  }
+}
+
+// The same where positions are indices: then a bucket is a matter of key - query, of the diagonal.  A lane takes squares of V keys by V queries
+// one after another down a diagonal, which all have the same 2 V - 1 diagonals, and keeps their sums in registers: one addition an element,
+// and every load a whole pack.  64 lanes have neighbouring squares.  A wavefront's unit of work is 64 such columns of squares, `seg`
+// squares of each (of the same queries), for `samples` samples; at its end its diagonals are joined in LDS and added to their buckets.
+constexpr int kUnits = 8192;  // units that the work is cut into, if they have 4 squares at least
+
+struct Diagonals {
+  uint32_t squares;       // of V queries
+  uint32_t columns, segs, batches;  // units of a head
+  int seg, samples;
+};
+
+template <int DT, bool SCORES>
+__global__ __launch_bounds__(kThreads) void bias_grad_index_kernel(Shape p, Diagonals u, const typename Elem<DT>::type *dout, tbe_bias_strides ds,
+                                                                   float *part, float scale, typename Elem<DT>::type *dscores, tbe_bias_strides es) {
+  using E = typename Elem<DT>::type;
+  constexpr int V = 16 / sizeof(E), kDiagonals = 64 * V + V - 1;
+  __shared__ __align__(16) Finder find;
+  __shared__ float diagonals[kWaves][kDiagonals + 1];
+  extern __shared__ float sums[];  // [kWaves][buckets]
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, h = blockIdx.y;
+  float *diag = diagonals[wave], *sum = sums + wave * p.buckets;
+  load_finder(p, find);
+  for (int k = threadIdx.x; k < kWaves * p.buckets; k += kThreads) sums[k] = 0.0f;
+  __syncthreads();
+  const int keys = (int)p.s.keys, queries = (int)p.s.queries, packs = (int)p.packs, squares = (int)u.squares;
+  const int64_t units = (int64_t)u.columns * u.segs * u.batches;
+  const bool short_row = keys < V;
+  for (int64_t w = (int64_t)blockIdx.x * kWaves + wave; w < units; w += (int64_t)gridDim.x * kWaves) {
+    const int column = (int)(w % u.columns), s = (int)(w / u.columns % u.segs);
+    const int64_t b0 = w / u.columns / u.segs * u.samples, b1 = min(b0 + u.samples, p.s.batch);
+    const int first = 64 * column - (squares - 1), D = first + lane;  // key square less query square
+    const int lo = max(s * u.seg, -(first + 63)), hi = min(min((s + 1) * u.seg, squares), packs - first);
+    if (lo >= hi) continue;
+    const bool later = p.s.causal && (int64_t)D * V - (V - 1) - p.s.query_offset > 0;  // all of them masked
+    float acc[2 * V - 1];
+#pragma unroll
+    for (int k = 0; k < 2 * V - 1; k++) acc[k] = 0.0f;
+    for (int64_t b = b0; b < b1; b++) {
+      const int64_t len = p.s.d_key_lengths ? p.s.d_key_lengths[b] : p.s.keys;
+      const E *in = dout + b * ds.sample + h * ds.head;
+      for (int q = lo; q < hi; q++) {
+        const int j = (q + D) * V, i = q * V;
+        const bool on = q + D >= 0 && q + D < packs;
+        const int left = (int)max(min(len - j, (int64_t)V), (int64_t)0);  // keys that are not beyond the sample's
+        if (!on || (!SCORES && (later || left == 0))) continue;
+        Pack<E, V> x[V];
+        const int back = j + V > keys ? j + V - keys : 0;  // places of the last pack that are beyond the row
+        const E *from = in + (int64_t)i * ds.query + j - (short_row ? 0 : back);
+        const int64_t last = (int64_t)min(V, queries - i) - 1;
+        if (!short_row) {
+#pragma unroll
+          for (int r = 0; r < V; r++) x[r] = read_pack<E, V>(from + min((int64_t)r, last) * ds.query);
+          if (back)  // that pack ends where the row does: down with it
+#pragma unroll
+            for (int r = 0; r < V; r++) {
+              uint64_t v[2];
+              __builtin_memcpy(v, &x[r], 16);
+              const int bits = back * 8 * (int)sizeof(E);
+              const uint64_t lo = bits >= 64 ? v[1] >> (bits - 64) : v[0] >> bits | v[1] << (64 - bits);
+              v[1] = bits >= 64 ? 0 : v[1] >> bits;
+              v[0] = lo;
+              __builtin_memcpy(&x[r], v, 16);
+            }
+        } else {
+#pragma unroll
+          for (int r = 0; r < V; r++)
+#pragma unroll
+            for (int v = 0; v < V; v++) x[r].e[v] = from[min((int64_t)r, last) * ds.query + min(v, keys - 1)];
+        }
+        const int rows = queries - i;
+        if (!SCORES && left == V && rows >= V) {
+#pragma unroll
+          for (int r = 0; r < V; r++)
+#pragma unroll
+            for (int v = 0; v < V; v++) acc[V - 1 + v - r] += (float)x[r].e[v];
+          continue;
+        }
+#pragma unroll
+        for (int r = 0; r < V; r++) {
+#pragma unroll
+          for (int v = 0; v < V; v++) {
+            const float g = v < left && r < rows ? (float)x[r].e[v] : 0.0f;
+            acc[V - 1 + v - r] += g;
+            if (SCORES) x[r].e[v] = (E)(p.s.causal && (int64_t)D * V + v - r - p.s.query_offset > 0 ? 0.0f : g * scale);
+          }
+          if (SCORES && r < rows) {
+            E *to = dscores + b * es.sample + h * es.head + (int64_t)(i + r) * es.query + j;
+            if (!back) write_pack<E, V>(to, x[r]);
+            else
+#pragma unroll
+              for (int v = 0; v < V; v++)
+                if (j + v < keys) to[v] = x[r].e[v];
+          }
+        }
+      }
+    }
+    // diag[k]: diagonal first * V - (V - 1) + k.  A lane's upper V diagonals first, then its lower ones to the upper ones of the lane before
+#pragma unroll
+    for (int k = 0; k < V; k++) diag[lane * V + V - 1 + k] = acc[V - 1 + k];
+    if (lane < V - 1) diag[lane] = 0.0f;
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int k = 0; k < V - 1; k++) diag[lane * V + k] += acc[k];
+    __builtin_amdgcn_wave_barrier();
+    for (int k0 = 0; k0 < kDiagonals; k0 += 64) {
+      const int64_t ahead = (int64_t)first * V - (V - 1) + k0 + lane - p.s.query_offset;
+      const bool there = k0 + lane < kDiagonals && !(p.s.causal && ahead > 0);
+      const int c = bucket_of(p, find, ahead);
+      const float v = there ? diag[k0 + lane] : 0.0f;
+      uint64_t todo = __ballot(there);
+      while (todo) {  // a bucket at a time: one, unless the diagonals are near
+        const int one = __shfl(c, __ffsll((unsigned long long)todo) - 1);
+        const bool mine = there && c == one;
+        float r = mine ? v : 0.0f;
+        for (int k = 32; k; k >>= 1) r += __shfl_xor(r, k);
+        if (lane == 0) sum[one] += r;
+        todo &= ~__ballot(mine);
+      }
+    }
+    __builtin_amdgcn_wave_barrier();
+  }
+  __syncthreads();
+  for (int k = threadIdx.x; k < p.buckets; k += kThreads) {
+    float v = 0.0f;
+    for (int w = 0; w < kWaves; w++) v += sums[w * p.buckets + k];
+    part[((int64_t)blockIdx.x * p.heads + h) * p.buckets + k] = v;
   }
 }
 
@@ -432,6 +587,32 @@ int tbe_bias_backward(tbe_bias_handle s, const tbe_bias_shape *shape, const void
   const tbe_bias_strides es = d_dscores ? *dscores_strides : tbe_bias_strides{0, 0, 0};
   int parts = 0;
   if (any) {
+    if (!p.s.d_query_pos && !p.s.d_key_pos) {
+      // Units long enough that joining their diagonals does not count, and enough of them for all CUs.
+      const int V = 16 / elem_bytes(p.s.dtype);
+      Diagonals u;
+      u.squares = (uint32_t)((p.s.queries + V - 1) / V);
+      u.columns = (u.squares + p.packs - 1 + 63) / 64;
+      const int64_t squares = (int64_t)u.columns * u.squares * p.s.batch * p.heads;  // times 64, some of them beyond the scores
+      const int64_t steps = squares / kUnits < 4 ? 4 : squares / kUnits > 64 ? 64 : squares / kUnits;
+      u.seg = (int)(steps < u.squares ? steps : u.squares);
+      u.segs = (u.squares + u.seg - 1) / u.seg;
+      const int64_t samples = steps / u.seg;
+      u.samples = (int)(samples < p.s.batch ? samples : p.s.batch);
+      u.batches = (uint32_t)((p.s.batch + u.samples - 1) / u.samples);
+      const int64_t units = (int64_t)u.columns * u.segs * u.batches, blocks = (units + kWaves - 1) / kWaves;
+      parts = (int)(blocks < kMaxParts ? blocks : kMaxParts);
+      const dim3 grid((unsigned)parts, (unsigned)p.heads);
+      const size_t lds = (size_t)kWaves * p.buckets * sizeof(float);
+#define LAUNCH(DT, SCORES)                                                                                                                    \
+  bias_grad_index_kernel<DT, SCORES><<<grid, kThreads, lds, (hipStream_t)stream>>>(p, u, (const Elem<DT>::type *)d_dout, *dout_strides, s->part, scale, \
+                                                                                   (Elem<DT>::type *)d_dscores, es)
+#define LAUNCH2(DT) (d_dscores ? LAUNCH(DT, true) : LAUNCH(DT, false))
+      if (p.s.dtype == TBE_FP32) LAUNCH2(TBE_FP32);
+      else if (p.s.dtype == TBE_FP16) LAUNCH2(TBE_FP16);
+      else LAUNCH2(TBE_BF16);
+#undef LAUNCH
+    } else {
     // heads of a workgroup: all, unless their sums take more than 8 KB of a wavefront, or the tiles are too few to fill the GPU
     const int64_t tiles = (p.s.queries * p.packs + 64 * kTile - 1) / (64 * kTile) * p.s.batch;
     int group = p.heads;
@@ -448,6 +629,7 @@ int tbe_bias_backward(tbe_bias_handle s, const tbe_bias_shape *shape, const void
     if (p.s.dtype == TBE_FP32) LAUNCH2(TBE_FP32);
     else if (p.s.dtype == TBE_FP16) LAUNCH2(TBE_FP16);
     else LAUNCH2(TBE_BF16);
+    }
 #undef LAUNCH2
 #undef LAUNCH
   }
