@@ -203,28 +203,21 @@ __global__ __launch_bounds__(kThreads) void bias_forward_kernel(Shape p, int gro
   }
 }
 
-// Gradient of the table.  A wavefront takes tiles of 64 * kTile packs of keys, leaves their buckets in LDS and goes through the heads with them:
-// every lane adds to sums of its own in LDS, [buckets + 1][64 lanes] (no two lanes on one bank; the row more takes what is masked), the 64
-// lanes' sums of a head are then added up into the wavefront's [heads][buckets].  One lane, one order: the same bits each time.
-// (Additions by LDS atomics into fewer slots took several times as long: 711 us for the gradient of 16 x 8 x 1024 x 1024.)
-constexpr int kTile = 8, kAhead = 4;  // packs of a lane in a tile, and on their way at once
+// Gradient of the table.  A wavefront finds the buckets of 64 packs of keys at a time and keeps those packs that are not masked altogether in
+// a list in LDS.  Whenever the list has kRounds * 64 packs, it goes through the heads with them: every lane adds to sums of its own in LDS,
+// [buckets + 1][64 lanes] (no two lanes on one bank; the row more takes what is masked), and the 64 lanes' sums of a head are then
+// added up into the wavefront's [heads][buckets].  One lane, one order: the same bits each time.  What bounds it is the way through LDS
+// and back of each addition, so a masked pack costs nothing here.
+// (Additions by LDS atomics take several times as long, also without two lanes on one bank: 295 us instead of 81 for 256 x 4 x 199 x 199.)
+constexpr int kRounds = 4, kList = (kRounds + 1) * 64;
 
 // LDS of a wavefront, in floats
-__host__ __device__ inline int grad_floats(int buckets, int group, int V) { return (buckets + 1) * 64 + kTile * 64 * V / 2 + ((group * buckets + 3) & ~3); }
-
-// where a pack's keys lie (as find_keys has them)
-template <int V>
-__device__ inline void place_of(const Shape &p, uint32_t item, uint32_t &i, uint32_t &from, uint32_t &mine) {
-  const uint32_t keys = (uint32_t)p.s.keys;
-  i = div_by(item, p.packs_magic);
-  const uint32_t j = (item - i * p.packs) * V;
-  from = keys >= V && j + V > keys ? keys - V : j;
-  mine = ~((1u << (j - from)) - 1) & ((1u << min((uint32_t)V, keys - from)) - 1);
+__host__ __device__ inline int grad_floats(int buckets, int group, int V) {
+  return (buckets + 1) * 64 + kList * (V / 2 + 2) + ((group * buckets + 3) & ~3);
 }
 
-template <int DT, bool SCORES>
-__global__ __launch_bounds__(kThreads) void bias_grad_kernel(Shape p, int group, const typename Elem<DT>::type *dout, tbe_bias_strides ds, float *part,
-                                                             float scale, typename Elem<DT>::type *dscores, tbe_bias_strides es) {
+template <int DT>
+__global__ __launch_bounds__(kThreads) void bias_grad_kernel(Shape p, int group, const typename Elem<DT>::type *dout, tbe_bias_strides ds, float *part) {
   using E = typename Elem<DT>::type;
   constexpr int V = 16 / sizeof(E);
   using Codes = Pack<uint16_t, V>;
@@ -232,76 +225,53 @@ __global__ __launch_bounds__(kThreads) void bias_grad_kernel(Shape p, int group,
   extern __shared__ __align__(16) float lds[];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x / 64, h0 = blockIdx.y * group, heads = min(group, p.heads - h0);
   const int rows = p.buckets + 1, own = grad_floats(p.buckets, group, V);
-  float *lanes = lds + wave * own, *sum = lanes + rows * 64 + kTile * 64 * V / 2;
-  Codes *codes = (Codes *)(lanes + rows * 64) + lane;
+  float *lanes = lds + wave * own;
+  Codes *codes = (Codes *)(lanes + rows * 64);                   // [kList]
+  int64_t *from = (int64_t *)(codes + kList);                    // [kList]: where in dout
+  float *sum = (float *)(from + kList);
   load_finder(p, find);
   for (int k = threadIdx.x; k < waves * own; k += blockDim.x) lds[k] = 0.0f;
   __syncthreads();
-  const uint32_t items = (uint32_t)(p.s.queries * p.packs), tiles = (items + 64 * kTile - 1) / (64 * kTile);
-  const uint32_t none = (uint32_t)p.buckets | (uint32_t)p.buckets << 16;
+  const uint32_t items = (uint32_t)(p.s.queries * p.packs), steps = (items + 63) / 64;
   const bool short_row = p.s.keys < V;
-  // a row of lanes' sums is added up by 64 / width lanes
-  int width = 1;
+  int width = 1;  // 64 / width lanes add up a row of lanes' sums
   while (width < p.buckets && width < 64) width *= 2;
-  for (int64_t w = (int64_t)blockIdx.x * waves + wave; w < tiles * p.s.batch; w += (int64_t)gridDim.x * waves) {
-    const int64_t b = w / tiles;
-    const uint32_t first = (uint32_t)(w - b * tiles) * (64 * kTile) + lane;
-#pragma unroll 1
-    for (int r = 0; r < kTile; r++) {
-      const uint32_t item = first + r * 64;
-      Keys<V> k;
-      find_keys<V>(p, find, b, min(item, items - 1), k);
-      const uint32_t out = item < items ? k.masked | k.twice | ~((1u << k.n) - 1) : ~0u;
+
+  auto load = [&](int h, Pack<E, V>(&x)[kRounds]) {
+    const E *in = dout + (h0 + h) * ds.head;
+    if (!short_row) {
+#pragma unroll
+      for (int r = 0; r < kRounds; r++) x[r] = read_pack<E, V>(in + from[r * 64 + lane]);
+    } else {
+#pragma unroll
+      for (int r = 0; r < kRounds; r++)
+#pragma unroll
+        for (int v = 0; v < V; v++) x[r].e[v] = in[from[r * 64 + lane] + min(v, (int)p.s.keys - 1)];
+    }
+  };
+  // the first n packs of the list, through all heads
+  auto through_heads = [&](int n) {
+    for (int k = n + lane; k < kRounds * 64; k += 64) {  // places that no pack has taken
       Codes c;
 #pragma unroll
-      for (int v = 0; v < V; v++) c.e[v] = (uint16_t)(out >> v & 1 ? p.buckets : k.bucket[v]);
-      codes[r * 64] = c;
+      for (int v = 0; v < V; v++) c.e[v] = (uint16_t)p.buckets;
+      codes[k] = c;
+      from[k] = 0;
     }
+    __builtin_amdgcn_wave_barrier();
+    Pack<E, V> x[kRounds], next[kRounds];
+    load(0, next);
 #pragma unroll 1
     for (int h = 0; h < heads; h++) {
-      const E *in = dout + b * ds.sample + (h0 + h) * ds.head;
-#pragma unroll 1
-      for (int r0 = 0; r0 < kTile; r0 += kAhead) {
-        Pack<E, V> x[kAhead];
-        uint32_t c[kAhead][V / 2];
-        const E *from[kAhead];
 #pragma unroll
-        for (int r = 0; r < kAhead; r++) {
-          uint32_t i, j, mine;
-          place_of<V>(p, min(first + (r0 + r) * 64, items - 1), i, j, mine);
-          __builtin_memcpy(c[r], &codes[(r0 + r) * 64], sizeof c[r]);
-          bool any = false;
+      for (int r = 0; r < kRounds; r++) x[r] = next[r];
+      if (h + 1 < heads) load(h + 1, next);
 #pragma unroll
-          for (int v = 0; v < V / 2; v++) any |= c[r][v] != none;
-          from[r] = in + (any ? i * ds.query + j : 0);  // lanes that want nothing read one place, and need no branch
-        }
-        if (!short_row) {
+      for (int r = 0; r < kRounds; r++) {
+        if (r * 64 >= n) break;  // the same in all lanes
+        const Codes c = codes[r * 64 + lane];
 #pragma unroll
-          for (int r = 0; r < kAhead; r++) x[r] = read_pack<E, V>(from[r]);
-        } else {
-#pragma unroll
-          for (int r = 0; r < kAhead; r++)
-#pragma unroll
-            for (int v = 0; v < V; v++) x[r].e[v] = from[r][min(v, (int)p.s.keys - 1)];
-        }
-#pragma unroll
-        for (int r = 0; r < kAhead; r++) {
-#pragma unroll
-          for (int v = 0; v < V; v++) lanes[(v % 2 ? c[r][v / 2] >> 16 : c[r][v / 2] & 0xFFFFu) * 64 + lane] += (float)x[r].e[v];
-          if (SCORES) {
-            uint32_t i, j, mine;
-            place_of<V>(p, min(first + (r0 + r) * 64, items - 1), i, j, mine);
-            if (first + (r0 + r) * 64 >= items) mine = 0;
-            E *to = dscores + b * es.sample + (h0 + h) * es.head + i * es.query + j;
-#pragma unroll
-            for (int v = 0; v < V; v++)
-              x[r].e[v] = (E)((int)(v % 2 ? c[r][v / 2] >> 16 : c[r][v / 2] & 0xFFFFu) == p.buckets ? 0.0f : (float)x[r].e[v] * scale);
-            if (mine == (1u << V) - 1) write_pack<E, V>(to, x[r]);
-            else
-              for (int v = 0; v < V; v++)
-                if (mine >> v & 1) to[v] = x[r].e[v];
-          }
-        }
+        for (int v = 0; v < V; v++) lanes[c.e[v] * 64 + lane] += (float)x[r].e[v];
       }
       // lanes' sums of this head, and zeros for the next one's (the row of what is masked may hold anything)
       for (int c0 = 0; c0 < p.buckets; c0 += width) {
@@ -317,13 +287,88 @@ __global__ __launch_bounds__(kThreads) void bias_grad_kernel(Shape p, int group,
         for (int k = width; k < 64; k *= 2) v += __shfl_xor(v, k);
         if (c < p.buckets && lane < width) sum[h * p.buckets + c] += v;
       }
+      __builtin_amdgcn_wave_barrier();
+    }
+  };
+
+  int n = 0;  // packs in the list
+  for (int64_t w = (int64_t)blockIdx.x * waves + wave; w < steps * p.s.batch; w += (int64_t)gridDim.x * waves) {
+    const int64_t b = w / steps;
+    const uint32_t item = (uint32_t)(w - b * steps) * 64 + lane;
+    Keys<V> k;
+    find_keys<V>(p, find, b, min(item, items - 1), k);
+    const uint32_t mine = item < items ? ~k.twice & ((1u << k.n) - 1) : 0u, out = k.masked | ~mine;
+    Codes c;
+    bool any = false;
+#pragma unroll
+    for (int v = 0; v < V; v++) {
+      c.e[v] = (uint16_t)(out >> v & 1 ? p.buckets : k.bucket[v]);
+      any |= c.e[v] != p.buckets;
+    }
+    const uint64_t listed = __ballot(any);
+    if (any) {
+      const int at = n + __popcll(listed & ((1ull << lane) - 1));
+      codes[at] = c;
+      from[at] = b * ds.sample + k.i * ds.query + k.j;
+    }
+    n += __popcll(listed);
+    __builtin_amdgcn_wave_barrier();
+    if (n >= kRounds * 64) {
+      through_heads(kRounds * 64);
+      n -= kRounds * 64;
+      if (lane < n) {  // what the list had more is its beginning now
+        codes[lane] = codes[kRounds * 64 + lane];
+        from[lane] = from[kRounds * 64 + lane];
+      }
+      __builtin_amdgcn_wave_barrier();
     }
   }
+  if (n) through_heads(n);
   __syncthreads();
   for (int k = threadIdx.x; k < heads * p.buckets; k += blockDim.x) {
     float v = 0.0f;
     for (int w = 0; w < waves; w++) v += lds[(w + 1) * own - ((group * p.buckets + 3) & ~3) + k];
     part[((int64_t)blockIdx.x * p.heads + h0) * p.buckets + k] = v;
+  }
+}
+
+// Gradient of the scores where positions are given: an element at a time, after the table's (in place it may take d_dout's place).
+template <int DT>
+__global__ __launch_bounds__(kThreads) void bias_scores_kernel(Shape p, const typename Elem<DT>::type *dout, tbe_bias_strides ds, float scale,
+                                                               typename Elem<DT>::type *dscores, tbe_bias_strides es) {
+  using E = typename Elem<DT>::type;
+  constexpr int V = 16 / sizeof(E);
+  const int64_t items = p.s.queries * p.packs, blocks = (items + kThreads - 1) / kThreads;
+  for (int64_t w = blockIdx.x; w < blocks * p.s.batch; w += gridDim.x) {
+    const int64_t b = w / blocks, item = (w - b * blocks) * kThreads + threadIdx.x;
+    if (item >= items) continue;
+    const int64_t i = (int64_t)div_by((uint32_t)item, p.packs_magic), j = (item - i * p.packs) * V;
+    const int64_t q = p.s.d_query_pos ? p.s.d_query_pos[b * p.s.query_pos_stride + i] : p.s.query_offset + i;
+    const int64_t len = p.s.d_key_lengths ? p.s.d_key_lengths[b] : p.s.keys;
+    const int n = (int)min((int64_t)V, p.s.keys - j);
+    uint32_t keep = 0;
+#pragma unroll
+    for (int v = 0; v < V; v++) {
+      const int64_t at = j + min(v, n - 1), pos = p.s.d_key_pos ? p.s.d_key_pos[b * p.s.key_pos_stride + at] : at;
+      const bool later = p.s.causal && pos > q, beyond = j + v >= len;
+      keep |= (later | beyond) ? 0u : 1u << v;
+    }
+    for (int h = 0; h < p.heads; h++) {
+      const E *in = dout + b * ds.sample + h * ds.head + i * ds.query + j;
+      E *to = dscores + b * es.sample + h * es.head + i * es.query + j;
+      Pack<E, V> x;
+      if (n == V) x = read_pack<E, V>(in);
+      else
+#pragma unroll
+        for (int v = 0; v < V; v++) x.e[v] = in[min(v, n - 1)];
+#pragma unroll
+      for (int v = 0; v < V; v++) x.e[v] = (E)(keep >> v & 1 ? (float)x.e[v] * scale : 0.0f);
+      if (n == V) write_pack<E, V>(to, x);
+      else
+#pragma unroll
+        for (int v = 0; v < V; v++)
+          if (v < n) to[v] = x.e[v];
+    }
   }
 }
 
@@ -611,27 +656,33 @@ int tbe_bias_backward(tbe_bias_handle s, const tbe_bias_shape *shape, const void
       if (p.s.dtype == TBE_FP32) LAUNCH2(TBE_FP32);
       else if (p.s.dtype == TBE_FP16) LAUNCH2(TBE_FP16);
       else LAUNCH2(TBE_BF16);
-#undef LAUNCH
-    } else {
-    // heads of a workgroup: all, unless their sums take more than 8 KB of a wavefront, or the tiles are too few to fill the GPU
-    const int64_t tiles = (p.s.queries * p.packs + 64 * kTile - 1) / (64 * kTile) * p.s.batch;
-    int group = p.heads;
-    while (group > 1 && group * p.buckets > kSums) group = (group + 1) / 2;
-    while (group > 1 && tiles * ((p.heads + group - 1) / group) < kFill) group = (group + 1) / 2;
-    const int waves = p.buckets <= 128 ? 4 : 2;
-    parts = (int)((tiles + waves - 1) / waves < kMaxParts ? (tiles + waves - 1) / waves : kMaxParts);
-    const dim3 grid((unsigned)parts, (unsigned)((p.heads + group - 1) / group));
-    const size_t lds = (size_t)waves * grad_floats(p.buckets, group, 16 / elem_bytes(p.s.dtype)) * sizeof(float);
-#define LAUNCH(DT, SCORES)                                                                                                                 \
-  bias_grad_kernel<DT, SCORES><<<grid, 64 * waves, lds, (hipStream_t)stream>>>(p, group, (const Elem<DT>::type *)d_dout, *dout_strides, s->part, \
-                                                                             scale, (Elem<DT>::type *)d_dscores, es)
-#define LAUNCH2(DT) (d_dscores ? LAUNCH(DT, true) : LAUNCH(DT, false))
-    if (p.s.dtype == TBE_FP32) LAUNCH2(TBE_FP32);
-    else if (p.s.dtype == TBE_FP16) LAUNCH2(TBE_FP16);
-    else LAUNCH2(TBE_BF16);
-    }
 #undef LAUNCH2
 #undef LAUNCH
+    } else {
+      // heads of a workgroup: all, unless their sums take more than 8 KB of a wavefront, or there are too few packs to fill the GPU
+      const int64_t steps = (p.s.queries * p.packs + 63) / 64 * p.s.batch, lists = (steps + kRounds - 1) / kRounds;
+      int group = p.heads;
+      while (group > 1 && group * p.buckets > kSums) group = (group + 1) / 2;
+      while (group > 1 && lists * ((p.heads + group - 1) / group) < kFill) group = (group + 1) / 2;
+      const int waves = p.buckets <= 128 ? 4 : 2;
+      parts = (int)((lists + waves - 1) / waves < kMaxParts ? (lists + waves - 1) / waves : kMaxParts);
+      const dim3 grid((unsigned)parts, (unsigned)((p.heads + group - 1) / group));
+      const size_t lds = (size_t)waves * grad_floats(p.buckets, group, 16 / elem_bytes(p.s.dtype)) * sizeof(float);
+      const int64_t blocks = blocks_of(p);
+      const dim3 all((unsigned)(blocks < 4096 ? blocks : 4096));
+#define LAUNCH2(DT)                                                                                                                              \
+  do {                                                                                                                                           \
+    if (d_dtable)                                                                                                                                \
+      bias_grad_kernel<DT><<<grid, 64 * waves, lds, (hipStream_t)stream>>>(p, group, (const Elem<DT>::type *)d_dout, *dout_strides, s->part);    \
+    if (d_dscores)                                                                                                                               \
+      bias_scores_kernel<DT><<<all, kThreads, 0, (hipStream_t)stream>>>(p, (const Elem<DT>::type *)d_dout, *dout_strides, scale,                 \
+                                                                        (Elem<DT>::type *)d_dscores, es);                                        \
+  } while (0)
+      if (p.s.dtype == TBE_FP32) LAUNCH2(TBE_FP32);
+      else if (p.s.dtype == TBE_FP16) LAUNCH2(TBE_FP16);
+      else LAUNCH2(TBE_BF16);
+    }
+#undef LAUNCH2
   }
   if (d_dtable)
     bias_join_kernel<<<dim3((unsigned)((p.heads * p.buckets + kWaves - 1) / kWaves)), kThreads, 0, (hipStream_t)stream>>>(s->part, parts, p.heads,
