@@ -31,7 +31,7 @@ SOURCES = ["tbe_api.hip", "tbe_sort.hip", "tbe_cache.hip", "tbe_one.hip", "tbe_m
 FLAGS = ["-O3", "-std=c++17", "--offload-arch=gfx950", "-fPIC",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops", "-Wall", "-Wno-unused-function"]
 IMPATIENT = {polls: os.path.join(HERE, f"libtbe_polls{polls}.so") for polls in (0, 1)}
-POLLING = ["tbe_sort.hip", "tbe_cache.hip"]  # the sources whose kernels look
+POLLING = ["tbe_sort.hip", "tbe_cache.hip", "tbe_scan.hip"]  # the sources whose kernels look
 REMARKS = ["-Rpass-analysis=kernel-resource-usage"]
 HARMLESS = "'-packed-fp32-ops' is not a recognized feature for this target (ignoring feature)"
 MIN_VGPRS = {"transfer_kernel": 128}  # kernel-name substring -> fewest vector registers it must allocate

@@ -4,11 +4,14 @@
 // A row maps the state h to a h + b, element by element, with a = f and b = (1 - f) x (or x); where a bag starts the state
 // before does not count: a = 0, b = f h0 + ....  Two such maps, one after the other, are one again, (a2 a1, a2 b1 + b2), so the
 // rows of all bags are cut into chunks of equal length wherever the bags begin, and no bag's length matters:
-//   sum    every chunk's map, from the rows after the last start in it                       (scan_sum_kernel)
-//   join   the states before the chunks, by a scan over the chunks' maps                     (scan_join_kernel)
-//   apply  every chunk's rows from the state before it                                       (scan_apply_kernel, scan_grad_kernel)
-// One chunk needs the last one only.  The gradient runs the other way with c_t = f_t g_t = f_t (dy_t + c_{t+1}), reset where a bag
-// ends, beside the forward's states again from those before the chunks, which the forward saved.
+//   prepare  where the chunks' bags begin; the offsets are looked over           (scan_prepare_kernel)
+//   sum      every chunk's map, from the rows after the last start in it         (scan_sum_kernel)
+//   join     the states before the chunks, by a scan over the chunks' maps       (scan_join_kernel)
+//   apply    every chunk's rows from the state before it                         (scan_apply_kernel, scan_grad_kernel)
+// One chunk needs the last one only.  Where bags are short, most chunks have a start and so a state behind them that nothing before
+// them has a part in: then there are no `sum` and `join`, and `apply` hears from the chunks before (behind) it, see hear_from.
+// The gradient runs the other way with c_t = f_t g_t = f_t (dy_t + c_{t+1}), reset where a bag ends, beside the forward's states again
+// from those before the chunks, which the forward saved.
 //
 // A row lies on L lanes of V elements (16 bytes; one element where dim is no multiple of that), a lane has R rows in a row in
 // registers, 32 elements of each input.  The maps of a wavefront's 64 / L lane groups are joined by exchange between lanes, those of
@@ -17,12 +20,14 @@
 #include <new>
 
 #include "tbe_dense.h"
+#include "tbe_internal.h"
 
 using namespace tbe;
 
 namespace {
 
 constexpr int kThreads = 256, kWaves = kThreads / 64;
+constexpr int64_t kChainedBags = 2;  // chunks that a bag may have on average for them to hear from each other
 constexpr int kJoinChannels = 16, kJoinSegments = 64;
 
 // How the rows of a handle are cut: a function of dim and the type alone, because the backward uses what the forward saved.
@@ -76,10 +81,12 @@ struct Rows {
   float *maps;          // [chunks][2][dim]: a and b of the chunks
   float *before;        // [chunks][dim]: states before the chunks
   float *behind;        // [chunks][dim]: c behind the chunks
+  uint64_t *words;      // [chunks][2][dim]: what chunks say to each other
+  const uint32_t *call;  // number of this call
   int64_t h0s, bags, rows;
   int32_t *bag_of, *err;  // bag_of[chunks]: first bag that a chunk looks at
   int dim, L, tiles, chunk_rows, chunks;
-  bool coupled;
+  bool coupled, chained;  // chained: chunks hear from each other instead of sum and join
 };
 
 template <class E, int V, bool ALIGNED>
@@ -103,19 +110,32 @@ __device__ inline void store_pack(E *p, const Pack<E, V> &r) {
   }
 }
 
-// first bag that ends at `row` or behind it (bags if none): every wavefront for itself, 64 places at a time
-__device__ inline int64_t first_bag(const int64_t *off, int64_t bags, int64_t row) {
-  const int lane = threadIdx.x & 63;
-  int64_t lo = 0, hi = bags;  // it is one of lo .. hi
-  while (lo < hi) {
-    const int64_t step = (hi - lo + 63) / 64, p = lo + (lane + 1) * step - 1;
-    const uint64_t there = __ballot(p >= hi || off[p + 1] >= row);
-    if (!there) return hi;
-    const int64_t k = __ffsll((unsigned long long)there) - 1;
-    hi = min(hi, lo + (k + 1) * step - 1);
-    lo += k * step;
+// For every chunk the first bag that ends at its first row or behind it; offsets that do not ascend from 0 to rows are reported; the
+// words of this call get a number of their own.
+__global__ __launch_bounds__(kThreads) void scan_prepare_kernel(const int64_t *off, int64_t bags, int64_t rows, int chunk_rows, int chunks, int32_t *bag_of,
+                                                                uint32_t *call, int32_t *err) {
+  const int64_t b = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+  if (b == 0) ++*call;
+  int first = 0, n = 0;  // chunks first .. first + n - 1 have this bag
+  if (b < bags) {
+    const int64_t before = b ? off[b] : -1, s = off[b], e = off[b + 1];
+    if (s > e || s < 0 || e > rows || (b == 0 && s != 0) || (b == bags - 1 && e != rows)) {
+      *err = 1;
+    } else {
+      first = before < 0 ? 0 : (int)(before / chunk_rows) + 1;
+      n = (int)min(e / chunk_rows + 1, (int64_t)chunks) - first;
+    }
   }
-  return lo;
+  if (n > 0 && n <= 2) {
+    bag_of[first] = (int32_t)b;
+    if (n == 2) bag_of[first + 1] = (int32_t)b;
+  }
+  uint64_t longer = __ballot(n > 2);  // a long bag at a time, by the whole wavefront
+  while (longer) {
+    const int l = __ffsll((unsigned long long)longer) - 1, lf = __shfl(first, l), ln = __shfl(n, l), lb = __shfl((int)b, l);
+    for (int k = threadIdx.x & 63; k < ln; k += 64) bag_of[lf + k] = lb;
+    longer &= longer - 1;
+  }
 }
 
 // Where the chunk's bags start and end: marks[2 r] is 1 + the bag that starts at row r of the chunk, marks[2 r + 1] 1 + the bag whose last
@@ -132,7 +152,7 @@ __device__ inline void mark_bags(const A &a, int chunk, int64_t row0, int64_t fr
   for (int64_t b = from + group; b < a.bags; b += groups) {
     const int64_t s = a.off[b], e = a.off[b + 1];
     if (s >= end && !very_last) break;
-    if (s < 0 || s > e || e > a.rows) continue;  // check_offsets reports it
+    if (s < 0 || s > e || e > a.rows) continue;  // reported already
     if (s == e) {
       if (s >= row0 && (s < end || very_last)) empty(b);
     } else if (l == 0) {
@@ -149,12 +169,101 @@ __device__ inline void mark_bags(const A &a, int chunk, int64_t row0, int64_t fr
   __syncthreads();
 }
 
-// all offsets, once in a call
-template <class A>
-__device__ inline void check_offsets(const A &a) {
-  const int64_t id = (int64_t)blockIdx.x * kThreads + threadIdx.x, n = (int64_t)gridDim.x * kThreads;
-  for (int64_t b = id; b < a.bags; b += n)
-    if (a.off[b] > a.off[b + 1] || (b == 0 && a.off[0] != 0) || (b == a.bags - 1 && a.off[a.bags] != a.rows)) *a.err = 1;
+// A word is a number with the call and what it is: the state behind (BACK: before) a chunk, or the b of its map, whose a is in the second
+// word.  Each word says by itself whether it is there.
+constexpr uint32_t kSaysMap = 1, kSaysState = 2;
+__device__ inline uint64_t word_of(float v, uint32_t call, uint32_t kind) { return (uint64_t)(call << 2 | kind) << 32 | __float_as_uint(v); }
+__device__ inline void put_word(uint64_t *p, uint64_t v) { __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+
+// Workgroups begin in the order of their numbers as a rule, but nothing waits for that: where a chunk has said nothing for as many looks as
+// this, the rows of the bag are gone through from its start.
+constexpr int kLooks = 16 * kPolls;  // a millisecond or so
+__device__ inline bool get_word(const uint64_t *p, uint64_t &w, uint32_t call) {  // w: what a first look found
+  for (int k = 0; (uint32_t)(w >> 34) != (call & 0x3FFFFFFFu); k++) {
+    if (k >= kLooks) return false;
+    __builtin_amdgcn_s_sleep(1);
+    w = look(p);
+  }
+  return true;
+}
+
+// The state before the chunk (BACK: behind it), for element d: from the nearest chunk that has said its state, through the maps of those in
+// between, one after the other.  Every state that is said was found in this order too, so it has the same bits wherever it is found.
+template <bool BACK, class A>
+__device__ inline bool hear_from(const A &a, int chunk, int d, uint32_t call, float &s) {
+  constexpr int kAtOnce = 4;
+  const int n = BACK ? a.chunks - 1 - chunk : chunk;  // chunks before this one; the first of them always says its state
+  s = 0.0f;
+  if (n == 0) return true;
+  const uint64_t *first = a.words + (int64_t)(BACK ? chunk + 1 : chunk - 1) * 2 * a.dim + d;
+  const int64_t step = (BACK ? 2 : -2) * (int64_t)a.dim;
+  int k = 0;  // chunks to go through
+  for (bool found = false; !found;) {
+    uint64_t w[kAtOnce];
+#pragma unroll
+    for (int q = 0; q < kAtOnce; q++) w[q] = look(first + min(k + q, n - 1) * step);
+#pragma unroll
+    for (int q = 0; q < kAtOnce; q++) {
+      if (found) continue;
+      if (!get_word(first + min(k, n - 1) * step, w[q], call)) return false;
+      found = (w[q] >> 32 & 3) == kSaysState;
+      s = __uint_as_float((uint32_t)w[q]);
+      k += found ? 0 : 1;
+    }
+  }
+  while (k > 0) {
+    uint64_t h[kAtOnce], m[kAtOnce];
+#pragma unroll
+    for (int q = 0; q < kAtOnce; q++) {
+      const uint64_t *p = first + max(k - 1 - q, 0) * step;
+      h[q] = look(p);
+      m[q] = look(p + a.dim);
+    }
+#pragma unroll
+    for (int q = 0; q < kAtOnce; q++) {
+      if (k == 0) continue;
+      k--;
+      if ((h[q] >> 32 & 3) == kSaysState) s = __uint_as_float((uint32_t)h[q]);
+      else if (!get_word(first + k * step + a.dim, m[q], call)) return false;
+      else s = go(__uint_as_float((uint32_t)m[q]), __uint_as_float((uint32_t)h[q]), s);
+    }
+  }
+  return true;
+}
+
+// The same from the rows themselves.  Where a bag starts (ends) with the chunk, nothing asks for it.
+template <bool BACK, class A>
+__device__ float walk_to(const A &a, int chunk, int d) {
+  const int64_t row = (int64_t)(BACK ? chunk + 1 : chunk) * a.chunk_rows, b = a.bag_of[BACK ? chunk + 1 : chunk];
+  if (b >= a.bags) return 0.0f;
+  const int64_t lo = a.off[b], hi = a.off[b + 1];
+  if (lo < 0 || lo >= row || hi <= row || hi > a.rows) return 0.0f;
+  float s = BACK ? (a.dlast ? a.dlast[b * a.dim + d] : 0.0f) : (a.h0 ? a.h0[b * a.h0s + d] : 0.0f);
+  for (int64_t k = 0; k < (BACK ? hi - row : row - lo); k++) {
+    const int64_t t = BACK ? hi - 1 - k : lo + k;
+    const float q = gate((float)a.u[t * a.us + d]);
+    if (BACK) s = keep_of(q) * ((a.dy ? (float)a.dy[t * a.dys + d] : 0.0f) + s);
+    else s = keep_of(q) * s + (a.coupled ? take_of(q) : 1.0f) * (float)a.x[t * a.xs + d];
+  }
+  return s;
+}
+
+// What the chunk says of element d: its state where nothing before it has a part in that, else its map; then, told the state before it, the
+// one behind it.  Returns the state before it.
+template <bool BACK, class A>
+__device__ inline float hear_and_say(const A &a, int chunk, int d, uint32_t call, float A1, float H1) {
+  uint64_t *w = a.words + (int64_t)chunk * 2 * a.dim + d;
+  const bool known = signbit(A1);
+  if (known) {
+    put_word(w, word_of(H1, call, kSaysState));
+  } else {
+    put_word(w + a.dim, word_of(A1, call, kSaysMap));
+    put_word(w, word_of(H1, call, kSaysMap));
+  }
+  float s;
+  if (!hear_from<BACK>(a, chunk, d, call, s)) s = walk_to<BACK>(a, chunk, d);
+  if (!known) put_word(w, word_of(go(A1, H1, s), call, kSaysState));
+  return s;
 }
 
 // (A, H) becomes the map of all lane groups of the wavefront up to this one (BACK: from the last one down to it)
@@ -171,8 +280,8 @@ __device__ inline void scan_wave(float (&A)[V], float (&H)[V], int L) {
   }
 }
 
-// The wavefronts' maps go to LDS (tot: [kWaves][2][C]); join_waves, a lane for an element, leaves there the states before (behind)
-// the wavefronts and returns that after all of them; start_of_lane goes on from there to that before (behind) the lane's rows.
+// The wavefronts' maps go to LDS (tot: [kWaves][2][C]); map_of_waves, a lane for an element, has the map of all of them, join_waves leaves
+// there the states before (behind) the wavefronts; start_of_lane goes on from there to that before (behind) the lane's rows.
 template <int V, bool BACK>
 __device__ inline void tell_wave(const float (&A)[V], const float (&H)[V], int L, float *tot) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, C = L * V, c = (lane & (L - 1)) * V;
@@ -184,14 +293,25 @@ __device__ inline void tell_wave(const float (&A)[V], const float (&H)[V], int L
     }
 }
 template <bool BACK>
-__device__ inline void join_waves(float *tot, int C, int c, float &A, float &s) {
+__device__ inline void map_of_waves(const float *tot, int C, int c, float &A, float &H) {
+  A = 1.0f;
+  H = 0.0f;
+#pragma unroll
+  for (int k = 0; k < kWaves; k++) {
+    const int w = BACK ? kWaves - 1 - k : k;
+    const float wa = tot[(w * 2) * C + c], wh = tot[(w * 2 + 1) * C + c];
+    H = go(wa, wh, H);
+    A = signbit(wa) ? wa : wa * A;
+  }
+}
+template <bool BACK>
+__device__ inline void join_waves(float *tot, int C, int c, float s) {
 #pragma unroll
   for (int k = 0; k < kWaves; k++) {
     const int w = BACK ? kWaves - 1 - k : k;
     const float wa = tot[(w * 2) * C + c], wh = tot[(w * 2 + 1) * C + c];
     tot[(w * 2) * C + c] = s;
     s = go(wa, wh, s);
-    A = signbit(wa) ? wa : wa * A;
   }
 }
 template <int V, bool BACK>
@@ -218,10 +338,8 @@ __global__ __launch_bounds__(kThreads) void scan_sum_kernel(Rows<DT> a) {
   __shared__ int32_t edge[2];
   const int chunk = blockIdx.x / a.tiles, tile = blockIdx.x % a.tiles, C = a.L * V;
   int32_t *marks = (int32_t *)(lds + kWaves * 2 * C);
-  const int64_t row0 = (int64_t)chunk * a.chunk_rows, from = first_bag(a.off, a.bags, row0);
-  if (threadIdx.x == 0) a.bag_of[chunk] = (int32_t)from;  // the same from every tile
-  check_offsets(a);
-  mark_bags(a, chunk, row0, from, marks, edge, [](int64_t) {});
+  const int64_t row0 = (int64_t)chunk * a.chunk_rows;
+  mark_bags(a, chunk, row0, a.bag_of[chunk], marks, edge, [](int64_t) {});
   const int group = threadIdx.x / a.L, l = threadIdx.x & (a.L - 1), c0 = (tile * a.L + l) * V, r0 = group * R;
   const int rows = (int)min((int64_t)a.chunk_rows, a.rows - row0), lo = BACK ? 0 : edge[0], hi = BACK ? min(edge[1], rows - 1) : rows - 1;
   const E *in = BACK ? a.dy : a.x;
@@ -264,10 +382,10 @@ __global__ __launch_bounds__(kThreads) void scan_sum_kernel(Rows<DT> a) {
   tell_wave<V, BACK>(A, H, a.L, lds);
   __syncthreads();
   for (int c = threadIdx.x; c < C && tile * C + c < a.dim; c += kThreads) {
-    float A1 = 1.0f, s = 0.0f;
-    join_waves<BACK>(lds, C, c, A1, s);
+    float A1, H1;
+    map_of_waves<BACK>(lds, C, c, A1, H1);
     a.maps[(int64_t)chunk * 2 * a.dim + tile * C + c] = A1;
-    a.maps[((int64_t)chunk * 2 + 1) * a.dim + tile * C + c] = s;
+    a.maps[((int64_t)chunk * 2 + 1) * a.dim + tile * C + c] = H1;
   }
 }
 
@@ -334,8 +452,7 @@ __global__ __launch_bounds__(kThreads) void scan_apply_kernel(Rows<DT> a) {
       xv[j] = load_pack<E, V, ALIGNED>(a.x + (row0 + r0 + j) * a.xs + c0);
     }
   }
-  if (a.chunks == 1) check_offsets(a);
-  mark_bags(a, chunk, row0, a.chunks > 1 ? a.bag_of[chunk] : 0, marks, edge, [&](int64_t b) {
+  mark_bags(a, chunk, row0, a.bag_of[chunk], marks, edge, [&](int64_t b) {
     if (a.last && on)
 #pragma unroll
       for (int v = 0; v < V; v++) a.last[b * a.dim + c0 + v] = a.h0 ? a.h0[b * a.h0s + c0 + v] : 0.0f;
@@ -364,8 +481,20 @@ __global__ __launch_bounds__(kThreads) void scan_apply_kernel(Rows<DT> a) {
   tell_wave<V, false>(A, H, a.L, lds);
   __syncthreads();
   for (int c = threadIdx.x; c < C; c += kThreads) {
-    float A1 = 1.0f, s = a.chunks > 1 && tile * C + c < a.dim ? a.before[(int64_t)chunk * a.dim + tile * C + c] : 0.0f;
-    join_waves<false>(lds, C, c, A1, s);
+    const int d = tile * C + c;
+    float s = 0.0f;
+    if (a.chunks > 1 && d < a.dim) {
+      float *before = a.before ? a.before + (int64_t)chunk * a.dim + d : nullptr;
+      if (a.chained) {
+        float A1, H1;
+        map_of_waves<false>(lds, C, c, A1, H1);
+        s = hear_and_say<false>(a, chunk, d, *a.call, A1, H1);
+        if (before) *before = s;
+      } else {
+        s = *before;
+      }
+    }
+    join_waves<false>(lds, C, c, s);
   }
   __syncthreads();
   float h[V];
@@ -397,7 +526,8 @@ __global__ __launch_bounds__(kThreads) void scan_grad_kernel(Rows<DT> a) {
   constexpr int R = 32 / V;
   extern __shared__ float lds[];
   __shared__ int32_t edge[2];
-  const int chunk = blockIdx.x / a.tiles, tile = blockIdx.x % a.tiles, C = a.L * V;
+  // from the last chunk on: what a chunk hears of is behind it
+  const int chunk = a.chunks - 1 - blockIdx.x / a.tiles, tile = blockIdx.x % a.tiles, C = a.L * V;
   float *back = lds + kWaves * 2 * C;
   int32_t *marks = (int32_t *)(back + kWaves * 2 * C);
   const int64_t row0 = (int64_t)chunk * a.chunk_rows;
@@ -416,8 +546,7 @@ __global__ __launch_bounds__(kThreads) void scan_grad_kernel(Rows<DT> a) {
       if (a.dy) gv[j] = load_pack<E, V, ALIGNED>(a.dy + (row0 + r0 + j) * a.dys + c0);
     }
   }
-  if (a.chunks == 1) check_offsets(a);
-  mark_bags(a, chunk, row0, a.chunks > 1 ? a.bag_of[chunk] : 0, marks, edge, [&](int64_t b) {
+  mark_bags(a, chunk, row0, a.bag_of[chunk], marks, edge, [&](int64_t b) {
     if (a.dh0 && on)
 #pragma unroll
       for (int v = 0; v < V; v++) a.dh0[b * a.dim + c0 + v] = a.dlast ? a.dlast[b * a.dim + c0 + v] : 0.0f;
@@ -464,11 +593,20 @@ __global__ __launch_bounds__(kThreads) void scan_grad_kernel(Rows<DT> a) {
   tell_wave<V, true>(B, G, a.L, back);
   __syncthreads();
   for (int c = threadIdx.x; c < C; c += kThreads) {
-    const bool in = a.chunks > 1 && tile * C + c < a.dim;
-    float A1 = 1.0f, s = in ? a.before[(int64_t)chunk * a.dim + tile * C + c] : 0.0f;
-    join_waves<false>(lds, C, c, A1, s);
-    s = in ? a.behind[(int64_t)chunk * a.dim + tile * C + c] : 0.0f;
-    join_waves<true>(back, C, c, A1, s);
+    const int d = tile * C + c;
+    float s = 0.0f, g = 0.0f;
+    if (a.chunks > 1 && d < a.dim) {
+      s = a.before[(int64_t)chunk * a.dim + d];
+      if (a.chained) {
+        float A1, H1;
+        map_of_waves<true>(back, C, c, A1, H1);
+        g = hear_and_say<true>(a, chunk, d, *a.call, A1, H1);
+      } else {
+        g = a.behind[(int64_t)chunk * a.dim + d];
+      }
+    }
+    join_waves<false>(lds, C, c, s);
+    join_waves<true>(back, C, c, g);
   }
   __syncthreads();
   float h[R][V], s[V];
@@ -549,6 +687,8 @@ struct tbe_scan_t : DenseBase {
   float *maps = nullptr;     // device [chunks][2][dim]
   float *states = nullptr;   // device [chunks][dim]: before the chunks where the caller saves none, behind them in the backward
   int32_t *bag_of = nullptr; // device [chunks]
+  uint32_t *call = nullptr;  // device: number of the call
+  uint64_t *words = nullptr; // device [chunks][2][dim]
 };
 
 namespace {
@@ -574,14 +714,17 @@ template <int DT, int V, bool ALIGNED>
 int run(const tbe_scan_t *s, const Rows<DT> &a, bool grad, hipStream_t stream) noexcept {
   const dim3 grid((unsigned)(a.chunks * a.tiles)), joins((unsigned)((a.dim + kJoinChannels - 1) / kJoinChannels));
   const size_t tot = (size_t)kWaves * 2 * a.L * V * sizeof(float), marks = (size_t)a.chunk_rows * 2 * sizeof(int32_t);
+  scan_prepare_kernel<<<dim3((unsigned)((a.bags + kThreads - 1) / kThreads)), kThreads, 0, stream>>>(a.off, a.bags, a.rows, a.chunk_rows, a.chunks, a.bag_of,
+                                                                                                  s->call, a.err);
+  const bool joined = a.chunks > 1 && !a.chained;
   if (!grad) {
-    if (a.chunks > 1) {
+    if (joined) {
       scan_sum_kernel<DT, V, ALIGNED, false><<<grid, kThreads, tot + marks, stream>>>(a);
       scan_join_kernel<false><<<joins, kJoinChannels * kJoinSegments, 0, stream>>>(a.maps, a.before, a.chunks, a.dim);
     }
     scan_apply_kernel<DT, V, ALIGNED><<<grid, kThreads, tot + marks, stream>>>(a);
   } else {
-    if (a.chunks > 1) {
+    if (joined) {
       scan_sum_kernel<DT, V, ALIGNED, true><<<grid, kThreads, tot + marks, stream>>>(a);
       scan_join_kernel<true><<<joins, kJoinChannels * kJoinSegments, 0, stream>>>(a.maps, a.behind, a.chunks, a.dim);
     }
@@ -617,6 +760,8 @@ Rows<DT> rows_of(const tbe_scan_t *s, const void *x, int64_t xs, const void *u, 
   a.h0s = h0s;
   a.maps = s->maps;
   a.bag_of = s->bag_of;
+  a.words = s->words;
+  a.call = s->call;
   a.err = s->err;
   a.dim = s->dim;
   a.L = s->cut.L;
@@ -624,6 +769,8 @@ Rows<DT> rows_of(const tbe_scan_t *s, const void *x, int64_t xs, const void *u, 
   a.chunk_rows = s->cut.rows;
   a.chunks = (int)chunks_of(s, rows);
   a.coupled = s->coupled;
+  // A chunk of mean rows or more has a start as a rule; with longer bags the chunks would wait for long chains of others.
+  a.chained = rows <= bags * kChainedBags * s->cut.rows;
   return a;
 }
 
@@ -632,7 +779,7 @@ int forward(const tbe_scan_t *s, Rows<DT> a, void *y, int64_t ys, float *last, f
   a.y = (typename Elem<DT>::type *)y;
   a.ys = ys;
   a.last = last;
-  a.before = saved ? saved : s->states;
+  a.before = saved ? saved : a.chained ? nullptr : s->states;
   return run_type<DT>(s, a, false, stream);
 }
 
@@ -686,12 +833,12 @@ int tbe_scan_create(tbe_scan_handle *out, int32_t dim, int32_t dtype, int32_t co
     delete s;
     return report(TBE_ELIMIT, "more rows than one launch can take");
   }
-  // one block: [err][bag_of][maps][states]
+  // one block: [err, call][bag_of][words][maps][states]
   const size_t bag_bytes = ((size_t)chunks * sizeof(int32_t) + 255) & ~(size_t)255, floats = (size_t)chunks * dim;
   char *block = nullptr;
   hipError_t e = hipGetDevice(&s->device);
-  if (e == hipSuccess) e = hipMalloc((void **)&block, 256 + bag_bytes + floats * 3 * sizeof(float));
-  if (e == hipSuccess) e = hipMemset(block, 0, 256);
+  if (e == hipSuccess) e = hipMalloc((void **)&block, 256 + bag_bytes + floats * 7 * sizeof(float));
+  if (e == hipSuccess) e = hipMemset(block, 0, 256 + bag_bytes + floats * 4 * sizeof(float));
   if (e != hipSuccess) {
     (void)hipFree(block);
     delete s;
@@ -699,7 +846,9 @@ int tbe_scan_create(tbe_scan_handle *out, int32_t dim, int32_t dtype, int32_t co
   }
   s->err = (int32_t *)block;
   s->bag_of = (int32_t *)(block + 256);
-  s->maps = (float *)(block + 256 + bag_bytes);
+  s->call = (uint32_t *)(block + 128);
+  s->words = (uint64_t *)(block + 256 + bag_bytes);
+  s->maps = (float *)(s->words + floats * 2);
   s->states = s->maps + floats * 2;
   *out = s;
   return TBE_OK;
