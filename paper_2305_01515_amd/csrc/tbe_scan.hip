@@ -4,8 +4,8 @@
 // A row maps the state h to a h + b, element by element, with a = f and b = (1 - f) x (or x); where a bag starts the state
 // before does not count: a = 0, b = f h0 + ....  Two such maps, one after the other, are one again, (a2 a1, a2 b1 + b2), so the
 // rows of all bags are cut into chunks of equal length wherever the bags begin, and no bag's length matters:
-//   prepare  where the chunks' bags begin; the offsets are looked over           (scan_prepare_kernel)
-//   sum      every chunk's map, from the rows after the last start in it         (scan_sum_kernel)
+//   prepare  marks at the rows where bags start and end; the offsets are looked over  (scan_prepare_kernel)
+//   sum      every chunk's map                                                   (scan_sum_kernel)
 //   join     the states before the chunks, by a scan over the chunks' maps       (scan_join_kernel)
 //   apply    every chunk's rows from the state before it                         (scan_apply_kernel, scan_grad_kernel)
 // One chunk needs the last one only.  Where bags are short, most chunks have a start and so a state behind them that nothing before
@@ -66,6 +66,13 @@ __device__ inline float gate(float u) {
   const float e = __builtin_amdgcn_exp2f(fabsf(u) * -1.44269504f), s = e * __builtin_amdgcn_rcpf(1.0f + e);
   return u >= 0.0f ? -s : s;
 }
+// f and (1 - f) x, or x
+__device__ inline void gated(float u, float x, bool coupled, float &f, float &b) {
+  const float e = __builtin_amdgcn_exp2f(u * -1.44269504f);  // infinite below u = -88
+  f = __builtin_amdgcn_rcpf(1.0f + e);
+  const float i = u < -80.0f ? 1.0f : e * f;
+  b = coupled ? i * x : x;
+}
 __device__ inline float keep_of(float q) { return signbit(q) ? 1.0f + q : q; }
 __device__ inline float take_of(float q) { return signbit(q) ? -q : 1.0f - q; }
 
@@ -82,9 +89,9 @@ struct Rows {
   float *before;        // [chunks][dim]: states before the chunks
   float *behind;        // [chunks][dim]: c behind the chunks
   uint64_t *words;      // [chunks][2][dim]: what chunks say to each other
-  const uint32_t *call;  // number of this call
+  const ulonglong2 *marks;  // [rows]: call << 32 | the bag that starts at a row, and the same of the bag whose last row it is
+  uint32_t *call;       // [0] number of this call, [1] of the next
   int64_t h0s, bags, rows;
-  int32_t *bag_of, *err;  // bag_of[chunks]: first bag that a chunk looks at
   int dim, L, tiles, chunk_rows, chunks;
   bool coupled, chained;  // chained: chunks hear from each other instead of sum and join
 };
@@ -110,61 +117,42 @@ __device__ inline void store_pack(E *p, const Pack<E, V> &r) {
   }
 }
 
-// For every chunk the first bag that ends at its first row or behind it; offsets that do not ascend from 0 to rows are reported; the
-// words of this call get a number of their own.
-__global__ __launch_bounds__(kThreads) void scan_prepare_kernel(const int64_t *off, int64_t bags, int64_t rows, int chunk_rows, int chunks, int32_t *bag_of,
-                                                                uint32_t *call, int32_t *err) {
+// Marks at the rows where bags start and end, with the number of the call (those of earlier calls are not cleared); empty bags get
+// their last state (BACK: gradient of the first) here; offsets that do not ascend from 0 to rows are reported.
+__global__ __launch_bounds__(kThreads) void scan_prepare_kernel(const int64_t *off, int64_t bags, int64_t rows, ulonglong2 *marks, uint32_t *call, int dim,
+                                                                const float *from, int64_t stride, float *to, int32_t *err) {
   const int64_t b = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-  if (b == 0) ++*call;
-  int first = 0, n = 0;  // chunks first .. first + n - 1 have this bag
+  const uint32_t now = call[1];
+  if (b == 0) call[0] = now;
+  bool empty = false;
   if (b < bags) {
-    const int64_t before = b ? off[b] : -1, s = off[b], e = off[b + 1];
+    const int64_t s = off[b], e = off[b + 1];
     if (s > e || s < 0 || e > rows || (b == 0 && s != 0) || (b == bags - 1 && e != rows)) {
       *err = 1;
+    } else if (s == e) {
+      empty = true;
     } else {
-      first = before < 0 ? 0 : (int)(before / chunk_rows) + 1;
-      n = (int)min(e / chunk_rows + 1, (int64_t)chunks) - first;
+      const unsigned long long mark = (unsigned long long)now << 32 | (uint32_t)b;
+      marks[s].x = mark;
+      marks[e - 1].y = mark;
     }
   }
-  if (n > 0 && n <= 2) {
-    bag_of[first] = (int32_t)b;
-    if (n == 2) bag_of[first + 1] = (int32_t)b;
-  }
-  uint64_t longer = __ballot(n > 2);  // a long bag at a time, by the whole wavefront
-  while (longer) {
-    const int l = __ffsll((unsigned long long)longer) - 1, lf = __shfl(first, l), ln = __shfl(n, l), lb = __shfl((int)b, l);
-    for (int k = threadIdx.x & 63; k < ln; k += 64) bag_of[lf + k] = lb;
-    longer &= longer - 1;
+  if (!to) return;
+  uint64_t todo = __ballot(empty);  // an empty bag at a time, by the whole wavefront
+  while (todo) {
+    const int64_t one = __shfl((int)b, __ffsll((unsigned long long)todo) - 1);
+    for (int d = threadIdx.x & 63; d < dim; d += 64) to[one * dim + d] = from ? from[one * stride + d] : 0.0f;
+    todo &= todo - 1;
   }
 }
 
-// Where the chunk's bags start and end: marks[2 r] is 1 + the bag that starts at row r of the chunk, marks[2 r + 1] 1 + the bag whose last
-// row that is; edge[0] is the last row with a start (0 if none), edge[1] the first with an end (the last row if none).  `empty` gets
-// the empty bags that lie in the chunk (those behind all rows: in the last chunk), a lane group each.
-template <class A, class F>
-__device__ inline void mark_bags(const A &a, int chunk, int64_t row0, int64_t from, int32_t *marks, int32_t *edge, F empty) {
-  for (int k = threadIdx.x; k < 2 * a.chunk_rows; k += kThreads) marks[k] = 0;
-  if (threadIdx.x == 0) { edge[0] = 0; edge[1] = a.chunk_rows - 1; }
-  __syncthreads();
-  const int64_t end = min(row0 + a.chunk_rows, a.rows);
-  const bool very_last = chunk == a.chunks - 1;
-  const int group = threadIdx.x / a.L, groups = kThreads / a.L, l = threadIdx.x & (a.L - 1);
-  for (int64_t b = from + group; b < a.bags; b += groups) {
-    const int64_t s = a.off[b], e = a.off[b + 1];
-    if (s >= end && !very_last) break;
-    if (s < 0 || s > e || e > a.rows) continue;  // reported already
-    if (s == e) {
-      if (s >= row0 && (s < end || very_last)) empty(b);
-    } else if (l == 0) {
-      if (s >= row0 && s < end) {
-        marks[2 * (int)(s - row0)] = (int32_t)b + 1;
-        atomicMax(&edge[0], (int32_t)(s - row0));
-      }
-      if (e > row0 && e <= end) {
-        marks[2 * (int)(e - 1 - row0) + 1] = (int32_t)b + 1;
-        atomicMin(&edge[1], (int32_t)(e - 1 - row0));
-      }
-    }
+// The chunk's marks in LDS: [2 r] is 1 + the bag that starts at row r of the chunk, [2 r + 1] 1 + the bag whose last row that is, or 0.
+template <class A>
+__device__ inline void fetch_marks(const A &a, int64_t row0, uint32_t call, int32_t *marks) {
+  for (int k = threadIdx.x; k < a.chunk_rows; k += kThreads) {
+    const ulonglong2 m = row0 + k < a.rows ? a.marks[row0 + k] : ulonglong2{0, 0};
+    marks[2 * k] = (uint32_t)(m.x >> 32) == call ? (int32_t)(uint32_t)m.x + 1 : 0;
+    marks[2 * k + 1] = (uint32_t)(m.y >> 32) == call ? (int32_t)(uint32_t)m.y + 1 : 0;
   }
   __syncthreads();
 }
@@ -231,16 +219,20 @@ __device__ inline bool hear_from(const A &a, int chunk, int d, uint32_t call, fl
   return true;
 }
 
-// The same from the rows themselves.  Where a bag starts (ends) with the chunk, nothing asks for it.
+// The same from the rows themselves, from the start (end) of the bag on.  Where a bag starts (ends) with the chunk, nothing asks for it.
 template <bool BACK, class A>
-__device__ float walk_to(const A &a, int chunk, int d) {
-  const int64_t row = (int64_t)(BACK ? chunk + 1 : chunk) * a.chunk_rows, b = a.bag_of[BACK ? chunk + 1 : chunk];
-  if (b >= a.bags) return 0.0f;
-  const int64_t lo = a.off[b], hi = a.off[b + 1];
-  if (lo < 0 || lo >= row || hi <= row || hi > a.rows) return 0.0f;
+__device__ float walk_to(const A &a, int chunk, int d, uint32_t call) {
+  const int64_t row = (int64_t)(BACK ? chunk + 1 : chunk) * a.chunk_rows;  // the state before this row
+  int64_t t = BACK ? row : row - 1;
+  unsigned long long m;
+  for (;; t += BACK ? 1 : -1) {
+    m = BACK ? a.marks[t].y : a.marks[t].x;
+    if ((uint32_t)(m >> 32) == call) break;
+    if (BACK ? t + 1 >= a.rows : t <= 0) return 0.0f;
+  }
+  const int64_t b = (uint32_t)m;
   float s = BACK ? (a.dlast ? a.dlast[b * a.dim + d] : 0.0f) : (a.h0 ? a.h0[b * a.h0s + d] : 0.0f);
-  for (int64_t k = 0; k < (BACK ? hi - row : row - lo); k++) {
-    const int64_t t = BACK ? hi - 1 - k : lo + k;
+  for (; BACK ? t >= row : t < row; t += BACK ? -1 : 1) {
     const float q = gate((float)a.u[t * a.us + d]);
     if (BACK) s = keep_of(q) * ((a.dy ? (float)a.dy[t * a.dys + d] : 0.0f) + s);
     else s = keep_of(q) * s + (a.coupled ? take_of(q) : 1.0f) * (float)a.x[t * a.xs + d];
@@ -261,7 +253,7 @@ __device__ inline float hear_and_say(const A &a, int chunk, int d, uint32_t call
     put_word(w, word_of(H1, call, kSaysMap));
   }
   float s;
-  if (!hear_from<BACK>(a, chunk, d, call, s)) s = walk_to<BACK>(a, chunk, d);
+  if (!hear_from<BACK>(a, chunk, d, call, s)) s = walk_to<BACK>(a, chunk, d, call);
   if (!known) put_word(w, word_of(go(A1, H1, s), call, kSaysState));
   return s;
 }
@@ -335,19 +327,17 @@ __global__ __launch_bounds__(kThreads) void scan_sum_kernel(Rows<DT> a) {
   using E = typename Elem<DT>::type;
   constexpr int R = 32 / V;
   extern __shared__ float lds[];
-  __shared__ int32_t edge[2];
   const int chunk = blockIdx.x / a.tiles, tile = blockIdx.x % a.tiles, C = a.L * V;
   int32_t *marks = (int32_t *)(lds + kWaves * 2 * C);
   const int64_t row0 = (int64_t)chunk * a.chunk_rows;
-  mark_bags(a, chunk, row0, a.bag_of[chunk], marks, edge, [](int64_t) {});
   const int group = threadIdx.x / a.L, l = threadIdx.x & (a.L - 1), c0 = (tile * a.L + l) * V, r0 = group * R;
-  const int rows = (int)min((int64_t)a.chunk_rows, a.rows - row0), lo = BACK ? 0 : edge[0], hi = BACK ? min(edge[1], rows - 1) : rows - 1;
+  const int rows = (int)min((int64_t)a.chunk_rows, a.rows - row0);
   const E *in = BACK ? a.dy : a.x;
   const int64_t stride = BACK ? a.dys : a.xs;
   Pack<E, V> xv[R], uv[R];
 #pragma unroll
   for (int j = 0; j < R; j++) {
-    const bool on = r0 + j >= lo && r0 + j <= hi && c0 < a.dim;
+    const bool on = r0 + j < rows && c0 < a.dim;
     xv[j] = {};
     uv[j] = {};
     if (on) {
@@ -355,6 +345,7 @@ __global__ __launch_bounds__(kThreads) void scan_sum_kernel(Rows<DT> a) {
       if (in) xv[j] = load_pack<E, V, ALIGNED>(in + (row0 + r0 + j) * stride + c0);
     }
   }
+  fetch_marks(a, row0, a.call[0], marks);
   float A[V], H[V];
 #pragma unroll
   for (int v = 0; v < V; v++) { A[v] = 1.0f; H[v] = 0.0f; }
@@ -368,13 +359,14 @@ __global__ __launch_bounds__(kThreads) void scan_sum_kernel(Rows<DT> a) {
 #pragma unroll
       for (int v = 0; v < V; v++) {
         A[v] = kReset;
-        H[v] = s ? s[at + v] : 0.0f;
+        H[v] = s && c0 < a.dim ? s[at + v] : 0.0f;
       }
     }
 #pragma unroll
     for (int v = 0; v < V; v++) {
-      const float q = gate((float)uv[j].e[v]), f = keep_of(q), x = (float)xv[j].e[v];
-      H[v] = BACK ? f * (H[v] + x) : f * H[v] + (a.coupled ? take_of(q) * x : x);
+      float f, b;
+      gated((float)uv[j].e[v], (float)xv[j].e[v], !BACK && a.coupled, f, b);
+      H[v] = BACK ? f * (H[v] + b) : f * H[v] + b;
       A[v] *= f;
     }
   }
@@ -435,7 +427,6 @@ __global__ __launch_bounds__(kThreads) void scan_apply_kernel(Rows<DT> a) {
   using E = typename Elem<DT>::type;
   constexpr int R = 32 / V;
   extern __shared__ float lds[];
-  __shared__ int32_t edge[2];
   const int chunk = blockIdx.x / a.tiles, tile = blockIdx.x % a.tiles, C = a.L * V;
   int32_t *marks = (int32_t *)(lds + kWaves * 2 * C);
   const int64_t row0 = (int64_t)chunk * a.chunk_rows;
@@ -452,12 +443,10 @@ __global__ __launch_bounds__(kThreads) void scan_apply_kernel(Rows<DT> a) {
       xv[j] = load_pack<E, V, ALIGNED>(a.x + (row0 + r0 + j) * a.xs + c0);
     }
   }
-  mark_bags(a, chunk, row0, a.bag_of[chunk], marks, edge, [&](int64_t b) {
-    if (a.last && on)
-#pragma unroll
-      for (int v = 0; v < V; v++) a.last[b * a.dim + c0 + v] = a.h0 ? a.h0[b * a.h0s + c0 + v] : 0.0f;
-  });
-  float q[R][V], A[V], H[V];
+  const uint32_t call = a.call[0];
+  if (blockIdx.x == 0 && threadIdx.x == 0) a.call[1] = call + 1;  // nothing looks at that one in this kernel
+  fetch_marks(a, row0, call, marks);
+  float f[R][V], b[R][V], A[V], H[V];
 #pragma unroll
   for (int v = 0; v < V; v++) { A[v] = 1.0f; H[v] = 0.0f; }
 #pragma unroll
@@ -471,10 +460,9 @@ __global__ __launch_bounds__(kThreads) void scan_apply_kernel(Rows<DT> a) {
       }
 #pragma unroll
     for (int v = 0; v < V; v++) {
-      q[j][v] = gate((float)uv[j].e[v]);
-      const float f = keep_of(q[j][v]), x = (float)xv[j].e[v];
-      H[v] = f * H[v] + (a.coupled ? take_of(q[j][v]) * x : x);
-      A[v] *= f;
+      gated((float)uv[j].e[v], (float)xv[j].e[v], a.coupled, f[j][v], b[j][v]);
+      H[v] = f[j][v] * H[v] + b[j][v];
+      A[v] *= f[j][v];
     }
   }
   scan_wave<V, false>(A, H, a.L);
@@ -488,7 +476,7 @@ __global__ __launch_bounds__(kThreads) void scan_apply_kernel(Rows<DT> a) {
       if (a.chained) {
         float A1, H1;
         map_of_waves<false>(lds, C, c, A1, H1);
-        s = hear_and_say<false>(a, chunk, d, *a.call, A1, H1);
+        s = hear_and_say<false>(a, chunk, d, call, A1, H1);
         if (before) *before = s;
       } else {
         s = *before;
@@ -509,8 +497,7 @@ __global__ __launch_bounds__(kThreads) void scan_apply_kernel(Rows<DT> a) {
     Pack<E, V> out;
 #pragma unroll
     for (int v = 0; v < V; v++) {
-      const float x = (float)xv[j].e[v];
-      h[v] = keep_of(q[j][v]) * h[v] + (a.coupled ? take_of(q[j][v]) * x : x);
+      h[v] = f[j][v] * h[v] + b[j][v];
       out.e[v] = (E)h[v];
     }
     if (a.y && r0 + j < rows) store_pack<E, V, ALIGNED>(a.y + (row0 + r0 + j) * a.ys + c0, out);
@@ -525,7 +512,6 @@ __global__ __launch_bounds__(kThreads) void scan_grad_kernel(Rows<DT> a) {
   using E = typename Elem<DT>::type;
   constexpr int R = 32 / V;
   extern __shared__ float lds[];
-  __shared__ int32_t edge[2];
   // from the last chunk on: what a chunk hears of is behind it
   const int chunk = a.chunks - 1 - blockIdx.x / a.tiles, tile = blockIdx.x % a.tiles, C = a.L * V;
   float *back = lds + kWaves * 2 * C;
@@ -546,11 +532,9 @@ __global__ __launch_bounds__(kThreads) void scan_grad_kernel(Rows<DT> a) {
       if (a.dy) gv[j] = load_pack<E, V, ALIGNED>(a.dy + (row0 + r0 + j) * a.dys + c0);
     }
   }
-  mark_bags(a, chunk, row0, a.bag_of[chunk], marks, edge, [&](int64_t b) {
-    if (a.dh0 && on)
-#pragma unroll
-      for (int v = 0; v < V; v++) a.dh0[b * a.dim + c0 + v] = a.dlast ? a.dlast[b * a.dim + c0 + v] : 0.0f;
-  });
+  const uint32_t call = a.call[0];
+  if (blockIdx.x == 0 && threadIdx.x == 0) a.call[1] = call + 1;  // nothing looks at that one in this kernel
+  fetch_marks(a, row0, call, marks);
   float q[R][V], A[V], H[V], B[V], G[V];
 #pragma unroll
   for (int v = 0; v < V; v++) { A[v] = B[v] = 1.0f; H[v] = G[v] = 0.0f; }
@@ -600,7 +584,7 @@ __global__ __launch_bounds__(kThreads) void scan_grad_kernel(Rows<DT> a) {
       if (a.chained) {
         float A1, H1;
         map_of_waves<true>(back, C, c, A1, H1);
-        g = hear_and_say<true>(a, chunk, d, *a.call, A1, H1);
+        g = hear_and_say<true>(a, chunk, d, call, A1, H1);
       } else {
         g = a.behind[(int64_t)chunk * a.dim + d];
       }
@@ -609,7 +593,7 @@ __global__ __launch_bounds__(kThreads) void scan_grad_kernel(Rows<DT> a) {
     join_waves<true>(back, C, c, g);
   }
   __syncthreads();
-  float h[R][V], s[V];
+  float w[R][V], s[V];  // w: du / g
   start_of_lane<V, false>(A, H, a.L, lds, s);
 #pragma unroll
   for (int j = 0; j < R; j++) {
@@ -619,9 +603,9 @@ __global__ __launch_bounds__(kThreads) void scan_grad_kernel(Rows<DT> a) {
       for (int v = 0; v < V; v++) s[v] = a.h0 && on ? a.h0[(int64_t)(bag - 1) * a.h0s + c0 + v] : 0.0f;
 #pragma unroll
     for (int v = 0; v < V; v++) {
-      const float x = (float)xv[j].e[v];
-      h[j][v] = a.coupled ? s[v] - x : s[v];
-      s[v] = keep_of(q[j][v]) * s[v] + (a.coupled ? take_of(q[j][v]) * x : x);
+      const float x = (float)xv[j].e[v], f = keep_of(q[j][v]), i = take_of(q[j][v]);
+      w[j][v] = (f * i) * (a.coupled ? s[v] - x : s[v]);
+      s[v] = f * s[v] + (a.coupled ? i * x : x);
     }
   }
   start_of_lane<V, true>(B, G, a.L, back, s);
@@ -637,7 +621,7 @@ __global__ __launch_bounds__(kThreads) void scan_grad_kernel(Rows<DT> a) {
     for (int v = 0; v < V; v++) {
       const float f = keep_of(q[j][v]), i = take_of(q[j][v]), g = (float)gv[j].e[v] + s[v];
       dx.e[v] = (E)(a.coupled ? i * g : g);
-      du.e[v] = (E)(g * h[j][v] * (f * i));
+      du.e[v] = (E)(g * w[j][v]);
       s[v] = f * g;
     }
     if (r0 + j < rows) {
@@ -648,14 +632,6 @@ __global__ __launch_bounds__(kThreads) void scan_grad_kernel(Rows<DT> a) {
 #pragma unroll
       for (int v = 0; v < V; v++) a.dh0[(int64_t)(bag - 1) * a.dim + c0 + v] = s[v];
   }
-}
-
-// Bags without any row in the whole call: where they start is where they end.
-__global__ __launch_bounds__(kThreads) void scan_empty_kernel(const int64_t *off, int64_t bags, int dim, const float *from, int64_t stride, float *to,
-                                                              int32_t *err) {
-  const int64_t id = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-  if (id <= bags && off[id] != 0) *err = 1;
-  for (int64_t k = id; k < bags * dim; k += (int64_t)gridDim.x * kThreads) to[k] = from ? from[k / dim * stride + k % dim] : 0.0f;
 }
 
 template <int DT>
@@ -686,8 +662,8 @@ struct tbe_scan_t : DenseBase {
   int32_t *err = nullptr;    // device: 1 = bad offsets, 2 = slot out of range
   float *maps = nullptr;     // device [chunks][2][dim]
   float *states = nullptr;   // device [chunks][dim]: before the chunks where the caller saves none, behind them in the backward
-  int32_t *bag_of = nullptr; // device [chunks]
-  uint32_t *call = nullptr;  // device: number of the call
+  ulonglong2 *marks = nullptr; // device [rows]
+  uint32_t *call = nullptr;  // device [2]
   uint64_t *words = nullptr; // device [chunks][2][dim]
 };
 
@@ -714,8 +690,9 @@ template <int DT, int V, bool ALIGNED>
 int run(const tbe_scan_t *s, const Rows<DT> &a, bool grad, hipStream_t stream) noexcept {
   const dim3 grid((unsigned)(a.chunks * a.tiles)), joins((unsigned)((a.dim + kJoinChannels - 1) / kJoinChannels));
   const size_t tot = (size_t)kWaves * 2 * a.L * V * sizeof(float), marks = (size_t)a.chunk_rows * 2 * sizeof(int32_t);
-  scan_prepare_kernel<<<dim3((unsigned)((a.bags + kThreads - 1) / kThreads)), kThreads, 0, stream>>>(a.off, a.bags, a.rows, a.chunk_rows, a.chunks, a.bag_of,
-                                                                                                  s->call, a.err);
+  scan_prepare_kernel<<<dim3((unsigned)((a.bags + kThreads - 1) / kThreads)), kThreads, 0, stream>>>(
+      a.off, a.bags, a.rows, s->marks, s->call, a.dim, grad ? a.dlast : a.h0, grad ? a.dim : a.h0s, grad ? a.dh0 : a.last, s->err);
+  if (a.rows == 0) return check_launch();
   const bool joined = a.chunks > 1 && !a.chained;
   if (!grad) {
     if (joined) {
@@ -759,10 +736,9 @@ Rows<DT> rows_of(const tbe_scan_t *s, const void *x, int64_t xs, const void *u, 
   a.h0 = h0;
   a.h0s = h0s;
   a.maps = s->maps;
-  a.bag_of = s->bag_of;
+  a.marks = s->marks;
   a.words = s->words;
   a.call = s->call;
-  a.err = s->err;
   a.dim = s->dim;
   a.L = s->cut.L;
   a.tiles = s->cut.tiles;
@@ -800,14 +776,6 @@ int backward(const tbe_scan_t *s, Rows<DT> a, const float *saved, const void *dy
   return run_type<DT>(s, a, true, stream);
 }
 
-int only_empty(const tbe_scan_t *s, const int64_t *off, int64_t bags, const float *from, int64_t stride, float *to, hipStream_t stream) noexcept {
-  const int64_t n = to ? bags * s->dim : 0, most = n > bags + 1 ? n : bags + 1;
-  const int64_t blocks = (most + kThreads - 1) / kThreads;
-  scan_empty_kernel<<<dim3((unsigned)(blocks > bags / kThreads + 4096 ? bags / kThreads + 4096 : blocks)), kThreads, 0, stream>>>(
-      off, bags, to ? s->dim : 0, from, stride, to, s->err);
-  return check_launch();
-}
-
 }  // namespace
 
 extern "C" {
@@ -833,21 +801,23 @@ int tbe_scan_create(tbe_scan_handle *out, int32_t dim, int32_t dtype, int32_t co
     delete s;
     return report(TBE_ELIMIT, "more rows than one launch can take");
   }
-  // one block: [err, call][bag_of][words][maps][states]
-  const size_t bag_bytes = ((size_t)chunks * sizeof(int32_t) + 255) & ~(size_t)255, floats = (size_t)chunks * dim;
+  // one block: [err, call][marks][words][maps][states]
+  const size_t mark_bytes = (size_t)max_rows * sizeof(ulonglong2), floats = (size_t)chunks * dim, zeros = 256 + mark_bytes + floats * 4 * sizeof(float);
+  const uint32_t first_call = 1;  // zeros are of no call
   char *block = nullptr;
   hipError_t e = hipGetDevice(&s->device);
-  if (e == hipSuccess) e = hipMalloc((void **)&block, 256 + bag_bytes + floats * 7 * sizeof(float));
-  if (e == hipSuccess) e = hipMemset(block, 0, 256 + bag_bytes + floats * 4 * sizeof(float));
+  if (e == hipSuccess) e = hipMalloc((void **)&block, zeros + floats * 3 * sizeof(float));
+  if (e == hipSuccess) e = hipMemset(block, 0, zeros);
+  if (e == hipSuccess) e = hipMemcpy(block + 132, &first_call, sizeof first_call, hipMemcpyHostToDevice);
   if (e != hipSuccess) {
     (void)hipFree(block);
     delete s;
     return report_hip(e);
   }
   s->err = (int32_t *)block;
-  s->bag_of = (int32_t *)(block + 256);
+  s->marks = (ulonglong2 *)(block + 256);
   s->call = (uint32_t *)(block + 128);
-  s->words = (uint64_t *)(block + 256 + bag_bytes);
+  s->words = (uint64_t *)(block + 256 + mark_bytes);
   s->maps = (float *)(s->words + floats * 2);
   s->states = s->maps + floats * 2;
   *out = s;
@@ -873,7 +843,6 @@ int tbe_scan_forward(tbe_scan_handle s, const void *d_x, int64_t x_stride, const
   if (d_y && y_stride < s->dim) return report(TBE_EINVAL, "a stride below dim");
   if (bags == 0) return TBE_OK;
   hipStream_t st = (hipStream_t)stream;
-  if (rows == 0) return only_empty(s, d_offsets, bags, d_h0, h0_stride, d_last, st);
 #define ROWS(DT) rows_of<DT>(s, d_x, x_stride, d_u, u_stride, d_offsets, bags, rows, d_h0, h0_stride)
   if (s->dtype == TBE_FP32) return forward<TBE_FP32>(s, ROWS(TBE_FP32), d_y, y_stride, d_last, d_saved, st);
   if (s->dtype == TBE_FP16) return forward<TBE_FP16>(s, ROWS(TBE_FP16), d_y, y_stride, d_last, d_saved, st);
@@ -889,7 +858,6 @@ int tbe_scan_backward(tbe_scan_handle s, const void *d_x, int64_t x_stride, cons
   if ((d_dy && dy_stride < s->dim) || dx_stride < s->dim || du_stride < s->dim) return report(TBE_EINVAL, "a stride below dim");
   if (bags == 0) return TBE_OK;
   hipStream_t st = (hipStream_t)stream;
-  if (rows == 0) return only_empty(s, d_offsets, bags, d_dlast, s->dim, d_dh0, st);
 #define BACKWARD(DT) backward<DT>(s, ROWS(DT), d_saved, d_dy, dy_stride, d_dlast, d_dx, dx_stride, d_du, du_stride, d_dh0, st)
   if (s->dtype == TBE_FP32) return BACKWARD(TBE_FP32);
   if (s->dtype == TBE_FP16) return BACKWARD(TBE_FP16);
