@@ -28,7 +28,7 @@ namespace {
 
 constexpr int kThreads = 256, kWaves = kThreads / 64;
 constexpr int64_t kChainedBags = 2;  // chunks that a bag may have on average for them to hear from each other
-constexpr int kJoinChannels = 16, kJoinSegments = 64;
+constexpr int kJoinChannels = 4, kJoinSegments = 256;
 
 // How the rows of a handle are cut: a function of dim and the type alone, because the backward uses what the forward saved.
 struct Cut {
@@ -179,7 +179,7 @@ __device__ inline bool get_word(const uint64_t *p, uint64_t &w, uint32_t call) {
 // between, one after the other.  Every state that is said was found in this order too, so it has the same bits wherever it is found.
 template <bool BACK, class A>
 __device__ inline bool hear_from(const A &a, int chunk, int d, uint32_t call, float &s) {
-  constexpr int kAtOnce = 4;
+  constexpr int kAtOnce = 2;
   const int n = BACK ? a.chunks - 1 - chunk : chunk;  // chunks before this one; the first of them always says its state
   s = 0.0f;
   if (n == 0) return true;
@@ -321,6 +321,15 @@ __device__ inline void start_of_lane(const float (&A)[V], const float (&H)[V], i
 // Rows behind the last one are taken for rows of zeros: nothing comes after them, and the gradient's way back from them ends at the
 // last row, where a bag ends.
 
+// V fp32 numbers of a row, or zeros without one
+template <int V>
+__device__ inline void load_row(const float *p, int64_t at, bool there, float (&v)[V]) {
+#pragma unroll
+  for (int k = 0; k < V; k++) v[k] = p && there ? p[at + k] : 0.0f;
+}
+
+__device__ inline void opaque(float &x) { asm volatile("" : "+v"(x)); }
+
 // Maps of the chunks: of h from x and u, BACK: of c from dy and u.
 template <int DT, int V, bool ALIGNED, bool BACK>
 __global__ __launch_bounds__(kThreads) void scan_sum_kernel(Rows<DT> a) {
@@ -381,44 +390,74 @@ __global__ __launch_bounds__(kThreads) void scan_sum_kernel(Rows<DT> a) {
   }
 }
 
-// States before the chunks (BACK: behind them) from their maps.  A workgroup has 16 elements; its lanes take 64 segments of the chunks
-// each, whose maps one wavefront for each element joins by exchange between lanes.
+// States before the chunks (BACK: behind them) from their maps.  A workgroup has 4 elements; its lanes take 256 segments of the chunks, up
+// to kKept of each in registers, and a wavefront for each element joins the segments, 4 a lane, by exchange between lanes.  (With 16
+// elements and 64 segments a workgroup there were too few lanes for the way to memory: 24 us instead of 8 for 3837 chunks of 128.)
 template <bool BACK>
 __global__ __launch_bounds__(kJoinChannels *kJoinSegments) void scan_join_kernel(const float *maps, float *state, int chunks, int dim) {
-  __shared__ float tot[2][kJoinChannels][kJoinSegments + 1];
+  constexpr int kKept = 8;
+  __shared__ float tot[2][kJoinChannels][kJoinSegments];
   const int c = threadIdx.x % kJoinChannels, seg = threadIdx.x / kJoinChannels, d = blockIdx.x * kJoinChannels + c;
   const int per = (chunks + kJoinSegments - 1) / kJoinSegments, k0 = min(seg * per, chunks), k1 = min(k0 + per, chunks);
   const bool on = d < dim;
-  float A = 1.0f, H = 0.0f;
-#pragma unroll 8
-  for (int k = k0; k < k1; k++) {
-    const int64_t at = (int64_t)(BACK ? chunks - 1 - k : k) * 2 * dim + d;
-    const float a = on ? maps[at] : 1.0f, h = on ? maps[at + dim] : 0.0f;
-    H = go(a, h, H);
-    A = signbit(a) ? a : a * A;
+  auto at = [&](int k) { return (int64_t)(BACK ? chunks - 1 - k : k) * 2 * dim + d; };
+  float A = 1.0f, H = 0.0f, ka[kKept], kh[kKept];
+#pragma unroll
+  for (int q = 0; q < kKept; q++) {
+    ka[q] = on && k0 + q < k1 ? maps[at(k0 + q)] : 1.0f;
+    kh[q] = on && k0 + q < k1 ? maps[at(k0 + q) + dim] : 0.0f;
   }
+#pragma unroll
+  for (int q = 0; q < kKept; q++) {
+    H = go(ka[q], kh[q], H);
+    A = signbit(ka[q]) ? ka[q] : ka[q] * A;
+  }
+  if (on)
+#pragma unroll 8
+    for (int k = k0 + kKept; k < k1; k++) {
+      const float a = maps[at(k)], h = maps[at(k) + dim];
+      H = go(a, h, H);
+      A = signbit(a) ? a : a * A;
+    }
   tot[0][c][seg] = A;
   tot[1][c][seg] = H;
   __syncthreads();
-  {
-    const int w = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    float a = tot[0][w][lane], h = tot[1][w][lane];
+  const int w = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  if (w < kJoinChannels) {
+    constexpr int kEach = kJoinSegments / 64;
+    float a[kEach], h[kEach], la = 1.0f, lh = 0.0f;
+#pragma unroll
+    for (int q = 0; q < kEach; q++) {
+      a[q] = tot[0][w][lane * kEach + q];
+      h[q] = tot[1][w][lane * kEach + q];
+      lh = go(a[q], h[q], lh);
+      la = signbit(a[q]) ? a[q] : a[q] * la;
+    }
 #pragma unroll
     for (int k = 1; k < 64; k *= 2) {
-      const float pa = __shfl_up(a, k), ph = __shfl_up(h, k);
-      if (lane >= k) join(pa, ph, a, h);
+      const float pa = __shfl_up(la, k), ph = __shfl_up(lh, k);
+      if (lane >= k) join(pa, ph, la, lh);
     }
-    const float s = __shfl_up(h, 1);
-    tot[1][w][lane] = lane ? s : 0.0f;
+    float s = __shfl_up(lh, 1);
+    s = lane ? s : 0.0f;
+#pragma unroll
+    for (int q = 0; q < kEach; q++) {
+      tot[1][w][lane * kEach + q] = s;
+      s = go(a[q], h[q], s);
+    }
   }
   __syncthreads();
-  float s = tot[1][c][seg];
   if (!on) return;
+  float s = tot[1][c][seg];
+#pragma unroll
+  for (int q = 0; q < kKept; q++) {
+    if (k0 + q < k1) state[(int64_t)(BACK ? chunks - 1 - k0 - q : k0 + q) * dim + d] = s;
+    s = go(ka[q], kh[q], s);
+  }
 #pragma unroll 8
-  for (int k = k0; k < k1; k++) {
-    const int64_t chunk = BACK ? chunks - 1 - k : k, at = chunk * 2 * dim + d;
-    state[chunk * dim + d] = s;
-    s = go(maps[at], maps[at + dim], s);
+  for (int k = k0 + kKept; k < k1; k++) {
+    state[(int64_t)(BACK ? chunks - 1 - k : k) * dim + d] = s;
+    s = go(maps[at(k)], maps[at(k) + dim], s);
   }
 }
 
@@ -446,23 +485,38 @@ __global__ __launch_bounds__(kThreads) void scan_apply_kernel(Rows<DT> a) {
   const uint32_t call = a.call[0];
   if (blockIdx.x == 0 && threadIdx.x == 0) a.call[1] = call + 1;  // nothing looks at that one in this kernel
   fetch_marks(a, row0, call, marks);
+  // The first start among the lane's rows: its state is asked for before the gates are computed.
+  int first = R;
+#pragma unroll
+  for (int j = R - 1; j >= 0; j--) first = marks[2 * (r0 + j)] ? j : first;
+  float early[V];
+  load_row(a.h0, first < R ? (int64_t)(marks[2 * (r0 + first)] - 1) * a.h0s + c0 : 0, first < R && on, early);
   float f[R][V], b[R][V], A[V], H[V];
 #pragma unroll
+  for (int j = 0; j < R; j++)
+#pragma unroll
+    for (int v = 0; v < V; v++) gated((float)uv[j].e[v], (float)xv[j].e[v], a.coupled, f[j][v], b[j][v]);
+#pragma unroll
   for (int v = 0; v < V; v++) { A[v] = 1.0f; H[v] = 0.0f; }
+  uint32_t starts = 0;
 #pragma unroll
   for (int j = 0; j < R; j++) {
     const int32_t bag = marks[2 * (r0 + j)];
-    if (bag)
+    if (bag) {  // what the bag starts from goes into b
+      if (j != first) load_row(a.h0, (int64_t)(bag - 1) * a.h0s + c0, on, early);
+      starts |= 1u << j;
 #pragma unroll
       for (int v = 0; v < V; v++) {
+        b[j][v] += f[j][v] * early[v];
         A[v] = kReset;
-        H[v] = a.h0 && on ? a.h0[(int64_t)(bag - 1) * a.h0s + c0 + v] : 0.0f;
+        H[v] = b[j][v];
       }
+    } else {
 #pragma unroll
-    for (int v = 0; v < V; v++) {
-      gated((float)uv[j].e[v], (float)xv[j].e[v], a.coupled, f[j][v], b[j][v]);
-      H[v] = f[j][v] * H[v] + b[j][v];
-      A[v] *= f[j][v];
+      for (int v = 0; v < V; v++) {
+        H[v] = f[j][v] * H[v] + b[j][v];
+        A[v] *= f[j][v];
+      }
     }
   }
   scan_wave<V, false>(A, H, a.L);
@@ -490,14 +544,11 @@ __global__ __launch_bounds__(kThreads) void scan_apply_kernel(Rows<DT> a) {
   if (!on) return;
 #pragma unroll
   for (int j = 0; j < R; j++) {
-    const int32_t bag = marks[2 * (r0 + j)], ended = marks[2 * (r0 + j) + 1];
-    if (bag)
-#pragma unroll
-      for (int v = 0; v < V; v++) h[v] = a.h0 ? a.h0[(int64_t)(bag - 1) * a.h0s + c0 + v] : 0.0f;
+    const int32_t ended = marks[2 * (r0 + j) + 1];
     Pack<E, V> out;
 #pragma unroll
     for (int v = 0; v < V; v++) {
-      h[v] = f[j][v] * h[v] + b[j][v];
+      h[v] = starts >> j & 1 ? b[j][v] : f[j][v] * h[v] + b[j][v];
       out.e[v] = (E)h[v];
     }
     if (a.y && r0 + j < rows) store_pack<E, V, ALIGNED>(a.y + (row0 + r0 + j) * a.ys + c0, out);
@@ -535,21 +586,36 @@ __global__ __launch_bounds__(kThreads) void scan_grad_kernel(Rows<DT> a) {
   const uint32_t call = a.call[0];
   if (blockIdx.x == 0 && threadIdx.x == 0) a.call[1] = call + 1;  // nothing looks at that one in this kernel
   fetch_marks(a, row0, call, marks);
+  // The first start and the last end among the lane's rows: what belongs to them is asked for before the gates are computed.
+  int first = R, last = -1;
+#pragma unroll
+  for (int j = R - 1; j >= 0; j--) first = marks[2 * (r0 + j)] ? j : first;
+#pragma unroll
+  for (int j = 0; j < R; j++) last = marks[2 * (r0 + j) + 1] ? j : last;
+  float start[V], finish[V];
+  load_row(a.h0, first < R ? (int64_t)(marks[2 * (r0 + first)] - 1) * a.h0s + c0 : 0, first < R && on, start);
+  load_row(a.dlast, last >= 0 ? (int64_t)(marks[2 * (r0 + last) + 1] - 1) * a.dim + c0 : 0, last >= 0 && on, finish);
   float q[R][V], A[V], H[V], B[V], G[V];
+#pragma unroll
+  for (int j = 0; j < R; j++)
+#pragma unroll
+    for (int v = 0; v < V; v++) q[j][v] = gate((float)uv[j].e[v]);
 #pragma unroll
   for (int v = 0; v < V; v++) { A[v] = B[v] = 1.0f; H[v] = G[v] = 0.0f; }
 #pragma unroll
   for (int j = 0; j < R; j++) {
     const int32_t bag = marks[2 * (r0 + j)];
-    if (bag)
+    if (bag) {
+      float h0[V];
+      if (j != first) load_row(a.h0, (int64_t)(bag - 1) * a.h0s + c0, on, h0);
 #pragma unroll
       for (int v = 0; v < V; v++) {
         A[v] = kReset;
-        H[v] = a.h0 && on ? a.h0[(int64_t)(bag - 1) * a.h0s + c0 + v] : 0.0f;
+        H[v] = j != first ? h0[v] : start[v];
       }
+    }
 #pragma unroll
     for (int v = 0; v < V; v++) {
-      q[j][v] = gate((float)uv[j].e[v]);
       const float f = keep_of(q[j][v]), x = (float)xv[j].e[v];
       H[v] = f * H[v] + (a.coupled ? take_of(q[j][v]) * x : x);
       A[v] *= f;
@@ -558,14 +624,18 @@ __global__ __launch_bounds__(kThreads) void scan_grad_kernel(Rows<DT> a) {
 #pragma unroll
   for (int j = R - 1; j >= 0; j--) {
     const int32_t ended = marks[2 * (r0 + j) + 1];
-    if (ended)
+    if (ended) {
+      float dl[V];
+      if (j != last) load_row(a.dlast, (int64_t)(ended - 1) * a.dim + c0, on, dl);
 #pragma unroll
       for (int v = 0; v < V; v++) {
         B[v] = kReset;
-        G[v] = a.dlast && on ? a.dlast[(int64_t)(ended - 1) * a.dim + c0 + v] : 0.0f;
+        G[v] = j != last ? dl[v] : finish[v];
       }
+    }
 #pragma unroll
     for (int v = 0; v < V; v++) {
+      opaque(q[j][v]);  // gates are unpacked anew for each pass: kept, they take half the registers
       const float f = keep_of(q[j][v]);
       G[v] = f * (G[v] + (float)gv[j].e[v]);
       B[v] *= f;
@@ -598,11 +668,15 @@ __global__ __launch_bounds__(kThreads) void scan_grad_kernel(Rows<DT> a) {
 #pragma unroll
   for (int j = 0; j < R; j++) {
     const int32_t bag = marks[2 * (r0 + j)];
-    if (bag)
+    if (bag) {
+      if (j != first) load_row(a.h0, (int64_t)(bag - 1) * a.h0s + c0, on, s);
+      else
 #pragma unroll
-      for (int v = 0; v < V; v++) s[v] = a.h0 && on ? a.h0[(int64_t)(bag - 1) * a.h0s + c0 + v] : 0.0f;
+        for (int v = 0; v < V; v++) s[v] = start[v];
+    }
 #pragma unroll
     for (int v = 0; v < V; v++) {
+      opaque(q[j][v]);
       const float x = (float)xv[j].e[v], f = keep_of(q[j][v]), i = take_of(q[j][v]);
       w[j][v] = (f * i) * (a.coupled ? s[v] - x : s[v]);
       s[v] = f * s[v] + (a.coupled ? i * x : x);
@@ -613,12 +687,16 @@ __global__ __launch_bounds__(kThreads) void scan_grad_kernel(Rows<DT> a) {
 #pragma unroll
   for (int j = R - 1; j >= 0; j--) {
     const int32_t bag = marks[2 * (r0 + j)], ended = marks[2 * (r0 + j) + 1];
-    if (ended)
+    if (ended) {
+      if (j != last) load_row(a.dlast, (int64_t)(ended - 1) * a.dim + c0, on, s);
+      else
 #pragma unroll
-      for (int v = 0; v < V; v++) s[v] = a.dlast ? a.dlast[(int64_t)(ended - 1) * a.dim + c0 + v] : 0.0f;
+        for (int v = 0; v < V; v++) s[v] = finish[v];
+    }
     Pack<E, V> dx, du;
 #pragma unroll
     for (int v = 0; v < V; v++) {
+      opaque(q[j][v]);
       const float f = keep_of(q[j][v]), i = take_of(q[j][v]), g = (float)gv[j].e[v] + s[v];
       dx.e[v] = (E)(a.coupled ? i * g : g);
       du.e[v] = (E)(g * w[j][v]);
