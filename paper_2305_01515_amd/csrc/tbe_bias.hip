@@ -394,7 +394,7 @@ __global__ __launch_bounds__(kThreads) void bias_scores_kernel(Shape p, const ty
 // one after another down a diagonal, which all have the same 2 V - 1 diagonals, and keeps their sums in registers: one addition an element,
 // and every load a whole pack.  64 lanes have neighbouring squares.  A wavefront's unit of work is 64 such columns of squares, `seg`
 // squares of each (of the same queries), for `samples` samples; at its end its diagonals are joined in LDS and added to their buckets.
-constexpr int kUnits = 8192;  // units that the work is cut into, if they have 4 squares at least
+constexpr int kUnits = 4096;  // units that the work is cut into, if they have 4 squares at least (16 x 8 x 1024 x 1024: 52 us; 8192: 65)
 
 struct Diagonals {
   uint32_t squares;       // of V queries
@@ -403,7 +403,7 @@ struct Diagonals {
 };
 
 template <int DT, bool SCORES>
-__global__ __launch_bounds__(kThreads) void bias_grad_index_kernel(Shape p, Diagonals u, const typename Elem<DT>::type *dout, tbe_bias_strides ds,
+__global__ __launch_bounds__(kThreads, SCORES ? 2 : 4) void bias_grad_index_kernel(Shape p, Diagonals u, const typename Elem<DT>::type *dout, tbe_bias_strides ds,
                                                                    float *part, float scale, typename Elem<DT>::type *dscores, tbe_bias_strides es) {
   using E = typename Elem<DT>::type;
   constexpr int V = 16 / sizeof(E), kDiagonals = 64 * V + V - 1;
@@ -461,18 +461,16 @@ __global__ __launch_bounds__(kThreads) void bias_grad_index_kernel(Shape p, Diag
             for (int v = 0; v < V; v++) x[r].e[v] = from[min((int64_t)r, last) * ds.query + min(v, keys - 1)];
         }
         const int rows = queries - i;
-        if (!SCORES && left == V && rows >= V) {
+        if (left < V || rows < V)
 #pragma unroll
           for (int r = 0; r < V; r++)
 #pragma unroll
-            for (int v = 0; v < V; v++) acc[V - 1 + v - r] += (float)x[r].e[v];
-          continue;
-        }
+            for (int v = 0; v < V; v++) x[r].e[v] = v < left && r < rows ? x[r].e[v] : (E)0.0f;
 #pragma unroll
         for (int r = 0; r < V; r++) {
 #pragma unroll
           for (int v = 0; v < V; v++) {
-            const float g = v < left && r < rows ? (float)x[r].e[v] : 0.0f;
+            const float g = (float)x[r].e[v];
             acc[V - 1 + v - r] += g;
             if (SCORES) x[r].e[v] = (E)(p.s.causal && (int64_t)D * V + v - r - p.s.query_offset > 0 ? 0.0f : g * scale);
           }

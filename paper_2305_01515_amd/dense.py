@@ -39,6 +39,7 @@ class AdamWTensor(C.Structure):
 
 
 _ready = False
+_current_raw_stream = torch._C._cuda_getCurrentRawStream
 
 
 def _lib() -> C.CDLL:
@@ -79,18 +80,19 @@ class _Handle:
 
     def _stream(self) -> int:
         """the current stream, for the next call: behind this object's last call on another one"""
-        current = torch.cuda.current_stream(self.device)
-        if self._last is None or self._last.cuda_stream != current.cuda_stream:
+        current = _current_raw_stream(self.device.index)
+        if self._last is None or self._last.cuda_stream != current:
             if torch.cuda.is_current_stream_capturing():
-                return current.cuda_stream
+                return current
+            stream = torch.cuda.current_stream(self.device)
             if self._last is not None:
-                current.wait_stream(self._last)
-            self._last = current
-        return current.cuda_stream
+                stream.wait_stream(self._last)
+            self._last = stream
+        return current
 
     def _tensor(self, name: str, t: torch.Tensor, dtype: torch.dtype, shape) -> int:
         """address of a tensor whose type, device and shape have been looked at"""
-        if t.dtype != dtype or t.device != self.device or t.shape != torch.Size(shape):
+        if t.dtype != dtype or t.device != self.device or t.shape != shape:
             raise ValueError(f"{name}: {dtype} {tuple(shape)} on {self.device} is wanted, got {t.dtype} {tuple(t.shape)} on {t.device}")
         return t.data_ptr()
 
