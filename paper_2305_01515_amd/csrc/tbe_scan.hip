@@ -27,6 +27,7 @@ using namespace tbe;
 namespace {
 
 constexpr int kThreads = 256, kWaves = kThreads / 64;
+constexpr int kGradThreads = 512, kGradWaves = kGradThreads / 64;  // the gradient: a chunk's rows on twice the lanes
 constexpr int64_t kChainedBags = 2;  // chunks that a bag may have on average for them to hear from each other
 constexpr int kJoinChannels = 4, kJoinSegments = 256;
 
@@ -73,8 +74,8 @@ __device__ inline void gated(float u, float x, bool coupled, float &f, float &b)
   const float i = u < -80.0f ? 1.0f : e * f;
   b = coupled ? i * x : x;
 }
-__device__ inline float keep_of(float q) { return signbit(q) ? 1.0f + q : q; }
-__device__ inline float take_of(float q) { return signbit(q) ? -q : 1.0f - q; }
+__device__ inline float keep_of(float q) { return signbit(q) ? 1.0f - fabsf(q) : q; }
+__device__ inline float take_of(float q) { return signbit(q) ? -q : 1.0f - fabsf(q); }
 
 template <int DT>
 struct Rows {
@@ -147,9 +148,9 @@ __global__ __launch_bounds__(kThreads) void scan_prepare_kernel(const int64_t *o
 }
 
 // The chunk's marks in LDS: [2 r] is 1 + the bag that starts at row r of the chunk, [2 r + 1] 1 + the bag whose last row that is, or 0.
-template <class A>
+template <int THREADS, class A>
 __device__ inline void fetch_marks(const A &a, int64_t row0, uint32_t call, int32_t *marks) {
-  for (int k = threadIdx.x; k < a.chunk_rows; k += kThreads) {
+  for (int k = threadIdx.x; k < a.chunk_rows; k += THREADS) {
     const ulonglong2 m = row0 + k < a.rows ? a.marks[row0 + k] : ulonglong2{0, 0};
     marks[2 * k] = (uint32_t)(m.x >> 32) == call ? (int32_t)(uint32_t)m.x + 1 : 0;
     marks[2 * k + 1] = (uint32_t)(m.y >> 32) == call ? (int32_t)(uint32_t)m.y + 1 : 0;
@@ -258,16 +259,26 @@ __device__ inline float hear_and_say(const A &a, int chunk, int d, uint32_t call
   return s;
 }
 
-// (A, H) becomes the map of all lane groups of the wavefront up to this one (BACK: from the last one down to it)
+// (A, H) becomes the map of all lane groups of the wavefront up to this one (BACK: from the last one down to it); reset: whether a bag starts
+// (ends) among their rows, the same for all elements, so that what joins is a matter of lanes and not of each element.
 template <int V, bool BACK>
-__device__ inline void scan_wave(float (&A)[V], float (&H)[V], int L) {
+__device__ inline void scan_wave(float (&A)[V], float (&H)[V], bool &reset, int L) {
   const int lane = threadIdx.x & 63;
   for (int k = L; k < 64; k *= 2) {
-    const bool has = BACK ? lane + k < 64 : lane >= k;
+    float pa[V], ph[V];
 #pragma unroll
     for (int v = 0; v < V; v++) {
-      const float pa = BACK ? __shfl_down(A[v], k) : __shfl_up(A[v], k), ph = BACK ? __shfl_down(H[v], k) : __shfl_up(H[v], k);
-      if (has) join(pa, ph, A[v], H[v]);
+      pa[v] = BACK ? __shfl_down(A[v], k) : __shfl_up(A[v], k);
+      ph[v] = BACK ? __shfl_down(H[v], k) : __shfl_up(H[v], k);
+    }
+    const bool pr = BACK ? __shfl_down((int)reset, k) : __shfl_up((int)reset, k), has = BACK ? lane + k < 64 : lane >= k;
+    if (has && !reset) {
+#pragma unroll
+      for (int v = 0; v < V; v++) {
+        H[v] = A[v] * ph[v] + H[v];
+        A[v] *= pa[v];
+      }
+      reset = pr;
     }
   }
 }
@@ -284,42 +295,39 @@ __device__ inline void tell_wave(const float (&A)[V], const float (&H)[V], int L
       tot[(wave * 2 + 1) * C + c + v] = H[v];
     }
 }
-template <bool BACK>
+template <bool BACK, int W>
 __device__ inline void map_of_waves(const float *tot, int C, int c, float &A, float &H) {
   A = 1.0f;
   H = 0.0f;
 #pragma unroll
-  for (int k = 0; k < kWaves; k++) {
-    const int w = BACK ? kWaves - 1 - k : k;
+  for (int k = 0; k < W; k++) {
+    const int w = BACK ? W - 1 - k : k;
     const float wa = tot[(w * 2) * C + c], wh = tot[(w * 2 + 1) * C + c];
     H = go(wa, wh, H);
     A = signbit(wa) ? wa : wa * A;
   }
 }
-template <bool BACK>
+template <bool BACK, int W>
 __device__ inline void join_waves(float *tot, int C, int c, float s) {
 #pragma unroll
-  for (int k = 0; k < kWaves; k++) {
-    const int w = BACK ? kWaves - 1 - k : k;
+  for (int k = 0; k < W; k++) {
+    const int w = BACK ? W - 1 - k : k;
     const float wa = tot[(w * 2) * C + c], wh = tot[(w * 2 + 1) * C + c];
     tot[(w * 2) * C + c] = s;
     s = go(wa, wh, s);
   }
 }
 template <int V, bool BACK>
-__device__ inline void start_of_lane(const float (&A)[V], const float (&H)[V], int L, const float *tot, float (&s)[V]) {
+__device__ inline void start_of_lane(const float (&A)[V], const float (&H)[V], bool reset, int L, const float *tot, float (&s)[V]) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, C = L * V, c = (lane & (L - 1)) * V;
-  const bool first = BACK ? lane >= 64 - L : lane < L;
+  const bool first = BACK ? lane >= 64 - L : lane < L, pr = BACK ? __shfl_down((int)reset, L) : __shfl_up((int)reset, L);
 #pragma unroll
   for (int v = 0; v < V; v++) {
     const float w = tot[(wave * 2) * C + c + v];
     const float pa = BACK ? __shfl_down(A[v], L) : __shfl_up(A[v], L), ph = BACK ? __shfl_down(H[v], L) : __shfl_up(H[v], L);
-    s[v] = first ? w : go(pa, ph, w);
+    s[v] = first ? w : pr ? ph : pa * w + ph;
   }
 }
-
-// Rows behind the last one are taken for rows of zeros: nothing comes after them, and the gradient's way back from them ends at the
-// last row, where a bag ends.
 
 // V fp32 numbers of a row, or zeros without one
 template <int V>
@@ -354,8 +362,9 @@ __global__ __launch_bounds__(kThreads) void scan_sum_kernel(Rows<DT> a) {
       if (in) xv[j] = load_pack<E, V, ALIGNED>(in + (row0 + r0 + j) * stride + c0);
     }
   }
-  fetch_marks(a, row0, a.call[0], marks);
+  fetch_marks<kThreads>(a, row0, a.call[0], marks);
   float A[V], H[V];
+  bool reset = false;
 #pragma unroll
   for (int v = 0; v < V; v++) { A[v] = 1.0f; H[v] = 0.0f; }
 #pragma unroll
@@ -363,6 +372,7 @@ __global__ __launch_bounds__(kThreads) void scan_sum_kernel(Rows<DT> a) {
     const int j = BACK ? R - 1 - k : k;
     const int32_t bag = marks[2 * (r0 + j) + (BACK ? 1 : 0)];
     if (bag) {
+      reset = true;
       const float *s = BACK ? a.dlast : a.h0;
       const int64_t at = (int64_t)(bag - 1) * (BACK ? a.dim : a.h0s) + c0;
 #pragma unroll
@@ -379,12 +389,12 @@ __global__ __launch_bounds__(kThreads) void scan_sum_kernel(Rows<DT> a) {
       A[v] *= f;
     }
   }
-  scan_wave<V, BACK>(A, H, a.L);
+  scan_wave<V, BACK>(A, H, reset, a.L);
   tell_wave<V, BACK>(A, H, a.L, lds);
   __syncthreads();
   for (int c = threadIdx.x; c < C && tile * C + c < a.dim; c += kThreads) {
     float A1, H1;
-    map_of_waves<BACK>(lds, C, c, A1, H1);
+    map_of_waves<BACK, kWaves>(lds, C, c, A1, H1);
     a.maps[(int64_t)chunk * 2 * a.dim + tile * C + c] = A1;
     a.maps[((int64_t)chunk * 2 + 1) * a.dim + tile * C + c] = H1;
   }
@@ -484,7 +494,7 @@ __global__ __launch_bounds__(kThreads) void scan_apply_kernel(Rows<DT> a) {
   }
   const uint32_t call = a.call[0];
   if (blockIdx.x == 0 && threadIdx.x == 0) a.call[1] = call + 1;  // nothing looks at that one in this kernel
-  fetch_marks(a, row0, call, marks);
+  fetch_marks<kThreads>(a, row0, call, marks);
   // The first start among the lane's rows: its state is asked for before the gates are computed.
   int first = R;
 #pragma unroll
@@ -519,7 +529,8 @@ __global__ __launch_bounds__(kThreads) void scan_apply_kernel(Rows<DT> a) {
       }
     }
   }
-  scan_wave<V, false>(A, H, a.L);
+  bool reset = starts != 0;
+  scan_wave<V, false>(A, H, reset, a.L);
   tell_wave<V, false>(A, H, a.L, lds);
   __syncthreads();
   for (int c = threadIdx.x; c < C; c += kThreads) {
@@ -529,18 +540,18 @@ __global__ __launch_bounds__(kThreads) void scan_apply_kernel(Rows<DT> a) {
       float *before = a.before ? a.before + (int64_t)chunk * a.dim + d : nullptr;
       if (a.chained) {
         float A1, H1;
-        map_of_waves<false>(lds, C, c, A1, H1);
+        map_of_waves<false, kWaves>(lds, C, c, A1, H1);
         s = hear_and_say<false>(a, chunk, d, call, A1, H1);
         if (before) *before = s;
       } else {
         s = *before;
       }
     }
-    join_waves<false>(lds, C, c, s);
+    join_waves<false, kWaves>(lds, C, c, s);
   }
   __syncthreads();
   float h[V];
-  start_of_lane<V, false>(A, H, a.L, lds, h);
+  start_of_lane<V, false>(A, H, reset, a.L, lds, h);
   if (!on) return;
 #pragma unroll
   for (int j = 0; j < R; j++) {
@@ -559,14 +570,14 @@ __global__ __launch_bounds__(kThreads) void scan_apply_kernel(Rows<DT> a) {
 }
 
 template <int DT, int V, bool ALIGNED>
-__global__ __launch_bounds__(kThreads) void scan_grad_kernel(Rows<DT> a) {
+__global__ __launch_bounds__(kGradThreads, V == 1 ? 2 : 4) void scan_grad_kernel(Rows<DT> a) {
   using E = typename Elem<DT>::type;
-  constexpr int R = 32 / V;
+  constexpr int R = 32 * kThreads / kGradThreads / V;
   extern __shared__ float lds[];
   // from the last chunk on: what a chunk hears of is behind it
   const int chunk = a.chunks - 1 - blockIdx.x / a.tiles, tile = blockIdx.x % a.tiles, C = a.L * V;
-  float *back = lds + kWaves * 2 * C;
-  int32_t *marks = (int32_t *)(back + kWaves * 2 * C);
+  float *back = lds + kGradWaves * 2 * C;
+  int32_t *marks = (int32_t *)(back + kGradWaves * 2 * C);
   const int64_t row0 = (int64_t)chunk * a.chunk_rows;
   const int group = threadIdx.x / a.L, l = threadIdx.x & (a.L - 1), c0 = (tile * a.L + l) * V, r0 = group * R;
   const int rows = (int)min((int64_t)a.chunk_rows, a.rows - row0);
@@ -585,7 +596,7 @@ __global__ __launch_bounds__(kThreads) void scan_grad_kernel(Rows<DT> a) {
   }
   const uint32_t call = a.call[0];
   if (blockIdx.x == 0 && threadIdx.x == 0) a.call[1] = call + 1;  // nothing looks at that one in this kernel
-  fetch_marks(a, row0, call, marks);
+  fetch_marks<kGradThreads>(a, row0, call, marks);
   // The first start and the last end among the lane's rows: what belongs to them is asked for before the gates are computed.
   int first = R, last = -1;
 #pragma unroll
@@ -641,39 +652,35 @@ __global__ __launch_bounds__(kThreads) void scan_grad_kernel(Rows<DT> a) {
       B[v] *= f;
     }
   }
-  scan_wave<V, false>(A, H, a.L);
+  bool reset = first < R, reset_back = last >= 0;
+  scan_wave<V, false>(A, H, reset, a.L);
   tell_wave<V, false>(A, H, a.L, lds);
-  scan_wave<V, true>(B, G, a.L);
+  scan_wave<V, true>(B, G, reset_back, a.L);
   tell_wave<V, true>(B, G, a.L, back);
   __syncthreads();
-  for (int c = threadIdx.x; c < C; c += kThreads) {
+  for (int c = threadIdx.x; c < C; c += kGradThreads) {
     const int d = tile * C + c;
     float s = 0.0f, g = 0.0f;
     if (a.chunks > 1 && d < a.dim) {
       s = a.before[(int64_t)chunk * a.dim + d];
       if (a.chained) {
         float A1, H1;
-        map_of_waves<true>(back, C, c, A1, H1);
+        map_of_waves<true, kGradWaves>(back, C, c, A1, H1);
         g = hear_and_say<true>(a, chunk, d, call, A1, H1);
       } else {
         g = a.behind[(int64_t)chunk * a.dim + d];
       }
     }
-    join_waves<false>(lds, C, c, s);
-    join_waves<true>(back, C, c, g);
+    join_waves<false, kGradWaves>(lds, C, c, s);
+    join_waves<true, kGradWaves>(back, C, c, g);
   }
   __syncthreads();
   float w[R][V], s[V];  // w: du / g
-  start_of_lane<V, false>(A, H, a.L, lds, s);
+  start_of_lane<V, false>(A, H, reset, a.L, lds, s);
 #pragma unroll
   for (int j = 0; j < R; j++) {
     const int32_t bag = marks[2 * (r0 + j)];
-    if (bag) {
-      if (j != first) load_row(a.h0, (int64_t)(bag - 1) * a.h0s + c0, on, s);
-      else
-#pragma unroll
-        for (int v = 0; v < V; v++) s[v] = start[v];
-    }
+    if (bag) load_row(a.h0, (int64_t)(bag - 1) * a.h0s + c0, on, s);  // again: kept from above, it would take registers
 #pragma unroll
     for (int v = 0; v < V; v++) {
       opaque(q[j][v]);
@@ -682,17 +689,12 @@ __global__ __launch_bounds__(kThreads) void scan_grad_kernel(Rows<DT> a) {
       s[v] = f * s[v] + (a.coupled ? i * x : x);
     }
   }
-  start_of_lane<V, true>(B, G, a.L, back, s);
+  start_of_lane<V, true>(B, G, reset_back, a.L, back, s);
   if (!on) return;
 #pragma unroll
   for (int j = R - 1; j >= 0; j--) {
     const int32_t bag = marks[2 * (r0 + j)], ended = marks[2 * (r0 + j) + 1];
-    if (ended) {
-      if (j != last) load_row(a.dlast, (int64_t)(ended - 1) * a.dim + c0, on, s);
-      else
-#pragma unroll
-        for (int v = 0; v < V; v++) s[v] = finish[v];
-    }
+    if (ended) load_row(a.dlast, (int64_t)(ended - 1) * a.dim + c0, on, s);
     Pack<E, V> dx, du;
 #pragma unroll
     for (int v = 0; v < V; v++) {
@@ -783,7 +785,7 @@ int run(const tbe_scan_t *s, const Rows<DT> &a, bool grad, hipStream_t stream) n
       scan_sum_kernel<DT, V, ALIGNED, true><<<grid, kThreads, tot + marks, stream>>>(a);
       scan_join_kernel<true><<<joins, kJoinChannels * kJoinSegments, 0, stream>>>(a.maps, a.behind, a.chunks, a.dim);
     }
-    scan_grad_kernel<DT, V, ALIGNED><<<grid, kThreads, 2 * tot + marks, stream>>>(a);
+    scan_grad_kernel<DT, V, ALIGNED><<<grid, kGradThreads, 2 * tot * kGradWaves / kWaves + marks, stream>>>(a);
   }
   return check_launch();
 }
