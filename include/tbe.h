@@ -510,7 +510,8 @@ int tbe_plan_placement(const tbe_place_table *tables, int32_t num_tables, const 
  * Gated linear recurrence over the rows of every bag.  With f = 1 / (1 + exp(-u)), element by element,
  *   h_t = f_t h_{t-1} + (1 - f_t) x_t   (coupled = 1)   or   h_t = f_t h_{t-1} + x_t   (coupled = 0)
  * for the rows t = offsets[b] .. offsets[b+1]-1 of bag b in turn, from h = d_h0[b] (null: zero).
- * dim: elements of a row, 1 .. 65536; max_bags, max_rows: what a call may bring at most.
+ * dim: elements of a row, 1 .. 65536; max_bags, max_rows: what a call may bring at most (scratch memory: 16 bytes
+ * for each of max_rows and 28 * dim for each chunk of them, which has 8192 elements, or somewhat fewer where dim is no power of two).
  */
 typedef struct tbe_scan_t *tbe_scan_handle;
 int tbe_scan_create(tbe_scan_handle *out, int32_t dim, int32_t dtype, int32_t coupled, int64_t max_bags,
@@ -582,13 +583,14 @@ typedef struct {
 } tbe_bias_strides;
 
 /* d_out = d_scores * scale + table[bucket] (d_scores null: the table's value alone), mask_value where masked whatever the
- * scores hold there.  d_table: [buckets, heads] of table_dtype.  d_out may be d_scores. */
+ * scores hold there.  d_table: [buckets, heads] of table_dtype.  d_out may be d_scores, with the same strides.  Positions lie less
+ * than 2^62 apart. */
 int tbe_bias_forward(tbe_bias_handle s, const tbe_bias_shape *shape, const void *d_table, int32_t table_dtype,
                      const void *d_scores, const tbe_bias_strides *scores_strides, float scale, float mask_value, void *d_out,
                      const tbe_bias_strides *out_strides, void *stream);
 
 /* d_dtable (fp32 [buckets, heads], or null) = sums of d_dout over everything unmasked, by bucket and head; the same inputs give the
- * same bits.  d_dscores (or null) = d_dout * scale, 0 where masked; it may be d_dout.  What d_dout holds at masked places has
+ * same bits.  d_dscores (or null) = d_dout * scale, 0 where masked; it may be d_dout, with the same strides.  What d_dout holds at masked places has
  * no influence. */
 int tbe_bias_backward(tbe_bias_handle s, const tbe_bias_shape *shape, const void *d_dout,
                       const tbe_bias_strides *dout_strides, float *d_dtable, float scale, void *d_dscores,

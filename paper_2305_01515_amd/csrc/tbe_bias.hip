@@ -567,7 +567,6 @@ extern "C" {
 int tbe_bias_destroy(tbe_bias_handle s) {
   if (!s) return TBE_OK;
   (void)hipFree(s->map);
-  (void)hipFree(s->part);
   delete s;
   return TBE_OK;
 }
@@ -602,9 +601,9 @@ int tbe_bias_create(tbe_bias_handle *out, int32_t heads, const int64_t *h_thresh
     map.reached[c] = (uint8_t)all;
     if (some - all > s->steps) s->steps = some - all;
   }
-  hipError_t e = hipGetDevice(&s->device);
-  if (e == hipSuccess) e = hipMalloc((void **)&s->map, sizeof(Buckets));
-  if (e == hipSuccess) e = hipMalloc((void **)&s->part, (size_t)kMaxParts * heads * s->buckets * sizeof(float));
+  hipError_t e = hipGetDevice(&s->device);  // one block: [map][part]
+  if (e == hipSuccess) e = hipMalloc((void **)&s->map, sizeof(Buckets) + (size_t)kMaxParts * heads * s->buckets * sizeof(float));
+  s->part = (float *)(s->map + 1);
   if (e == hipSuccess) e = hipMemcpy(s->map, &map, sizeof map, hipMemcpyHostToDevice);
   if (e != hipSuccess) {
     (void)tbe_bias_destroy(s);

@@ -28,7 +28,7 @@ namespace {
 
 constexpr int kThreads = 256, kWaves = kThreads / 64;
 constexpr int kGradThreads = 512, kGradWaves = kGradThreads / 64;  // the gradient: a chunk's rows on twice the lanes
-constexpr int64_t kChainedBags = 2;  // chunks that a bag may have on average for them to hear from each other
+constexpr int64_t kChainedBags = 16;  // chunks that a bag may have on average for them to hear from each other
 constexpr int kJoinChannels = 4, kJoinSegments = 256;
 
 // How the rows of a handle are cut: a function of dim and the type alone, because the backward uses what the forward saved.
@@ -402,7 +402,7 @@ __global__ __launch_bounds__(kThreads) void scan_sum_kernel(Rows<DT> a) {
 
 // States before the chunks (BACK: behind them) from their maps.  A workgroup has 4 elements; its lanes take 256 segments of the chunks, up
 // to kKept of each in registers, and a wavefront for each element joins the segments, 4 a lane, by exchange between lanes.  (With 16
-// elements and 64 segments a workgroup there were too few lanes for the way to memory: 24 us instead of 8 for 3837 chunks of 128.)
+// elements and 64 segments a workgroup there were too few lanes for the way to memory: 15.5 us instead of 11.9 for 2347 chunks of 64.)
 template <bool BACK>
 __global__ __launch_bounds__(kJoinChannels *kJoinSegments) void scan_join_kernel(const float *maps, float *state, int chunks, int dim) {
   constexpr int kKept = 8;
@@ -825,7 +825,9 @@ Rows<DT> rows_of(const tbe_scan_t *s, const void *x, int64_t xs, const void *u, 
   a.chunk_rows = s->cut.rows;
   a.chunks = (int)chunks_of(s, rows);
   a.coupled = s->coupled;
-  // A chunk of mean rows or more has a start as a rule; with longer bags the chunks would wait for long chains of others.
+  // With bags of many chunks a chunk goes through long chains of others.  262144 rows, forward and backward in us, chunks that hear / sum and
+  // join: rows of 128 in bfloat16 (chunks of 64), bags of 64 rows 51 + 126 / 98 + 161, 512: 59 + 139 / 97 + 160, 2048: 86 + 187 / 97 + 160,
+  // 65536: 491 + 665 / 97 + 159; of 64 in fp32 (chunks of 128), 128: 39 + 79 / 68 + 101, 2048: 48 + 91 / 68 + 100, 65536: 188 + 267 / 68 + 99.
   a.chained = rows <= bags * kChainedBags * s->cut.rows;
   return a;
 }

@@ -112,6 +112,7 @@ class _ScanFunction(torch.autograd.Function):
     @staticmethod
     def forward(ctx, plan, x, u, offsets, h0):
         y, last, saved = plan.forward(x, u, offsets, h0, save=True)
+        ctx.set_materialize_grads(False)
         ctx.plan = plan
         ctx.save_for_backward(x, u, offsets, h0, saved)
         return y, last
