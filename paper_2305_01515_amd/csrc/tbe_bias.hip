@@ -23,6 +23,7 @@ constexpr int kSums = 2048;                  // numbers of a wavefront's sums of
 constexpr int kForward = 1024;               // workgroups of the forward
 constexpr int kHeads = 4;                    // packs of scores on their way at once: as many heads
 constexpr int kFill = 2048;                  // wavefronts that the gradient wants at least
+constexpr size_t kLds = 160 << 10;            // of a CU
 constexpr int kMaxParts = 1024;              // workgroups whose sums of a head are added up
 
 struct Buckets {  // in device memory
@@ -155,6 +156,8 @@ __device__ inline void place_of(const Shape &p, uint32_t item, uint32_t &i, uint
 
 // PLAIN: every pack is written whole (two that overlap write the same), which spares a branch a head (16 x 2048 x 2048: 41 us, without 26).
 // Not for rows shorter than a pack, nor where a pack that is read may be written already by the one that overlaps it.
+// Bound by memory: 512 x 8 x 1 x 1001 in fp32 8.6 us, 256 x 4 x 199 x 199 in binary16 31 us (5.2 TB/s), 16 x 2048 x 2048 in bfloat16, written only,
+// 27 us (5 TB/s).
 // A workgroup has a group of heads (blockIdx.y), whose part of the table it keeps in LDS, and of all samples' packs of keys every
 // gridDim.x-th 256.
 template <int DT, bool SCORES, bool PLAIN>
@@ -225,7 +228,7 @@ __global__ __launch_bounds__(kThreads) void bias_forward_kernel(Shape p, int gro
 // a list in LDS.  Whenever the list has kRounds * 64 packs, it goes through the heads with them: every lane adds to sums of its own in LDS,
 // [buckets + 1][64 lanes] (no two lanes on one bank; the row more takes what is masked), and the 64 lanes' sums of a head are then
 // added up into the wavefront's [heads][buckets].  One lane, one order: the same bits each time.  What bounds it is the way through LDS
-// and back of each addition, so a masked pack costs nothing here.
+// and back of each addition (256 x 4 x 199 x 199, two thirds masked: 55 us), so a masked pack costs nothing here.
 // (Additions by LDS atomics take several times as long, also without two lanes on one bank: 295 us instead of 81 for 256 x 4 x 199 x 199.)
 constexpr int kRounds = 4, kList = (kRounds + 1) * 64;
 
@@ -394,6 +397,8 @@ __global__ __launch_bounds__(kThreads) void bias_scores_kernel(Shape p, const ty
 // one after another down a diagonal, which all have the same 2 V - 1 diagonals, and keeps their sums in registers: one addition an element,
 // and every load a whole pack.  64 lanes have neighbouring squares.  A wavefront's unit of work is 64 such columns of squares, `seg`
 // squares of each (of the same queries), for `samples` samples; at its end its diagonals are joined in LDS and added to their buckets.
+// Bound by the latency of memory, with four wavefronts a SIMD: 16 x 8 x 1024 x 1024 in bfloat16 52 us (5.1 TB/s) where the cache holds the
+// scores, 60 where not; by the kernel above 140.
 constexpr int kUnits = 4096;  // units that the work is cut into, if they have 4 squares at least (16 x 8 x 1024 x 1024: 52 us; 8192: 65)
 
 struct Diagonals {
@@ -518,7 +523,7 @@ __global__ __launch_bounds__(kThreads, SCORES ? 2 : 4) void bias_grad_index_kern
   }
 }
 
-// a wavefront for each number of the table's gradient
+// A wavefront for each number of the table's gradient; 5 us for up to 1024 sums of each.
 __global__ __launch_bounds__(kThreads) void bias_join_kernel(const float *part, int parts, int heads, int buckets, float *dtable) {
   const int id = blockIdx.x * kWaves + (threadIdx.x >> 6), lane = threadIdx.x & 63, h = id / buckets, c = id % buckets;
   if (h >= heads) return;
@@ -683,10 +688,12 @@ int tbe_bias_backward(tbe_bias_handle s, const tbe_bias_shape *shape, const void
       int group = p.heads;
       while (group > 1 && group * p.buckets > kSums) group = (group + 1) / 2;
       while (group > 1 && lists * ((p.heads + group - 1) / group) < kFill) group = (group + 1) / 2;
-      const int waves = p.buckets <= 128 ? 4 : 2;
+      // wavefronts of a workgroup: as many as have room for their sums beside the finder
+      const size_t own = grad_floats(p.buckets, group, 16 / elem_bytes(p.s.dtype)) * sizeof(float);
+      const int waves = 4 * own + sizeof(Finder) <= kLds ? 4 : 3 * own + sizeof(Finder) <= kLds ? 3 : 2 * own + sizeof(Finder) <= kLds ? 2 : 1;
       parts = (int)((lists + waves - 1) / waves < kMaxParts ? (lists + waves - 1) / waves : kMaxParts);
       const dim3 grid((unsigned)parts, (unsigned)((p.heads + group - 1) / group));
-      const size_t lds = (size_t)waves * grad_floats(p.buckets, group, 16 / elem_bytes(p.s.dtype)) * sizeof(float);
+      const size_t lds = waves * own;
       const int64_t blocks = blocks_of(p);
       const dim3 all((unsigned)(blocks < 4096 ? blocks : 4096));
 #define LAUNCH2(DT)                                                                                                                              \

@@ -218,6 +218,21 @@ def test_graph_replays():
             assert torch.equal(a, b)
 
 
+@pytest.mark.parametrize("heads", [1, 8, 20])
+@pytest.mark.parametrize("count", [31, 32, 47, 48, 63, 64, 65, 95, 100, 126, 127])
+@pytest.mark.parametrize("both", [False, True])
+def test_numbers_of_buckets_and_heads(count, heads, both):
+    """what a workgroup keeps of sums and of the table grows with both, and has to fit"""
+    c = Case(2, heads, 21, 45, list(range(1, 2 * count, 2)), both=both, positions="any", causal=heads == 8, dtype="bf16" if count % 2 else "f32", seed=count)
+    plan = c.plan()
+    dt = TYPES[c.dtype][0]
+    c.check_values(plan.forward(c.table.cuda(), shape=(2, 21, 45), dtype=dt, **c.where()), None, 1.0, -math.inf)
+    dout = c.scores().cuda()
+    c.check_gradient(plan.backward(dout, **c.where()), dout)
+    i = Case(2, heads, 21, 45, list(range(1, 2 * count, 2)), both=both, causal=heads == 8, dtype=c.dtype, seed=count)
+    i.check_gradient(i.plan().backward(dout, **i.where()), dout)
+
+
 def test_empty_sizes():
     c = Case(1, 2, 5, 5, LOG, both=True)
     plan = c.plan()

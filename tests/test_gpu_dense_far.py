@@ -1,0 +1,78 @@
+"""Rows, scores and weights whose places do not fit 32 bits: the same bits as from a compact copy."""
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+
+def far(t, stride):
+    """t's rows, `stride` elements apart"""
+    room = torch.empty((t.shape[0] - 1) * stride + t.shape[1], dtype=t.dtype, device="cuda")
+    v = room.as_strided(t.shape, (stride, 1))
+    v.copy_(t)
+    return v
+
+
+@pytest.mark.parametrize("lengths", [[200, 0, 400, 1], [600], [3] * 200])
+def test_scan_rows_far_apart(lengths):
+    from paper_2305_01515_amd.dense import Scan
+    n, dim, stride = sum(lengths), 64, 1 << 22  # 2.5 G elements
+    g = torch.Generator().manual_seed(1)
+    x, u, dy = (torch.randn(n, dim, generator=g).bfloat16().cuda() for _ in range(3))
+    off = torch.tensor([0] + lengths).cumsum(0).cuda()
+    plan = Scan(dim, torch.bfloat16, len(lengths), n)
+    y, last, saved = plan.forward(x, u, off, save=True)
+    want = plan.backward(x, u, off, saved, dy, last)
+    fx, fu, fy = far(x, stride), far(u, stride), torch.empty((n - 1) * stride + dim, dtype=torch.bfloat16, device="cuda").as_strided((n, dim), (stride, 1))
+    y2, last2, saved2 = plan.forward(fx, fu, off, y=fy, save=True)
+    assert torch.equal(y, y2) and torch.equal(last, last2) and torch.equal(saved, saved2)
+    got = plan.backward(fx, fu, off, saved2, far(dy, stride), last2)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+def test_scan_states_far_apart():
+    from paper_2305_01515_amd.dense import Scan
+    dim, slots, stride = 64, 700, 1 << 22  # 2.9 G elements of fp32
+    g = torch.Generator().manual_seed(2)
+    state, x, u = (torch.randn(k, dim, generator=g).cuda() for k in (slots, 9, 9))
+    slot = torch.tensor([699, 0, 650, 3, 512, 511, 640, 1, 698]).cuda()
+    plan = Scan(dim, torch.float32, 9, 9)
+    wide = far(state, stride)
+    assert torch.equal(plan.step(wide, x, u, slot), plan.step(state, x, u, slot))
+    assert torch.equal(wide, state)
+
+
+@pytest.mark.parametrize("times", [False, True])
+@pytest.mark.parametrize("keys", [64, 61])
+def test_scores_far_apart(keys, times):
+    from paper_2305_01515_amd.dense import RelativeBias
+    b, h, q = 3, 2, 40
+    g = torch.Generator().manual_seed(3)
+    scores, table = torch.randn(b, h, q, keys, generator=g).half().cuda(), torch.randn(10, h, generator=g).cuda()
+    strides = (1 << 30, 1 << 29, 1 << 23, 1)
+    room = torch.empty(2 * (1 << 30) + (1 << 29) + 39 * (1 << 23) + keys, dtype=torch.float16, device="cuda")
+    wide = room.as_strided(scores.shape, strides)
+    wide.copy_(scores)
+    where = dict(causal=True, key_lengths=torch.tensor([keys, 5, 30]).cuda())
+    if times:
+        t = torch.randint(0, 9, (b, keys), generator=g).cumsum(1).cuda()
+        where.update(q_pos=t[:, :q].contiguous(), k_pos=t)
+    plan = RelativeBias(h, [1, 2, 5, 20], bidirectional=True)
+    want, grads = plan.forward(table, scores=scores, **where), plan.backward(scores, want_dscores=True, **where)
+    got = plan.backward(wide, want_dscores=True, **where)
+    assert torch.equal(got[0], grads[0]) and torch.equal(got[1], grads[1])
+    assert torch.equal(plan.forward(table, scores=wide, out=wide, **where), want)
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_a_tensor_of_more_than_2_31_weights(bits):
+    """all weights alike: what becomes of one becomes of all, but that codes are drawn for each"""
+    from paper_2305_01515_amd.dense import AdamW
+    n = (1 << 31) + 5000
+    p, g = torch.ones(n, dtype=torch.bfloat16, device="cuda"), torch.full((n,), 0.25, dtype=torch.bfloat16, device="cuda")
+    opt = AdamW([p], lr=0.125, weight_decay=0.0, state_bits=bits)
+    opt.step([g])
+    assert float(p.min()) == float(p.max()) == 0.875
+    for k in "mv":
+        s = opt.states[k]
+        assert bool((s[:n] == s[0]).all()) and not bool(s[n:].any())
