@@ -13,8 +13,8 @@
 // The gradient runs the other way with c_t = f_t g_t = f_t (dy_t + c_{t+1}), reset where a bag ends, beside the forward's states again
 // from those before the chunks, which the forward saved.
 //
-// A row lies on L lanes of V elements (16 bytes; one element where dim is no multiple of that), a lane has R rows in a row in
-// registers, 32 elements of each input (16 in the gradient, which keeps more of each).  The maps of a wavefront's 64 / L lane groups are
+// A row lies on L lanes of V elements (16 bytes, or the largest half of that, quarter, ... that divides dim), a lane has R rows in a row in
+// registers, 32 elements of each input or fewer (apply_threads, grad_threads).  The maps of a wavefront's 64 / L lane groups are
 // joined by exchange between lanes, those of the workgroup's wavefronts through LDS.
 #include <cmath>
 #include <new>
@@ -27,7 +27,9 @@ using namespace tbe;
 namespace {
 
 constexpr int kThreads = 256, kWaves = kThreads / 64;
-constexpr int kGradThreads = 512, kGradWaves = kGradThreads / 64;  // the gradient: a chunk's rows on twice the lanes
+// A chunk's rows lie on as many lanes as leave four wavefronts a SIMD room for their registers: single elements and the gradient on more.
+constexpr int apply_threads(int V) { return V <= 2 ? 2 * kThreads : kThreads; }
+constexpr int grad_threads(int V) { return V <= 2 ? 4 * kThreads : 2 * kThreads; }
 constexpr int64_t kChainedBags = 16;  // chunks that a bag may have on average for them to hear from each other
 constexpr int kJoinChannels = 4, kJoinSegments = 256;
 
@@ -40,8 +42,8 @@ struct Cut {
 
 Cut cut_of(int dim, int dtype) {
   Cut c;
-  const int wide = 16 / elem_bytes(dtype);
-  c.V = dim % wide ? 1 : wide;
+  c.V = 16 / elem_bytes(dtype);
+  while (dim % c.V) c.V /= 2;
   c.R = 32 / c.V;
   const int lanes = dim / c.V;
   c.L = c.V == 1 ? 2 : 1;  // at least 2 for single elements: a chunk has 4096 rows at most
@@ -97,25 +99,16 @@ struct Rows {
   bool coupled, chained;  // chained: chunks hear from each other instead of sum and join
 };
 
-template <class E, int V, bool ALIGNED>
+// V elements at any address that an element may have
+template <class E, int V>
 __device__ inline Pack<E, V> load_pack(const E *p) {
   Pack<E, V> r;
-  if constexpr (ALIGNED) {
-    r = *(const Pack<E, V> *)p;
-  } else {
-#pragma unroll
-    for (int v = 0; v < V; v++) r.e[v] = p[v];
-  }
+  __builtin_memcpy(&r, p, sizeof r);
   return r;
 }
-template <class E, int V, bool ALIGNED>
+template <class E, int V>
 __device__ inline void store_pack(E *p, const Pack<E, V> &r) {
-  if constexpr (ALIGNED) {
-    *(Pack<E, V> *)p = r;
-  } else {
-#pragma unroll
-    for (int v = 0; v < V; v++) p[v] = r.e[v];
-  }
+  __builtin_memcpy(p, &r, sizeof r);
 }
 
 // Marks at the rows where bags start and end, with the number of the call (those of earlier calls are not cleared); empty bags get
@@ -339,7 +332,7 @@ __device__ inline void load_row(const float *p, int64_t at, bool there, float (&
 __device__ inline void opaque(float &x) { asm volatile("" : "+v"(x)); }
 
 // Maps of the chunks: of h from x and u, BACK: of c from dy and u.  Bound by memory (3 bags of 100 k rows of 64 in fp32: 26 us, 6 TB/s).
-template <int DT, int V, bool ALIGNED, bool BACK>
+template <int DT, int V, bool BACK>
 __global__ __launch_bounds__(kThreads) void scan_sum_kernel(Rows<DT> a) {
   using E = typename Elem<DT>::type;
   constexpr int R = 32 / V;
@@ -358,8 +351,8 @@ __global__ __launch_bounds__(kThreads) void scan_sum_kernel(Rows<DT> a) {
     xv[j] = {};
     uv[j] = {};
     if (on) {
-      uv[j] = load_pack<E, V, ALIGNED>(a.u + (row0 + r0 + j) * a.us + c0);
-      if (in) xv[j] = load_pack<E, V, ALIGNED>(in + (row0 + r0 + j) * stride + c0);
+      uv[j] = load_pack<E, V>(a.u + (row0 + r0 + j) * a.us + c0);
+      if (in) xv[j] = load_pack<E, V>(in + (row0 + r0 + j) * stride + c0);
     }
   }
   fetch_marks<kThreads>(a, row0, a.call[0], marks);
@@ -475,13 +468,13 @@ __global__ __launch_bounds__(kJoinChannels *kJoinSegments) void scan_join_kernel
 // the second way through the rows is one multiplication and addition an element.  Bound by memory where chunks need not hear from
 // each other (3 bags of 100 k rows of 64 in fp32: 38 us, 6 TB/s), else half by vector instructions (32 an element), half by the way over two
 // hand-overs in LDS and a word of another chunk (8192 bags of 30 rows of 128 in binary16: 46 us, 4.2 TB/s).
-template <int DT, int V, bool ALIGNED>
-__global__ __launch_bounds__(kThreads) void scan_apply_kernel(Rows<DT> a) {
+template <int DT, int V>
+__global__ __launch_bounds__(apply_threads(V)) void scan_apply_kernel(Rows<DT> a) {
   using E = typename Elem<DT>::type;
-  constexpr int R = 32 / V;
+  constexpr int T = apply_threads(V), W = T / 64, R = 32 * kThreads / T / V;
   extern __shared__ float lds[];
   const int chunk = blockIdx.x / a.tiles, tile = blockIdx.x % a.tiles, C = a.L * V;
-  int32_t *marks = (int32_t *)(lds + kWaves * 2 * C);
+  int32_t *marks = (int32_t *)(lds + W * 2 * C);
   const int64_t row0 = (int64_t)chunk * a.chunk_rows;
   const int group = threadIdx.x / a.L, l = threadIdx.x & (a.L - 1), c0 = (tile * a.L + l) * V, r0 = group * R;
   const int rows = (int)min((int64_t)a.chunk_rows, a.rows - row0);
@@ -492,13 +485,13 @@ __global__ __launch_bounds__(kThreads) void scan_apply_kernel(Rows<DT> a) {
     xv[j] = {};
     uv[j] = {};
     if (on && r0 + j < rows) {
-      uv[j] = load_pack<E, V, ALIGNED>(a.u + (row0 + r0 + j) * a.us + c0);
-      xv[j] = load_pack<E, V, ALIGNED>(a.x + (row0 + r0 + j) * a.xs + c0);
+      uv[j] = load_pack<E, V>(a.u + (row0 + r0 + j) * a.us + c0);
+      xv[j] = load_pack<E, V>(a.x + (row0 + r0 + j) * a.xs + c0);
     }
   }
   const uint32_t call = a.call[0];
   if (blockIdx.x == 0 && threadIdx.x == 0) a.call[1] = call + 1;  // nothing looks at that one in this kernel
-  fetch_marks<kThreads>(a, row0, call, marks);
+  fetch_marks<T>(a, row0, call, marks);
   // The first start among the lane's rows: its state is asked for before the gates are computed.
   int first = R;
 #pragma unroll
@@ -537,21 +530,21 @@ __global__ __launch_bounds__(kThreads) void scan_apply_kernel(Rows<DT> a) {
   scan_wave<V, false>(A, H, reset, a.L);
   tell_wave<V, false>(A, H, a.L, lds);
   __syncthreads();
-  for (int c = threadIdx.x; c < C; c += kThreads) {
+  for (int c = threadIdx.x; c < C; c += T) {
     const int d = tile * C + c;
     float s = 0.0f;
     if (a.chunks > 1 && d < a.dim) {
       float *before = a.before ? a.before + (int64_t)chunk * a.dim + d : nullptr;
       if (a.chained) {
         float A1, H1;
-        map_of_waves<false, kWaves>(lds, C, c, A1, H1);
+        map_of_waves<false, W>(lds, C, c, A1, H1);
         s = hear_and_say<false>(a, chunk, d, call, A1, H1);
         if (before) *before = s;
       } else {
         s = *before;
       }
     }
-    join_waves<false, kWaves>(lds, C, c, s);
+    join_waves<false, W>(lds, C, c, s);
   }
   __syncthreads();
   float h[V];
@@ -566,7 +559,7 @@ __global__ __launch_bounds__(kThreads) void scan_apply_kernel(Rows<DT> a) {
       h[v] = starts >> j & 1 ? b[j][v] : f[j][v] * h[v] + b[j][v];
       out.e[v] = (E)h[v];
     }
-    if (a.y && r0 + j < rows) store_pack<E, V, ALIGNED>(a.y + (row0 + r0 + j) * a.ys + c0, out);
+    if (a.y && r0 + j < rows) store_pack<E, V>(a.y + (row0 + r0 + j) * a.ys + c0, out);
     if (ended && a.last)
 #pragma unroll
       for (int v = 0; v < V; v++) a.last[(int64_t)(ended - 1) * a.dim + c0 + v] = h[v];
@@ -576,15 +569,15 @@ __global__ __launch_bounds__(kThreads) void scan_apply_kernel(Rows<DT> a) {
 // The gradient of a chunk's rows: the states from that before it, c from that behind it, each joined like the forward's, then dx and du.  16
 // elements a lane: with 32, as in the forward, two wavefronts a SIMD have room instead of four (120 us instead of 114 for 8192 bags of 30 rows of
 // 128 in bfloat16, 80 instead of 75 for 3 bags of 100 k rows of 64 in fp32).  Bound by vector instructions, 83 an element, 0.6 of the time.
-template <int DT, int V, bool ALIGNED>
-__global__ __launch_bounds__(kGradThreads, V == 1 ? 2 : 4) void scan_grad_kernel(Rows<DT> a) {
+template <int DT, int V>
+__global__ __launch_bounds__(grad_threads(V), 4) void scan_grad_kernel(Rows<DT> a) {
   using E = typename Elem<DT>::type;
-  constexpr int R = 32 * kThreads / kGradThreads / V;
+  constexpr int T = grad_threads(V), W = T / 64, R = 32 * kThreads / T / V;
   extern __shared__ float lds[];
   // from the last chunk on: what a chunk hears of is behind it
   const int chunk = a.chunks - 1 - blockIdx.x / a.tiles, tile = blockIdx.x % a.tiles, C = a.L * V;
-  float *back = lds + kGradWaves * 2 * C;
-  int32_t *marks = (int32_t *)(back + kGradWaves * 2 * C);
+  float *back = lds + W * 2 * C;
+  int32_t *marks = (int32_t *)(back + W * 2 * C);
   const int64_t row0 = (int64_t)chunk * a.chunk_rows;
   const int group = threadIdx.x / a.L, l = threadIdx.x & (a.L - 1), c0 = (tile * a.L + l) * V, r0 = group * R;
   const int rows = (int)min((int64_t)a.chunk_rows, a.rows - row0);
@@ -596,14 +589,14 @@ __global__ __launch_bounds__(kGradThreads, V == 1 ? 2 : 4) void scan_grad_kernel
     uv[j] = {};
     gv[j] = {};
     if (on && r0 + j < rows) {
-      uv[j] = load_pack<E, V, ALIGNED>(a.u + (row0 + r0 + j) * a.us + c0);
-      xv[j] = load_pack<E, V, ALIGNED>(a.x + (row0 + r0 + j) * a.xs + c0);
-      if (a.dy) gv[j] = load_pack<E, V, ALIGNED>(a.dy + (row0 + r0 + j) * a.dys + c0);
+      uv[j] = load_pack<E, V>(a.u + (row0 + r0 + j) * a.us + c0);
+      xv[j] = load_pack<E, V>(a.x + (row0 + r0 + j) * a.xs + c0);
+      if (a.dy) gv[j] = load_pack<E, V>(a.dy + (row0 + r0 + j) * a.dys + c0);
     }
   }
   const uint32_t call = a.call[0];
   if (blockIdx.x == 0 && threadIdx.x == 0) a.call[1] = call + 1;  // nothing looks at that one in this kernel
-  fetch_marks<kGradThreads>(a, row0, call, marks);
+  fetch_marks<T>(a, row0, call, marks);
   // The first start and the last end among the lane's rows: what belongs to them is asked for before the gates are computed.
   int first = R, last = -1;
 #pragma unroll
@@ -665,21 +658,21 @@ __global__ __launch_bounds__(kGradThreads, V == 1 ? 2 : 4) void scan_grad_kernel
   scan_wave<V, true>(B, G, reset_back, a.L);
   tell_wave<V, true>(B, G, a.L, back);
   __syncthreads();
-  for (int c = threadIdx.x; c < C; c += kGradThreads) {
+  for (int c = threadIdx.x; c < C; c += T) {
     const int d = tile * C + c;
     float s = 0.0f, g = 0.0f;
     if (a.chunks > 1 && d < a.dim) {
       s = a.before[(int64_t)chunk * a.dim + d];
       if (a.chained) {
         float A1, H1;
-        map_of_waves<true, kGradWaves>(back, C, c, A1, H1);
+        map_of_waves<true, W>(back, C, c, A1, H1);
         g = hear_and_say<true>(a, chunk, d, call, A1, H1);
       } else {
         g = a.behind[(int64_t)chunk * a.dim + d];
       }
     }
-    join_waves<false, kGradWaves>(lds, C, c, s);
-    join_waves<true, kGradWaves>(back, C, c, g);
+    join_waves<false, W>(lds, C, c, s);
+    join_waves<true, W>(back, C, c, g);
   }
   __syncthreads();
   float w[R][V], s[V];  // w: du / g
@@ -712,8 +705,8 @@ __global__ __launch_bounds__(kGradThreads, V == 1 ? 2 : 4) void scan_grad_kernel
       s[v] = f * g;
     }
     if (r0 + j < rows) {
-      store_pack<E, V, ALIGNED>(a.dx + (row0 + r0 + j) * a.dxs + c0, dx);
-      store_pack<E, V, ALIGNED>(a.du + (row0 + r0 + j) * a.dus + c0, du);
+      store_pack<E, V>(a.dx + (row0 + r0 + j) * a.dxs + c0, dx);
+      store_pack<E, V>(a.du + (row0 + r0 + j) * a.dus + c0, du);
     }
     if (bag && a.dh0)
 #pragma unroll
@@ -774,39 +767,37 @@ dim3 grid_of(int64_t n) { return dim3((unsigned)((n + kThreads - 1) / kThreads))
 
 int64_t chunks_of(const tbe_scan_t *s, int64_t rows) { return (rows + s->cut.rows - 1) / s->cut.rows; }
 
-template <int DT, int V, bool ALIGNED>
+template <int DT, int V>
 int run(const tbe_scan_t *s, const Rows<DT> &a, bool grad, hipStream_t stream) noexcept {
   const dim3 grid((unsigned)(a.chunks * a.tiles)), joins((unsigned)((a.dim + kJoinChannels - 1) / kJoinChannels));
-  const size_t tot = (size_t)kWaves * 2 * a.L * V * sizeof(float), marks = (size_t)a.chunk_rows * 2 * sizeof(int32_t);
+  const size_t tot = (size_t)2 * a.L * V * sizeof(float),  // of a wavefront
+       marks = (size_t)a.chunk_rows * 2 * sizeof(int32_t);
   scan_prepare_kernel<<<dim3((unsigned)((a.bags + kThreads - 1) / kThreads)), kThreads, 0, stream>>>(
       a.off, a.bags, a.rows, s->marks, s->call, a.dim, grad ? a.dlast : a.h0, grad ? a.dim : a.h0s, grad ? a.dh0 : a.last, s->err);
   if (a.rows == 0) return check_launch();
   const bool joined = a.chunks > 1 && !a.chained;
   if (!grad) {
     if (joined) {
-      scan_sum_kernel<DT, V, ALIGNED, false><<<grid, kThreads, tot + marks, stream>>>(a);
+      scan_sum_kernel<DT, V, false><<<grid, kThreads, kWaves * tot + marks, stream>>>(a);
       scan_join_kernel<false><<<joins, kJoinChannels * kJoinSegments, 0, stream>>>(a.maps, a.before, a.chunks, a.dim);
     }
-    scan_apply_kernel<DT, V, ALIGNED><<<grid, kThreads, tot + marks, stream>>>(a);
+    scan_apply_kernel<DT, V><<<grid, apply_threads(V), apply_threads(V) / 64 * tot + marks, stream>>>(a);
   } else {
     if (joined) {
-      scan_sum_kernel<DT, V, ALIGNED, true><<<grid, kThreads, tot + marks, stream>>>(a);
+      scan_sum_kernel<DT, V, true><<<grid, kThreads, kWaves * tot + marks, stream>>>(a);
       scan_join_kernel<true><<<joins, kJoinChannels * kJoinSegments, 0, stream>>>(a.maps, a.behind, a.chunks, a.dim);
     }
-    scan_grad_kernel<DT, V, ALIGNED><<<grid, kGradThreads, 2 * tot * kGradWaves / kWaves + marks, stream>>>(a);
+    scan_grad_kernel<DT, V><<<grid, grad_threads(V), grad_threads(V) / 64 * 2 * tot + marks, stream>>>(a);
   }
   return check_launch();
 }
 
-bool aligned16(const void *p, int64_t stride, int es) { return ((uintptr_t)p | (uint64_t)(stride * es)) % 16 == 0; }
-
 template <int DT>
-int run_type(const tbe_scan_t *s, Rows<DT> a, bool grad, hipStream_t stream) noexcept {
-  constexpr int wide = 16 / (int)sizeof(typename Elem<DT>::type), es = sizeof(typename Elem<DT>::type);
-  if (s->cut.V == 1) return run<DT, 1, true>(s, a, grad, stream);
-  const bool al = aligned16(a.x, a.xs, es) && aligned16(a.u, a.us, es) && (!a.y || aligned16(a.y, a.ys, es)) && (!a.dy || aligned16(a.dy, a.dys, es)) &&
-                  (!grad || (aligned16(a.dx, a.dxs, es) && aligned16(a.du, a.dus, es)));
-  return al ? run<DT, wide, true>(s, a, grad, stream) : run<DT, wide, false>(s, a, grad, stream);
+int run_type(const tbe_scan_t *s, const Rows<DT> &a, bool grad, hipStream_t stream) noexcept {
+  if constexpr (DT != TBE_FP32)
+    if (s->cut.V == 8) return run<DT, 8>(s, a, grad, stream);
+  if (s->cut.V == 4) return run<DT, 4>(s, a, grad, stream);
+  return s->cut.V == 2 ? run<DT, 2>(s, a, grad, stream) : run<DT, 1>(s, a, grad, stream);
 }
 
 template <int DT>
