@@ -38,14 +38,14 @@ class AdamWTensor(C.Structure):
                 ("weight_decay", C.c_double)]
 
 
-_ready = False
+_ready = None  # the library object whose arguments have their types
 _current_raw_stream = torch._C._cuda_getCurrentRawStream
 
 
 def _lib() -> C.CDLL:
     global _ready
     l = _tbe.lib()
-    if not _ready:
+    if _ready is not l:
         vp, i32, i64, f32, f64 = C.c_void_p, C.c_int32, C.c_int64, C.c_float, C.c_double
         batch = [vp, vp, i64, vp, i64, vp, i64, i64, vp, i64]
         l.tbe_scan_create.argtypes = [C.POINTER(vp), i32, i32, i32, i64, i64]
@@ -61,7 +61,7 @@ def _lib() -> C.CDLL:
         l.tbe_scan_check.argtypes = [vp, vp]
         for n in ("tbe_scan_destroy", "tbe_bias_destroy", "tbe_adamw_destroy"):
             getattr(l, n).argtypes = [vp]
-        _ready = True
+        _ready = l
     return l
 
 
