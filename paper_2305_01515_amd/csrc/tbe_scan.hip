@@ -175,7 +175,7 @@ __device__ inline bool get_word(const uint64_t *p, uint64_t &w, uint32_t call) {
 template <bool BACK, class A>
 __device__ inline bool hear_from(const A &a, int chunk, int d, uint32_t call, float &s) {
   constexpr int kAtOnce = 2;
-  const int n = BACK ? a.chunks - 1 - chunk : chunk;  // chunks before this one; the first of them always says its state
+  const int n = BACK ? a.chunks - 1 - chunk : chunk;  // chunks before this one; the first of them says its state and never a map
   s = 0.0f;
   if (n == 0) return true;
   const uint64_t *first = a.words + (int64_t)(BACK ? chunk + 1 : chunk - 1) * 2 * a.dim + d;
@@ -191,7 +191,7 @@ __device__ inline bool hear_from(const A &a, int chunk, int d, uint32_t call, fl
       if (!get_word(first + min(k, n - 1) * step, w[q], call)) return false;
       found = (w[q] >> 32 & 3) == kSaysState;
       s = __uint_as_float((uint32_t)w[q]);
-      k += found ? 0 : 1;
+      if (!found && ++k == n) return false;  // behind the first of them there are no words
     }
   }
   while (k > 0) {
@@ -236,13 +236,14 @@ __device__ float walk_to(const A &a, int chunk, int d, uint32_t call) {
 }
 
 // What the chunk says of element d: its state where nothing before it has a part in that, else its map; then, told the state before it, the
-// one behind it.  Returns the state before it.
+// one behind it.  The first chunk has nothing before it, also where no bag starts in it (offsets that begin later) and where a NaN gate has
+// taken the sign from its -0.  Returns the state before it.
 template <bool BACK, class A>
 __device__ inline float hear_and_say(const A &a, int chunk, int d, uint32_t call, float A1, float H1) {
   uint64_t *w = a.words + (int64_t)chunk * 2 * a.dim + d;
-  const bool known = signbit(A1);
+  const bool known = signbit(A1) || (BACK ? chunk == a.chunks - 1 : chunk == 0);
   if (known) {
-    put_word(w, word_of(H1, call, kSaysState));
+    put_word(w, word_of(go(A1, H1, 0.0f), call, kSaysState));
   } else {
     put_word(w + a.dim, word_of(A1, call, kSaysMap));
     put_word(w, word_of(H1, call, kSaysMap));
