@@ -405,6 +405,7 @@ struct Diagonals {
   uint32_t squares;       // of V queries
   uint32_t columns, segs, batches;  // units of a head
   int seg, samples;
+  bool band;              // columns are counted from the first one that a segment's squares lie in (few keys: most have nothing of it)
 };
 
 template <int DT, bool SCORES>
@@ -424,7 +425,8 @@ __global__ __launch_bounds__(kThreads, SCORES ? 2 : 4) void bias_grad_index_kern
   const int64_t units = (int64_t)u.columns * u.segs * u.batches;
   const bool short_row = keys < V;
   for (int64_t w = (int64_t)blockIdx.x * kWaves + wave; w < units; w += (int64_t)gridDim.x * kWaves) {
-    const int column = (int)(w % u.columns), s = (int)(w / u.columns % u.segs);
+    const int s = (int)(w / u.columns % u.segs);
+    const int column = (int)(w % u.columns) + (u.band ? (squares - min((s + 1) * u.seg, squares)) / 64 : 0);
     const int64_t b0 = w / u.columns / u.segs * u.samples, b1 = min(b0 + u.samples, p.s.batch);
     const int first = 64 * column - (squares - 1), D = first + lane;  // key square less query square
     const int lo = max(s * u.seg, -(first + 63)), hi = min(min((s + 1) * u.seg, squares), packs - first);
@@ -661,11 +663,15 @@ int tbe_bias_backward(tbe_bias_handle s, const tbe_bias_shape *shape, const void
       const int V = 16 / elem_bytes(p.s.dtype);
       Diagonals u;
       u.squares = (uint32_t)((p.s.queries + V - 1) / V);
-      u.columns = (u.squares + p.packs - 1 + 63) / 64;
-      const int64_t squares = (int64_t)u.columns * u.squares * p.s.batch * p.heads;  // times 64, some of them beyond the scores
+      const uint32_t columns = (u.squares + p.packs - 1 + 63) / 64;
+      const int64_t squares = (int64_t)columns * u.squares * p.s.batch * p.heads;  // times 64, some of them beyond the scores
       const int64_t steps = squares / kUnits < 4 ? 4 : squares / kUnits > 64 ? 64 : squares / kUnits;
       u.seg = (int)(steps < u.squares ? steps : u.squares);
       u.segs = (u.squares + u.seg - 1) / u.seg;
+      // A segment's squares lie on packs + seg - 1 neighbouring diagonals, the units on all columns would grow with the queries' square.
+      const uint32_t band = (p.packs + u.seg - 2 + 63) / 64 + 1;
+      u.band = band <= columns / 2;
+      u.columns = u.band ? band : columns;
       const int64_t samples = steps / u.seg;
       u.samples = (int)(samples < p.s.batch ? samples : p.s.batch);
       u.batches = (uint32_t)((p.s.batch + u.samples - 1) / u.samples);
