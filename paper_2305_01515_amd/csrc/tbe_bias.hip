@@ -126,7 +126,7 @@ __device__ inline void find_keys(const Shape &p, const Finder &f, int64_t b, uin
     for (int v = 0; v < V; v++) k.bucket[v] += d[v] >= f.threshold[k.bucket[v]];
   const int apart = p.both ? p.thresholds + 1 : 0;
   k.masked = p.s.causal ? after : 0u;
-  const int64_t left = len - (int64_t)from;  // keys from here that are not masked
+  const int64_t left = max(len, (int64_t)0) - (int64_t)from;  // keys from here that are not masked
   k.masked |= left >= V ? 0u : left <= 0 ? ~0u : ~0u << left;
   k.masked &= (1u << V) - 1;
 #pragma unroll
@@ -436,7 +436,8 @@ __global__ __launch_bounds__(kThreads, SCORES ? 2 : 4) void bias_grad_index_kern
 #pragma unroll
     for (int k = 0; k < 2 * V - 1; k++) acc[k] = 0.0f;
     for (int64_t b = b0; b < b1; b++) {
-      const int64_t len = p.s.d_key_lengths ? p.s.d_key_lengths[b] : p.s.keys;
+      // at most the keys: a short row's places beyond them hold its last key again
+      const int64_t len = p.s.d_key_lengths ? max(min(p.s.d_key_lengths[b], p.s.keys), (int64_t)0) : p.s.keys;
       const E *in = dout + b * ds.sample + h * ds.head;
       for (int q = lo; q < hi; q++) {
         const int j = (q + D) * V, i = q * V;
