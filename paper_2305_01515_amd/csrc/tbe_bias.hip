@@ -440,12 +440,12 @@ __global__ __launch_bounds__(kThreads, SCORES ? 2 : 4) void bias_grad_index_kern
       const int64_t len = p.s.d_key_lengths ? max(min(p.s.d_key_lengths[b], p.s.keys), (int64_t)0) : p.s.keys;
       const E *in = dout + b * ds.sample + h * ds.head;
       for (int q = lo; q < hi; q++) {
-        const int j = (q + D) * V, i = q * V;
+        const int j = (int)((uint32_t)(q + D) * V), i = q * V;  // j where `on`
         const bool on = q + D >= 0 && q + D < packs;
         const int left = (int)max(min(len - j, (int64_t)V), (int64_t)0);  // keys that are not beyond the sample's
         if (!on || (!SCORES && (later || left == 0))) continue;
         Pack<E, V> x[V];
-        const int back = j + V > keys ? j + V - keys : 0;  // places of the last pack that are beyond the row
+        const int back = keys - j < V ? V - (keys - j) : 0;  // places of the last pack that are beyond the row (j + V may be 2^31)
         const E *from = in + (int64_t)i * ds.query + j - (short_row ? 0 : back);
         const int64_t last = (int64_t)min(V, queries - i) - 1;
         if (!short_row) {

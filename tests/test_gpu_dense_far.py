@@ -76,3 +76,18 @@ def test_a_tensor_of_more_than_2_31_weights(bits):
     for k in "mv":
         s = opt.states[k]
         assert bool((s[:n] == s[0]).all()) and not bool(s[n:].any())
+
+
+def test_rows_of_almost_2_31_keys():
+    """the last pack of a row ends at key 2^31: what is behind the row is neither counted nor written"""
+    from paper_2305_01515_amd.dense import RelativeBias
+    keys = (1 << 31) - 1
+    plan = RelativeBias(1, [1, 1 << 20, 1 << 30])
+    dout = torch.zeros(2, 1, 1, keys, dtype=torch.bfloat16, device="cuda")
+    ends = torch.arange(1, 21, dtype=torch.bfloat16, device="cuda")
+    dout[0, 0, 0, -20:], dout[1, 0, 0, :20], dout[1, 0, 0, -20:] = ends, 2 * ends, 4 * ends
+    dtable, dscores = plan.backward(dout, q_offset=keys - 1, want_dscores=True, scale=0.5)
+    assert dtable[:, 0].tolist() == [100.0, 950.0, 0.0, 420.0]  # the newest key, the 19 before it, the first ones
+    dout *= 0.5
+    assert torch.equal(dscores, dout)
+    assert plan.backward(dout, q_offset=keys - 1)[:, 0].tolist() == [50.0, 475.0, 0.0, 210.0]
