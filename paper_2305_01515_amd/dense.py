@@ -96,6 +96,12 @@ class _Handle:
             raise ValueError(f"{name}: {dtype} {tuple(shape)} on {self.device} is wanted, got {t.dtype} {tuple(t.shape)} on {t.device}")
         return t.data_ptr()
 
+    def _whole(self, name: str, t: torch.Tensor, dtype: torch.dtype, shape) -> int:
+        """the same of a tensor whose elements lie one behind another"""
+        if not t.is_contiguous():
+            raise ValueError(f"{name}: contiguous")
+        return self._tensor(name, t, dtype, shape)
+
     def close(self):
         if self._h:
             getattr(_lib(), self._destroy)(self._h)
@@ -174,7 +180,7 @@ class Scan(_Handle):
         dx, du = (torch.empty(n, self.dim, dtype=self.dtype, device=self.device) for _ in range(2))
         dh0 = torch.empty(bags, self.dim, dtype=torch.float32, device=self.device) if h0 is not None else None
         want = self._check(_lib().tbe_scan_saved_floats(self._h, n), "tbe_scan_saved_floats")
-        sp = self._tensor("saved", saved, torch.float32, (want,))
+        sp = self._whole("saved", saved, torch.float32, (want,))
         dyp = self._rows("dy", dy, n) if dy is not None else (None, 0)
         lp = self._tensor("dlast", dlast, torch.float32, (bags, self.dim)) if dlast is not None else None
         self._check(_lib().tbe_scan_backward(*args, sp, *dyp, lp, dx.data_ptr(), self.dim, du.data_ptr(), self.dim,
@@ -335,7 +341,7 @@ class AdamW(_Handle):
         kinds = {"m": (torch.float32, total * BLOCK), "v": (torch.float32, total * BLOCK)} if state_bits == 32 else \
             {"m": (torch.uint8, total * BLOCK), "v": (torch.uint8, total * BLOCK), "m_scale": (torch.float32, total), "v_scale": (torch.float32, total)}
         self.states = states or {k: torch.zeros(n, dtype=d, device=self.device) for k, (d, n) in kinds.items()}
-        address = {k: self._tensor(k, self.states[k], d, (n,)) for k, (d, n) in kinds.items()}
+        address = {k: self._whole(k, self.states[k], d, (n,)) for k, (d, n) in kinds.items()}
         self._decay, self._address, self._blocks = decay, address, blocks
         self._grads = (C.c_void_p * max(1, len(self.params)))()
         self._plan(list(grad_dtypes) if grad_dtypes is not None else [p.dtype for p in self.params])
@@ -345,7 +351,7 @@ class AdamW(_Handle):
         tensors, at = (AdamWTensor * max(1, len(self.params)))(), 0
         for i, (p, w, blocks) in enumerate(zip(self.params, self.master, self._blocks)):
             a, scale = self._address, self.state_bits == 8
-            tensors[i] = AdamWTensor(p.data_ptr(), self._tensor("master", w, torch.float32, p.shape) if w is not None else None,
+            tensors[i] = AdamWTensor(p.data_ptr(), self._whole("master", w, torch.float32, p.shape) if w is not None else None,
                                      a["m"] + at * BLOCK * size, a["v"] + at * BLOCK * size, a["m_scale"] + 4 * at if scale else None,
                                      a["v_scale"] + 4 * at if scale else None, p.numel(), DTYPES[p.dtype], DTYPES[grad_dtypes[i]], self._decay[i])
             at += blocks
