@@ -316,7 +316,9 @@ class AdamW(_Handle):
     copies beside 16-bit parameters, True to make them from the parameters, or a list of tensors.  weight_decay: one number or one for each
     parameter.  grad_dtypes: types of the gradients, the parameters' own unless given (a step whose gradients have others makes the
     plan anew).  States of all parameters lie one behind another in `states` ("m", "v" and for 8 bits "m_scale", "v_scale"), each
-    parameter's from a multiple of 256 elements on: that is what a checkpoint holds, with `step_count`."""
+    parameter's from a multiple of 256 elements on: that is what a checkpoint holds, with `step_count`.  A step takes parameters, `master` and
+    `states` as they are then: other tensors of the same sizes in their place, and parameters that have got other storage, make the
+    plan anew."""
     _destroy = "tbe_adamw_destroy"
 
     def __init__(self, params: Sequence[torch.Tensor], lr: float = 1e-3, betas: Tuple[float, float] = (0.9, 0.999), eps: float = 1e-8,
@@ -329,8 +331,7 @@ class AdamW(_Handle):
         if len(decay) != len(self.params):
             raise ValueError("weight_decay: one number, or one for each parameter")
         for p in self.params:
-            if p.dtype not in DTYPES or p.device != self.device or not p.is_contiguous():
-                raise ValueError(f"parameters are contiguous, {', '.join(map(str, DTYPES))}, on {self.device}")
+            self._parameter(p)
         if master is True:
             master = [p.detach().float() if p.dtype != torch.float32 else None for p in self.params]
         self.master = list(master) if master else [None] * len(self.params)
@@ -341,23 +342,36 @@ class AdamW(_Handle):
         kinds = {"m": (torch.float32, total * BLOCK), "v": (torch.float32, total * BLOCK)} if state_bits == 32 else \
             {"m": (torch.uint8, total * BLOCK), "v": (torch.uint8, total * BLOCK), "m_scale": (torch.float32, total), "v_scale": (torch.float32, total)}
         self.states = states or {k: torch.zeros(n, dtype=d, device=self.device) for k, (d, n) in kinds.items()}
-        address = {k: self._whole(k, self.states[k], d, (n,)) for k, (d, n) in kinds.items()}
-        self._decay, self._address, self._blocks = decay, address, blocks
+        self._decay, self._blocks, self._kinds = decay, blocks, kinds
         self._grads = (C.c_void_p * max(1, len(self.params)))()
         self._plan(list(grad_dtypes) if grad_dtypes is not None else [p.dtype for p in self.params])
 
+    def _parameter(self, p):
+        if p.dtype not in DTYPES or p.device != self.device or not p.is_contiguous():
+            raise ValueError(f"parameters are contiguous, {', '.join(map(str, DTYPES))}, on {self.device}")
+
+    def _others(self):
+        """what the plan has the addresses of beside the parameters, as it is now"""
+        return [None if t is None else (t.data_ptr(), t.dtype, t.shape, t.is_contiguous()) for t in (*self.master, *map(self.states.get, self._kinds))]
+
     def _plan(self, grad_dtypes):
-        size = 4 if self.state_bits == 32 else 1
+        """a handle for the parameters, copies and states as they are now"""
+        if len(self.params) != len(self._blocks) or len(self.master) != len(self._blocks):
+            raise ValueError("as many parameters and copies as there were")
+        a = {k: self._whole(k, self.states[k], d, (n,)) for k, (d, n) in self._kinds.items()}
+        size, scale = 4 if self.state_bits == 32 else 1, self.state_bits == 8
         tensors, at = (AdamWTensor * max(1, len(self.params)))(), 0
         for i, (p, w, blocks) in enumerate(zip(self.params, self.master, self._blocks)):
-            a, scale = self._address, self.state_bits == 8
+            self._parameter(p)
+            if -(-p.numel() // BLOCK) != blocks:
+                raise ValueError(f"parameter {i}: {p.numel()} elements, its states have {blocks * BLOCK}")
             tensors[i] = AdamWTensor(p.data_ptr(), self._whole("master", w, torch.float32, p.shape) if w is not None else None,
                                      a["m"] + at * BLOCK * size, a["v"] + at * BLOCK * size, a["m_scale"] + 4 * at if scale else None,
                                      a["v_scale"] + 4 * at if scale else None, p.numel(), DTYPES[p.dtype], DTYPES[grad_dtypes[i]], self._decay[i])
             at += blocks
         self.close()
         self._check(_lib().tbe_adamw_create(C.byref(self._h), tensors, len(self.params), self.state_bits), "tbe_adamw_create")
-        self._grad_dtypes = grad_dtypes
+        self._planned, self._planned_others = [(p.data_ptr(), p.dtype, p.shape, g) for p, g in zip(self.params, grad_dtypes)], self._others()
 
     def step(self, grads: Optional[Sequence[Optional[torch.Tensor]]] = None, lr: Optional[float] = None, grad_scale: Optional[torch.Tensor] = None):
         """grads: one for each parameter (None: its parameter stays as it is); without, the parameters' own `.grad`.
@@ -365,17 +379,22 @@ class AdamW(_Handle):
         grads = [p.grad for p in self.params] if grads is None else grads
         if len(grads) != len(self.params):
             raise ValueError("grads: one for each parameter")
-        ptrs = self._grads
-        for i, (p, g) in enumerate(zip(self.params, grads)):
+        # Parameters, copies and states may have another storage than at the last step (moved to the host and back, loaded, assigned).
+        ptrs, same = self._grads, len(self.params) == len(self._planned) and self._others() == self._planned_others
+        for i, (p, g, (address, dtype, shape, grad_dtype)) in enumerate(zip(self.params, grads, self._planned)):
+            now = p.shape
+            if p.data_ptr() != address or p.dtype is not dtype or now != shape or not p.is_contiguous():
+                same = False
             if g is None:
                 ptrs[i] = None
                 continue
-            if g.shape != p.shape or g.device != self.device or not g.is_contiguous() or g.dtype not in DTYPES:
-                raise ValueError(f"gradient {i}: contiguous, of the parameter's shape {tuple(p.shape)}, on {self.device}")
+            if g.shape != now or g.device != self.device or not g.is_contiguous() or g.dtype not in DTYPES:
+                raise ValueError(f"gradient {i}: contiguous, of the parameter's shape {tuple(now)}, on {self.device}")
+            if g.dtype is not grad_dtype:
+                same = False
             ptrs[i] = g.data_ptr()
-        known = self._grad_dtypes
-        if any(g is not None and g.dtype != d for g, d in zip(grads, known)):
-            self._plan([g.dtype if g is not None else d for g, d in zip(grads, known)])
+        if not same:
+            self._plan([known[3] if g is None else g.dtype for g, known in zip(grads, self._planned)])
         gs = self._tensor("grad_scale", grad_scale, torch.float32, grad_scale.shape) if grad_scale is not None else None
         if grad_scale is not None and grad_scale.numel() != 1:
             raise ValueError("grad_scale: one number")
