@@ -6,7 +6,8 @@ AdamW         the step of a model's dense weights, many tensors in one launch, w
 
 Argument marshalling only: every step runs in the HIP kernels of the library.  A call enqueues on the current stream, behind
 this object's last call if that was on another one (an object's calls share its scratch memory; replays of a captured graph
-are the caller's to order).  No call waits for the GPU, apart from `Scan.check`.
+are the caller's to order; graphs need the objects whose calls they hold).  No call waits for the GPU, apart from `Scan.check` and a
+step of `AdamW` that makes its plan anew, which no capture can hold.
 """
 from __future__ import annotations
 
@@ -40,6 +41,10 @@ class AdamWTensor(C.Structure):
 
 _ready = None  # the library object whose arguments have their types
 _current_raw_stream = torch._C._cuda_getCurrentRawStream
+# of a tensor, without the look for the attribute at each
+_shape, _dtype = torch.Tensor.shape.__get__, torch.Tensor.dtype.__get__
+_address, _dense, _gpu = torch.Tensor.data_ptr, torch.Tensor.is_contiguous, torch.Tensor.get_device
+_capturing = torch.cuda.is_current_stream_capturing
 
 
 def _lib() -> C.CDLL:
@@ -57,7 +62,7 @@ def _lib() -> C.CDLL:
         l.tbe_bias_forward.argtypes = [vp, C.POINTER(BiasShape), vp, i32, vp, C.POINTER(BiasStrides), f32, f32, vp, C.POINTER(BiasStrides), vp]
         l.tbe_bias_backward.argtypes = [vp, C.POINTER(BiasShape), vp, C.POINTER(BiasStrides), vp, f32, vp, C.POINTER(BiasStrides), vp]
         l.tbe_adamw_create.argtypes = [C.POINTER(vp), C.POINTER(AdamWTensor), i32, i32]
-        l.tbe_adamw_step.argtypes = [vp, C.POINTER(vp), i64, f64, f64, f64, f64, C.c_uint32, vp, vp]
+        l.tbe_adamw_step.argtypes = [vp, vp, i64, f64, f64, f64, f64, C.c_uint32, vp, vp]
         l.tbe_scan_check.argtypes = [vp, vp]
         for n in ("tbe_scan_destroy", "tbe_bias_destroy", "tbe_adamw_destroy"):
             getattr(l, n).argtypes = [vp]
@@ -82,7 +87,7 @@ class _Handle:
         """the current stream, for the next call: behind this object's last call on another one"""
         current = _current_raw_stream(self.device.index)
         if self._last is None or self._last.cuda_stream != current:
-            if torch.cuda.is_current_stream_capturing():
+            if _capturing():
                 return current
             stream = torch.cuda.current_stream(self.device)
             if self._last is not None:
@@ -325,6 +330,7 @@ class AdamW(_Handle):
                  weight_decay: Union[float, Sequence[float]] = 0.01, state_bits: int = 32, master=None, seed: int = 0, step: int = 0,
                  states: Optional[Dict[str, torch.Tensor]] = None, grad_dtypes: Optional[Sequence[torch.dtype]] = None):
         super().__init__()
+        self._kept: List[C.c_void_p] = []  # handles of earlier plans
         self.params = list(params)
         self.lr, self.betas, self.eps, self.seed, self.step_count, self.state_bits = lr, betas, eps, seed, step, state_bits
         decay = list(weight_decay) if isinstance(weight_decay, (list, tuple)) else [weight_decay] * len(self.params)
@@ -344,20 +350,31 @@ class AdamW(_Handle):
         self.states = states or {k: torch.zeros(n, dtype=d, device=self.device) for k, (d, n) in kinds.items()}
         self._decay, self._blocks, self._kinds = decay, blocks, kinds
         self._grads = (C.c_void_p * max(1, len(self.params)))()
+        self._grads_at, self._gpus = C.addressof(self._grads), [self.device.index] * len(self.params)
+        self._captured = False  # whether a step of this plan has been captured
         self._plan(list(grad_dtypes) if grad_dtypes is not None else [p.dtype for p in self.params])
+
+    def close(self):
+        super().close()
+        while self._kept:
+            _lib().tbe_adamw_destroy(self._kept.pop())
 
     def _parameter(self, p):
         if p.dtype not in DTYPES or p.device != self.device or not p.is_contiguous():
             raise ValueError(f"parameters are contiguous, {', '.join(map(str, DTYPES))}, on {self.device}")
 
-    def _others(self):
-        """what the plan has the addresses of beside the parameters, as it is now"""
-        return [None if t is None else (t.data_ptr(), t.dtype, t.shape, t.is_contiguous()) for t in (*self.master, *map(self.states.get, self._kinds))]
+    def _places(self):
+        """what the plan holds of parameters, copies and states, as it is now; the parameters' shapes first"""
+        t = [*self.params, *map(self.states.__getitem__, self._kinds), *(w for w in self.master if w is not None)]
+        return [*map(_shape, t)], [*map(_address, t)], [*map(_dtype, t)], [*map(_dense, t)], len(self.params), \
+            [w is None for w in self.master] if len(t) > len(self.params) + len(self._kinds) else len(self.master)
 
     def _plan(self, grad_dtypes):
         """a handle for the parameters, copies and states as they are now"""
         if len(self.params) != len(self._blocks) or len(self.master) != len(self._blocks):
             raise ValueError("as many parameters and copies as there were")
+        if _capturing():
+            raise RuntimeError("a plan is made outside of a capture: take a step with these parameters, states and types of gradients before it")
         a = {k: self._whole(k, self.states[k], d, (n,)) for k, (d, n) in self._kinds.items()}
         size, scale = 4 if self.state_bits == 32 else 1, self.state_bits == 8
         tensors, at = (AdamWTensor * max(1, len(self.params)))(), 0
@@ -369,9 +386,14 @@ class AdamW(_Handle):
                                      a["m"] + at * BLOCK * size, a["v"] + at * BLOCK * size, a["m_scale"] + 4 * at if scale else None,
                                      a["v_scale"] + 4 * at if scale else None, p.numel(), DTYPES[p.dtype], DTYPES[grad_dtypes[i]], self._decay[i])
             at += blocks
-        self.close()
-        self._check(_lib().tbe_adamw_create(C.byref(self._h), tensors, len(self.params), self.state_bits), "tbe_adamw_create")
-        self._planned, self._planned_others = [(p.data_ptr(), p.dtype, p.shape, g) for p, g in zip(self.params, grad_dtypes)], self._others()
+        h = C.c_void_p()
+        self._check(_lib().tbe_adamw_create(C.byref(h), tensors, len(self.params), self.state_bits), "tbe_adamw_create")
+        if self._h and self._captured:
+            self._kept.append(self._h)  # graphs may hold steps of it
+        elif self._h:
+            _lib().tbe_adamw_destroy(self._h)
+        self._h, self._captured, self._enqueue = h, False, _lib().tbe_adamw_step
+        self._planned, self._grad_dtypes = self._places(), grad_dtypes
 
     def step(self, grads: Optional[Sequence[Optional[torch.Tensor]]] = None, lr: Optional[float] = None, grad_scale: Optional[torch.Tensor] = None):
         """grads: one for each parameter (None: its parameter stays as it is); without, the parameters' own `.grad`.
@@ -380,24 +402,28 @@ class AdamW(_Handle):
         if len(grads) != len(self.params):
             raise ValueError("grads: one for each parameter")
         # Parameters, copies and states may have another storage than at the last step (moved to the host and back, loaded, assigned).
-        ptrs, same = self._grads, len(self.params) == len(self._planned) and self._others() == self._planned_others
-        for i, (p, g, (address, dtype, shape, grad_dtype)) in enumerate(zip(self.params, grads, self._planned)):
-            now = p.shape
-            if p.data_ptr() != address or p.dtype is not dtype or now != shape or not p.is_contiguous():
-                same = False
-            if g is None:
-                ptrs[i] = None
-                continue
-            if g.shape != now or g.device != self.device or not g.is_contiguous() or g.dtype not in DTYPES:
-                raise ValueError(f"gradient {i}: contiguous, of the parameter's shape {tuple(now)}, on {self.device}")
-            if g.dtype is not grad_dtype:
-                same = False
-            ptrs[i] = g.data_ptr()
-        if not same:
-            self._plan([known[3] if g is None else g.dtype for g, known in zip(grads, self._planned)])
-        gs = self._tensor("grad_scale", grad_scale, torch.float32, grad_scale.shape) if grad_scale is not None else None
-        if grad_scale is not None and grad_scale.numel() != 1:
-            raise ValueError("grad_scale: one number")
-        self._check(_lib().tbe_adamw_step(self._h, ptrs, self.step_count + 1, self.lr if lr is None else lr, *self.betas, self.eps,
-                                          self.seed & 0xFFFFFFFF, gs, self._stream()), "tbe_adamw_step")
+        places, ptrs, stream = self._places(), self._grads, self._stream()
+        shapes = places[0][:len(self.params)]
+        try:
+            fine = [*map(_shape, grads)] == shapes and [*map(_dtype, grads)] == self._grad_dtypes and all(map(_dense, grads)) and \
+                [*map(_gpu, grads)] == self._gpus
+        except TypeError:  # a parameter without a gradient
+            fine = False
+        if not fine:
+            for i, (g, shape) in enumerate(zip(grads, shapes)):
+                if g is not None and (g.shape != shape or g.device != self.device or not g.is_contiguous() or g.dtype not in DTYPES):
+                    raise ValueError(f"gradient {i}: contiguous, of the parameter's shape {tuple(shape)}, on {self.device}")
+            dtypes = [d if g is None else g.dtype for g, d in zip(grads, self._grad_dtypes)]
+        if places != self._planned or not fine and dtypes != self._grad_dtypes:
+            self._plan(self._grad_dtypes if fine else dtypes)
+        ptrs[:] = [*map(_address, grads)] if fine else [None if g is None else g.data_ptr() for g in grads]
+        if stream and _capturing():  # the default stream cannot be
+            self._captured = True
+        gs = None
+        if grad_scale is not None:
+            gs = self._tensor("grad_scale", grad_scale, torch.float32, grad_scale.shape)
+            if grad_scale.numel() != 1:
+                raise ValueError("grad_scale: one number")
+        self._check(self._enqueue(self._h, self._grads_at, self.step_count + 1, self.lr if lr is None else lr, *self.betas, self.eps,
+                                  self.seed & 0xFFFFFFFF, gs, stream), "tbe_adamw_step")
         self.step_count += 1
