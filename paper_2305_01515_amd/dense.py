@@ -5,7 +5,7 @@ RelativeBias  a learned table looked up by the bucket of a distance between two 
 AdamW         the step of a model's dense weights, many tensors in one launch, with states in 32 or 8 bits
 
 Argument marshalling only: every step runs in the HIP kernels of the library.  A call enqueues on the current stream, behind
-this object's last call if that was on another one (an object's calls share its scratch memory; replays of a captured graph
+this object's last call or its constructor if that was on another one (an object's calls share its scratch memory; replays of a captured graph
 are the caller's to order; graphs need the objects whose calls they hold).  No call waits for the GPU, apart from `Scan.check` and a
 step of `AdamW` that makes its plan anew, which no capture can hold.
 """
@@ -76,7 +76,8 @@ class _Handle:
     def __init__(self):
         self._h = C.c_void_p()
         self.device = torch.device("cuda", torch.cuda.current_device())
-        self._last: Optional[torch.cuda.Stream] = None  # the stream of the last call
+        # the stream of the last call; before the first one that of the constructor, which fills states and copies there
+        self._last = torch.cuda.current_stream(self.device)
 
     def _check(self, rc: int, what: str):
         if rc < 0:
@@ -86,12 +87,11 @@ class _Handle:
     def _stream(self) -> int:
         """the current stream, for the next call: behind this object's last call on another one"""
         current = _current_raw_stream(self.device.index)
-        if self._last is None or self._last.cuda_stream != current:
+        if self._last.cuda_stream != current:
             if _capturing():
                 return current
             stream = torch.cuda.current_stream(self.device)
-            if self._last is not None:
-                stream.wait_stream(self._last)
+            stream.wait_stream(self._last)
             self._last = stream
         return current
 
