@@ -16,6 +16,7 @@ import math
 from typing import Dict, List, Optional, Sequence, Tuple, Union
 
 import torch
+from torch.autograd.function import once_differentiable
 
 from . import tbe as _tbe
 
@@ -129,6 +130,7 @@ class _ScanFunction(torch.autograd.Function):
         return y, last
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dy, dlast):
         x, u, offsets, h0, saved = ctx.saved_tensors
         dx, du, dh0 = ctx.plan.backward(x, u, offsets, saved, dy, dlast, h0)
@@ -139,7 +141,7 @@ class Scan(_Handle):
     """h_t = f_t h_{t-1} + (1 - f_t) x_t (coupled), or + x_t, with f = sigmoid(u), over the rows of every bag.
 
     x, u: [rows, dim] of `dtype` (rows may lie apart); offsets: int64 [bags + 1] on the GPU; h0: fp32 [bags, dim] or None.
-    Calling the object gives (y, last) with gradients to x, u and h0."""
+    Calling the object gives (y, last) with gradients to x, u and h0 (not with gradients of those: asking for them raises)."""
     _destroy = "tbe_scan_destroy"
 
     def __init__(self, dim: int, dtype: torch.dtype, max_bags: int, max_rows: int, coupled: bool = True):
@@ -230,6 +232,7 @@ class _BiasFunction(torch.autograd.Function):
         return plan.forward(table, scores=scores, **where)
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dout):
         where = {k: v for k, v in ctx.where.items() if k in ("q_pos", "k_pos", "q_offset", "key_lengths", "causal")}
         want_table, want_scores = ctx.needs_input_grad[1], ctx.needs_input_grad[2]
@@ -243,7 +246,7 @@ class RelativeBias(_Handle):
 
     thresholds: distances at which the buckets 1, 2, ... begin (see `log_thresholds`).  bidirectional: keys after the query have
     buckets of their own; else they are at distance 0.  Calling the object gives the biased scores with gradients to the table
-    and the scores."""
+    and the scores (not with gradients of those: asking for them raises)."""
     _destroy = "tbe_bias_destroy"
 
     def __init__(self, heads: int, thresholds: Sequence[int], bidirectional: bool = False):
