@@ -8,6 +8,7 @@ Argument marshalling only: every step runs in the HIP kernels of the library.  A
 this object's last call or its constructor if that was on another one (an object's calls share its scratch memory; replays of a captured graph
 are the caller's to order; graphs need the objects whose calls they hold).  No call waits for the GPU, apart from `Scan.check` and a
 step of `AdamW` that makes its plan anew, which no capture can hold.
+What a call writes into a tensor that it was given counts for autograd as changed in place.
 """
 from __future__ import annotations
 
@@ -17,6 +18,7 @@ from typing import Dict, List, Optional, Sequence, Tuple, Union
 
 import torch
 from torch.autograd.function import once_differentiable
+from torch.autograd.graph import increment_version as _written
 
 from . import tbe as _tbe
 
@@ -168,6 +170,7 @@ class Scan(_Handle):
     def forward(self, x, u, offsets, h0=None, y: Optional[torch.Tensor] = None, want_y: bool = True, save: bool = False):
         """(y, last, saved): h of every row (None without want_y), fp32 [bags, dim] after the last rows, what `backward` needs"""
         n, bags, args = self._batch(x, u, offsets, h0)
+        given = y
         if y is None and want_y:
             y = torch.empty(n, self.dim, dtype=self.dtype, device=self.device)
         last = torch.empty(bags, self.dim, dtype=torch.float32, device=self.device)
@@ -176,6 +179,8 @@ class Scan(_Handle):
         yp = self._rows("y", y, n) if y is not None else (None, 0)
         self._check(_lib().tbe_scan_forward(*args, *yp, last.data_ptr(), saved.data_ptr() if save else None, self._stream()),
                     "tbe_scan_forward")
+        if given is not None:
+            _written(given)
         return y, last, saved
 
     def backward(self, x, u, offsets, saved, dy=None, dlast=None, h0=None):
@@ -204,9 +209,11 @@ class Scan(_Handle):
                 self._tensor("slots", slots, torch.int64, (n,)) if slots is not None else None, *self._rows("x", x, n), *self._rows("u", u, n))
         if slots is not None and not slots.is_contiguous():
             raise ValueError("slots: a contiguous vector")
+        written = (state,) if y is None else (state, y)
         y = torch.empty(n, self.dim, dtype=self.dtype, device=self.device) if y is None else y
         yp = self._rows("y", y, n)
         self._check(_lib().tbe_scan_step(self._h, *args, n, *yp, self._stream()), "tbe_scan_step")
+        _written(written)
         return y
 
     def check(self):
@@ -291,11 +298,14 @@ class RelativeBias(_Handle):
             raise ValueError(f"table: contiguous, {', '.join(map(str, DTYPES))}")
         tp = self._tensor("table", table, table.dtype, (self.buckets, self.heads))
         sp, ss = self._scores("scores", scores, dtype, shape) if scores is not None else (None, None)
+        given = out
         if out is None:
             out = torch.empty(shape[0], self.heads, shape[1], shape[2], dtype=dtype, device=self.device)
         op, os_ = self._scores("out", out, dtype, shape)
         self._check(_lib().tbe_bias_forward(self._h, C.byref(st), tp, DTYPES[table.dtype], sp, C.byref(ss) if ss else None, scale, mask_value, op,
                                             C.byref(os_), self._stream()), "tbe_bias_forward")
+        if given is not None:
+            _written(given)
         return out
 
     def backward(self, dout, q_pos=None, k_pos=None, q_offset: int = 0, key_lengths=None, causal: bool = False, want_dtable: bool = True,
@@ -429,4 +439,5 @@ class AdamW(_Handle):
                 raise ValueError("grad_scale: one number")
         self._check(self._enqueue(self._h, self._grads_at, self.step_count + 1, self.lr if lr is None else lr, *self.betas, self.eps,
                                   self.seed & 0xFFFFFFFF, gs, stream), "tbe_adamw_step")
+        _written(self.params if fine else [p for p, g in zip(self.params, grads) if g is not None])
         self.step_count += 1

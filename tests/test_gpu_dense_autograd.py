@@ -34,3 +34,60 @@ def test_gradients_of_gradients_raise(call):
     first = torch.autograd.grad((run() ** 2).sum(), leaves)
     for a, b in zip(grads, first):
         assert torch.equal(a, b)
+
+
+def test_a_weight_that_a_graph_holds_may_not_be_stepped():
+    from paper_2305_01515_amd.dense import AdamW
+    w, other = (torch.nn.Parameter(torch.randn(4, 4).cuda()) for _ in range(2))
+    x = torch.randn(4, 4).cuda().requires_grad_()
+    opt = AdamW([w, other])
+    loss, fine = (x @ w).sum(), (x @ other).sum()
+    opt.step([torch.ones(4, 4).cuda(), None])
+    fine.backward()  # that one has been left as it is
+    with pytest.raises(RuntimeError, match="inplace operation"):
+        loss.backward()
+    loss = (x @ w).sum()
+    opt.step([torch.ones(4, 4).cuda()] * 2)
+    with pytest.raises(RuntimeError, match="inplace operation"):
+        loss.backward()
+
+
+def test_outputs_and_states_that_were_given():
+    """what an earlier product saved has been written over: its backward raises"""
+    plan, (x, u, off, h0), _ = scan_call()
+    w = torch.randn(8, 8).cuda().requires_grad_()
+    y, state = torch.randn(10, 8).cuda(), torch.randn(12, 8).cuda()
+    loss = (y @ w).sum()
+    plan.forward(x.detach(), u.detach(), off, y=y)
+    with pytest.raises(RuntimeError, match="inplace operation"):
+        loss.backward()
+    loss = (state @ w).sum()
+    plan.step(state, x.detach(), u.detach())
+    with pytest.raises(RuntimeError, match="inplace operation"):
+        loss.backward()
+    loss = (y @ w).sum()
+    plan.step(state, x.detach(), u.detach(), y=y)
+    with pytest.raises(RuntimeError, match="inplace operation"):
+        loss.backward()
+    bias, (table, scores), _ = bias_call()
+    out = torch.randn(3, 2, 4, 5).cuda()
+    loss = (out * scores).sum()
+    bias.forward(table.detach(), scores=scores.detach(), out=out)
+    with pytest.raises(RuntimeError, match="inplace operation"):
+        loss.backward()
+
+
+def test_under_inference_mode():
+    from paper_2305_01515_amd.dense import AdamW
+    plan, (x, u, off, h0), _ = scan_call()
+    bias, (table, scores), _ = bias_call()
+    w = torch.ones(5).cuda()
+    opt = AdamW([w])
+    with torch.inference_mode():
+        state, y, out = torch.zeros(10, 8).cuda(), torch.empty(10, 8).cuda(), torch.empty(3, 2, 4, 5).cuda()
+        plan.step(state, x, u, y=y)
+        assert torch.equal(y, state) and bool((state != 0).any())
+        plan.forward(x, u, off, y=y)
+        bias.forward(table, scores=scores, out=out)
+        opt.step([torch.ones(5).cuda()])
+    assert bool((w < 1).all())
