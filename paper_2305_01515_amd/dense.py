@@ -231,19 +231,23 @@ def log_thresholds(buckets: int, far: int) -> List[int]:
     return t[:buckets - 1]
 
 
+_WHERE = ("q_pos", "k_pos", "key_lengths"), ("q_offset", "causal")  # tensors and numbers that say where scores are
+
+
 class _BiasFunction(torch.autograd.Function):
     @staticmethod
     def forward(ctx, plan, table, scores, where):
-        ctx.plan, ctx.where = plan, where
-        ctx.table_dtype, ctx.has_scores = table.dtype, scores is not None
+        ctx.plan, ctx.where, ctx.scale = plan, {k: where[k] for k in _WHERE[1] if k in where}, where.get("scale", 1.0)
+        ctx.save_for_backward(*(where.get(k) for k in _WHERE[0]))
+        ctx.table_dtype = table.dtype
         return plan.forward(table, scores=scores, **where)
 
     @staticmethod
     @once_differentiable
     def backward(ctx, dout):
-        where = {k: v for k, v in ctx.where.items() if k in ("q_pos", "k_pos", "q_offset", "key_lengths", "causal")}
+        where = dict(zip(_WHERE[0], ctx.saved_tensors), **ctx.where)
         want_table, want_scores = ctx.needs_input_grad[1], ctx.needs_input_grad[2]
-        got = ctx.plan.backward(dout, want_dtable=want_table, want_dscores=want_scores, scale=ctx.where.get("scale", 1.0), **where)
+        got = ctx.plan.backward(dout, want_dtable=want_table, want_dscores=want_scores, scale=ctx.scale, **where)
         dtable, dscores = got if want_scores else (got, None)
         return None, dtable.to(ctx.table_dtype) if want_table else None, dscores, None
 

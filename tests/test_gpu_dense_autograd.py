@@ -91,3 +91,18 @@ def test_under_inference_mode():
         bias.forward(table, scores=scores, out=out)
         opt.step([torch.ones(5).cuda()])
     assert bool((w < 1).all())
+
+
+@pytest.mark.parametrize("name", ["q_pos", "k_pos", "key_lengths"])
+def test_positions_and_lengths_that_change_before_the_backward(name):
+    """a buffer that holds the next batch's by then: the gradient would be that of other buckets"""
+    where = dict(q_pos=torch.arange(4).expand(3, 4).contiguous().cuda(), k_pos=torch.arange(5).expand(3, 5).contiguous().cuda(),
+                 key_lengths=torch.tensor([5, 2, 0]).cuda())
+    _, leaves, run = bias_call(mask_value=0.0, scale=0.5, **where)
+    first = torch.autograd.grad(run().square().sum(), leaves)
+    again = torch.autograd.grad(run().square().sum(), leaves)
+    assert all(torch.equal(a, b) for a, b in zip(first, again))
+    loss = run().sum()
+    where[name].add_(1)
+    with pytest.raises(RuntimeError, match="inplace operation"):
+        loss.backward()
