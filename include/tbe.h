@@ -627,6 +627,13 @@ int tbe_adamw_destroy(tbe_adamw_handle s);
 int tbe_adamw_step(tbe_adamw_handle s, const void *const *h_grads, int64_t step, double lr, double beta1, double beta2,
                    double eps, uint32_t seed, const float *d_grad_scale, void *stream);
 
+/* The same with the number of the step in device memory: *d_step is how many steps there have been, the call adds one on the GPU and takes
+ * the step of that number (of number 1 below that).  It is for steps that are captured: each replay is a step of its own, whereas a
+ * captured tbe_adamw_step repeats its number, and with it the corrections 1 - beta^step and, with states in 8 bits, the same draws between
+ * codes for ever.  lr, betas, eps, seed and the gradients' addresses are those of the captured call in both. */
+int tbe_adamw_step_counted(tbe_adamw_handle s, const void *const *h_grads, int64_t *d_step, double lr, double beta1,
+                           double beta2, double eps, uint32_t seed, const float *d_grad_scale, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -41,12 +41,29 @@ struct Step {
   uint32_t key;  // of seed and step
 };
 
+// What of a Step goes by its number, where that is in device memory
+struct Counted {
+  float rate, root;
+  uint32_t key;
+};
+
 __host__ __device__ inline uint32_t mix(uint32_t x) {  // multiplications by odd words (fractions of the roots of 2 and 3)
   x ^= x >> 16;
   x *= 0x6A09E667u;
   x ^= x >> 15;
   x *= 0xBB67AE85u;
   return x ^ (x >> 16);
+}
+
+__host__ __device__ inline Counted counted_of(int64_t step, double lr, double beta1, double beta2, uint32_t seed) {
+  return {(float)(lr / (1.0 - pow(beta1, (double)step))), (float)(1.0 / sqrt(1.0 - pow(beta2, (double)step))), mix(mix(seed) ^ (uint32_t)step)};
+}
+
+// A lane in front of a step that is counted on the GPU: 2 us.  (One in the step's own kernel would have to wait for all of it, or count in each workgroup.)
+__global__ void adamw_count_kernel(int64_t *step, double lr, double beta1, double beta2, uint32_t seed, Counted *out) {
+  const int64_t n = max(*step + 1, (int64_t)1);
+  *step = n;
+  *out = counted_of(n, lr, beta1, beta2, seed);
 }
 
 // Addresses that come out of memory: told to be of device memory, or the compiler takes instructions that look for LDS as well.
@@ -193,7 +210,12 @@ __device__ inline void step_block(const Tensor &ts, const void *gp, uint32_t key
 
 template <bool EIGHT>
 __global__ __launch_bounds__(kThreads) void adamw_kernel(const Tensor *tensors, const int64_t *chunk_list, int first_tensor, Grads grads, Step st,
-                                                         const float *grad_scale) {
+                                                         const float *grad_scale, const Counted *counted) {
+  if (counted) {
+    st.rate = counted->rate;
+    st.root = counted->root;
+    st.key = counted->key;
+  }
   const int64_t word = chunk_list[blockIdx.x];
   const int t = (int)(word >> 40);
   const void *gp = global((const char *)grads.p[t - first_tensor]);
@@ -226,7 +248,44 @@ struct tbe_adamw_t : DenseBase {
   Tensor *tensors = nullptr;   // device [n]
   int64_t *chunk_list = nullptr; // device: tensor << 40 | chunk of it, for every workgroup
   int64_t *first = nullptr;    // host [n + 1]: first workgroup of a tensor
+  Counted *counted = nullptr;  // device
 };
+
+namespace {
+
+// A step with the number `step`, or with that behind *d_step
+int run(tbe_adamw_t *s, const void *const *h_grads, int64_t step, int64_t *d_step, double lr, double beta1, double beta2, double eps, uint32_t seed,
+        const float *d_grad_scale, hipStream_t stream) noexcept {
+  if (int rc = check_handle(s)) return rc;
+  if (!h_grads) return report(TBE_EINVAL, "null gradients");
+  if (!(lr >= 0.0) || !std::isfinite(lr) || !(beta1 >= 0.0 && beta1 < 1.0) || !(beta2 >= 0.0 && beta2 < 1.0) || !(eps >= 0.0) || !std::isfinite(eps))
+    return report(TBE_EINVAL, "lr and eps are at least 0, the betas at least 0 and below 1");
+  Step st;
+  st.beta1 = (float)beta1;
+  st.one_minus_beta1 = (float)(1.0 - beta1);
+  st.beta2 = (float)beta2;
+  st.one_minus_beta2 = (float)(1.0 - beta2);
+  st.eps = (float)eps;
+  st.lr = lr;
+  const Counted c = counted_of(step, lr, beta1, beta2, seed);
+  st.rate = c.rate;
+  st.root = c.root;
+  st.key = c.key;
+  if (d_step) adamw_count_kernel<<<1, 1, 0, stream>>>(d_step, lr, beta1, beta2, seed, s->counted);
+  const Counted *counted = d_step ? s->counted : nullptr;
+  for (int t0 = 0; t0 < s->n; t0 += kMaxGrads) {
+    const int t1 = t0 + kMaxGrads < s->n ? t0 + kMaxGrads : s->n;
+    const int64_t first = s->first[t0], count = s->first[t1] - first;
+    if (count == 0) continue;
+    Grads g = {};
+    for (int t = t0; t < t1; t++) g.p[t - t0] = h_grads[t];
+    if (s->bits == 8) adamw_kernel<true><<<dim3((unsigned)count), kThreads, 0, stream>>>(s->tensors, s->chunk_list + first, t0, g, st, d_grad_scale, counted);
+    else adamw_kernel<false><<<dim3((unsigned)count), kThreads, 0, stream>>>(s->tensors, s->chunk_list + first, t0, g, st, d_grad_scale, counted);
+  }
+  return check_launch();
+}
+
+}  // namespace
 
 extern "C" {
 
@@ -276,7 +335,8 @@ int tbe_adamw_create(tbe_adamw_handle *out, const tbe_adamw_tensor *h_tensors, i
     }
     s->first[num_tensors] = at;
     hipError_t e = hipGetDevice(&s->device);
-    if (e == hipSuccess) e = hipMalloc((void **)&s->tensors, num_tensors * sizeof(Tensor));
+    if (e == hipSuccess) e = hipMalloc((void **)&s->tensors, num_tensors * sizeof(Tensor) + sizeof(Counted));  // one block: [tensors][counted]
+    s->counted = (Counted *)(s->tensors + num_tensors);
     if (e == hipSuccess) e = hipMalloc((void **)&s->chunk_list, (chunks + 1) * sizeof(int64_t));
     if (e == hipSuccess) e = hipMemcpy(s->tensors, host, num_tensors * sizeof(Tensor), hipMemcpyHostToDevice);
     if (e == hipSuccess) e = hipMemcpy(s->chunk_list, list, chunks * sizeof(int64_t), hipMemcpyHostToDevice);
@@ -294,31 +354,14 @@ int tbe_adamw_create(tbe_adamw_handle *out, const tbe_adamw_tensor *h_tensors, i
 
 int tbe_adamw_step(tbe_adamw_handle s, const void *const *h_grads, int64_t step, double lr, double beta1, double beta2, double eps, uint32_t seed,
                    const float *d_grad_scale, void *stream) {
-  if (int rc = check_handle(s)) return rc;
-  if (!h_grads) return report(TBE_EINVAL, "null gradients");
-  if (step < 1) return report(TBE_EINVAL, "the first step is step 1");
-  if (!(lr >= 0.0) || !std::isfinite(lr) || !(beta1 >= 0.0 && beta1 < 1.0) || !(beta2 >= 0.0 && beta2 < 1.0) || !(eps >= 0.0) || !std::isfinite(eps))
-    return report(TBE_EINVAL, "lr and eps are at least 0, the betas at least 0 and below 1");
-  Step st;
-  st.beta1 = (float)beta1;
-  st.one_minus_beta1 = (float)(1.0 - beta1);
-  st.beta2 = (float)beta2;
-  st.one_minus_beta2 = (float)(1.0 - beta2);
-  st.rate = (float)(lr / (1.0 - std::pow(beta1, (double)step)));
-  st.root = (float)(1.0 / std::sqrt(1.0 - std::pow(beta2, (double)step)));
-  st.eps = (float)eps;
-  st.lr = lr;
-  st.key = mix(mix(seed) ^ (uint32_t)step);
-  for (int t0 = 0; t0 < s->n; t0 += kMaxGrads) {
-    const int t1 = t0 + kMaxGrads < s->n ? t0 + kMaxGrads : s->n;
-    const int64_t first = s->first[t0], count = s->first[t1] - first;
-    if (count == 0) continue;
-    Grads g = {};
-    for (int t = t0; t < t1; t++) g.p[t - t0] = h_grads[t];
-    if (s->bits == 8) adamw_kernel<true><<<dim3((unsigned)count), kThreads, 0, (hipStream_t)stream>>>(s->tensors, s->chunk_list + first, t0, g, st, d_grad_scale);
-    else adamw_kernel<false><<<dim3((unsigned)count), kThreads, 0, (hipStream_t)stream>>>(s->tensors, s->chunk_list + first, t0, g, st, d_grad_scale);
-  }
-  return check_launch();
+  if (s && step < 1) return report(TBE_EINVAL, "the first step is step 1");
+  return run(s, h_grads, step, nullptr, lr, beta1, beta2, eps, seed, d_grad_scale, (hipStream_t)stream);
+}
+
+int tbe_adamw_step_counted(tbe_adamw_handle s, const void *const *h_grads, int64_t *d_step, double lr, double beta1, double beta2, double eps, uint32_t seed,
+                           const float *d_grad_scale, void *stream) {
+  if (s && !d_step) return report(TBE_EINVAL, "null step number");
+  return run(s, h_grads, 1, d_step, lr, beta1, beta2, eps, seed, d_grad_scale, (hipStream_t)stream);
 }
 
 }  // extern "C"

@@ -14,6 +14,7 @@ from __future__ import annotations
 
 import ctypes as C
 import math
+import warnings
 from typing import Dict, List, Optional, Sequence, Tuple, Union
 
 import torch
@@ -66,6 +67,7 @@ def _lib() -> C.CDLL:
         l.tbe_bias_backward.argtypes = [vp, C.POINTER(BiasShape), vp, C.POINTER(BiasStrides), vp, f32, vp, C.POINTER(BiasStrides), vp]
         l.tbe_adamw_create.argtypes = [C.POINTER(vp), C.POINTER(AdamWTensor), i32, i32]
         l.tbe_adamw_step.argtypes = [vp, vp, i64, f64, f64, f64, f64, C.c_uint32, vp, vp]
+        l.tbe_adamw_step_counted.argtypes = [vp, vp, vp, f64, f64, f64, f64, C.c_uint32, vp, vp]
         l.tbe_scan_check.argtypes = [vp, vp]
         for n in ("tbe_scan_destroy", "tbe_bias_destroy", "tbe_adamw_destroy"):
             getattr(l, n).argtypes = [vp]
@@ -338,18 +340,20 @@ class AdamW(_Handle):
     copies beside 16-bit parameters, True to make them from the parameters, or a list of tensors.  weight_decay: one number or one for each
     parameter.  grad_dtypes: types of the gradients, the parameters' own unless given (a step whose gradients have others makes the
     plan anew).  States of all parameters lie one behind another in `states` ("m", "v" and for 8 bits "m_scale", "v_scale"), each
-    parameter's from a multiple of 256 elements on: that is what a checkpoint holds, with `step_count`.  A step takes parameters, `master` and
+    parameter's from a multiple of 256 elements on: that is what a checkpoint holds, with `step_count`.  capturable: the number of the step is counted on the
+    GPU, in `states["step"]`, so that each replay of a captured step is a step of its own (without, all have the captured one's
+    number; lr, betas and the gradients' places are the captured ones in both).  A step takes parameters, `master` and
     `states` as they are then: other tensors of the same sizes in their place, and parameters that have got other storage, make the
     plan anew."""
     _destroy = "tbe_adamw_destroy"
 
     def __init__(self, params: Sequence[torch.Tensor], lr: float = 1e-3, betas: Tuple[float, float] = (0.9, 0.999), eps: float = 1e-8,
                  weight_decay: Union[float, Sequence[float]] = 0.01, state_bits: int = 32, master=None, seed: int = 0, step: int = 0,
-                 states: Optional[Dict[str, torch.Tensor]] = None, grad_dtypes: Optional[Sequence[torch.dtype]] = None):
+                 states: Optional[Dict[str, torch.Tensor]] = None, grad_dtypes: Optional[Sequence[torch.dtype]] = None, capturable: bool = False):
         super().__init__()
         self._kept: List[C.c_void_p] = []  # handles of earlier plans
         self.params = list(params)
-        self.lr, self.betas, self.eps, self.seed, self.step_count, self.state_bits = lr, betas, eps, seed, step, state_bits
+        self.lr, self.betas, self.eps, self.seed, self._steps, self.state_bits, self.capturable = lr, betas, eps, seed, step, state_bits, capturable
         decay = list(weight_decay) if isinstance(weight_decay, (list, tuple)) else [weight_decay] * len(self.params)
         if len(decay) != len(self.params):
             raise ValueError("weight_decay: one number, or one for each parameter")
@@ -365,6 +369,8 @@ class AdamW(_Handle):
         kinds = {"m": (torch.float32, total * BLOCK), "v": (torch.float32, total * BLOCK)} if state_bits == 32 else \
             {"m": (torch.uint8, total * BLOCK), "v": (torch.uint8, total * BLOCK), "m_scale": (torch.float32, total), "v_scale": (torch.float32, total)}
         self.states = states or {k: torch.zeros(n, dtype=d, device=self.device) for k, (d, n) in kinds.items()}
+        if capturable:  # a step number among the given states goes before `step`
+            self.states = {"step": torch.full((1,), step, dtype=torch.int64, device=self.device), **self.states}
         self._decay, self._blocks, self._kinds = decay, blocks, kinds
         self._grads = (C.c_void_p * max(1, len(self.params)))()
         self._grads_at, self._gpus = C.addressof(self._grads), [self.device.index] * len(self.params)
@@ -375,6 +381,21 @@ class AdamW(_Handle):
         super().close()
         while self._kept:
             _lib().tbe_adamw_destroy(self._kept.pop())
+
+    @property
+    def step_count(self) -> int:
+        """steps so far (capturable: waits for them)"""
+        if not self.capturable:
+            return self._steps
+        self._stream()
+        return int(self.states["step"])
+
+    @step_count.setter
+    def step_count(self, n: int):
+        self._steps = n
+        if self.capturable:
+            self._stream()
+            self.states["step"].fill_(n)
 
     def _parameter(self, p):
         if p.dtype not in DTYPES or p.device != self.device or not p.is_contiguous():
@@ -409,7 +430,7 @@ class AdamW(_Handle):
             self._kept.append(self._h)  # graphs may hold steps of it
         elif self._h:
             _lib().tbe_adamw_destroy(self._h)
-        self._h, self._captured, self._enqueue = h, False, _lib().tbe_adamw_step
+        self._h, self._captured, self._enqueue = h, False, _lib().tbe_adamw_step_counted if self.capturable else _lib().tbe_adamw_step
         self._planned, self._grad_dtypes = self._places(), grad_dtypes
 
     def step(self, grads: Optional[Sequence[Optional[torch.Tensor]]] = None, lr: Optional[float] = None, grad_scale: Optional[torch.Tensor] = None):
@@ -436,12 +457,15 @@ class AdamW(_Handle):
         ptrs[:] = [*map(_address, grads)] if fine else [None if g is None else g.data_ptr() for g in grads]
         if stream and _capturing():  # the default stream cannot be
             self._captured = True
+            if not self.capturable:
+                warnings.warn("the replays of this captured step all have its number (step_count): capturable=True counts them")
         gs = None
         if grad_scale is not None:
             gs = self._tensor("grad_scale", grad_scale, torch.float32, grad_scale.shape)
             if grad_scale.numel() != 1:
                 raise ValueError("grad_scale: one number")
-        self._check(self._enqueue(self._h, self._grads_at, self.step_count + 1, self.lr if lr is None else lr, *self.betas, self.eps,
-                                  self.seed & 0xFFFFFFFF, gs, stream), "tbe_adamw_step")
+        number = self._whole("step", self.states["step"], torch.int64, (1,)) if self.capturable else self._steps + 1
+        self._check(self._enqueue(self._h, self._grads_at, number, self.lr if lr is None else lr, *self.betas, self.eps, self.seed & 0xFFFFFFFF, gs,
+                                  stream), "tbe_adamw_step")
         _written(self.params if fine else [p for p, g in zip(self.params, grads) if g is not None])
-        self.step_count += 1
+        self._steps += 1

@@ -55,3 +55,9 @@ def test_log_thresholds(buckets, far):
     from paper_2305_01515_amd.dense import log_thresholds
     t = log_thresholds(buckets, far)
     assert len(t) == buckets - 1 and all(b > a for a, b in zip([0] + t, t)) and all(x <= max(far, 2 * buckets) for x in t)
+
+
+def test_adamw_counted():
+    l, ptr = lib(), (C.c_void_p * 1)(16)
+    assert l.tbe_adamw_step_counted(None, ptr, None, 0.0, 0.9, 0.9, 0.0, 0, None, None) == -1
+    assert b"null handle" in l.tbe_last_error(None)
