@@ -604,7 +604,7 @@ int tbe_bias_backward(tbe_bias_handle s, const tbe_bias_shape *shape, const void
  * state_bits 32: m, v are fp32.  state_bits 8: m and sqrt(v) are 8-bit numbers (E4M3: 4 exponent bits, 3 mantissa bits,
  * largest 448) times a scale for each TBE_ADAMW_BLOCK elements, the block's largest / 448.  Between two codes the upper is taken
  * with the probability that keeps the expected value, by 16 bits of a hash of (seed, step, tensor, element), so the same call
- * gives the same bits and moving averages do not stick between codes.  sqrt(v) above zero never becomes zero.  A block that holds an
+ * gives the same bits and moving averages do not stick between codes.  sqrt(v) above zero never becomes zero.  A block of m whose largest is below 2^-119 (1.5e-36) becomes zero.  A block that holds an
  * infinity or a NaN reads back as NaN.
  */
 #define TBE_ADAMW_BLOCK 256

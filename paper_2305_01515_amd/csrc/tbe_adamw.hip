@@ -189,7 +189,9 @@ __device__ inline void step_block(const Tensor &ts, const void *gp, uint32_t key
       v_top = max(v_top, __float_as_uint(r[k]));
     }
   const float mt = __uint_as_float(wave_top(m_top)), vt = __uint_as_float(wave_top(v_top));
-  const bool mu = mt > 0.0f && mt < INFINITY, vu = vt > 0.0f && vt < INFINITY;
+  // 448 / mt is a number of fp32 from 2^-119 up (a root of an fp32 number is never below that): a block below is stored as zeros, its codes would
+  // all be that of the largest.  (Taken times 2^64 first, 172 M weights take 526 us instead of 520.)
+  const bool mu = mt >= 0x1p-119f && mt < INFINITY, vu = vt > 0.0f && vt < INFINITY;
   const float mi = (1.0f / mt) * 448.0f, vi = (1.0f / vt) * 448.0f;
   uint32_t mw = 0, vw = 0;
 #pragma unroll
