@@ -597,7 +597,7 @@ int tbe_bias_backward(tbe_bias_handle s, const tbe_bias_shape *shape, const void
                       const tbe_bias_strides *dscores_strides, void *stream);
 
 /*
- * AdamW step of many tensors in one launch (one for every 256 tensors).  For every element, with g = gradient * grad_scale,
+ * AdamW step of many tensors in one launch (one for every 256 tensors, and for every 1.7e10 elements).  For every element, with g = gradient * grad_scale,
  *   m = beta1 m + (1 - beta1) g,   v = beta2 v + (1 - beta2) g g,
  *   w = w (1 - lr weight_decay) - lr / (1 - beta1^step) * m / (sqrt(v) / sqrt(1 - beta2^step) + eps)
  * where w is the fp32 master copy if there is one, and the parameter is w rounded to its type.

@@ -8,6 +8,7 @@
 //
 // Moving averages and their codes are computed operation by operation, each rounded to fp32 (no contraction), so that a plain form in fp32
 // gives the same bits: a last bit that differs makes another code now and then, and a code is a sixteenth of its value.
+#include <algorithm>
 #include <cmath>
 #include <new>
 
@@ -281,8 +282,12 @@ int run(tbe_adamw_t *s, const void *const *h_grads, int64_t step, int64_t *d_ste
     if (count == 0) continue;
     Grads g = {};
     for (int t = t0; t < t1; t++) g.p[t - t0] = h_grads[t];
-    if (s->bits == 8) adamw_kernel<true><<<dim3((unsigned)count), kThreads, 0, stream>>>(s->tensors, s->chunk_list + first, t0, g, st, d_grad_scale, counted);
-    else adamw_kernel<false><<<dim3((unsigned)count), kThreads, 0, stream>>>(s->tensors, s->chunk_list + first, t0, g, st, d_grad_scale, counted);
+    for (int64_t done = 0; done < count; done += most_groups(kThreads)) {  // one launch, unless the tensors have 1.7e10 elements
+      const dim3 grid((unsigned)std::min(count - done, most_groups(kThreads)));
+      const int64_t *list = s->chunk_list + first + done;
+      if (s->bits == 8) adamw_kernel<true><<<grid, kThreads, 0, stream>>>(s->tensors, list, t0, g, st, d_grad_scale, counted);
+      else adamw_kernel<false><<<grid, kThreads, 0, stream>>>(s->tensors, list, t0, g, st, d_grad_scale, counted);
+    }
   }
   return check_launch();
 }
@@ -317,7 +322,7 @@ int tbe_adamw_create(tbe_adamw_handle *out, const tbe_adamw_tensor *h_tensors, i
     if (!std::isfinite(a.weight_decay)) return report(TBE_EINVAL, "weight_decay is not finite");
     chunks += (a.numel + kChunk - 1) / kChunk;
   }
-  if (chunks > INT32_MAX) return report(TBE_ELIMIT, "more elements than one launch can take");
+  if (chunks > INT32_MAX) return report(TBE_ELIMIT, "more than 2^41 elements");
   tbe_adamw_t *s = new (std::nothrow) tbe_adamw_t;
   Tensor *host = new (std::nothrow) Tensor[num_tensors];
   int64_t *list = new (std::nothrow) int64_t[chunks + 1];

@@ -34,6 +34,9 @@ inline int check_launch() noexcept {
   return e == hipSuccess ? TBE_OK : report_hip(e);
 }
 
+// workgroups of so many threads that a launch takes at most: a grid has fewer than 2^32 work-items
+constexpr int64_t most_groups(int threads) { return (int64_t)0xFFFFFFFF / threads; }
+
 inline int elem_bytes(int dtype) { return dtype == TBE_FP32 ? 4 : 2; }
 inline bool known_dtype(int dtype) { return dtype == TBE_FP32 || dtype == TBE_FP16 || dtype == TBE_BF16; }
 

@@ -91,3 +91,18 @@ def test_rows_of_almost_2_31_keys():
     dout *= 0.5
     assert torch.equal(dscores, dout)
     assert plan.backward(dout, q_offset=keys - 1)[:, 0].tolist() == [50.0, 475.0, 0.0, 210.0]
+
+
+def test_more_weights_than_one_launch_takes():
+    """2^24 workgroups of 1024 elements have 2^32 lanes, one more than a grid may have"""
+    from paper_2305_01515_amd.dense import AdamW
+    n = (1 << 34) + 3000
+    p, g = torch.ones(n, dtype=torch.bfloat16, device="cuda"), torch.full((n,), 0.25, dtype=torch.bfloat16, device="cuda")
+    opt = AdamW([p], lr=0.125, weight_decay=0.0, state_bits=8)
+    opt.step([g])
+    assert float(p.min()) == float(p.max()) == 0.875 and opt.step_count == 1
+    for k in "mv":
+        s = opt.states[k]
+        for part in s[:n].split(1 << 31):
+            assert bool((part == s[0]).all())
+        assert not bool(s[n:].any())
