@@ -16,6 +16,7 @@
 // A row lies on L lanes of V elements (16 bytes, or the largest half of that, quarter, ... that divides dim), a lane has R rows in a row in
 // registers, 32 elements of each input or fewer (apply_threads, grad_threads).  The maps of a wavefront's 64 / L lane groups are
 // joined by exchange between lanes, those of the workgroup's wavefronts through LDS.
+#include <algorithm>
 #include <cmath>
 #include <new>
 
@@ -716,12 +717,12 @@ __global__ __launch_bounds__(grad_threads(V), 4) void scan_grad_kernel(Rows<DT> 
   }
 }
 
-// One row for each of many states, a lane an element: 2 us for 7 rows of 64; what counts is the call.
+// One row for each of many states, a lane an element, from element `first` on: 2 us for 7 rows of 64; what counts is the call.
 template <int DT>
-__global__ __launch_bounds__(kThreads) void scan_step_kernel(float *state, int64_t ss, int64_t slots, const int64_t *slot_of, const typename Elem<DT>::type *x,
+__global__ __launch_bounds__(kThreads) void scan_step_kernel(int64_t first, float *state, int64_t ss, int64_t slots, const int64_t *slot_of, const typename Elem<DT>::type *x,
                                                              int64_t xs, const typename Elem<DT>::type *u, int64_t us, int64_t rows, int dim,
                                                              bool coupled, typename Elem<DT>::type *y, int64_t ys, int32_t *err) {
-  const int64_t id = (int64_t)blockIdx.x * kThreads + threadIdx.x, r = id / dim;
+  const int64_t id = first + (int64_t)blockIdx.x * kThreads + threadIdx.x, r = id / dim;
   const int d = (int)(id % dim);
   if (r >= rows) return;
   const int64_t slot = slot_of ? slot_of[r] : r;
@@ -764,8 +765,6 @@ int check_batch(tbe_scan_t *s, const void *x, int64_t xs, const void *u, int64_t
   if (h0 && h0s != 0 && h0s < s->dim) return report(TBE_EINVAL, "a stride of d_h0 that is neither 0 nor dim or more");
   return TBE_OK;
 }
-
-dim3 grid_of(int64_t n) { return dim3((unsigned)((n + kThreads - 1) / kThreads)); }
 
 int64_t chunks_of(const tbe_scan_t *s, int64_t rows) { return (rows + s->cut.rows - 1) / s->cut.rows; }
 
@@ -958,13 +957,16 @@ int tbe_scan_step(tbe_scan_handle s, float *d_state, int64_t state_stride, int64
   if (!d_state || !d_x || !d_u) return report(TBE_EINVAL, "null states, rows or gates");
   if (!d_slots && rows > slots) return report(TBE_EINVAL, "more rows than states");
   if (state_stride < s->dim || x_stride < s->dim || u_stride < s->dim || (d_y && y_stride < s->dim)) return report(TBE_EINVAL, "a stride below dim");
-  const dim3 grid = grid_of(rows * s->dim);
+  const int64_t groups = (rows * s->dim + kThreads - 1) / kThreads;
 #define LAUNCH(DT)                                                                                                                            \
-  scan_step_kernel<DT><<<grid, kThreads, 0, (hipStream_t)stream>>>(d_state, state_stride, slots, d_slots, (const Elem<DT>::type *)d_x, x_stride,        \
-                                                         (const Elem<DT>::type *)d_u, u_stride, rows, s->dim, s->coupled, (Elem<DT>::type *)d_y, y_stride, s->err)
-  if (s->dtype == TBE_FP32) LAUNCH(TBE_FP32);
-  else if (s->dtype == TBE_FP16) LAUNCH(TBE_FP16);
-  else LAUNCH(TBE_BF16);
+  scan_step_kernel<DT><<<grid, kThreads, 0, (hipStream_t)stream>>>(done * kThreads, d_state, state_stride, slots, d_slots, (const Elem<DT>::type *)d_x, \
+                                                         x_stride, (const Elem<DT>::type *)d_u, u_stride, rows, s->dim, s->coupled, (Elem<DT>::type *)d_y, y_stride, s->err)
+  for (int64_t done = 0; done < groups; done += most_groups(kThreads)) {  // one launch, unless the rows have 2^32 elements
+    const dim3 grid((unsigned)std::min(groups - done, most_groups(kThreads)));
+    if (s->dtype == TBE_FP32) LAUNCH(TBE_FP32);
+    else if (s->dtype == TBE_FP16) LAUNCH(TBE_FP16);
+    else LAUNCH(TBE_BF16);
+  }
 #undef LAUNCH
   return check_launch();
 }

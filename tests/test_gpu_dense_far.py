@@ -106,3 +106,24 @@ def test_more_weights_than_one_launch_takes():
         for part in s[:n].split(1 << 31):
             assert bool((part == s[0]).all())
         assert not bool(s[n:].any())
+
+
+@pytest.mark.parametrize("slots", [False, True])
+def test_more_states_than_one_launch_takes(slots):
+    """2^32 elements and more, a lane each, one more than a grid may have; the same bits as two halves"""
+    from paper_2305_01515_amd.dense import Scan
+    dim, n = 128, (1 << 25) + 77
+    plan = Scan(dim, torch.bfloat16, 1, 1)
+    g = torch.Generator(device="cuda").manual_seed(1)
+    x, u = (torch.empty(n, dim, dtype=torch.bfloat16, device="cuda").normal_(generator=g) for _ in range(2))
+    state = torch.empty(n, dim, device="cuda").normal_(generator=g)
+    other, half = state.clone(), n // 2
+    slot = torch.arange(n - 1, -1, -1, device="cuda") if slots else None
+    y = plan.step(state, x, u, slot)
+    plan.check()
+    if slots:
+        first, last = plan.step(other, x[:half], u[:half], slot[:half]), plan.step(other, x[half:], u[half:], slot[half:])
+    else:
+        first, last = plan.step(other[:half], x[:half], u[:half]), plan.step(other[half:], x[half:], u[half:])
+    assert torch.equal(y[:half], first) and torch.equal(y[half:], last) and torch.equal(state, other)
+    assert bool((y[-1] != 0).all())
