@@ -511,7 +511,8 @@ int tbe_plan_placement(const tbe_place_table *tables, int32_t num_tables, const 
  *   h_t = f_t h_{t-1} + (1 - f_t) x_t   (coupled = 1)   or   h_t = f_t h_{t-1} + x_t   (coupled = 0)
  * for the rows t = offsets[b] .. offsets[b+1]-1 of bag b in turn, from h = d_h0[b] (null: zero).
  * dim: elements of a row, 1 .. 65536; max_bags, max_rows: what a call may bring at most (scratch memory: 16 bytes
- * for each of max_rows and 28 * dim for each chunk of them, which has 8192 elements, or somewhat fewer where dim is no power of two).
+ * for each of max_rows and 28 * dim for each chunk of them, which has 8192 elements, or somewhat fewer where dim is no power of two).  A call
+ * takes some 2^36 elements, the gradient half as many where dim is no multiple of 4 (TBE_ELIMIT).
  */
 typedef struct tbe_scan_t *tbe_scan_handle;
 int tbe_scan_create(tbe_scan_handle *out, int32_t dim, int32_t dtype, int32_t coupled, int64_t max_bags,

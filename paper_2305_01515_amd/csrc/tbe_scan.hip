@@ -879,7 +879,7 @@ int tbe_scan_create(tbe_scan_handle *out, int32_t dim, int32_t dtype, int32_t co
   s->max_rows = max_rows;
   s->cut = cut_of(dim, dtype);
   const int64_t chunks = chunks_of(s, max_rows);
-  if (chunks * s->cut.tiles > INT32_MAX / kThreads) {
+  if (chunks * s->cut.tiles > INT32_MAX / kThreads) {  // the most that a launch of the forward has, with up to 512 lanes a workgroup
     delete s;
     return report(TBE_ELIMIT, "more rows than one launch can take");
   }
@@ -938,6 +938,7 @@ int tbe_scan_backward(tbe_scan_handle s, const void *d_x, int64_t x_stride, cons
   if (int rc = check_batch(s, d_x, x_stride, d_u, u_stride, d_offsets, bags, rows, d_h0, h0_stride)) return rc;
   if (rows > 0 && (!d_saved || !d_dx || !d_du)) return report(TBE_EINVAL, "null pointer for what the forward saved or for a gradient");
   if ((d_dy && dy_stride < s->dim) || dx_stride < s->dim || du_stride < s->dim) return report(TBE_EINVAL, "a stride below dim");
+  if (chunks_of(s, rows) * s->cut.tiles > most_groups(grad_threads(s->cut.V))) return report(TBE_ELIMIT, "more rows than one launch can take");
   if (bags == 0) return TBE_OK;
   hipStream_t st = (hipStream_t)stream;
 #define BACKWARD(DT) backward<DT>(s, ROWS(DT), d_saved, d_dy, dy_stride, d_dlast, d_dx, dx_stride, d_du, du_stride, d_dh0, st)

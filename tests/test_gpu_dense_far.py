@@ -127,3 +127,18 @@ def test_more_states_than_one_launch_takes(slots):
         first, last = plan.step(other[:half], x[:half], u[:half]), plan.step(other[half:], x[half:], u[half:])
     assert torch.equal(y[:half], first) and torch.equal(y[half:], last) and torch.equal(state, other)
     assert bool((y[-1] != 0).all())
+
+
+def test_a_gradient_of_more_rows_than_a_launch_takes_is_refused():
+    """2^22 workgroups of 1024 lanes: one more than a grid may have; the forward's have 512.  Nothing is enqueued."""
+    import ctypes as C
+    from paper_2305_01515_amd import dense
+    dim, rows = 65535, 1 << 19
+    plan = dense.Scan(dim, torch.float16, 1, rows)
+    off, t = torch.tensor([0, rows]).cuda(), torch.zeros(8).cuda()
+    a = t.data_ptr()
+    args = (plan._h, a, dim, a, dim, off.data_ptr(), 1, rows, None, 0, a, a, dim, None, a, dim, a, dim, None, None)
+    assert dense._lib().tbe_scan_backward(*args) == -5
+    assert b"one launch" in dense._lib().tbe_last_error(None)
+    torch.cuda.synchronize()
+    assert not bool(t.any())
