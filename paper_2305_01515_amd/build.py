@@ -8,7 +8,8 @@ for the properties the library relies on:
   - `backward_rest_kernel`, which waits for gathered rows, leaves room for four wavefronts a SIMD in each of its instances;
   - no kernel spills registers to scratch memory.
 Beside it, for the tests, it builds the library twice more, with workgroups that look 0 and 1 times at what another one has
-yet to say before they count that one's part themselves (64 times in libtbe.so, which a run without contention never reaches).
+yet to say before they count that one's part themselves (64 times in libtbe.so, which a run without contention never reaches),
+and whose scans number their calls from shortly before 2^30 and 2^32 on.
 
 The packed-fp32 target feature is switched off for the device pass.  hipcc hands `-Xclang` options
 to the host pass as well, which does not know the feature and says so once per file and pass;
@@ -30,6 +31,7 @@ SOURCES = ["tbe_api.hip", "tbe_sort.hip", "tbe_cache.hip", "tbe_one.hip", "tbe_m
            "tbe_scan.hip", "tbe_bias.hip", "tbe_adamw.hip"]
 FLAGS = ["-O3", "-std=c++17", "--offload-arch=gfx950", "-fPIC",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops", "-Wall", "-Wno-unused-function"]
+FIRST_CALL = {0: 0x3FFFFFFD, 1: 0xFFFFFFFD}  # of a scan's handle in those builds: its calls' numbers pass 2^30 and 2^32 soon
 IMPATIENT = {polls: os.path.join(HERE, f"libtbe_polls{polls}.so") for polls in (0, 1)}
 POLLING = ["tbe_sort.hip", "tbe_cache.hip", "tbe_scan.hip"]  # the sources whose kernels look
 REMARKS = ["-Rpass-analysis=kernel-resource-usage"]
@@ -69,7 +71,7 @@ def parse_resource_usage(stderr: str):
 
 def _compile(hipcc: str, src: str, verbose: bool, polls=None):
     obj = os.path.join(OBJ, os.path.splitext(src)[0] + ("" if polls is None else f"_polls{polls}") + ".o")
-    cmd = [hipcc] + FLAGS + ([] if polls is None else [f"-DTBE_POLLS={polls}"]) + REMARKS + ["-c", os.path.join(CSRC, src), "-o", obj]
+    cmd = [hipcc] + FLAGS + ([] if polls is None else [f"-DTBE_POLLS={polls}", f"-DTBE_FIRST_CALL={FIRST_CALL[polls]}u"]) + REMARKS + ["-c", os.path.join(CSRC, src), "-o", obj]
     if verbose:
         print(" ".join(cmd), flush=True)
     p = subprocess.run(cmd, capture_output=True, text=True)

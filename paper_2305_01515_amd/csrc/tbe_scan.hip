@@ -27,6 +27,10 @@ using namespace tbe;
 
 namespace {
 
+#ifndef TBE_FIRST_CALL  // tests begin near the ends of the numbers
+#define TBE_FIRST_CALL 1
+#endif
+
 constexpr int kThreads = 256, kWaves = kThreads / 64;
 // A chunk's rows lie on as many lanes as leave four wavefronts a SIMD room for their registers: single elements and the gradient on more.
 // (200000 rows of 33 in fp32, bags of 30: 67 + 77 us; with half the lanes 102 + 95.)
@@ -101,6 +105,11 @@ struct Rows {
   bool coupled, chained;  // chained: chunks hear from each other instead of sum and join
 };
 
+// Numbers of calls: none whose 30 bits in a word are zero, as memory is that no call has written.  (What a chunk said 2^30 - 1 calls ago would
+// pass for new, if no call since then had as many chunks and another one looks before it speaks.)
+constexpr uint32_t kWordCall = 0x3FFFFFFFu;
+__device__ inline uint32_t call_after(uint32_t call) { return (call + 1) & kWordCall ? call + 1 : call + 2; }
+
 // V elements at any address that an element may have
 template <class E, int V>
 __device__ inline Pack<E, V> load_pack(const E *p) {
@@ -163,7 +172,7 @@ __device__ inline void put_word(uint64_t *p, uint64_t v) { __hip_atomic_store(p,
 // this, the rows of the bag are gone through from its start.
 constexpr int kLooks = 16 * kPolls;  // a millisecond or so
 __device__ inline bool get_word(const uint64_t *p, uint64_t &w, uint32_t call) {  // w: what a first look found
-  for (int k = 0; (uint32_t)(w >> 34) != (call & 0x3FFFFFFFu); k++) {
+  for (int k = 0; (uint32_t)(w >> 34) != (call & kWordCall); k++) {
     if (k >= kLooks) return false;
     __builtin_amdgcn_s_sleep(1);
     w = look(p);
@@ -493,7 +502,7 @@ __global__ __launch_bounds__(apply_threads(V)) void scan_apply_kernel(Rows<DT> a
     }
   }
   const uint32_t call = a.call[0];
-  if (blockIdx.x == 0 && threadIdx.x == 0) a.call[1] = call + 1;  // nothing looks at that one in this kernel
+  if (blockIdx.x == 0 && threadIdx.x == 0) a.call[1] = call_after(call);  // nothing looks at that one in this kernel
   fetch_marks<T>(a, row0, call, marks);
   // The first start among the lane's rows: its state is asked for before the gates are computed.
   int first = R;
@@ -598,7 +607,7 @@ __global__ __launch_bounds__(grad_threads(V), 4) void scan_grad_kernel(Rows<DT> 
     }
   }
   const uint32_t call = a.call[0];
-  if (blockIdx.x == 0 && threadIdx.x == 0) a.call[1] = call + 1;  // nothing looks at that one in this kernel
+  if (blockIdx.x == 0 && threadIdx.x == 0) a.call[1] = call_after(call);  // nothing looks at that one in this kernel
   fetch_marks<T>(a, row0, call, marks);
   // The first start and the last end among the lane's rows: what belongs to them is asked for before the gates are computed.
   int first = R, last = -1;
@@ -885,7 +894,7 @@ int tbe_scan_create(tbe_scan_handle *out, int32_t dim, int32_t dtype, int32_t co
   }
   // one block: [err, call][marks][words][maps][states]
   const size_t mark_bytes = (size_t)max_rows * sizeof(ulonglong2), floats = (size_t)chunks * dim, zeros = 256 + mark_bytes + floats * 4 * sizeof(float);
-  const uint32_t first_call = 1;  // zeros are of no call
+  const uint32_t first_call = TBE_FIRST_CALL;  // zeros are of no call
   char *block = nullptr;
   hipError_t e = hipGetDevice(&s->device);
   if (e == hipSuccess) e = hipMalloc((void **)&block, zeros + floats * 3 * sizeof(float));
