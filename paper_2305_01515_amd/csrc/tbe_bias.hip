@@ -566,6 +566,11 @@ int check_shape(tbe_bias_t *s, const tbe_bias_shape *p, Shape *out) noexcept {
   return TBE_OK;
 }
 
+// whether two sets of strides name the same places (those of a single sample, head or query name none)
+bool same_places(const Shape &p, const tbe_bias_strides &a, const tbe_bias_strides &b) {
+  return (p.s.batch < 2 || a.sample == b.sample) && (p.heads < 2 || a.head == b.head) && (p.s.queries < 2 || a.query == b.query);
+}
+
 int64_t blocks_of(const Shape &p) { return (p.s.queries * p.packs + kThreads - 1) / kThreads * p.s.batch; }
 
 }  // namespace
@@ -630,6 +635,7 @@ int tbe_bias_forward(tbe_bias_handle s, const tbe_bias_shape *shape, const void 
   if (p.s.batch * p.s.queries * p.s.keys == 0) return TBE_OK;
   if (!d_table || !d_out || !out_strides || (d_scores && !scores_strides)) return report(TBE_EINVAL, "null table, output or strides");
   const tbe_bias_strides ss = d_scores ? *scores_strides : tbe_bias_strides{0, 0, 0};
+  if (d_out == d_scores && !same_places(p, ss, *out_strides)) return report(TBE_EINVAL, "in place with other strides");
   const int group = p.heads < kTableFloats / p.buckets ? p.heads : kTableFloats / p.buckets, groups = (p.heads + group - 1) / group;
   const int64_t blocks = blocks_of(p);
   const dim3 grid((unsigned)(blocks < kForward ? blocks : kForward), (unsigned)groups);
@@ -656,7 +662,8 @@ int tbe_bias_backward(tbe_bias_handle s, const tbe_bias_shape *shape, const void
   if (int rc = check_shape(s, shape, &p)) return rc;
   const bool any = p.s.batch * p.s.queries * p.s.keys != 0;
   if (any && (!d_dout || !dout_strides || (d_dscores && !dscores_strides))) return report(TBE_EINVAL, "null gradient or strides");
-  const tbe_bias_strides es = d_dscores ? *dscores_strides : tbe_bias_strides{0, 0, 0};
+  const tbe_bias_strides es = any && d_dscores ? *dscores_strides : tbe_bias_strides{0, 0, 0};
+  if (any && d_dscores == d_dout && !same_places(p, *dout_strides, es)) return report(TBE_EINVAL, "in place with other strides");
   int parts = 0;
   if (any) {
     if (!p.s.d_query_pos && !p.s.d_key_pos) {

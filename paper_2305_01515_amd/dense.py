@@ -308,6 +308,8 @@ class RelativeBias(_Handle):
         if out is None:
             out = torch.empty(shape[0], self.heads, shape[1], shape[2], dtype=dtype, device=self.device)
         op, os_ = self._scores("out", out, dtype, shape)
+        if given is not None and any(n > 1 and s == 0 for n, s in zip(given.shape, given.stride())):
+            raise ValueError("out: every score has a place of its own")
         self._check(_lib().tbe_bias_forward(self._h, C.byref(st), tp, DTYPES[table.dtype], sp, C.byref(ss) if ss else None, scale, mask_value, op,
                                             C.byref(os_), self._stream()), "tbe_bias_forward")
         if given is not None:
