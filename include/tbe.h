@@ -526,6 +526,8 @@ int64_t tbe_scan_saved_floats(tbe_scan_handle s, int64_t rows);
  * d_x, d_u: rows of dim elements, x_stride / u_stride apart; d_offsets[bags + 1] ascending from 0 to rows; d_h0: fp32
  * rows h0_stride apart (0: one row for all bags) or null.  Writes, each unless null: d_y (h of every row), d_last (fp32
  * [bags, dim], h after a bag's last row; that of an empty bag is where it starts), d_saved (for tbe_scan_backward).
+ * What a call of tbe_scan_* writes may not overlap what it reads (d_y on d_x or d_u is refused): a chunk of rows may have to go through those before it
+ * once more.
  */
 int tbe_scan_forward(tbe_scan_handle s, const void *d_x, int64_t x_stride, const void *d_u, int64_t u_stride,
                      const int64_t *d_offsets, int64_t bags, int64_t rows, const float *d_h0, int64_t h0_stride, void *d_y,

@@ -932,6 +932,7 @@ int tbe_scan_forward(tbe_scan_handle s, const void *d_x, int64_t x_stride, const
                      void *stream) {
   if (int rc = check_batch(s, d_x, x_stride, d_u, u_stride, d_offsets, bags, rows, d_h0, h0_stride)) return rc;
   if (d_y && y_stride < s->dim) return report(TBE_EINVAL, "a stride below dim");
+  if (rows > 0 && d_y && (d_y == d_x || d_y == d_u)) return report(TBE_EINVAL, "the output is one of the inputs");
   if (bags == 0) return TBE_OK;
   hipStream_t st = (hipStream_t)stream;
 #define ROWS(DT) rows_of<DT>(s, d_x, x_stride, d_u, u_stride, d_offsets, bags, rows, d_h0, h0_stride)
@@ -947,6 +948,8 @@ int tbe_scan_backward(tbe_scan_handle s, const void *d_x, int64_t x_stride, cons
   if (int rc = check_batch(s, d_x, x_stride, d_u, u_stride, d_offsets, bags, rows, d_h0, h0_stride)) return rc;
   if (rows > 0 && (!d_saved || !d_dx || !d_du)) return report(TBE_EINVAL, "null pointer for what the forward saved or for a gradient");
   if ((d_dy && dy_stride < s->dim) || dx_stride < s->dim || du_stride < s->dim) return report(TBE_EINVAL, "a stride below dim");
+  for (const void *in : {d_x, d_u, d_dy})
+    if (rows > 0 && in && (d_dx == in || d_du == in)) return report(TBE_EINVAL, "an output is one of the inputs");
   if (chunks_of(s, rows) * s->cut.tiles > most_groups(grad_threads(s->cut.V))) return report(TBE_ELIMIT, "more rows than one launch can take");
   if (bags == 0) return TBE_OK;
   hipStream_t st = (hipStream_t)stream;
