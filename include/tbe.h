@@ -510,6 +510,8 @@ int tbe_plan_placement(const tbe_place_table *tables, int32_t num_tables, const 
  * Gated linear recurrence over the rows of every bag.  With f = 1 / (1 + exp(-u)), element by element,
  *   h_t = f_t h_{t-1} + (1 - f_t) x_t   (coupled = 1)   or   h_t = f_t h_{t-1} + x_t   (coupled = 0)
  * for the rows t = offsets[b] .. offsets[b+1]-1 of bag b in turn, from h = d_h0[b] (null: zero).
+ * f and 1 - f are off by up to (|u| + 8) 2^-24 of themselves.  Bits are the same from call to call, but for the last ones where a workgroup
+ * has heard nothing of another one for a millisecond or so (work of other streams in between) and finds a state by itself, in another order.
  * dim: elements of a row, 1 .. 65536; max_bags, max_rows: what a call may bring at most (scratch memory: 16 bytes
  * for each of max_rows and 28 * dim for each chunk of them, which has 8192 elements, or somewhat fewer where dim is no power of two).  A call
  * takes some 2^36 elements, the gradient half as many where dim is no multiple of 4 (TBE_ELIMIT).
@@ -578,7 +580,8 @@ typedef struct {
   const int64_t *d_key_pos;      /* [batch, keys], samples key_pos_stride apart (0: one for all), or null */
   int64_t query_pos_stride, key_pos_stride;
   const int64_t *d_key_lengths;  /* [batch]: keys from this index on are masked, or null */
-  int32_t causal;                /* 1: keys at later positions than the query are masked */
+  int32_t causal;                /* 1: keys at later positions than the query are masked; not those at the same one, so
+                                  * of events with one time stamp each sees the others (to mask by order, put -infinity into d_scores: a scale above 0 leaves it) */
   int32_t dtype;                 /* of scores, output and gradient */
 } tbe_bias_shape;
 typedef struct {

@@ -295,7 +295,8 @@ class RelativeBias(_Handle):
 
     def forward(self, table, shape: Optional[Tuple[int, int, int]] = None, dtype: Optional[torch.dtype] = None, scores=None, scale: float = 1.0,
                 q_pos=None, k_pos=None, q_offset: int = 0, key_lengths=None, causal: bool = False, mask_value: float = -math.inf, out=None):
-        """scores * scale + bias, or the bias alone for shape = (batch, queries, keys); mask_value where masked"""
+        """scores * scale + bias, or the bias alone for shape = (batch, queries, keys); mask_value where masked.  causal masks keys at later
+        positions than the query's: not those of the same time stamp, whatever their order (-inf in the scores stays -inf)"""
         if scores is not None:
             shape, dtype = (scores.shape[0], scores.shape[2], scores.shape[3]), scores.dtype
         dtype = dtype or table.dtype
