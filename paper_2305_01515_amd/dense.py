@@ -404,9 +404,12 @@ class AdamW(_Handle):
         if p.dtype not in DTYPES or p.device != self.device or not p.is_contiguous():
             raise ValueError(f"parameters are contiguous, {', '.join(map(str, DTYPES))}, on {self.device}")
 
+    def _tensors(self):
+        return [*self.params, *map(self.states.__getitem__, self._kinds), *(w for w in self.master if w is not None)]
+
     def _places(self):
         """what the plan holds of parameters, copies and states, as it is now; the parameters' shapes first"""
-        t = [*self.params, *map(self.states.__getitem__, self._kinds), *(w for w in self.master if w is not None)]
+        t = self._tensors()
         return [*map(_shape, t)], [*map(_address, t)], [*map(_dtype, t)], [*map(_dense, t)], len(self.params), \
             [w is None for w in self.master] if len(t) > len(self.params) + len(self._kinds) else len(self.master)
 
@@ -427,6 +430,9 @@ class AdamW(_Handle):
                                      a["m"] + at * BLOCK * size, a["v"] + at * BLOCK * size, a["m_scale"] + 4 * at if scale else None,
                                      a["v_scale"] + 4 * at if scale else None, p.numel(), DTYPES[p.dtype], DTYPES[grad_dtypes[i]], self._decay[i])
             at += blocks
+        held = sorted((t.data_ptr(), t.numel() * t.element_size()) for t in self._tensors() if t.numel())
+        if any(a + n > b for (a, n), (b, _) in zip(held, held[1:])):
+            raise ValueError("parameters, copies and states that share memory (a weight that is tied to another one is given once)")
         h = C.c_void_p()
         self._check(_lib().tbe_adamw_create(C.byref(h), tensors, len(self.params), self.state_bits), "tbe_adamw_create")
         if self._h and self._captured:
