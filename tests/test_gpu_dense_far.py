@@ -137,7 +137,7 @@ def test_a_gradient_of_more_rows_than_a_launch_takes_is_refused():
     plan = dense.Scan(dim, torch.float16, 1, rows)
     off, t = torch.tensor([0, rows]).cuda(), torch.zeros(8).cuda()
     a = t.data_ptr()
-    args = (plan._h, a, dim, a, dim, off.data_ptr(), 1, rows, None, 0, a, a, dim, None, a, dim, a, dim, None, None)
+    args = (plan._h, a, dim, a, dim, off.data_ptr(), 1, rows, None, 0, a, a, dim, None, a + 8, dim, a + 16, dim, None, None)
     assert dense._lib().tbe_scan_backward(*args) == -5
     assert b"one launch" in dense._lib().tbe_last_error(None)
     torch.cuda.synchronize()
