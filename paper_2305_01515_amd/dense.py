@@ -14,6 +14,7 @@ from __future__ import annotations
 
 import ctypes as C
 import math
+import operator
 import warnings
 from typing import Dict, List, Optional, Sequence, Tuple, Union
 
@@ -46,7 +47,7 @@ class AdamWTensor(C.Structure):
 _ready = None  # the library object whose arguments have their types
 _current_raw_stream = torch._C._cuda_getCurrentRawStream
 # of a tensor, without the look for the attribute at each
-_shape, _dtype = torch.Tensor.shape.__get__, torch.Tensor.dtype.__get__
+_shape, _dtype, _numel = torch.Tensor.shape.__get__, torch.Tensor.dtype.__get__, torch.Tensor.numel
 _address, _dense, _gpu = torch.Tensor.data_ptr, torch.Tensor.is_contiguous, torch.Tensor.get_device
 _capturing = torch.cuda.is_current_stream_capturing
 
@@ -377,6 +378,7 @@ class AdamW(_Handle):
         self._decay, self._blocks, self._kinds = decay, blocks, kinds
         self._grads = (C.c_void_p * max(1, len(self.params)))()
         self._grads_at, self._gpus = C.addressof(self._grads), [self.device.index] * len(self.params)
+        self._nones = [None] * len(self.params)
         self._captured = False  # whether a step of this plan has been captured
         self._plan(list(grad_dtypes) if grad_dtypes is not None else [p.dtype for p in self.params])
 
@@ -405,13 +407,14 @@ class AdamW(_Handle):
             raise ValueError(f"parameters are contiguous, {', '.join(map(str, DTYPES))}, on {self.device}")
 
     def _tensors(self):
-        return [*self.params, *map(self.states.__getitem__, self._kinds), *(w for w in self.master if w is not None)]
+        """parameters, states and copies"""
+        t, missing = [*self.params, *map(self.states.__getitem__, self._kinds)], [*map(operator.is_, self.master, self._nones)]
+        return t + [w for w in self.master if w is not None] if False in missing else t, missing
 
     def _places(self):
-        """what the plan holds of parameters, copies and states, as it is now; the parameters' shapes first"""
-        t = self._tensors()
-        return [*map(_shape, t)], [*map(_address, t)], [*map(_dtype, t)], [*map(_dense, t)], len(self.params), \
-            [w is None for w in self.master] if len(t) > len(self.params) + len(self._kinds) else len(self.master)
+        """what the plan holds of them, as it is now"""
+        t, missing = self._tensors()
+        return [*map(_numel, t)], [*map(_address, t)], [*map(_dtype, t)], [*map(_dense, t)], missing, len(self.params), len(self.master)
 
     def _plan(self, grad_dtypes):
         """a handle for the parameters, copies and states as they are now"""
@@ -430,7 +433,7 @@ class AdamW(_Handle):
                                      a["m"] + at * BLOCK * size, a["v"] + at * BLOCK * size, a["m_scale"] + 4 * at if scale else None,
                                      a["v_scale"] + 4 * at if scale else None, p.numel(), DTYPES[p.dtype], DTYPES[grad_dtypes[i]], self._decay[i])
             at += blocks
-        held = sorted((t.data_ptr(), t.numel() * t.element_size()) for t in self._tensors() if t.numel())
+        held = sorted((t.data_ptr(), t.numel() * t.element_size()) for t in self._tensors()[0] if t.numel())
         if any(a + n > b for (a, n), (b, _) in zip(held, held[1:])):
             raise ValueError("parameters, copies and states that share memory (a weight that is tied to another one is given once)")
         h = C.c_void_p()
@@ -440,7 +443,7 @@ class AdamW(_Handle):
         elif self._h:
             _lib().tbe_adamw_destroy(self._h)
         self._h, self._captured, self._enqueue = h, False, _lib().tbe_adamw_step_counted if self.capturable else _lib().tbe_adamw_step
-        self._planned, self._grad_dtypes = self._places(), grad_dtypes
+        self._planned, self._shapes, self._grad_dtypes = self._places(), [*map(_shape, self.params)], grad_dtypes
 
     def step(self, grads: Optional[Sequence[Optional[torch.Tensor]]] = None, lr: Optional[float] = None, grad_scale: Optional[torch.Tensor] = None):
         """grads: one for each parameter (None: its parameter stays as it is); without, the parameters' own `.grad`.
@@ -450,16 +453,15 @@ class AdamW(_Handle):
             raise ValueError("grads: one for each parameter")
         # Parameters, copies and states may have another storage than at the last step (moved to the host and back, loaded, assigned).
         places, ptrs, stream = self._places(), self._grads, self._stream()
-        shapes = places[0][:len(self.params)]
         try:
-            fine = [*map(_shape, grads)] == shapes and [*map(_dtype, grads)] == self._grad_dtypes and all(map(_dense, grads)) and \
+            fine = [*map(_shape, grads)] == self._shapes and [*map(_dtype, grads)] == self._grad_dtypes and all(map(_dense, grads)) and \
                 [*map(_gpu, grads)] == self._gpus
         except TypeError:  # a parameter without a gradient
             fine = False
         if not fine:
-            for i, (g, shape) in enumerate(zip(grads, shapes)):
-                if g is not None and (g.shape != shape or g.device != self.device or not g.is_contiguous() or g.dtype not in DTYPES):
-                    raise ValueError(f"gradient {i}: contiguous, of the parameter's shape {tuple(shape)}, on {self.device}")
+            for i, (g, p) in enumerate(zip(grads, self.params)):
+                if g is not None and (g.shape != p.shape or g.device != self.device or not g.is_contiguous() or g.dtype not in DTYPES):
+                    raise ValueError(f"gradient {i}: contiguous, of the parameter's shape {tuple(p.shape)}, on {self.device}")
             dtypes = [d if g is None else g.dtype for g, d in zip(grads, self._grad_dtypes)]
         if places != self._planned or not fine and dtypes != self._grad_dtypes:
             self._plan(self._grad_dtypes if fine else dtypes)
