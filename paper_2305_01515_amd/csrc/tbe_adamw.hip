@@ -1,7 +1,7 @@
 // AdamW over many tensors in one launch, states in 32 or 8 bits.  Contract: include/tbe.h.
 //
 // Bound by memory: 28 bytes an element with fp32 everywhere, 16 with states in 8 bits (fp32 weights and gradients, or 16-bit ones with an
-// fp32 copy).  172 M weights: 879 us (5.5 TB/s) and 521 us (5.3 TB/s).  A wavefront has a block of TBE_ADAMW_BLOCK elements, 4 side by
+// fp32 copy).  172 M weights: 880 us (5.5 TB/s) and 503 to 532 us by card (5.2 to 5.5 TB/s).  A wavefront has a block of TBE_ADAMW_BLOCK elements, 4 side by
 // side a lane, so that the largest of a block is an exchange between lanes and every load is 4 elements of its type.  (Two blocks a
 // wavefront took 4 % longer with fp32 states, 1.5 % in 8 bits.)  The types are the tensor's: one kernel has a body for
 // each combination and takes the one that its workgroup's tensor asks for.
