@@ -640,6 +640,119 @@ int tbe_adamw_step(tbe_adamw_handle s, const void *const *h_grads, int64_t step,
 int tbe_adamw_step_counted(tbe_adamw_handle s, const void *const *h_grads, int64_t *d_step, double lr, double beta1,
                            double beta2, double eps, uint32_t seed, const float *d_grad_scale, void *stream);
 
+/*
+ * Root-mean-square norm of rows, with the addition of a residual in front of it.  s = x + residual, rounded to the residual's type and stored
+ * (without a residual s = x, and nothing is stored);  out = s rstd weight,  rstd = 1 / sqrt(mean(s s) + eps), of the stored s.
+ * dim: 1 .. 32768.  dtype: of x and out; residual_dtype: dtype or TBE_FP32, -1 for a handle that has none.  max_rows: rows of a call
+ * at most.  d_summed may be d_residual, or d_x where they have one type, with the same strides; d_out may be neither of the inputs.
+ */
+typedef struct tbe_norm_t *tbe_norm_handle;
+int tbe_norm_create(tbe_norm_handle *out, int32_t dim, int32_t dtype, int32_t residual_dtype, double eps, int64_t max_rows);
+int tbe_norm_destroy(tbe_norm_handle s);
+typedef struct {
+  const void *d_x, *d_residual, *d_weight; /* d_residual: null, or rows of the residual's type; d_weight: dim numbers of weight_dtype */
+  int64_t x_stride, residual_stride, rows;
+  void *d_summed;                          /* with a residual */
+  int64_t summed_stride;
+  int32_t weight_dtype;
+} tbe_norm_batch;
+/* d_rstd: fp32 [rows] for the backward, or null. */
+int tbe_norm_forward(tbe_norm_handle s, const tbe_norm_batch *batch, void *d_out, int64_t out_stride, float *d_rstd, void *stream);
+/* The same with results in 8 bits (E4M3, round to nearest even) times a scale, the largest magnitude / 448, for each row (group 0) or each
+ * `group` elements of it (a power of two from 16 to 256; the last group of a row may be short): d_scales fp32 [rows, groups of a row].  A group
+ * whose largest is zero has zeros; one that holds an infinity or a NaN reads back as NaN. */
+int tbe_norm_quantise(tbe_norm_handle s, const tbe_norm_batch *batch, int32_t group, void *d_codes, int64_t codes_stride, float *d_scales,
+                      void *stream);
+/* With d = dout weight:  ds = rstd (d - s rstd mean(d s rstd)) + dsummed,  written to d_dx (of dtype) and d_dresidual (of the residual's
+ * type), each unless null;  d_dweight (fp32 [dim], or null) = the sum over rows of dout s rstd, the same bits for the same inputs. */
+typedef struct {
+  const void *d_summed, *d_dout, *d_dsummed, *d_weight; /* d_summed: the stored s (x without a residual); d_dsummed: null = zero */
+  int64_t summed_stride, dout_stride, dsummed_stride, rows;
+  const float *d_rstd;
+  void *d_dx, *d_dresidual;
+  int64_t dx_stride, dresidual_stride;
+  float *d_dweight;
+  int32_t weight_dtype, residual;                       /* residual: 1 if the forward added one */
+} tbe_norm_grad;
+int tbe_norm_backward(tbe_norm_handle s, const tbe_norm_grad *gradients, void *stream);
+
+/*
+ * Short causal convolution over the rows of every bag, element by element:  with e = the bag's `width` - 1 earlier rows (d_before; null: zero)
+ * and behind them its rows,
+ *   v_t = bias + sum over j < width of weight[j] e_{t+j},   y_t = v_t, or v_t / (1 + exp(-v_t)) with silu.
+ * dim: 1 .. 65536; width: 1 .. 8; dtype: of rows, earlier rows and results; weights (d_weight [dim, width], d_bias [dim] or null) are of
+ * weight_dtype.  max_bags, max_rows: what a call may bring at most.  What a call writes may not overlap what it reads.
+ */
+typedef struct tbe_conv_t *tbe_conv_handle;
+int tbe_conv_create(tbe_conv_handle *out, int32_t dim, int32_t width, int32_t dtype, int32_t silu, int64_t max_bags, int64_t max_rows);
+int tbe_conv_destroy(tbe_conv_handle s);
+typedef struct {
+  const void *d_x;          /* rows of dim elements, x_stride apart */
+  int64_t x_stride;
+  const int64_t *d_offsets; /* [bags + 1], ascending from 0 to rows */
+  int64_t bags, rows;
+  const void *d_weight, *d_bias;
+  const void *d_before;     /* [bags, width - 1, dim], contiguous, or null */
+  int32_t weight_dtype;
+} tbe_conv_batch;
+/* d_last (or null): [bags, width - 1, dim], the last rows of e: what d_before of the bag's continuation, and the state of tbe_conv_step, is. */
+int tbe_conv_forward(tbe_conv_handle s, const tbe_conv_batch *batch, void *d_y, int64_t y_stride, void *d_last, void *stream);
+/* d_dy, d_dlast (null = zero) to d_dx and, each unless null, d_dweight (fp32 [dim, width]), d_dbias (fp32 [dim]), d_dbefore
+ * ([bags, width - 1, dim] of dtype).  The same inputs give the same bits. */
+int tbe_conv_backward(tbe_conv_handle s, const tbe_conv_batch *batch, const void *d_dy, int64_t dy_stride, const void *d_dlast, void *d_dx,
+                      int64_t dx_stride, float *d_dweight, float *d_dbias, void *d_dbefore, void *stream);
+/* One more row for `rows` of the `slots` states d_state [slots, width - 1, dim] of dtype, in place.  d_slots null: row i belongs to state i.
+ * A negative slot leaves its row out (y = 0).  A slot twice in one call: undefined.  Of the batch: d_x, x_stride, rows, the weights. */
+int tbe_conv_step(tbe_conv_handle s, const tbe_conv_batch *batch, void *d_state, int64_t slots, const int64_t *d_slots, void *d_y,
+                  int64_t y_stride, void *stream);
+/* as tbe_scan_check */
+int tbe_conv_check(tbe_conv_handle s, void *stream);
+
+/*
+ * Selective scan over the rows of every bag.  An element d of a row has `states` states; with D_t = log(1 + exp(delta_t + delta_bias)),
+ *   h_t[n] = exp(D_t a[n]) h_{t-1}[n] + D_t b_t[n] x_t,   y_t = sum over n of c_t[n] h_t[n] + skip x_t,
+ * times z_t / (1 + exp(-z_t)) where d_z is given; h = d_h0[bag] (null: zero) before a bag's first row.  b_t and c_t are a row's own and shared by the
+ * dim / groups elements of a group.
+ * dim: 1 .. 65536; states: 1 .. 64; groups: 1, or such that dim / groups is a multiple of 64; dtype: of x, delta, z, b, c, y and their gradients.
+ * max_bags, max_rows: what a call may bring at most.  What a call writes may not overlap what it reads.
+ * The decays are found as powers of two of D_t (a log2(e)), so they are off by up to (|D_t a| + 8) 2^-23 of themselves; a decay's product
+ * over many rows is found from the sum of their D.  A decay below 2^-126 is zero.
+ */
+typedef struct tbe_ssm_t *tbe_ssm_handle;
+int tbe_ssm_create(tbe_ssm_handle *out, int32_t dim, int32_t states, int32_t groups, int32_t dtype, int64_t max_bags, int64_t max_rows);
+int tbe_ssm_destroy(tbe_ssm_handle s);
+typedef struct {
+  const void *d_x, *d_delta, *d_z;  /* rows of dim elements; d_z may be null */
+  const void *d_b, *d_c;            /* rows of groups * states numbers */
+  int64_t x_stride, delta_stride, z_stride, b_stride, c_stride;
+  const float *d_a;                 /* [dim, states] */
+  const float *d_skip, *d_delta_bias; /* [dim], or null */
+  const int64_t *d_offsets;         /* [bags + 1], ascending from 0 to rows */
+  int64_t bags, rows;
+  const float *d_h0;                /* [dim, states] of each bag, h0_stride apart (0: one for all), or null */
+  int64_t h0_stride;
+} tbe_ssm_batch;
+/* fp32 numbers that tbe_ssm_forward leaves in d_saved for the backward of `rows` rows: the states before every 16th row */
+int64_t tbe_ssm_saved_floats(tbe_ssm_handle s, int64_t rows);
+/* Writes d_y and, each unless null, d_last (fp32 [bags, dim, states], h after a bag's last row) and d_saved. */
+int tbe_ssm_forward(tbe_ssm_handle s, const tbe_ssm_batch *batch, void *d_y, int64_t y_stride, float *d_last, float *d_saved, void *stream);
+/* Gradients, of the rows (of dtype) and of what they share (fp32).  d_dz: with d_z only; d_dskip, d_ddelta_bias, d_dh0 (fp32 [bags, dim, states]):
+ * unless null.  The same inputs give the same bits. */
+typedef struct {
+  const void *d_dy;
+  int64_t dy_stride;
+  const float *d_dlast;             /* null = zero */
+  void *d_dx, *d_ddelta, *d_dz, *d_db, *d_dc; /* contiguous rows */
+  float *d_da, *d_dskip, *d_ddelta_bias, *d_dh0;
+} tbe_ssm_grads;
+int tbe_ssm_backward(tbe_ssm_handle s, const tbe_ssm_batch *batch, const float *d_saved, const tbe_ssm_grads *gradients, void *stream);
+/* One more row for `rows` of the `slots` states d_state (fp32 [dim, states] each, state_stride apart), in place; slots as in tbe_conv_step.
+ * Of the batch: everything but offsets, bags and h0. */
+int tbe_ssm_step(tbe_ssm_handle s, const tbe_ssm_batch *batch, float *d_state, int64_t state_stride, int64_t slots, const int64_t *d_slots, void *d_y,
+                 int64_t y_stride, void *stream);
+/* as tbe_scan_check */
+int tbe_ssm_check(tbe_ssm_handle s, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -28,7 +28,7 @@ CSRC = os.path.join(HERE, "csrc")
 OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libtbe.so")
 SOURCES = ["tbe_api.hip", "tbe_sort.hip", "tbe_cache.hip", "tbe_one.hip", "tbe_move.hip", "tbe_embed.hip", "tbe_place.hip",
-           "tbe_scan.hip", "tbe_bias.hip", "tbe_adamw.hip"]
+           "tbe_scan.hip", "tbe_bias.hip", "tbe_adamw.hip", "tbe_norm.hip", "tbe_conv.hip", "tbe_ssm.hip"]
 FLAGS = ["-O3", "-std=c++17", "--offload-arch=gfx950", "-fPIC",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops", "-Wall", "-Wno-unused-function"]
 FIRST_CALL = {0: 0x3FFFFFFD, 1: 0xFFFFFFFD}  # of a scan's handle in those builds: its calls' numbers pass 2^30 and 2^32 soon

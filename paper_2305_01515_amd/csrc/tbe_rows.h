@@ -1,0 +1,102 @@
+// Shared by the operators on rows (norm, short convolution, selective scan): packs at any address, parameters of any type, small
+// functions, sums of partial results.
+#pragma once
+#include "tbe_dense.h"
+
+namespace tbe {
+
+// V elements (the first `n` of them, if fewer) at any address that an element may have, as fp32; what is beyond n reads as zero
+template <class E, int V>
+__device__ inline void load_floats(const E *p, int n, float (&to)[V]) {
+  if (n >= V) {
+    Pack<E, V> r;
+    __builtin_memcpy(&r, p, sizeof r);
+#pragma unroll
+    for (int i = 0; i < V; ++i) to[i] = (float)r.e[i];
+  } else {
+#pragma unroll
+    for (int i = 0; i < V; ++i) to[i] = i < n ? (float)p[i] : 0.0f;
+  }
+}
+template <class E, int V>
+__device__ inline void store_floats(E *p, int n, const float (&from)[V]) {
+  if (n >= V) {
+    Pack<E, V> r;
+#pragma unroll
+    for (int i = 0; i < V; ++i) r.e[i] = (E)from[i];
+    __builtin_memcpy(p, &r, sizeof r);
+  } else {
+#pragma unroll
+    for (int i = 0; i < V; ++i)
+      if (i < n) p[i] = (E)from[i];
+  }
+}
+
+// parameters of a type that is known at run time only
+__device__ inline float load_param(const void *p, int dtype, int64_t i) {
+  return dtype == TBE_FP32 ? ((const float *)p)[i] : dtype == TBE_FP16 ? (float)((const _Float16 *)p)[i] : (float)((const __bf16 *)p)[i];
+}
+template <int V>
+__device__ inline void load_params(const void *p, int dtype, int64_t at, int n, float (&to)[V]) {
+  if (dtype == TBE_FP32) load_floats<float, V>((const float *)p + at, n, to);
+  else if (dtype == TBE_FP16) load_floats<_Float16, V>((const _Float16 *)p + at, n, to);
+  else load_floats<__bf16, V>((const __bf16 *)p + at, n, to);
+}
+
+constexpr float kLog2e = 1.44269504f, kLn2 = 0.693147181f;
+
+// The exponential is the hardware's power of two of the rounded v log2(e), so a sigmoid is off by up to (|v| + 8) 2^-24 of itself.
+__device__ inline float sigmoid(float v) {
+  const float e = __builtin_amdgcn_exp2f(fabsf(v) * -kLog2e), r = __builtin_amdgcn_rcpf(1.0f + e);
+  return v >= 0.0f ? r : e * r;
+}
+
+// Sums over the parts of [parts][n] fp32 numbers, in a fixed order: 32 columns a workgroup, 32 lanes a column with every 32nd part each.
+// A row of `width` columns has `cut` columns that go to `to`, one that goes to `next`, one that goes to `other` (each unless null).
+constexpr int kSumColumns = 32;
+__global__ __launch_bounds__(1024) static void sum_parts_kernel(const float *parts, int64_t count, int64_t n, int width, int cut, float *to, float *next,
+                                                                float *other) {
+  __shared__ float lds[32][kSumColumns + 1];
+  const int c = threadIdx.x % kSumColumns, s = threadIdx.x / kSumColumns;
+  const int64_t at = (int64_t)blockIdx.x * kSumColumns + c;
+  float v = 0.0f;
+  if (at < n) {
+#pragma unroll 8
+    for (int64_t p = s; p < count; p += 32) v += parts[p * n + at];
+  }
+  lds[s][c] = v;
+  for (int half = 16; half >= 1; half /= 2) {
+    __syncthreads();
+    if (s < half) lds[s][c] += lds[s + half][c];
+  }
+  if (s == 0 && at < n) {
+    const int64_t r = at / width;
+    const int k = (int)(at % width);
+    float *p = k < cut ? to + r * cut + k : k == cut ? next : other;
+    if (k >= cut && p) p += r;
+    if (p) *p = lds[0][c];
+  }
+}
+
+inline int64_t divide_up(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+inline void sum_parts(const float *parts, int64_t count, int64_t n, int width, int cut, float *to, float *next, float *other, hipStream_t st) {
+  sum_parts_kernel<<<dim3((unsigned)divide_up(n, kSumColumns)), dim3(1024), 0, st>>>(parts, count, n, width, cut, to, next, other);
+}
+
+// waits for the stream; what its kernels have reported in *d_err since the last look, which is cleared
+inline int check_errors(int32_t *d_err, hipStream_t st) {
+  int32_t err = 0;
+  hipError_t e = hipMemcpyAsync(&err, d_err, sizeof err, hipMemcpyDeviceToHost, st);
+  if (e == hipSuccess) e = hipStreamSynchronize(st);
+  if (e == hipSuccess && err) {
+    e = hipMemsetAsync(d_err, 0, sizeof err, st);
+    if (e == hipSuccess) e = hipStreamSynchronize(st);
+  }
+  if (e != hipSuccess) return report_hip(e);
+  if (err == 1) return report(TBE_EINVAL, "offsets that do not ascend from 0 to the number of rows");
+  if (err == 2) return report(TBE_ERANGE, "a slot is not below the number of states");
+  return TBE_OK;
+}
+
+}  // namespace tbe

@@ -1,0 +1,938 @@
+// Selective scan over the rows of every bag: forward, backward, one row for each of many states.
+// Contract: include/tbe.h.
+//
+//   D_t = log(1 + exp(delta_t + bias)),  h_t[n] = exp(D_t a[n]) h_{t-1}[n] + D_t b_t[n] x_t,  y_t = (sum_n c_t[n] h_t[n] + skip x_t) silu(z_t).
+//   Backward, with dv = dy silu(z):  g_t = c_t dv_t + exp(D_{t+1} a) g_{t+1} (a bag's last row: + dlast),  w_t = exp(D_t a) h_{t-1},
+//   dx = skip dv + D sum_n g b,  dD = sum_n g w a + x sum_n g b,  da = sum_t g w D,  db = sum over elements of g D x,  dc = sum of dv h.
+//
+// Bound by vector instructions: an element and a state take an exponential (as long as four others) and four more, 16 states 128 of them,
+// for 8 to 14 bytes of rows in 16 bits.  So the rows are gone through once where that can be, and no lane idles:
+//   units    The rows are cut every `unit` rows.  A bag of up to two units is not cut: the unit it starts in goes on to its end.
+//   ends     Units whose end cuts a bag find the state there from a zero one (or the bag's start), and the sum of the D: the
+//            product of the decays is the exponential of a times that                          (ssm_ends_kernel, ssm_grad_ends_kernel)
+//   join     states at the cuts, by a scan over the units in segments and one over the segments (ssm_join_kernel, ssm_segments_kernel)
+//   rows     every unit from the state before it                                                (ssm_kernel, ssm_grad_kernel)
+// Where no bag is longer than two units, `ends` and `join` find nothing to do.
+// Forward: a lane has an element with all of its states in registers, b and c come from LDS.  Backward: a lane has four states of an
+// element, so that 16 rows' w and decays stay in registers on the way back; states before every 16th row were saved by the forward.
+#include <algorithm>
+#include <new>
+
+#include "tbe_rows.h"
+
+using namespace tbe;
+
+namespace {
+
+constexpr int kBlock = 16;       // rows that are staged at once; states before each block are what the backward goes from
+constexpr int kSegment = 64;     // units that a lane of `join` goes through
+constexpr int kMostStates = 64;
+constexpr int kThreads = 256;
+constexpr int kGradWorkers = 1024;  // workgroups of the backward, together
+constexpr int kGradWaves = 8;       // wavefronts of one, at most
+
+struct Unit {
+  int64_t begin;  // first row
+  int32_t bag;    // that its first row by count belongs to
+  int32_t cut;    // 1: begins within a bag
+};
+
+struct SsmArgs {
+  const void *x, *delta, *z, *b, *c, *dy;
+  int64_t xs, ts, zs, bs, cs, dys;
+  const float *a, *skip, *bias, *h0, *dlast;
+  const int64_t *off;
+  int64_t bags, rows, h0s;
+  int dim, states, groups;
+  void *y, *dx, *ddelta, *dz, *db, *dc;
+  int64_t ys;
+  float *last, *saved, *dh0;
+  // scratch
+  Unit *units;
+  int2 *marks;      // [rows]: the bag that starts at a row, the bag whose last row it is; what the offsets do not confirm is of another call
+  float *ends;      // [units][dim][NP]: states at the ends; `join` puts what is before (behind) each unit in their place
+  float *spans;     // [units][dim]: sums of D
+  float *reach;     // [units][dim]: sum of D from the segment's start; negative: nothing of it gets here
+  float *seg_state; // [segments][dim][NP]
+  float *seg_reach; // [segments][dim]
+  float *seg_start; // [segments][dim][NP]
+  float *parts, *shared;
+  int32_t *err;
+  int64_t count;    // units
+  int unit;         // rows of one
+  int waves;        // of 64 elements that a row has
+  int64_t workers;
+  int blocks;       // workgroups that a row has in the backward
+};
+
+// how many of the ascending offsets[0 .. n) are at most `row`, the same in all lanes of a wavefront: 64 places are looked at at once
+__device__ inline int64_t count_up_to(const int64_t *off, int64_t n, int64_t row) {
+  int64_t lo = 0, hi = n;  // off[i] <= row for i < lo, not for i >= hi
+  while (lo < hi) {
+    const int64_t step = (hi - lo + 63) / 64, at = lo + (int64_t)(threadIdx.x & 63) * step;
+    const int c = __popcll(__ballot(at < hi && off[at] <= row));  // the first c places are
+    if (c == 0) return lo;
+    lo += (int64_t)(c - 1) * step + 1;
+    hi = min(hi, lo + step - 1);
+  }
+  return lo;
+}
+
+// Marks of the bags' first and last rows, what empty bags have, the units; offsets that do not ascend from 0 to rows are reported.
+// empty_to (or null): [bags, dim, states] that an empty bag has of empty_from (null: zero).
+__global__ __launch_bounds__(kThreads) void ssm_prepare_kernel(SsmArgs a, int64_t bag_groups, float *empty_to, const float *empty_from, int64_t empty_stride) {
+  const int lane = threadIdx.x & 63;
+  if (blockIdx.x < bag_groups) {
+    const int64_t b = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+    bool empty = false;
+    if (b < a.bags) {
+      const int64_t s = a.off[b], e = a.off[b + 1];
+      if (s > e || s < 0 || e > a.rows || (b == 0 && s != 0) || (b == a.bags - 1 && e != a.rows)) {
+        *a.err = 1;
+      } else if (s == e) {
+        empty = true;
+      } else {
+        a.marks[s].x = (int)b;
+        a.marks[e - 1].y = (int)b;
+      }
+    }
+    if (!empty_to) return;
+    const int64_t n = (int64_t)a.dim * a.states;
+    for (uint64_t m = __ballot(empty); m; m &= m - 1) {
+      const int64_t of = b - lane + __builtin_ctzll(m);
+      for (int64_t i = lane; i < n; i += 64) empty_to[of * n + i] = empty_from ? empty_from[of * empty_stride + i] : 0.0f;
+    }
+    return;
+  }
+  const int64_t k = ((int64_t)blockIdx.x - bag_groups) * (kThreads / 64) + threadIdx.x / 64;
+  if (k > a.count) return;
+  const int64_t r = k * a.unit;
+  Unit u{a.rows, 0, 0};
+  if (r < a.rows) {
+    const int64_t b = max(count_up_to(a.off, a.bags, r) - 1, (int64_t)0), s = a.off[b], e = a.off[b + 1];
+    u.bag = (int)b;
+    u.cut = s != r && e - s > 2 * a.unit;
+    // (offsets that do not ascend: the unit still begins within its own rows and those of the next two)
+    u.begin = s == r || u.cut ? r : min(max(e, r), min(r + 2 * a.unit, a.rows));
+  }
+  if (lane == 0) a.units[k] = u;
+}
+
+// D = log(1 + exp(u)): with e = exp(-|u|) and w = 1 + e rounded, log(1 + e) is log(w) and what the rounding left out
+__device__ inline float soft(float u) {
+  const float e = __builtin_amdgcn_exp2f(fabsf(u) * -kLog2e), w = 1.0f + e;
+  return fmaxf(u, 0.0f) + (__builtin_amdgcn_logf(w) * kLn2 + (e - (w - 1.0f)));
+}
+// a decay's product with a state that may be zero beside an infinite one
+__device__ inline float carried(float a2, float span, float h) { return h == 0.0f ? 0.0f : __builtin_amdgcn_exp2f(a2 * span) * h; }
+
+// State n of element d before unit k, as `join` left it
+template <int NP>
+__device__ inline float start_of(const SsmArgs &a, int64_t k, int d, int n, float a2) {
+  const float r = a.reach[k * a.dim + d], h = a.ends[(k * a.dim + d) * NP + n];
+  return r < 0.0f ? h : h + carried(a2, r, a.seg_start[(k / kSegment * a.dim + d) * NP + n]);
+}
+
+// b and c (or only one) of the rows row0 + [lo, hi) to LDS, zero beyond the states: to[row][n], to[row][NP + n]
+template <class E, int NP, int THREADS>
+__device__ inline void stage(const SsmArgs &a, int64_t row0, int lo, int hi, int group, float (*to)[2 * NP], bool with_b, bool with_c) {
+  for (int k = threadIdx.x; k < kBlock * 2 * NP; k += THREADS) {
+    const int t = k / (2 * NP), n = k % (2 * NP), s = n % NP;
+    const bool of_b = n < NP, in = t >= lo && t < hi && s < a.states && (of_b ? with_b : with_c);
+    const int64_t r = row0 + t;
+    const int at = group * a.states + s;
+    to[t][n] = in ? (float)(of_b ? ((const E *)a.b)[r * a.bs + at] : ((const E *)a.c)[r * a.cs + at]) : 0.0f;
+  }
+}
+
+// the bags that start and end in the rows row0 + [lo, hi), as masks of rows; `bag` of lane t: that of row t
+struct Marks {
+  uint32_t starts, ends;
+  int2 bag;
+};
+__device__ inline Marks marks_of(const SsmArgs &a, int64_t row0, int lo, int hi) {
+  const int t = threadIdx.x & 63;
+  const int64_t r = row0 + t;
+  int2 m = {-1, -1};
+  if (t >= lo && t < hi) m = a.marks[r];
+  const bool starts = m.x >= 0 && m.x < a.bags && a.off[m.x] == r && a.off[m.x + 1] > r;
+  const bool ends = m.y >= 0 && m.y < a.bags && a.off[m.y + 1] == r + 1 && a.off[m.y] <= r;
+  return {(uint32_t)__ballot(starts), (uint32_t)__ballot(ends), m};
+}
+
+// What a lane's element has of a row, read ahead
+template <class E>
+struct Raw {
+  E x, u, z;
+};
+
+template <class E, int NP, bool FULL>
+__global__ __launch_bounds__(64) void ssm_kernel(SsmArgs a) {
+  __shared__ float bc[kBlock][2 * NP];
+  const int64_t k = blockIdx.x / a.waves;
+  const int wave = (int)(blockIdx.x % a.waves), lane = threadIdx.x;
+  const Unit u = a.units[k];
+  const int64_t begin = u.begin, end = a.units[k + 1].begin;
+  if (begin >= end) return;
+  const int d = wave * 64 + lane, dc = min(d, a.dim - 1);
+  const bool in = d < a.dim;
+  const int group = a.groups > 1 ? wave * 64 / (a.dim / a.groups) : 0, N = a.states;
+  float h[NP], a2[NP];
+#pragma unroll
+  for (int n = 0; n < NP; ++n) {
+    a2[n] = FULL || n < N ? a.a[(int64_t)dc * N + n] * kLog2e : 0.0f;
+    h[n] = u.cut && (FULL || n < N) ? start_of<NP>(a, k, dc, n, a2[n]) : 0.0f;
+  }
+  const float bias = a.bias ? a.bias[dc] : 0.0f, skip = a.skip ? a.skip[dc] : 0.0f;
+  const E *x = (const E *)a.x + dc, *delta = (const E *)a.delta + dc, *z = a.z ? (const E *)a.z + dc : nullptr;
+  E *y = (E *)a.y + d;
+  Raw<E> ahead[4];
+  auto read = [&](int64_t r0) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int64_t r = min(max(r0 + i, begin), end - 1);
+      ahead[i].x = x[r * a.xs];
+      ahead[i].u = delta[r * a.ts];
+      if (z) ahead[i].z = z[r * a.zs];
+    }
+  };
+  read(begin & ~3ll);
+  for (int64_t row0 = begin & ~(int64_t)(kBlock - 1); row0 < end; row0 += kBlock) {
+    const int lo = (int)max(begin - row0, (int64_t)0), hi = (int)min(end - row0, (int64_t)kBlock);
+    __syncthreads();
+    stage<E, NP, 64>(a, row0, lo, hi, group, bc, true, true);
+    const Marks m = marks_of(a, row0, lo, hi);
+    __syncthreads();
+    if (a.saved && lo == 0 && in) {
+      float *to = a.saved + (row0 / kBlock * a.dim + d) * NP;
+#pragma unroll
+      for (int n = 0; n < NP; n += 4) *(float4 *)(to + n) = make_float4(h[n], h[n + 1], h[n + 2], h[n + 3]);
+    }
+    for (int t0 = lo & ~3; t0 < hi; t0 += 4) {
+      Raw<E> now[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) now[i] = ahead[i];
+      read(row0 + t0 + 4);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int t = t0 + i;
+        if (t < lo || t >= hi) continue;
+        if (m.starts >> t & 1) {
+          const int64_t bag = __builtin_amdgcn_readlane(m.bag.x, t);
+#pragma unroll
+          for (int n = 0; n < NP; ++n) h[n] = a.h0 && (FULL || n < N) ? a.h0[bag * a.h0s + (int64_t)dc * N + n] : 0.0f;
+        }
+        const float xv = (float)now[i].x, step = soft((float)now[i].u + bias), sx = step * xv;
+        float v = skip * xv;
+#pragma unroll
+        for (int n = 0; n < NP; ++n) {
+          const float g = __builtin_amdgcn_exp2f(step * a2[n]) * h[n] + sx * bc[t][n];
+          h[n] = FULL || n < N ? g : 0.0f;
+          v += bc[t][NP + n] * h[n];
+        }
+        if (z) {
+          const float zv = (float)now[i].z;
+          v *= zv * sigmoid(zv);
+        }
+        if (in) y[(row0 + t) * a.ys] = (E)v;
+        if ((m.ends >> t & 1) && a.last && in) {
+          const int64_t bag = __builtin_amdgcn_readlane(m.bag.y, t);
+          float *to = a.last + (bag * a.dim + d) * N;
+#pragma unroll
+          for (int n = 0; n < NP; ++n)
+            if (FULL || n < N) to[n] = h[n];
+        }
+      }
+    }
+  }
+}
+
+// The state at the end of a unit that the next one goes on from within a bag, from zero (the bag began before) or from the bag's start
+template <class E, int NP>
+__global__ __launch_bounds__(64) void ssm_ends_kernel(SsmArgs a) {
+  __shared__ float bc[kBlock][2 * NP];
+  const int64_t k = blockIdx.x / a.waves;
+  const Unit u = a.units[k], next = a.units[k + 1];
+  if (!next.cut) return;
+  const int wave = (int)(blockIdx.x % a.waves), lane = threadIdx.x, N = a.states;
+  const int64_t start = a.off[next.bag], begin = max(u.begin, start), end = next.begin;
+  const bool whole = u.cut && u.bag == next.bag;
+  const int d = wave * 64 + lane, dc = min(d, a.dim - 1), group = a.groups > 1 ? wave * 64 / (a.dim / a.groups) : 0;
+  float h[NP], a2[NP], span = 0.0f;
+#pragma unroll
+  for (int n = 0; n < NP; ++n) {
+    a2[n] = n < N ? a.a[(int64_t)dc * N + n] * kLog2e : 0.0f;
+    h[n] = !whole && a.h0 && n < N ? a.h0[next.bag * a.h0s + (int64_t)dc * N + n] : 0.0f;
+  }
+  const float bias = a.bias ? a.bias[dc] : 0.0f;
+  const E *x = (const E *)a.x + dc, *delta = (const E *)a.delta + dc;
+  for (int64_t row0 = begin & ~(int64_t)(kBlock - 1); row0 < end; row0 += kBlock) {
+    const int lo = (int)max(begin - row0, (int64_t)0), hi = (int)min(end - row0, (int64_t)kBlock);
+    __syncthreads();
+    stage<E, NP, 64>(a, row0, lo, hi, group, bc, true, false);
+    __syncthreads();
+#pragma unroll 4
+    for (int t = lo; t < hi; ++t) {
+      const float step = soft((float)delta[(row0 + t) * a.ts] + bias), sx = step * (float)x[(row0 + t) * a.xs];
+      span += step;
+#pragma unroll
+      for (int n = 0; n < NP; ++n) h[n] = __builtin_amdgcn_exp2f(step * a2[n]) * h[n] + sx * bc[t][n];
+    }
+  }
+  if (d >= a.dim) return;
+  float *to = a.ends + (k * a.dim + d) * NP;
+#pragma unroll
+  for (int n = 0; n < NP; n += 4) *(float4 *)(to + n) = make_float4(h[n], h[n + 1], h[n + 2], h[n + 3]);
+  a.spans[k * a.dim + d] = span;
+}
+
+// gradient of v = sum c h + skip x, from that of y
+__device__ inline float before_gate(float dy, bool gated, float z) { return gated ? dy * z * sigmoid(z) : dy; }
+
+// What a unit that begins within a bag tells the one before: exp(D a) g of its first row, from the bag's end or from zero
+template <class E, int NP>
+__global__ __launch_bounds__(64) void ssm_grad_ends_kernel(SsmArgs a) {
+  __shared__ float bc[kBlock][2 * NP];
+  const int64_t k = blockIdx.x / a.waves;
+  const Unit u = a.units[k], next = a.units[k + 1];
+  if (!u.cut) return;
+  const int wave = (int)(blockIdx.x % a.waves), lane = threadIdx.x, N = a.states;
+  const bool whole = next.cut && u.bag == next.bag;
+  const int64_t begin = u.begin, end = whole ? next.begin : min(next.begin, max(a.off[u.bag + 1], begin));
+  const int d = wave * 64 + lane, dc = min(d, a.dim - 1), group = a.groups > 1 ? wave * 64 / (a.dim / a.groups) : 0;
+  float g[NP], a2[NP], span = 0.0f;  // g: what the row before the last one seen gets
+#pragma unroll
+  for (int n = 0; n < NP; ++n) {
+    a2[n] = n < N ? a.a[(int64_t)dc * N + n] * kLog2e : 0.0f;
+    g[n] = !whole && a.dlast && n < N ? a.dlast[((int64_t)u.bag * a.dim + dc) * N + n] : 0.0f;
+  }
+  const float bias = a.bias ? a.bias[dc] : 0.0f;
+  const E *delta = (const E *)a.delta + dc, *dy = (const E *)a.dy + dc, *z = a.z ? (const E *)a.z + dc : nullptr;
+  for (int64_t row0 = (end - 1) & ~(int64_t)(kBlock - 1); row0 + kBlock > begin; row0 -= kBlock) {
+    const int lo = (int)max(begin - row0, (int64_t)0), hi = (int)min(end - row0, (int64_t)kBlock);
+    __syncthreads();
+    stage<E, NP, 64>(a, row0, lo, hi, group, bc, false, true);
+    __syncthreads();
+#pragma unroll 4
+    for (int t = hi - 1; t >= lo; --t) {
+      const int64_t r = row0 + t;
+      const float step = soft((float)delta[r * a.ts] + bias), dv = before_gate((float)dy[r * a.dys], z, z ? (float)z[r * a.zs] : 0.0f);
+      span += step;
+#pragma unroll
+      for (int n = 0; n < NP; ++n) g[n] = __builtin_amdgcn_exp2f(step * a2[n]) * (bc[t][NP + n] * dv + g[n]);
+    }
+  }
+  if (d >= a.dim) return;
+  float *to = a.ends + (k * a.dim + d) * NP;
+#pragma unroll
+  for (int n = 0; n < NP; n += 4) *(float4 *)(to + n) = make_float4(g[n], g[n + 1], g[n + 2], g[n + 3]);
+  a.spans[k * a.dim + d] = span;
+}
+
+// Whether unit k says something to the next one (BACK: the one before), and whether that has a part of what it has heard itself
+template <bool BACK>
+__device__ inline int says(const SsmArgs &a, int64_t k) {
+  const Unit u = a.units[k], next = a.units[k + 1];
+  return (BACK ? u.cut : next.cut) ? 1 + (u.cut && next.cut && u.bag == next.bag) : 0;
+}
+
+// A segment of units, a lane for each state of each element: what comes before (BACK: behind) each unit, but for what comes before the segment
+template <int NP, bool BACK>
+__global__ __launch_bounds__(kThreads) void ssm_join_kernel(SsmArgs a, int64_t segments, int groups) {
+  const int64_t seg = blockIdx.x / groups, i = (int64_t)(blockIdx.x % groups) * kThreads + threadIdx.x;
+  const int64_t k0 = seg * kSegment, k1 = min(k0 + kSegment, a.count);
+  const int lane = threadIdx.x & 63;
+  // of every unit of the segment, by the lanes of a wavefront
+  const int mine = k0 + lane < k1 ? says<BACK>(a, k0 + lane) : 0;
+  const uint64_t speak = __ballot(mine > 0), pass = __ballot(mine > 1);
+  const int64_t n_all = (int64_t)a.dim * NP;
+  const bool in = i < n_all;
+  const int64_t ic = in ? i : n_all - 1;
+  const int d = (int)(ic / NP), n = (int)(ic % NP);
+  if (!speak) {  // no cut bag: nothing to be written but that nothing gets through
+    if (in && n == 0) a.seg_reach[seg * a.dim + d] = -1.0f;
+    if (in) a.seg_state[seg * n_all + i] = 0.0f;
+    // the first unit (BACK: the last) may be told something by the segment before
+    const int64_t k = BACK ? k1 - 1 : k0;
+    if (in) a.ends[k * n_all + i] = 0.0f;
+    if (in && n == 0) a.reach[k * a.dim + d] = 0.0f;
+    return;
+  }
+  const float a2 = n < a.states ? a.a[(int64_t)d * a.states + n] * kLog2e : 0.0f;
+  float st = 0.0f, sum = 0.0f;  // sum < 0: nothing of what comes before the segment gets here
+  constexpr int R = 8;
+  for (int64_t j0 = 0; j0 < k1 - k0; j0 += R) {
+    float e[R], s[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      const int64_t j = j0 + r, k = BACK ? k1 - 1 - j : k0 + j;
+      const bool some = j < k1 - k0 && (speak >> (k - k0) & 1);
+      e[r] = some ? a.ends[k * n_all + ic] : 0.0f;
+      s[r] = some ? a.spans[k * a.dim + d] : 0.0f;
+    }
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      const int64_t j = j0 + r, k = BACK ? k1 - 1 - j : k0 + j;
+      if (j >= k1 - k0) break;
+      if (in) a.ends[k * n_all + i] = st;
+      if (in && n == 0) a.reach[k * a.dim + d] = sum;
+      const int64_t bit = k - k0;
+      if (pass >> bit & 1) {
+        st = carried(a2, s[r], st) + e[r];
+        sum = sum < 0.0f ? sum : sum + s[r];
+      } else {
+        st = e[r];  // zero where it says nothing
+        sum = -1.0f;
+      }
+    }
+  }
+  if (!in) return;
+  a.seg_state[seg * n_all + i] = st;
+  if (n == 0) a.seg_reach[seg * a.dim + d] = sum;
+}
+
+// What comes before (BACK: behind) each segment
+template <int NP, bool BACK>
+__global__ __launch_bounds__(64) void ssm_segments_kernel(SsmArgs a, int64_t segments) {
+  const int64_t i = (int64_t)blockIdx.x * 64 + threadIdx.x, n_all = (int64_t)a.dim * NP;
+  if (i >= n_all) return;
+  const int d = (int)(i / NP), n = (int)(i % NP);
+  const float a2 = n < a.states ? a.a[(int64_t)d * a.states + n] * kLog2e : 0.0f;
+  float st = 0.0f;
+  constexpr int R = 8;
+  for (int64_t j0 = 0; j0 < segments; j0 += R) {
+    float e[R], s[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      const int64_t j = min(j0 + r, segments - 1), k = BACK ? segments - 1 - j : j;
+      e[r] = a.seg_state[k * n_all + i];
+      s[r] = a.seg_reach[k * a.dim + d];
+    }
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      const int64_t j = j0 + r, k = BACK ? segments - 1 - j : j;
+      if (j >= segments) break;
+      a.seg_start[k * n_all + i] = st;
+      st = s[r] < 0.0f ? e[r] : carried(a2, s[r], st) + e[r];
+    }
+  }
+}
+
+// sum over the LPC lanes that share an element, the same in all of them
+template <int LPC>
+__device__ inline float lane_sum(float v) {
+#pragma unroll
+  for (int o = 1; o < LPC; o *= 2) v += __shfl_xor(v, o);
+  return v;
+}
+
+// Sums over the elements of a wavefront of 8 numbers a lane (db and dc of four states), to LDS: with each step half of the numbers go to
+// half of the lanes.
+template <int LEFT, int BIT, int LPC>
+__device__ inline void halve(float (&v)[8], int &first) {
+  if constexpr (BIT >= LPC) {
+    if constexpr (LEFT > 1) {
+      constexpr int half = LEFT / 2;
+      const bool up = threadIdx.x & BIT;
+#pragma unroll
+      for (int i = 0; i < half; ++i) {
+        const float keep = up ? v[i + half] : v[i], send = up ? v[i] : v[i + half];
+        v[i] = keep + __shfl_xor(send, BIT);
+      }
+      first += up ? half : 0;
+      halve<half, BIT / 2, LPC>(v, first);
+    } else {
+      v[0] += __shfl_xor(v[0], BIT);
+      halve<1, BIT / 2, LPC>(v, first);
+    }
+  }
+}
+template <int NP>
+__device__ inline void sum_elements(float (&v)[8], float *to) {
+  constexpr int LPC = NP / 4, left = LPC == 16 ? 2 : 1;
+  const int lane = threadIdx.x & 63, q = lane % LPC;
+  int first = 0;
+  halve<8, 32, LPC>(v, first);
+  if (LPC == 4 && (lane & 4)) return;  // whose number is another lane's too
+#pragma unroll
+  for (int i = 0; i < left; ++i) {
+    const int m = first + i;
+    to[(m >= 4 ? NP : 0) + 4 * q + (m & 3)] = v[i];
+  }
+}
+
+// Backward of a unit's rows: a lane has states 4 q .. 4 q + 3 of an element; a workgroup's wavefronts have elements side by side.
+template <class E, int NP>
+__global__ __launch_bounds__(64 * kGradWaves) void ssm_grad_kernel(SsmArgs a, int waves) {
+  constexpr int LPC = NP / 4, CPW = 64 / LPC, OWN = kBlock / LPC;  // lanes of an element, elements of a wavefront, rows whose scalars a lane finds
+  extern __shared__ float4 lds[];
+  float(*bc)[2 * NP] = (float(*)[2 * NP])lds;                                // [kBlock][2 NP]
+  float *part = (float *)lds + kBlock * 2 * NP;                              // [waves][kBlock][2 NP]
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, q = lane % LPC, e = lane / LPC, N = a.states;
+  float4(*row)[CPW] = (float4(*)[CPW])(part + waves * kBlock * 2 * NP) + wave * kBlock;  // [kBlock][CPW] of each wavefront: D, D x, dv
+  const int64_t worker = blockIdx.x / a.blocks;
+  const int block = (int)(blockIdx.x % a.blocks), d = (block * waves + wave) * CPW + e, dc = min(d, a.dim - 1);
+  const bool in = d < a.dim;
+  const int group = a.groups > 1 ? block * waves * CPW / (a.dim / a.groups) : 0;
+  float av[4], a2[4], da[4] = {0.0f, 0.0f, 0.0f, 0.0f}, dskip = 0.0f, dbias = 0.0f;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    av[j] = 4 * q + j < N ? a.a[(int64_t)dc * N + 4 * q + j] : 0.0f;
+    a2[j] = av[j] * kLog2e;
+  }
+  const float bias = a.bias ? a.bias[dc] : 0.0f, skip = a.skip ? a.skip[dc] : 0.0f;
+  for (int64_t k = worker; k < a.count; k += a.workers) {
+    const int64_t begin = a.units[k].begin, end = a.units[k + 1].begin;
+    if (begin >= end) continue;
+    float carry[4];  // exp(D a) g of the row behind
+#pragma unroll
+    for (int j = 0; j < 4; ++j) carry[j] = a.units[k + 1].cut && 4 * q + j < N ? start_of<NP>(a, k, dc, 4 * q + j, a2[j]) : 0.0f;
+    for (int64_t row0 = (end - 1) & ~(int64_t)(kBlock - 1); row0 + kBlock > begin; row0 -= kBlock) {
+      const int lo = (int)max(begin - row0, (int64_t)0), hi = (int)min(end - row0, (int64_t)kBlock);
+      __syncthreads();
+      for (int i = threadIdx.x; i < kBlock * 2 * NP; i += 64 * waves) {
+        const int t = i / (2 * NP), n = i % (2 * NP), s = n % NP;
+        const bool have = t >= lo && t < hi && s < N;
+        const int64_t r = row0 + t;
+        bc[t][n] = have ? (float)(n < NP ? ((const E *)a.b)[r * a.bs + group * N + s] : ((const E *)a.c)[r * a.cs + group * N + s]) : 0.0f;
+      }
+      const Marks m = marks_of(a, row0, lo, hi);
+      // scalars of the rows t with t % LPC = q
+      float xv[OWN], step[OWN], slope[OWN], dv[OWN], gate[OWN], own_v[OWN], own_b[OWN], own_w[OWN];
+#pragma unroll
+      for (int i = 0; i < OWN; ++i) {
+        const int t = i * LPC + q;
+        const int64_t r = row0 + min(max(t, lo), hi - 1);
+        xv[i] = (float)((const E *)a.x)[r * a.xs + dc];
+        const float u = (float)((const E *)a.delta)[r * a.ts + dc] + bias, dy = (float)((const E *)a.dy)[r * a.dys + dc];
+        step[i] = soft(u);
+        slope[i] = sigmoid(u);
+        dv[i] = dy;
+        gate[i] = 0.0f;
+        if (a.z) {
+          const float z = (float)((const E *)a.z)[r * a.zs + dc], f = sigmoid(z);
+          dv[i] = dy * z * f;
+          gate[i] = dy * (f * (1.0f + z * (1.0f - f)));
+        }
+        if (!in) dv[i] = xv[i] = 0.0f;  // elements beyond the row have no part of db and dc
+        own_v[i] = own_b[i] = own_w[i] = 0.0f;
+        row[t][e] = make_float4(step[i], step[i] * xv[i], dv[i], 0.0f);
+      }
+      __syncthreads();
+      // forward: w and the decays of the block's rows
+      float h[4], w[kBlock][4], decay[kBlock][4];
+      if (lo == 0) {
+        const float4 s = *(const float4 *)(a.saved + (row0 / kBlock * a.dim + dc) * NP + 4 * q);
+        h[0] = s.x, h[1] = s.y, h[2] = s.z, h[3] = s.w;
+      } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) h[j] = 0.0f;
+      }
+#pragma unroll
+      for (int t = 0; t < kBlock; ++t) {
+        if (t < lo || t >= hi) continue;
+        if (m.starts >> t & 1) {
+          const int64_t bag = __builtin_amdgcn_readlane(m.bag.x, t);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) h[j] = a.h0 && 4 * q + j < N ? a.h0[bag * a.h0s + (int64_t)dc * N + 4 * q + j] : 0.0f;
+        }
+        const float4 s = row[t][e], b = *(const float4 *)&bc[t][4 * q];
+        const float bj[4] = {b.x, b.y, b.z, b.w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          decay[t][j] = __builtin_amdgcn_exp2f(s.x * a2[j]);
+          w[t][j] = decay[t][j] * h[j];
+          h[j] = w[t][j] + s.y * bj[j];
+        }
+        if (a.z) {
+          const float4 c = *(const float4 *)&bc[t][NP + 4 * q];
+          const float v = lane_sum<LPC>((c.x * h[0] + c.y * h[1]) + (c.z * h[2] + c.w * h[3]));
+          own_v[t / LPC] = t % LPC == q ? v : own_v[t / LPC];
+        }
+      }
+      // and back
+#pragma unroll
+      for (int t = kBlock - 1; t >= 0; --t) {
+        if (t < lo || t >= hi) continue;
+        if (m.ends >> t & 1) {
+          const int64_t bag = __builtin_amdgcn_readlane(m.bag.y, t);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) carry[j] = a.dlast && 4 * q + j < N ? a.dlast[(bag * a.dim + dc) * N + 4 * q + j] : 0.0f;
+        }
+        const float4 s = row[t][e], b = *(const float4 *)&bc[t][4 * q], c = *(const float4 *)&bc[t][NP + 4 * q];
+        const float bj[4] = {b.x, b.y, b.z, b.w}, cj[4] = {c.x, c.y, c.z, c.w};
+        float gb = 0.0f, gwa = 0.0f, both[8];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const float g = cj[j] * s.z + carry[j], gw = g * w[t][j];
+          gb += g * bj[j];
+          gwa += gw * av[j];
+          da[j] += gw * s.x;
+          both[j] = g * s.y;
+          both[4 + j] = s.z * (w[t][j] + s.y * bj[j]);
+          carry[j] = decay[t][j] * g;
+        }
+        gb = lane_sum<LPC>(gb);
+        gwa = lane_sum<LPC>(gwa);
+        own_b[t / LPC] = t % LPC == q ? gb : own_b[t / LPC];
+        own_w[t / LPC] = t % LPC == q ? gwa : own_w[t / LPC];
+        sum_elements<NP>(both, part + (wave * kBlock + t) * 2 * NP);
+        if ((m.starts >> t & 1) && a.dh0 && in) {
+          const int64_t bag = __builtin_amdgcn_readlane(m.bag.x, t);
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            if (4 * q + j < N) a.dh0[(bag * a.dim + d) * N + 4 * q + j] = carry[j];
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < OWN; ++i) {
+        const int t = i * LPC + q;
+        if (t < lo || t >= hi || !in) continue;
+        const int64_t at = (row0 + t) * a.dim + d;
+        const float du = (own_w[i] + xv[i] * own_b[i]) * slope[i];
+        ((E *)a.dx)[at] = (E)(skip * dv[i] + step[i] * own_b[i]);
+        ((E *)a.ddelta)[at] = (E)du;
+        if (a.z) ((E *)a.dz)[at] = (E)(gate[i] * (own_v[i] + skip * xv[i]));
+        dskip += dv[i] * xv[i];
+        dbias += du;
+      }
+      __syncthreads();
+      for (int i = threadIdx.x; i < kBlock * 2 * NP; i += 64 * waves) {
+        const int t = i / (2 * NP), n = i % (2 * NP), s = n % NP;
+        if (t < lo || t >= hi || s >= N) continue;
+        float v = 0.0f;
+        for (int j = 0; j < waves; ++j) v += part[j * kBlock * 2 * NP + i];
+        const int64_t r = row0 + t;
+        if (a.shared) a.shared[((int64_t)block * a.rows + r) * 2 * N + (n < NP ? 0 : N) + s] = v;
+        else ((E *)(n < NP ? a.db : a.dc))[r * a.groups * N + group * N + s] = (E)v;
+      }
+    }
+  }
+  dskip = lane_sum<LPC>(dskip);
+  dbias = lane_sum<LPC>(dbias);
+  if (!in) return;
+  float *to = a.parts + (worker * a.dim + d) * (N + 2);
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+    if (4 * q + j < N) to[4 * q + j] = da[j];
+  if (q == 0) to[N] = dskip, to[N + 1] = dbias;
+}
+
+// db and dc from the sums of the workgroups that a group's elements lie on
+template <class E>
+__global__ __launch_bounds__(kThreads) void ssm_shared_kernel(SsmArgs a, int64_t first) {
+  const int64_t i = first + (int64_t)blockIdx.x * kThreads + threadIdx.x;
+  const int N = a.states, width = 2 * N, of_group = a.blocks / a.groups;
+  const int64_t r = i / (width * a.groups);
+  if (r >= a.rows) return;
+  const int k = (int)(i % (width * a.groups)), group = k / width, n = k % width;
+  float v = 0.0f;
+  for (int j = 0; j < of_group; ++j) v += a.shared[((int64_t)(group * of_group + j) * a.rows + r) * width + n];
+  ((E *)(n < N ? a.db : a.dc))[(r * a.groups + group) * N + n % N] = (E)v;
+}
+
+// One more row: LPC lanes with four states each for an element
+template <class E, int NP>
+__global__ __launch_bounds__(kThreads) void ssm_step_kernel(SsmArgs a, float *state, int64_t stride, int64_t slots, const int64_t *slot_of, int64_t first) {
+  constexpr int LPC = NP / 4;
+  const int N = a.states;
+  const int64_t i = first + ((int64_t)blockIdx.x * kThreads + threadIdx.x) / LPC, r = i / a.dim;
+  if (r >= a.rows) return;  // all lanes of an element
+  const int d = (int)(i - r * a.dim), q = threadIdx.x % LPC;
+  const int64_t slot = slot_of ? slot_of[r] : r;
+  float v = 0.0f;
+  if (slot >= 0 && slot < slots) {
+    float *s = state + slot * stride + (int64_t)d * N + 4 * q;
+    const int have = N - 4 * q;
+    float h[4], av[4], b[4], c[4];
+    load_floats<float, 4>(s, have, h);
+    load_floats<float, 4>(a.a + (int64_t)d * N + 4 * q, have, av);
+    const int at = (a.groups > 1 ? d / (a.dim / a.groups) : 0) * N + 4 * q;
+    load_floats<E, 4>((const E *)a.b + r * a.bs + at, have, b);
+    load_floats<E, 4>((const E *)a.c + r * a.cs + at, have, c);
+    const float x = (float)((const E *)a.x)[r * a.xs + d];
+    const float step = soft((float)((const E *)a.delta)[r * a.ts + d] + (a.bias ? a.bias[d] : 0.0f));
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      h[j] = __builtin_amdgcn_exp2f(step * (av[j] * kLog2e)) * h[j] + (step * x) * b[j];
+      if (j < have) v += c[j] * h[j];
+    }
+    store_floats<float, 4>(s, have, h);
+    v = lane_sum<LPC>(v);
+    if (a.skip) v += a.skip[d] * x;
+    if (a.z) {
+      const float z = (float)((const E *)a.z)[r * a.zs + d];
+      v *= z * sigmoid(z);
+    }
+  } else if (slot >= slots && q == 0) {
+    *a.err = 2;
+  }
+  if (a.y && q == 0) ((E *)a.y)[r * a.ys + d] = (E)v;
+}
+
+// How the rows are cut: a function of their number and dim, so that forward and backward do the same.  As few cuts as leave 8192 wavefronts
+// (eight a SIMD), down to 32 rows a unit.
+int unit_of(int64_t rows, int dim) {
+  int unit = 128;
+  while (unit > 32 && divide_up(rows, unit) * divide_up(dim, 64) < 8192) unit /= 2;
+  return unit;
+}
+int padded(int states) { return states <= 16 ? 16 : states <= 32 ? 32 : 64; }
+
+// How the elements of a row lie on the backward's workgroups
+struct GradLay {
+  int waves, blocks;  // of a workgroup; workgroups of a row
+};
+GradLay grad_lay(int dim, int groups, int np) {
+  const int each = 64 / (np / 4);  // elements of a wavefront
+  int waves = np == 64 ? 4 : kGradWaves;  // up to 52 KB of LDS
+  if (groups > 1) waves = std::min(waves, 64 / each);  // a workgroup's elements are of one group
+  else waves = (int)std::min<int64_t>(waves, divide_up(dim, each));
+  return {waves, (int)divide_up(dim, waves * each)};
+}
+int64_t workers_of(int64_t units, int blocks) { return std::max<int64_t>(1, std::min<int64_t>(units, kGradWorkers / blocks)); }
+
+}  // namespace
+
+struct tbe_ssm_t : DenseBase {
+  int dim, states, groups, dtype, np;
+  int64_t max_bags, max_rows;
+  char *block = nullptr;
+  int32_t *err;
+  SsmArgs scratch{};
+};
+
+namespace {
+
+int64_t most_units(int64_t rows, int dim) {  // of any number of rows up to this
+  return std::max(divide_up(rows, unit_of(rows, dim)), std::min(divide_up(rows, 32), divide_up(8192, divide_up(dim, 64)) * 2 + 1));
+}
+
+template <int NP, bool BACK>
+void join(const SsmArgs &a, hipStream_t st) {
+  const int64_t segments = divide_up(a.count, kSegment), groups = divide_up((int64_t)a.dim * NP, kThreads);
+  ssm_join_kernel<NP, BACK><<<dim3((unsigned)(segments * groups)), kThreads, 0, st>>>(a, segments, (int)groups);
+  ssm_segments_kernel<NP, BACK><<<dim3((unsigned)divide_up((int64_t)a.dim * NP, 64)), 64, 0, st>>>(a, segments);
+}
+
+void prepare(const SsmArgs &a, float *empty_to, const float *empty_from, int64_t stride, hipStream_t st) {
+  const int64_t bag_groups = divide_up(a.bags, kThreads), groups = bag_groups + divide_up(a.count + 1, kThreads / 64);
+  ssm_prepare_kernel<<<dim3((unsigned)groups), kThreads, 0, st>>>(a, bag_groups, empty_to, empty_from, stride);
+}
+
+template <class E, int NP>
+int forward(const SsmArgs &a, hipStream_t st) {
+  prepare(a, a.last, a.h0, a.h0s, st);
+  if (a.rows > 0) {
+    const dim3 grid((unsigned)(a.count * a.waves));
+    if (a.rows > 2 * a.unit) {  // else no bag is cut
+      ssm_ends_kernel<E, NP><<<grid, 64, 0, st>>>(a);
+      join<NP, false>(a, st);
+    }
+    if (a.states == NP) ssm_kernel<E, NP, true><<<grid, 64, 0, st>>>(a);
+    else ssm_kernel<E, NP, false><<<grid, 64, 0, st>>>(a);
+  }
+  return check_launch();
+}
+
+template <class E, int NP>
+int backward(SsmArgs a, const tbe_ssm_grads *g, hipStream_t st) {
+  prepare(a, a.dh0, a.dlast, (int64_t)a.dim * a.states, st);
+  const GradLay l = grad_lay(a.dim, a.groups, NP);
+  a.blocks = l.blocks;
+  a.workers = workers_of(a.count, l.blocks);
+  if (l.blocks / a.groups <= 1) a.shared = nullptr;
+  if (a.rows > 2 * a.unit) {
+    ssm_grad_ends_kernel<E, NP><<<dim3((unsigned)(a.count * a.waves)), 64, 0, st>>>(a);
+    join<NP, true>(a, st);
+  }
+  const size_t lds = (size_t)kBlock * 2 * NP * 4 * (1 + l.waves) + (size_t)l.waves * kBlock * (64 / (NP / 4)) * 16;
+  ssm_grad_kernel<E, NP><<<dim3((unsigned)(a.workers * l.blocks)), 64 * l.waves, lds, st>>>(a, l.waves);
+  if (a.shared) {
+    const int64_t groups = divide_up(a.rows * a.groups * 2 * a.states, kThreads);
+    for (int64_t done = 0; done < groups; done += most_groups(kThreads))
+      ssm_shared_kernel<E><<<dim3((unsigned)std::min(groups - done, most_groups(kThreads))), kThreads, 0, st>>>(a, done * kThreads);
+  }
+  sum_parts(a.parts, a.workers, (int64_t)a.dim * (a.states + 2), a.states + 2, a.states, g->d_da, g->d_dskip, g->d_ddelta_bias, st);
+  return check_launch();
+}
+
+template <class E, int NP>
+int step(const SsmArgs &a, float *state, int64_t stride, int64_t slots, const int64_t *slot_of, hipStream_t st) {
+  constexpr int each = kThreads / (NP / 4);  // elements of a workgroup
+  const int64_t groups = divide_up(a.rows * a.dim, each);
+  for (int64_t done = 0; done < groups; done += most_groups(kThreads))
+    ssm_step_kernel<E, NP><<<dim3((unsigned)std::min(groups - done, most_groups(kThreads))), kThreads, 0, st>>>(a, state, stride, slots, slot_of, done * each);
+  return check_launch();
+}
+
+// call<E, NP>() for the handle's type and number of states
+template <class E, class F>
+int of_states(int np, F call) {
+  return np == 16 ? call.template operator()<E, 16>() : np == 32 ? call.template operator()<E, 32>() : call.template operator()<E, 64>();
+}
+template <class F>
+int of_handle(tbe_ssm_handle s, F call) {
+  if (s->dtype == TBE_FP32) return of_states<float>(s->np, call);
+  if (s->dtype == TBE_FP16) return of_states<_Float16>(s->np, call);
+  return of_states<__bf16>(s->np, call);
+}
+struct Forward {
+  SsmArgs a;
+  hipStream_t st;
+  template <class E, int NP> int operator()() const { return forward<E, NP>(a, st); }
+};
+struct Backward {
+  SsmArgs a;
+  const tbe_ssm_grads *g;
+  hipStream_t st;
+  template <class E, int NP> int operator()() const { return backward<E, NP>(a, g, st); }
+};
+struct Step {
+  SsmArgs a;
+  float *state;
+  int64_t stride, slots;
+  const int64_t *slot_of;
+  hipStream_t st;
+  template <class E, int NP> int operator()() const { return step<E, NP>(a, state, stride, slots, slot_of, st); }
+};
+
+int check_batch(tbe_ssm_handle s, const tbe_ssm_batch *b, bool bags) {
+  if (int rc = check_handle(s)) return rc;
+  if (!b) return report(TBE_EINVAL, "null batch");
+  if (b->rows < 0 || (bags && b->bags < 0)) return report(TBE_EINVAL, "negative number of bags or rows");
+  if (bags && (b->bags > s->max_bags || b->rows > s->max_rows)) return report(TBE_ELIMIT, "more bags or rows than the handle was created for");
+  if (bags && b->bags == 0 && b->rows > 0) return report(TBE_EINVAL, "rows without a bag");
+  if (bags && b->bags > 0 && !b->d_offsets) return report(TBE_EINVAL, "null offsets");
+  if (!b->d_a || (b->rows > 0 && (!b->d_x || !b->d_delta || !b->d_b || !b->d_c))) return report(TBE_EINVAL, "null rows or decays");
+  const int64_t k = (int64_t)s->groups * s->states;
+  if (b->rows > 0 && (b->x_stride < s->dim || b->delta_stride < s->dim || (b->d_z && b->z_stride < s->dim) || b->b_stride < k || b->c_stride < k))
+    return report(TBE_EINVAL, "a stride below the length of a row");
+  if (bags && b->d_h0 && b->h0_stride != 0 && b->h0_stride < (int64_t)s->dim * s->states) return report(TBE_EINVAL, "a stride below the states of a bag");
+  return TBE_OK;
+}
+SsmArgs args_of(tbe_ssm_handle s, const tbe_ssm_batch *b) {
+  SsmArgs a = s->scratch;
+  a.x = b->d_x, a.delta = b->d_delta, a.z = b->d_z, a.b = b->d_b, a.c = b->d_c;
+  a.xs = b->x_stride, a.ts = b->delta_stride, a.zs = b->z_stride, a.bs = b->b_stride, a.cs = b->c_stride;
+  a.a = b->d_a, a.skip = b->d_skip, a.bias = b->d_delta_bias, a.off = b->d_offsets, a.bags = b->bags, a.rows = b->rows;
+  a.h0 = b->d_h0, a.h0s = b->h0_stride;
+  a.dim = s->dim, a.states = s->states, a.groups = s->groups, a.err = s->err;
+  a.unit = unit_of(b->rows, s->dim);
+  a.count = divide_up(b->rows, a.unit);
+  a.waves = (int)divide_up(s->dim, 64);
+  return a;
+}
+
+}  // namespace
+
+extern "C" {
+
+int tbe_ssm_create(tbe_ssm_handle *out, int32_t dim, int32_t states, int32_t groups, int32_t dtype, int64_t max_bags, int64_t max_rows) {
+  if (!out) return report(TBE_EINVAL, "null pointer for the handle");
+  *out = nullptr;
+  if (dim < 1 || dim > 65536) return report(TBE_EINVAL, "dim outside 1 .. 65536");
+  if (states < 1 || states > kMostStates) return report(TBE_EINVAL, "states outside 1 .. 64");
+  if (groups < 1 || (groups > 1 && (dim % groups || dim / groups % 64))) return report(TBE_EINVAL, "groups: 1, or such that each has a multiple of 64 elements");
+  if (!known_dtype(dtype)) return report(TBE_EINVAL, "unknown dtype");
+  if (max_bags < 0 || max_rows < 0) return report(TBE_EINVAL, "negative number of bags or rows");
+  if (max_bags > (1ll << 38) / dim / states || max_rows > (1ll << 38) / dim || max_bags >= INT32_MAX)
+    return report(TBE_ELIMIT, "more than 2^38 elements or states of bags, or 2^31 bags");
+  const int np = padded(states);
+  const int64_t units = most_units(max_rows, dim), segments = divide_up(units, kSegment), waves = divide_up(dim, 64);
+  if (units * waves > most_groups(64) || segments * divide_up((int64_t)dim * np, kThreads) > most_groups(kThreads))
+    return report(TBE_ELIMIT, "more rows than one launch can take");
+  tbe_ssm_t *s = new (std::nothrow) tbe_ssm_t;
+  if (!s) return report(TBE_ENOMEM, "no memory for the handle");
+  s->dim = dim, s->states = states, s->groups = groups, s->dtype = dtype, s->np = np, s->max_bags = max_bags, s->max_rows = max_rows;
+  const GradLay l = grad_lay(dim, groups, np);
+  int64_t at = 256;
+  auto take = [&](int64_t bytes) {
+    const int64_t from = at;
+    at += (bytes + 255) / 256 * 256;
+    return from;
+  };
+  const int64_t o_units = take((units + 1) * sizeof(Unit)), o_marks = take(max_rows * sizeof(int2)), o_ends = take(units * dim * np * 4),
+                o_spans = take(units * dim * 4), o_reach = take(units * dim * 4), o_state = take(segments * dim * np * 4),
+                o_sreach = take(segments * dim * 4), o_start = take(segments * dim * np * 4),
+                o_parts = take(workers_of(units, l.blocks) * dim * (states + 2) * 4),
+                o_shared = take(l.blocks / groups > 1 ? (int64_t)l.blocks * max_rows * 2 * states * 4 : 0);
+  hipError_t e = hipGetDevice(&s->device);
+  if (e == hipSuccess) e = hipMalloc((void **)&s->block, (size_t)at);
+  if (e == hipSuccess) e = hipMemset(s->block, 0, 256);
+  if (e != hipSuccess) {
+    (void)hipFree(s->block);
+    delete s;
+    return report_hip(e);
+  }
+  s->err = (int32_t *)s->block;
+  SsmArgs &a = s->scratch;
+  a.units = (Unit *)(s->block + o_units), a.marks = (int2 *)(s->block + o_marks), a.ends = (float *)(s->block + o_ends);
+  a.spans = (float *)(s->block + o_spans), a.reach = (float *)(s->block + o_reach), a.seg_state = (float *)(s->block + o_state);
+  a.seg_reach = (float *)(s->block + o_sreach), a.seg_start = (float *)(s->block + o_start), a.parts = (float *)(s->block + o_parts);
+  a.shared = (float *)(s->block + o_shared);
+  *out = s;
+  return TBE_OK;
+}
+
+int tbe_ssm_destroy(tbe_ssm_handle s) {
+  if (!s) return TBE_OK;
+  (void)hipFree(s->block);
+  delete s;
+  return TBE_OK;
+}
+
+int64_t tbe_ssm_saved_floats(tbe_ssm_handle s, int64_t rows) {
+  if (!s || rows < 0) return report(TBE_EINVAL, "null handle or a negative number of rows");
+  return divide_up(rows, kBlock) * s->dim * s->np;
+}
+
+int tbe_ssm_forward(tbe_ssm_handle s, const tbe_ssm_batch *b, void *d_y, int64_t y_stride, float *d_last, float *d_saved, void *stream) {
+  if (int rc = check_batch(s, b, true)) return rc;
+  if (b->rows > 0 && !d_y) return report(TBE_EINVAL, "null results");
+  if (b->rows > 0 && y_stride < s->dim) return report(TBE_EINVAL, "a stride below the length of a row");
+  for (const void *in : {b->d_x, b->d_delta, b->d_z, b->d_b, b->d_c})
+    if (b->rows > 0 && in && d_y == in) return report(TBE_EINVAL, "the output is one of the inputs");
+  if (d_last && d_last == b->d_h0) return report(TBE_EINVAL, "the output is one of the inputs");
+  if (b->bags == 0) return TBE_OK;
+  SsmArgs a = args_of(s, b);
+  a.y = d_y, a.ys = y_stride, a.last = d_last, a.saved = d_saved;
+  return of_handle(s, Forward{a, (hipStream_t)stream});
+}
+
+int tbe_ssm_backward(tbe_ssm_handle s, const tbe_ssm_batch *b, const float *d_saved, const tbe_ssm_grads *g, void *stream) {
+  if (int rc = check_batch(s, b, true)) return rc;
+  if (!g || !g->d_da) return report(TBE_EINVAL, "null gradients");
+  if (b->rows > 0 && (!d_saved || !g->d_dy || !g->d_dx || !g->d_ddelta || !g->d_db || !g->d_dc || (b->d_z && !g->d_dz)))
+    return report(TBE_EINVAL, "null pointer for what the forward saved or for a gradient");
+  if (b->rows > 0 && g->dy_stride < s->dim) return report(TBE_EINVAL, "a stride below the length of a row");
+  for (const void *in : {b->d_x, b->d_delta, b->d_z, b->d_b, b->d_c, g->d_dy})
+    for (const void *out : {(const void *)g->d_dx, (const void *)g->d_ddelta, (const void *)(b->d_z ? g->d_dz : nullptr), (const void *)g->d_db, (const void *)g->d_dc})
+      if (b->rows > 0 && in && in == out) return report(TBE_EINVAL, "an output is one of the inputs");
+  if (g->d_dh0 && (g->d_dh0 == b->d_h0 || g->d_dh0 == g->d_dlast)) return report(TBE_EINVAL, "an output is one of the inputs");
+  SsmArgs a = args_of(s, b);
+  a.saved = const_cast<float *>(d_saved), a.dy = g->d_dy, a.dys = g->dy_stride, a.dlast = g->d_dlast;
+  a.dx = g->d_dx, a.ddelta = g->d_ddelta, a.dz = g->d_dz, a.db = g->d_db, a.dc = g->d_dc, a.dh0 = g->d_dh0;
+  return of_handle(s, Backward{a, g, (hipStream_t)stream});
+}
+
+int tbe_ssm_step(tbe_ssm_handle s, const tbe_ssm_batch *b, float *d_state, int64_t state_stride, int64_t slots, const int64_t *d_slots, void *d_y,
+                 int64_t y_stride, void *stream) {
+  if (int rc = check_batch(s, b, false)) return rc;
+  if (slots < 0) return report(TBE_EINVAL, "negative number of slots");
+  if (b->rows > (1ll << 38) / s->dim / s->np) return report(TBE_ELIMIT, "more than 2^38 states");
+  if (b->rows == 0) return TBE_OK;
+  if (!d_state) return report(TBE_EINVAL, "null states");
+  if (!d_slots && b->rows > slots) return report(TBE_EINVAL, "more rows than states");
+  if (state_stride < (int64_t)s->dim * s->states || (d_y && y_stride < s->dim)) return report(TBE_EINVAL, "a stride below the length of a row or of a state");
+  SsmArgs a = args_of(s, b);
+  a.y = d_y, a.ys = y_stride;
+  return of_handle(s, Step{a, d_state, state_stride, slots, d_slots, (hipStream_t)stream});
+}
+
+int tbe_ssm_check(tbe_ssm_handle s, void *stream) {
+  if (int rc = check_handle(s)) return rc;
+  return check_errors(s->err, (hipStream_t)stream);
+}
+
+}  // extern "C"

@@ -3,6 +3,9 @@
 Scan          a gated linear recurrence over the rows of every bag, with its gradient, and its form for one new row
 RelativeBias  a learned table looked up by the bucket of a distance between two rows of a history, with its gradient
 AdamW         the step of a model's dense weights, many tensors in one launch, with states in 32 or 8 bits
+ShortConv     a causal convolution over a few rows of every bag, with its gradient, and its form for one new row
+SelectiveScan a selective state space scan over the rows of every bag, with its gradient, and its form for one new row
+RMSNorm       a root-mean-square norm with the residual's addition, with its gradient, and with results in 8 bits
 
 Argument marshalling only: every step runs in the HIP kernels of the library.  A call enqueues on the current stream, behind
 this object's last call or its constructor if that was on another one (an object's calls share its scratch memory; replays of a captured graph
@@ -44,6 +47,36 @@ class AdamWTensor(C.Structure):
                 ("weight_decay", C.c_double)]
 
 
+class NormBatch(C.Structure):
+    _fields_ = [("x", C.c_void_p), ("residual", C.c_void_p), ("weight", C.c_void_p), ("x_stride", C.c_int64), ("residual_stride", C.c_int64),
+                ("rows", C.c_int64), ("summed", C.c_void_p), ("summed_stride", C.c_int64), ("weight_dtype", C.c_int32)]
+
+
+class NormGrad(C.Structure):
+    _fields_ = [("summed", C.c_void_p), ("dout", C.c_void_p), ("dsummed", C.c_void_p), ("weight", C.c_void_p), ("summed_stride", C.c_int64),
+                ("dout_stride", C.c_int64), ("dsummed_stride", C.c_int64), ("rows", C.c_int64), ("rstd", C.c_void_p), ("dx", C.c_void_p),
+                ("dresidual", C.c_void_p), ("dx_stride", C.c_int64), ("dresidual_stride", C.c_int64), ("dweight", C.c_void_p),
+                ("weight_dtype", C.c_int32), ("residual", C.c_int32)]
+
+
+class ConvBatch(C.Structure):
+    _fields_ = [("x", C.c_void_p), ("x_stride", C.c_int64), ("offsets", C.c_void_p), ("bags", C.c_int64), ("rows", C.c_int64),
+                ("weight", C.c_void_p), ("bias", C.c_void_p), ("before", C.c_void_p), ("weight_dtype", C.c_int32)]
+
+
+class SsmBatch(C.Structure):
+    _fields_ = [("x", C.c_void_p), ("delta", C.c_void_p), ("z", C.c_void_p), ("b", C.c_void_p), ("c", C.c_void_p), ("x_stride", C.c_int64),
+                ("delta_stride", C.c_int64), ("z_stride", C.c_int64), ("b_stride", C.c_int64), ("c_stride", C.c_int64), ("a", C.c_void_p),
+                ("skip", C.c_void_p), ("delta_bias", C.c_void_p), ("offsets", C.c_void_p), ("bags", C.c_int64), ("rows", C.c_int64),
+                ("h0", C.c_void_p), ("h0_stride", C.c_int64)]
+
+
+class SsmGrads(C.Structure):
+    _fields_ = [("dy", C.c_void_p), ("dy_stride", C.c_int64), ("dlast", C.c_void_p), ("dx", C.c_void_p), ("ddelta", C.c_void_p),
+                ("dz", C.c_void_p), ("db", C.c_void_p), ("dc", C.c_void_p), ("da", C.c_void_p), ("dskip", C.c_void_p),
+                ("ddelta_bias", C.c_void_p), ("dh0", C.c_void_p)]
+
+
 _ready = None  # the library object whose arguments have their types
 _current_raw_stream = torch._C._cuda_getCurrentRawStream
 # of a tensor, without the look for the attribute at each
@@ -69,8 +102,21 @@ def _lib() -> C.CDLL:
         l.tbe_adamw_create.argtypes = [C.POINTER(vp), C.POINTER(AdamWTensor), i32, i32]
         l.tbe_adamw_step.argtypes = [vp, vp, i64, f64, f64, f64, f64, C.c_uint32, vp, vp]
         l.tbe_adamw_step_counted.argtypes = [vp, vp, vp, f64, f64, f64, f64, C.c_uint32, vp, vp]
-        l.tbe_scan_check.argtypes = [vp, vp]
-        for n in ("tbe_scan_destroy", "tbe_bias_destroy", "tbe_adamw_destroy"):
+        l.tbe_scan_check.argtypes = l.tbe_conv_check.argtypes = l.tbe_ssm_check.argtypes = [vp, vp]
+        l.tbe_norm_create.argtypes = [C.POINTER(vp), i32, i32, i32, f64, i64]
+        l.tbe_norm_forward.argtypes = [vp, C.POINTER(NormBatch), vp, i64, vp, vp]
+        l.tbe_norm_quantise.argtypes = [vp, C.POINTER(NormBatch), i32, vp, i64, vp, vp]
+        l.tbe_norm_backward.argtypes = [vp, C.POINTER(NormGrad), vp]
+        l.tbe_conv_create.argtypes = [C.POINTER(vp), i32, i32, i32, i32, i64, i64]
+        l.tbe_conv_forward.argtypes = [vp, C.POINTER(ConvBatch), vp, i64, vp, vp]
+        l.tbe_conv_backward.argtypes = [vp, C.POINTER(ConvBatch), vp, i64, vp, vp, i64, vp, vp, vp, vp]
+        l.tbe_conv_step.argtypes = [vp, C.POINTER(ConvBatch), vp, i64, vp, vp, i64, vp]
+        l.tbe_ssm_create.argtypes = [C.POINTER(vp), i32, i32, i32, i32, i64, i64]
+        l.tbe_ssm_saved_floats.argtypes, l.tbe_ssm_saved_floats.restype = [vp, i64], i64
+        l.tbe_ssm_forward.argtypes = [vp, C.POINTER(SsmBatch), vp, i64, vp, vp, vp]
+        l.tbe_ssm_backward.argtypes = [vp, C.POINTER(SsmBatch), vp, C.POINTER(SsmGrads), vp]
+        l.tbe_ssm_step.argtypes = [vp, C.POINTER(SsmBatch), vp, i64, i64, vp, vp, i64, vp]
+        for n in ("tbe_scan_destroy", "tbe_bias_destroy", "tbe_adamw_destroy", "tbe_norm_destroy", "tbe_conv_destroy", "tbe_ssm_destroy"):
             getattr(l, n).argtypes = [vp]
         _ready = l
     return l
@@ -112,6 +158,27 @@ class _Handle:
         if not t.is_contiguous():
             raise ValueError(f"{name}: contiguous")
         return self._tensor(name, t, dtype, shape)
+
+    def _rows_of(self, name: str, t: torch.Tensor, n: int, dim: int, dtype: torch.dtype) -> Tuple[int, int]:
+        """address of rows of `dim` elements that lie side by side, and how far apart the rows are"""
+        p = self._tensor(name, t, dtype, (n, dim))
+        stride = t.stride()
+        if dim > 1 and n and stride[1] != 1:
+            raise ValueError(f"{name}: the elements of a row lie side by side")
+        return p, (stride[0] if n > 1 else dim)
+
+    def _offsets(self, offsets: torch.Tensor) -> Tuple[int, int]:
+        """number of bags, address"""
+        bags = offsets.numel() - 1
+        if not offsets.is_contiguous() or offsets.dim() != 1 or bags < 0:
+            raise ValueError("offsets: a contiguous vector of bags + 1 numbers")
+        return bags, self._tensor("offsets", offsets, torch.int64, (bags + 1,))
+
+    def _slots(self, slots: Optional[torch.Tensor], n: int) -> Optional[int]:
+        return self._whole("slots", slots, torch.int64, (n,)) if slots is not None else None
+
+    def _empty(self, *shape, dtype: torch.dtype = torch.float32) -> torch.Tensor:
+        return torch.empty(shape, dtype=dtype, device=self.device)
 
     def close(self):
         if self._h:
@@ -480,3 +547,307 @@ class AdamW(_Handle):
                                   stream), "tbe_adamw_step")
         _written(self.params if fine else [p for p, g in zip(self.params, grads) if g is not None])
         self._steps += 1
+
+
+def _own_rows(t: Optional[torch.Tensor]) -> Optional[torch.Tensor]:
+    """a gradient as autograd brings it (expanded, transposed), as rows of their own"""
+    return t if t is None or t.is_contiguous() else t.contiguous()
+
+
+class _NormFunction(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, plan, x, weight, residual):
+        out, summed, rstd = plan.forward(x, weight, residual)
+        ctx.set_materialize_grads(False)
+        ctx.plan, ctx.added, ctx.kinds = plan, residual is not None, (x.dtype, weight.dtype)
+        ctx.save_for_backward(summed, rstd, weight)
+        return (out, summed) if ctx.added else out
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dout, dsummed=None):
+        summed, rstd, weight = ctx.saved_tensors
+        if dout is None:
+            dout = torch.zeros(summed.shape, dtype=ctx.kinds[0], device=summed.device)
+        dx, dresidual, dweight = ctx.plan.backward(_own_rows(dout), summed, rstd, weight, _own_rows(dsummed), added=ctx.added)
+        return None, dx, dweight.to(ctx.kinds[1]), dresidual
+
+
+class RMSNorm(_Handle):
+    """s = x + residual, in the residual's type; out = s / sqrt(mean(s s) + eps) * weight, row by row.
+
+    x: [rows, dim] of `dtype` (rows may lie apart), as all rows here; residual: the same of `residual_dtype` (`dtype` or fp32; None: calls have no residual); weight: [dim].
+    Calling the object gives (out, s), or out without a residual, with gradients to x, weight and residual (not with gradients of those: asking for them raises)."""
+    _destroy = "tbe_norm_destroy"
+
+    def __init__(self, dim: int, dtype: torch.dtype, max_rows: int, eps: float = 1e-6, residual_dtype: Optional[torch.dtype] = None):
+        super().__init__()
+        if dtype not in DTYPES or residual_dtype not in (None, dtype, torch.float32):
+            raise ValueError(f"rows are {', '.join(map(str, DTYPES))}, the residual of their type or fp32: got {dtype}, {residual_dtype}")
+        self.dim, self.dtype, self.residual_dtype = dim, dtype, residual_dtype
+        self._check(_lib().tbe_norm_create(C.byref(self._h), dim, DTYPES[dtype], -1 if residual_dtype is None else DTYPES[residual_dtype], eps, max_rows),
+                    "tbe_norm_create")
+
+    def _weight(self, weight) -> Tuple[int, int]:
+        if weight.dtype not in DTYPES:
+            raise ValueError(f"weight: {', '.join(map(str, DTYPES))}")
+        return self._whole("weight", weight, weight.dtype, (self.dim,)), DTYPES[weight.dtype]
+
+    def _batch(self, x, weight, residual, summed):
+        n = x.shape[0]
+        (xp, xs), (wp, wt), (rp, rs), (sp, ss) = self._rows_of("x", x, n, self.dim, self.dtype), self._weight(weight), (None, 0), (None, 0)
+        if residual is not None:
+            if self.residual_dtype is None:
+                raise ValueError("residual: the object was made without one (residual_dtype)")
+            rp, rs = self._rows_of("residual", residual, n, self.dim, self.residual_dtype)
+            given = summed
+            summed = self._empty(n, self.dim, dtype=self.residual_dtype) if given is None else given
+            sp, ss = self._rows_of("summed", summed, n, self.dim, self.residual_dtype)
+        elif summed is not None:
+            raise ValueError("summed: there is no residual")
+        else:
+            summed = x
+        return NormBatch(xp, rp, wp, xs, rs, n, sp, ss, wt), summed
+
+    def forward(self, x, weight, residual=None, out=None, summed=None):
+        """(out, summed, rstd): summed is the stored sum (x without a residual; `summed` may be `residual`), rstd fp32 [rows] what `backward` needs"""
+        b, s = self._batch(x, weight, residual, summed)
+        written = [t for t in (out, summed) if t is not None]
+        out = self._empty(b.rows, self.dim, dtype=self.dtype) if out is None else out
+        rstd = self._empty(b.rows)
+        self._check(_lib().tbe_norm_forward(self._h, C.byref(b), *self._rows_of("out", out, b.rows, self.dim, self.dtype), rstd.data_ptr(), self._stream()),
+                    "tbe_norm_forward")
+        if written:
+            _written(written)
+        return out, s, rstd
+
+    def quantise(self, x, weight, residual=None, group: int = 0, codes=None, summed=None):
+        """(codes, scales, summed): out in 8 bits (torch.float8_e4m3fn) times a scale for each row (group 0) or each `group` elements of it,
+        fp32 [rows, groups of a row]; no gradients"""
+        b, s = self._batch(x, weight, residual, summed)
+        written = [t for t in (codes, summed) if t is not None]
+        codes = self._empty(b.rows, self.dim, dtype=torch.float8_e4m3fn) if codes is None else codes
+        scales = self._empty(b.rows, -(-self.dim // group) if group > 0 else 1)
+        self._check(_lib().tbe_norm_quantise(self._h, C.byref(b), group, *self._rows_of("codes", codes, b.rows, self.dim, torch.float8_e4m3fn),
+                                             scales.data_ptr(), self._stream()), "tbe_norm_quantise")
+        if written:
+            _written(written)
+        return codes, scales, s
+
+    def backward(self, dout, summed, rstd, weight, dsummed=None, added: Optional[bool] = None):
+        """(dx, dresidual, dweight): dresidual is None without a residual (added; True unless the object has none) and dx itself where they have one type;
+        dweight fp32.  summed, rstd: what `forward` gave; dsummed: what comes to the stored sum from what else reads it"""
+        added = self.residual_dtype is not None if added is None else added
+        if added and self.residual_dtype is None:
+            raise ValueError("added: the object was made without a residual (residual_dtype)")
+        if dsummed is not None and not added:
+            raise ValueError("dsummed: there is no residual")
+        kind, n = self.residual_dtype if added else self.dtype, dout.shape[0]
+        (sp, ss), (op, os_), (wp, wt) = self._rows_of("summed", summed, n, self.dim, kind), self._rows_of("dout", dout, n, self.dim, self.dtype), self._weight(weight)
+        dp, ds = self._rows_of("dsummed", dsummed, n, self.dim, kind) if dsummed is not None else (None, 0)
+        dx, dweight = self._empty(n, self.dim, dtype=self.dtype), self._empty(self.dim)
+        apart = added and kind != self.dtype
+        dresidual = self._empty(n, self.dim, dtype=kind) if apart else dx if added else None
+        g = NormGrad(sp, op, dp, wp, ss, os_, ds, n, self._whole("rstd", rstd, torch.float32, (n,)), dx.data_ptr(),
+                     dresidual.data_ptr() if apart else None, self.dim, self.dim, dweight.data_ptr(), wt, int(added))
+        self._check(_lib().tbe_norm_backward(self._h, C.byref(g), self._stream()), "tbe_norm_backward")
+        return dx, dresidual, dweight
+
+    def __call__(self, x, weight, residual=None):
+        return _NormFunction.apply(self, x, weight, residual)
+
+
+class _ConvFunction(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, plan, x, offsets, weight, bias, before):
+        ctx.set_materialize_grads(False)
+        ctx.plan = plan
+        ctx.save_for_backward(x, offsets, weight, bias, before)
+        return plan.forward(x, offsets, weight, bias, before)
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dy, dlast):
+        x, offsets, weight, bias, before = ctx.saved_tensors
+        dy = torch.zeros(x.shape, dtype=x.dtype, device=x.device) if dy is None else _own_rows(dy)
+        dx, dweight, dbias, dbefore = ctx.plan.backward(x, offsets, weight, dy, bias, before, _own_rows(dlast))
+        return None, dx, None, dweight.to(weight.dtype), dbias.to(bias.dtype) if bias is not None else None, dbefore
+
+
+class ShortConv(_Handle):
+    """y_t = bias + sum over j < width of weight[:, j] e_{t+j}, or silu of that, over the rows of every bag, element by element, where e is `width` - 1
+    earlier rows of the bag and behind them its rows.
+
+    x: [rows, dim] of `dtype` (rows may lie apart); offsets: int64 [bags + 1] on the GPU; weight: [dim, width], bias: [dim] of its type or None; before:
+    [bags, width - 1, dim] of `dtype` or None (zero).  Calling the object gives (y, last), last being `before` of the bags' continuation and the state of `step`,
+    with gradients to x, weight, bias and before (not with gradients of those: asking for them raises)."""
+    _destroy = "tbe_conv_destroy"
+
+    def __init__(self, dim: int, width: int, dtype: torch.dtype, max_bags: int, max_rows: int, silu: bool = True):
+        super().__init__()
+        if dtype not in DTYPES:
+            raise ValueError(f"rows are {', '.join(map(str, DTYPES))}: got {dtype}")
+        self.dim, self.width, self.dtype = dim, width, dtype
+        self._check(_lib().tbe_conv_create(C.byref(self._h), dim, width, DTYPES[dtype], int(silu), max_bags, max_rows), "tbe_conv_create")
+
+    def _weights(self, weight, bias):
+        if weight.dtype not in DTYPES:
+            raise ValueError(f"weight: {', '.join(map(str, DTYPES))}")
+        return (self._whole("weight", weight, weight.dtype, (self.dim, self.width)),
+                self._whole("bias", bias, weight.dtype, (self.dim,)) if bias is not None else None)
+
+    def _batch(self, x, offsets, weight, bias, before):
+        n = x.shape[0]
+        bags, op = self._offsets(offsets)
+        bp = self._whole("before", before, self.dtype, (bags, self.width - 1, self.dim)) if before is not None else None
+        return ConvBatch(*self._rows_of("x", x, n, self.dim, self.dtype), op, bags, n, *self._weights(weight, bias), bp, DTYPES[weight.dtype])
+
+    def forward(self, x, offsets, weight, bias=None, before=None, y=None, want_last: bool = True):
+        """(y, last); last is None without want_last"""
+        b = self._batch(x, offsets, weight, bias, before)
+        given = y
+        y = self._empty(b.rows, self.dim, dtype=self.dtype) if y is None else y
+        last = self._empty(b.bags, self.width - 1, self.dim, dtype=self.dtype) if want_last else None
+        self._check(_lib().tbe_conv_forward(self._h, C.byref(b), *self._rows_of("y", y, b.rows, self.dim, self.dtype),
+                                            last.data_ptr() if want_last else None, self._stream()), "tbe_conv_forward")
+        if given is not None:
+            _written(given)
+        return y, last
+
+    def backward(self, x, offsets, weight, dy, bias=None, before=None, dlast=None):
+        """(dx, dweight, dbias, dbefore): dweight and dbias fp32; dbias and dbefore are None without bias and before"""
+        b = self._batch(x, offsets, weight, bias, before)
+        dx, dweight = self._empty(b.rows, self.dim, dtype=self.dtype), self._empty(self.dim, self.width)
+        dbias = self._empty(self.dim) if bias is not None else None
+        dbefore = self._empty(b.bags, self.width - 1, self.dim, dtype=self.dtype) if before is not None else None
+        lp = self._whole("dlast", dlast, self.dtype, (b.bags, self.width - 1, self.dim)) if dlast is not None else None
+        self._check(_lib().tbe_conv_backward(self._h, C.byref(b), *self._rows_of("dy", dy, b.rows, self.dim, self.dtype), lp, dx.data_ptr(), self.dim,
+                                             dweight.data_ptr(), dbias.data_ptr() if dbias is not None else None,
+                                             dbefore.data_ptr() if dbefore is not None else None, self._stream()), "tbe_conv_backward")
+        return dx, dweight, dbias, dbefore
+
+    def __call__(self, x, offsets, weight, bias=None, before=None):
+        return _ConvFunction.apply(self, x, offsets, weight, bias, before)
+
+    def step(self, state, x, weight, bias=None, slots=None, y=None):
+        """one more row for the states `slots` ([states, width - 1, dim]; int64; None: the first ones), in place; returns y"""
+        n = x.shape[0]
+        b = ConvBatch(*self._rows_of("x", x, n, self.dim, self.dtype), None, 0, n, *self._weights(weight, bias), None, DTYPES[weight.dtype])
+        written = (state,) if y is None else (state, y)
+        y = self._empty(n, self.dim, dtype=self.dtype) if y is None else y
+        sp = self._whole("state", state, self.dtype, (state.shape[0], self.width - 1, self.dim))
+        self._check(_lib().tbe_conv_step(self._h, C.byref(b), sp, state.shape[0], self._slots(slots, n), *self._rows_of("y", y, n, self.dim, self.dtype),
+                                         self._stream()), "tbe_conv_step")
+        _written(written)
+        return y
+
+    def check(self):
+        """waits, and raises if a call had offsets that do not ascend from 0 to its rows, or a slot that is none of the states"""
+        self._check(_lib().tbe_conv_check(self._h, self._stream()), "tbe_conv_check")
+
+
+class _SsmFunction(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, plan, x, delta, a, b, c, offsets, skip, delta_bias, z, h0):
+        y, last, saved = plan.forward(x, delta, a, b, c, offsets, skip, delta_bias, z, h0, save=True)
+        ctx.set_materialize_grads(False)
+        ctx.plan = plan
+        ctx.save_for_backward(x, delta, a, b, c, offsets, skip, delta_bias, z, h0, saved)
+        return y, last
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dy, dlast):
+        x, delta, a, b, c, offsets, skip, delta_bias, z, h0, saved = ctx.saved_tensors
+        dy = torch.zeros(x.shape, dtype=x.dtype, device=x.device) if dy is None else _own_rows(dy)
+        g = ctx.plan.backward(x, delta, a, b, c, offsets, saved, dy, _own_rows(dlast), skip, delta_bias, z, h0)
+        return (None, *(g.get(k) for k in ("x", "delta", "a", "b", "c")), None, *(g.get(k) for k in ("skip", "delta_bias", "z", "h0")))
+
+
+class SelectiveScan(_Handle):
+    """With D = softplus(delta + delta_bias): h_t[n] = exp(D_t a[n]) h_{t-1}[n] + D_t b_t[n] x_t,  y_t = sum over n of c_t[n] h_t[n] + skip x_t, times silu(z_t),
+    over the rows of every bag, for each element of a row.
+
+    x, delta, z: [rows, dim], b, c: [rows, groups * states] of `dtype` (rows may lie apart); a: fp32 [dim, states], skip, delta_bias: fp32 [dim]; offsets: int64 [bags + 1]
+    on the GPU; h0: fp32 [bags, dim, states] (bags may be expanded from one); skip, delta_bias, z, h0 may be None.  groups: each has a b and c of its own; more than
+    one only with a multiple of 64 elements each.  Calling the object gives (y, last), last fp32 [bags, dim, states] being h0 of the bags' continuation and the
+    state of `step`, with gradients to everything but offsets (not with gradients of those: asking for them raises)."""
+    _destroy = "tbe_ssm_destroy"
+
+    def __init__(self, dim: int, states: int, dtype: torch.dtype, max_bags: int, max_rows: int, groups: int = 1):
+        super().__init__()
+        if dtype not in DTYPES:
+            raise ValueError(f"rows are {', '.join(map(str, DTYPES))}: got {dtype}")
+        self.dim, self.states, self.groups, self.dtype = dim, states, groups, dtype
+        self._check(_lib().tbe_ssm_create(C.byref(self._h), dim, states, groups, DTYPES[dtype], max_bags, max_rows), "tbe_ssm_create")
+
+    def _batch(self, x, delta, a, b, c, skip, delta_bias, z, offsets=None, h0=None):
+        n, d, k, dt = x.shape[0], self.dim, self.groups * self.states, self.dtype
+        (xp, xs), (tp, ts), (bp, bs), (cp, cs) = self._rows_of("x", x, n, d, dt), self._rows_of("delta", delta, n, d, dt), self._rows_of("b", b, n, k, dt), \
+            self._rows_of("c", c, n, k, dt)
+        zp, zs = self._rows_of("z", z, n, d, dt) if z is not None else (None, 0)
+        bags, op = self._offsets(offsets) if offsets is not None else (0, None)
+        hp, hs = None, 0
+        if h0 is not None:
+            hp, hs = self._tensor("h0", h0, torch.float32, (bags, d, self.states)), h0.stride(0) if bags > 1 else d * self.states
+            if bags and not h0[0].is_contiguous():
+                raise ValueError("h0: the states of a bag lie one behind another")
+        vector = lambda name, t: self._whole(name, t, torch.float32, (d,)) if t is not None else None  # noqa: E731
+        return SsmBatch(xp, tp, zp, bp, cp, xs, ts, zs, bs, cs, self._whole("a", a, torch.float32, (d, self.states)), vector("skip", skip),
+                        vector("delta_bias", delta_bias), op, bags, n, hp, hs)
+
+    def forward(self, x, delta, a, b, c, offsets, skip=None, delta_bias=None, z=None, h0=None, y=None, want_last: bool = True, save: bool = False):
+        """(y, last, saved): last fp32 [bags, dim, states] after the last rows (None without want_last), what `backward` needs"""
+        t = self._batch(x, delta, a, b, c, skip, delta_bias, z, offsets, h0)
+        given = y
+        y = self._empty(t.rows, self.dim, dtype=self.dtype) if y is None else y
+        last = self._empty(t.bags, self.dim, self.states) if want_last else None
+        saved = self._empty(self._check(_lib().tbe_ssm_saved_floats(self._h, t.rows), "tbe_ssm_saved_floats")) if save else None
+        self._check(_lib().tbe_ssm_forward(self._h, C.byref(t), *self._rows_of("y", y, t.rows, self.dim, self.dtype), last.data_ptr() if want_last else None,
+                                           saved.data_ptr() if save else None, self._stream()), "tbe_ssm_forward")
+        if given is not None:
+            _written(given)
+        return y, last, saved
+
+    def backward(self, x, delta, a, b, c, offsets, saved, dy, dlast=None, skip=None, delta_bias=None, z=None, h0=None) -> Dict[str, torch.Tensor]:
+        """gradients by the arguments' names: of x, delta, a, b, c and of those of skip, delta_bias, z, h0 that there are (a, skip, delta_bias, h0 fp32)"""
+        t = self._batch(x, delta, a, b, c, skip, delta_bias, z, offsets, h0)
+        n, d, dt = t.rows, self.dim, self.dtype
+        sp = self._whole("saved", saved, torch.float32, (self._check(_lib().tbe_ssm_saved_floats(self._h, n), "tbe_ssm_saved_floats"),))
+        dyp = self._rows_of("dy", dy, n, d, dt)
+        lp = self._whole("dlast", dlast, torch.float32, (t.bags, d, self.states)) if dlast is not None else None
+        g = {"x": self._empty(n, d, dtype=dt), "delta": self._empty(n, d, dtype=dt), "a": self._empty(d, self.states),
+             "b": self._empty(n, self.groups * self.states, dtype=dt), "c": self._empty(n, self.groups * self.states, dtype=dt)}
+        if skip is not None:
+            g["skip"] = self._empty(d)
+        if delta_bias is not None:
+            g["delta_bias"] = self._empty(d)
+        if z is not None:
+            g["z"] = self._empty(n, d, dtype=dt)
+        if h0 is not None:
+            g["h0"] = self._empty(t.bags, d, self.states)
+        at = {k: v.data_ptr() for k, v in g.items()}
+        s = SsmGrads(*dyp, lp, *(at.get(k) for k in ("x", "delta", "z", "b", "c", "a", "skip", "delta_bias", "h0")))
+        self._check(_lib().tbe_ssm_backward(self._h, C.byref(t), sp, C.byref(s), self._stream()), "tbe_ssm_backward")
+        return g
+
+    def __call__(self, x, delta, a, b, c, offsets, skip=None, delta_bias=None, z=None, h0=None):
+        return _SsmFunction.apply(self, x, delta, a, b, c, offsets, skip, delta_bias, z, h0)
+
+    def step(self, state, x, delta, a, b, c, skip=None, delta_bias=None, z=None, slots=None, y=None):
+        """one more row for the states `slots` (fp32 [states of the store, dim, states], a store's states may lie apart; int64; None: the first ones), in place; returns y"""
+        t = self._batch(x, delta, a, b, c, skip, delta_bias, z)
+        n, count = t.rows, state.shape[0]
+        sp = self._tensor("state", state, torch.float32, (count, self.dim, self.states))
+        if count and not state[0].is_contiguous():
+            raise ValueError("state: the states of a slot lie one behind another")
+        written = (state,) if y is None else (state, y)
+        y = self._empty(n, self.dim, dtype=self.dtype) if y is None else y
+        self._check(_lib().tbe_ssm_step(self._h, C.byref(t), sp, state.stride(0) if count > 1 else self.dim * self.states, count, self._slots(slots, n),
+                                        *self._rows_of("y", y, n, self.dim, self.dtype), self._stream()), "tbe_ssm_step")
+        _written(written)
+        return y
+
+    def check(self):
+        """waits, and raises if a call had offsets that do not ascend from 0 to its rows, or a slot that is none of the states"""
+        self._check(_lib().tbe_ssm_check(self._h, self._stream()), "tbe_ssm_check")
