@@ -732,7 +732,7 @@ typedef struct {
   const float *d_h0;                /* [dim, states] of each bag, h0_stride apart (0: one for all), or null */
   int64_t h0_stride;
 } tbe_ssm_batch;
-/* fp32 numbers that tbe_ssm_forward leaves in d_saved for the backward of `rows` rows: the states before every 16th row */
+/* fp32 numbers that tbe_ssm_forward leaves in d_saved for the backward of `rows` rows: the states before every 8th row */
 int64_t tbe_ssm_saved_floats(tbe_ssm_handle s, int64_t rows);
 /* Writes d_y and, each unless null, d_last (fp32 [bags, dim, states], h after a bag's last row) and d_saved. */
 int tbe_ssm_forward(tbe_ssm_handle s, const tbe_ssm_batch *batch, void *d_y, int64_t y_stride, float *d_last, float *d_saved, void *stream);

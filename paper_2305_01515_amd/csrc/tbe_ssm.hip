@@ -14,7 +14,7 @@
 //   rows     every unit from the state before it                                                (ssm_kernel, ssm_grad_kernel)
 // Where no bag is longer than two units, `ends` and `join` find nothing to do.
 // Forward: a lane has an element with all of its states in registers, b and c come from LDS.  Backward: a lane has four states of an
-// element, so that 16 rows' w and decays stay in registers on the way back; states before every 16th row were saved by the forward.
+// element, so that 8 rows' w and decays stay in registers on the way back; states before every 8th row were saved by the forward.
 #include <algorithm>
 #include <new>
 
@@ -24,7 +24,8 @@ using namespace tbe;
 
 namespace {
 
-constexpr int kBlock = 16;       // rows that are staged at once; states before each block are what the backward goes from
+constexpr int kBlock = 16;       // rows that the forward stages at once
+constexpr int kSaved = 8;        // states before every so many rows are what the backward goes from: that many rows' w and decays fit its registers
 constexpr int kSegment = 64;     // units that a lane of `join` goes through
 constexpr int kMostStates = 64;
 constexpr int kThreads = 256;
@@ -49,7 +50,7 @@ struct SsmArgs {
   float *last, *saved, *dh0;
   // scratch
   Unit *units;
-  int2 *marks;      // [rows]: the bag that starts at a row, the bag whose last row it is; what the offsets do not confirm is of another call
+  int2 *marks;      // [rows]: the bag that starts at a row, the bag whose last row it is (-1: none)
   float *ends;      // [units][dim][NP]: states at the ends; `join` puts what is before (behind) each unit in their place
   float *spans;     // [units][dim]: sums of D
   float *reach;     // [units][dim]: sum of D from the segment's start; negative: nothing of it gets here
@@ -78,23 +79,19 @@ __device__ inline int64_t count_up_to(const int64_t *off, int64_t n, int64_t row
   return lo;
 }
 
-// Marks of the bags' first and last rows, what empty bags have, the units; offsets that do not ascend from 0 to rows are reported.
+// The units and the marks of their rows, what empty bags have; offsets that do not ascend from 0 to rows are reported.
 // empty_to (or null): [bags, dim, states] that an empty bag has of empty_from (null: zero).
+constexpr int kMostUnit = 128;
 __global__ __launch_bounds__(kThreads) void ssm_prepare_kernel(SsmArgs a, int64_t bag_groups, float *empty_to, const float *empty_from, int64_t empty_stride) {
+  __shared__ int2 marks[kThreads / 64][kMostUnit];
   const int lane = threadIdx.x & 63;
   if (blockIdx.x < bag_groups) {
     const int64_t b = (int64_t)blockIdx.x * kThreads + threadIdx.x;
     bool empty = false;
     if (b < a.bags) {
       const int64_t s = a.off[b], e = a.off[b + 1];
-      if (s > e || s < 0 || e > a.rows || (b == 0 && s != 0) || (b == a.bags - 1 && e != a.rows)) {
-        *a.err = 1;
-      } else if (s == e) {
-        empty = true;
-      } else {
-        a.marks[s].x = (int)b;
-        a.marks[e - 1].y = (int)b;
-      }
+      if (s > e || s < 0 || e > a.rows || (b == 0 && s != 0) || (b == a.bags - 1 && e != a.rows)) *a.err = 1;
+      else empty = s == e;
     }
     if (!empty_to) return;
     const int64_t n = (int64_t)a.dim * a.states;
@@ -105,17 +102,34 @@ __global__ __launch_bounds__(kThreads) void ssm_prepare_kernel(SsmArgs a, int64_
     return;
   }
   const int64_t k = ((int64_t)blockIdx.x - bag_groups) * (kThreads / 64) + threadIdx.x / 64;
-  if (k > a.count) return;
-  const int64_t r = k * a.unit;
+  const int64_t r = k * a.unit, to = min(r + a.unit, a.rows);
+  const bool some = k < a.count;  // a wavefront without a unit waits with the others
   Unit u{a.rows, 0, 0};
-  if (r < a.rows) {
-    const int64_t b = max(count_up_to(a.off, a.bags, r) - 1, (int64_t)0), s = a.off[b], e = a.off[b + 1];
-    u.bag = (int)b;
+  int2 *m = marks[threadIdx.x / 64];
+  int64_t head = 0;
+  if (some) {
+    head = max(count_up_to(a.off, a.bags, r) - 1, (int64_t)0);
+    const int64_t s = a.off[head], e = a.off[head + 1];
+    u.bag = (int)head;
     u.cut = s != r && e - s > 2 * a.unit;
     // (offsets that do not ascend: the unit still begins within its own rows and those of the next two)
     u.begin = s == r || u.cut ? r : min(max(e, r), min(r + 2 * a.unit, a.rows));
+    for (int i = lane; i < a.unit; i += 64) m[i] = {-1, -1};
   }
-  if (lane == 0) a.units[k] = u;
+  if (lane == 0 && k <= a.count) a.units[k] = u;
+  __syncthreads();
+  if (some) {
+    for (int64_t b = head + lane; b < a.bags; b += 64) {
+      const int64_t s = a.off[b], e = a.off[b + 1];
+      if (s >= to) break;
+      if (e <= s) continue;
+      if (s >= r) m[s - r].x = (int)b;
+      if (e > r && e <= to) m[e - 1 - r].y = (int)b;
+    }
+  }
+  __syncthreads();
+  if (some)
+    for (int64_t i = lane; i < to - r; i += 64) a.marks[r + i] = m[i];
 }
 
 // D = log(1 + exp(u)): with e = exp(-|u|) and w = 1 + e rounded, log(1 + e) is log(w) and what the rounding left out
@@ -152,12 +166,9 @@ struct Marks {
 };
 __device__ inline Marks marks_of(const SsmArgs &a, int64_t row0, int lo, int hi) {
   const int t = threadIdx.x & 63;
-  const int64_t r = row0 + t;
   int2 m = {-1, -1};
-  if (t >= lo && t < hi) m = a.marks[r];
-  const bool starts = m.x >= 0 && m.x < a.bags && a.off[m.x] == r && a.off[m.x + 1] > r;
-  const bool ends = m.y >= 0 && m.y < a.bags && a.off[m.y + 1] == r + 1 && a.off[m.y] <= r;
-  return {(uint32_t)__ballot(starts), (uint32_t)__ballot(ends), m};
+  if (t >= lo && t < hi) m = a.marks[row0 + t];
+  return {(uint32_t)__ballot(m.x >= 0), (uint32_t)__ballot(m.y >= 0), m};
 }
 
 // What a lane's element has of a row, read ahead
@@ -181,11 +192,18 @@ __global__ __launch_bounds__(64) void ssm_kernel(SsmArgs a) {
 #pragma unroll
   for (int n = 0; n < NP; ++n) {
     a2[n] = FULL || n < N ? a.a[(int64_t)dc * N + n] * kLog2e : 0.0f;
-    h[n] = u.cut && (FULL || n < N) ? start_of<NP>(a, k, dc, n, a2[n]) : 0.0f;
+    h[n] = 0.0f;
+  }
+  if (u.cut) {
+#pragma unroll
+    for (int n = 0; n < NP; ++n) h[n] = FULL || n < N ? start_of<NP>(a, k, dc, n, a2[n]) : 0.0f;
   }
   const float bias = a.bias ? a.bias[dc] : 0.0f, skip = a.skip ? a.skip[dc] : 0.0f;
-  const E *x = (const E *)a.x + dc, *delta = (const E *)a.delta + dc, *z = a.z ? (const E *)a.z + dc : nullptr;
+  const bool gated = a.z;
+  const E *x = (const E *)a.x + dc, *delta = (const E *)a.delta + dc, *z = (const E *)(gated ? a.z : a.x) + dc;
+  const int64_t zs = gated ? a.zs : a.xs;
   E *y = (E *)a.y + d;
+  // Four rows are read ahead of those that are gone through, b, c and marks a block ahead.
   Raw<E> ahead[4];
   auto read = [&](int64_t r0) {
 #pragma unroll
@@ -193,34 +211,63 @@ __global__ __launch_bounds__(64) void ssm_kernel(SsmArgs a) {
       const int64_t r = min(max(r0 + i, begin), end - 1);
       ahead[i].x = x[r * a.xs];
       ahead[i].u = delta[r * a.ts];
-      if (z) ahead[i].z = z[r * a.zs];
+      ahead[i].z = z[r * zs];
     }
   };
+  constexpr int PIECES = kBlock * 2 * NP / 64;  // of a block's b and c that a lane brings: number `mine` of rows `mine_row`, + ROWS, ...
+  constexpr int ROWS = 64 / (2 * NP) > 0 ? 64 / (2 * NP) : 1, PARTS = 2 * NP > 64 ? 2 * NP / 64 : 1;
+  E shared[PIECES];
+  int2 mark;
+  auto bring = [&](int64_t row0) {
+#pragma unroll
+    for (int p = 0; p < PIECES; ++p) {
+      const int n = PARTS > 1 ? p % PARTS * 64 + lane : lane % (2 * NP), t = PARTS > 1 ? p / PARTS : p * ROWS + lane / (2 * NP);
+      const int64_t r = min(max(row0 + t, begin), end - 1);
+      const int at = group * N + min(n % NP, N - 1);
+      shared[p] = n < NP ? ((const E *)a.b)[r * a.bs + at] : ((const E *)a.c)[r * a.cs + at];
+    }
+    mark = a.marks[min(max(row0 + (lane & (kBlock - 1)), begin), end - 1)];
+  };
+  const int64_t from = begin & ~(int64_t)(kBlock - 1);
+  bring(from);
   read(begin & ~3ll);
-  for (int64_t row0 = begin & ~(int64_t)(kBlock - 1); row0 < end; row0 += kBlock) {
+  for (int64_t row0 = from; row0 < end; row0 += kBlock) {
     const int lo = (int)max(begin - row0, (int64_t)0), hi = (int)min(end - row0, (int64_t)kBlock);
     __syncthreads();
-    stage<E, NP, 64>(a, row0, lo, hi, group, bc, true, true);
-    const Marks m = marks_of(a, row0, lo, hi);
-    __syncthreads();
-    if (a.saved && lo == 0 && in) {
-      float *to = a.saved + (row0 / kBlock * a.dim + d) * NP;
 #pragma unroll
-      for (int n = 0; n < NP; n += 4) *(float4 *)(to + n) = make_float4(h[n], h[n + 1], h[n + 2], h[n + 3]);
+    for (int p = 0; p < PIECES; ++p) {
+      const int n = PARTS > 1 ? p % PARTS * 64 + lane : lane % (2 * NP), t = PARTS > 1 ? p / PARTS : p * ROWS + lane / (2 * NP);
+      bc[t][n] = FULL || n % NP < N ? (float)shared[p] : 0.0f;
     }
+    const int2 bag_of = mark;
+    const bool mine = lane >= lo && lane < hi;
+    const uint32_t starts = (uint32_t)__ballot(mine && mark.x >= 0), ends = (uint32_t)__ballot(mine && mark.y >= 0);
+    bring(row0 + kBlock);
+    __syncthreads();
     for (int t0 = lo & ~3; t0 < hi; t0 += 4) {
       Raw<E> now[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) now[i] = ahead[i];
       read(row0 + t0 + 4);
+      if (a.saved && (t0 & (kSaved - 1)) == 0 && t0 >= lo && in) {
+        float *to = a.saved + ((row0 + t0) / kSaved * a.dim + d) * NP;
+#pragma unroll
+        for (int n = 0; n < NP; n += 4) *(float4 *)(to + n) = make_float4(h[n], h[n + 1], h[n + 2], h[n + 3]);
+      }
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const int t = t0 + i;
         if (t < lo || t >= hi) continue;
-        if (m.starts >> t & 1) {
-          const int64_t bag = __builtin_amdgcn_readlane(m.bag.x, t);
+        if (starts >> t & 1) {
+          const int64_t bag = __builtin_amdgcn_readlane(bag_of.x, t);
+          if (a.h0) {
+            const float *p = a.h0 + bag * a.h0s + (int64_t)dc * N;
 #pragma unroll
-          for (int n = 0; n < NP; ++n) h[n] = a.h0 && (FULL || n < N) ? a.h0[bag * a.h0s + (int64_t)dc * N + n] : 0.0f;
+            for (int n = 0; n < NP; ++n) h[n] = FULL || n < N ? p[n] : 0.0f;
+          } else {
+#pragma unroll
+            for (int n = 0; n < NP; ++n) h[n] = 0.0f;
+          }
         }
         const float xv = (float)now[i].x, step = soft((float)now[i].u + bias), sx = step * xv;
         float v = skip * xv;
@@ -230,13 +277,13 @@ __global__ __launch_bounds__(64) void ssm_kernel(SsmArgs a) {
           h[n] = FULL || n < N ? g : 0.0f;
           v += bc[t][NP + n] * h[n];
         }
-        if (z) {
+        if (gated) {
           const float zv = (float)now[i].z;
           v *= zv * sigmoid(zv);
         }
         if (in) y[(row0 + t) * a.ys] = (E)v;
-        if ((m.ends >> t & 1) && a.last && in) {
-          const int64_t bag = __builtin_amdgcn_readlane(m.bag.y, t);
+        if ((ends >> t & 1) && a.last && in) {
+          const int64_t bag = __builtin_amdgcn_readlane(bag_of.y, t);
           float *to = a.last + (bag * a.dim + d) * N;
 #pragma unroll
           for (int n = 0; n < NP; ++n)
@@ -418,190 +465,225 @@ __global__ __launch_bounds__(64) void ssm_segments_kernel(SsmArgs a, int64_t seg
   }
 }
 
+template <int CTRL>
+__device__ inline float moved(float v) {  // of the lane that CTRL says, in the same 16 lanes
+  return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, 0xF, 0xF, true));
+}
+constexpr int kSwap1 = 0xB1, kSwap2 = 0x4E, kMirror8 = 0x141, kMirror16 = 0x140, kTurn8 = 0x128, kAhead4 = 0x104;
+
 // sum over the LPC lanes that share an element, the same in all of them
 template <int LPC>
 __device__ inline float lane_sum(float v) {
-#pragma unroll
-  for (int o = 1; o < LPC; o *= 2) v += __shfl_xor(v, o);
+  v += moved<kSwap1>(v);
+  v += moved<kSwap2>(v);
+  if constexpr (LPC >= 8) v += moved<kMirror8>(v);
+  if constexpr (LPC >= 16) v += moved<kMirror16>(v);
   return v;
 }
 
 // Sums over the elements of a wavefront of 8 numbers a lane (db and dc of four states), to LDS: with each step half of the numbers go to
-// half of the lanes.
-template <int LEFT, int BIT, int LPC>
-__device__ inline void halve(float (&v)[8], int &first) {
-  if constexpr (BIT >= LPC) {
-    if constexpr (LEFT > 1) {
-      constexpr int half = LEFT / 2;
-      const bool up = threadIdx.x & BIT;
+// half of the lanes, by exchanges of halves and of 16 lanes between two registers.
+template <int HALF>
+__device__ inline void halve32(float (&v)[8]) {
 #pragma unroll
-      for (int i = 0; i < half; ++i) {
-        const float keep = up ? v[i + half] : v[i], send = up ? v[i] : v[i + half];
-        v[i] = keep + __shfl_xor(send, BIT);
-      }
-      first += up ? half : 0;
-      halve<half, BIT / 2, LPC>(v, first);
-    } else {
-      v[0] += __shfl_xor(v[0], BIT);
-      halve<1, BIT / 2, LPC>(v, first);
-    }
+  for (int i = 0; i < HALF; ++i) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(unsigned, v[i]), __builtin_bit_cast(unsigned, v[i + HALF]), false, false);
+    const unsigned low = r[0], high = r[1];  // (a cast of the element itself is compiled to one of the first, ROCm 7.2)
+    v[i] = __builtin_bit_cast(float, low) + __builtin_bit_cast(float, high);
   }
 }
-template <int NP>
-__device__ inline void sum_elements(float (&v)[8], float *to) {
-  constexpr int LPC = NP / 4, left = LPC == 16 ? 2 : 1;
-  const int lane = threadIdx.x & 63, q = lane % LPC;
-  int first = 0;
-  halve<8, 32, LPC>(v, first);
-  if (LPC == 4 && (lane & 4)) return;  // whose number is another lane's too
+template <int HALF>
+__device__ inline void halve16(float (&v)[8]) {
 #pragma unroll
-  for (int i = 0; i < left; ++i) {
-    const int m = first + i;
-    to[(m >= 4 ? NP : 0) + 4 * q + (m & 3)] = v[i];
+  for (int i = 0; i < HALF; ++i) {
+    const auto r = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(unsigned, v[i]), __builtin_bit_cast(unsigned, v[i + HALF]), false, false);
+    const unsigned low = r[0], high = r[1];
+    v[i] = __builtin_bit_cast(float, low) + __builtin_bit_cast(float, high);
+  }
+}
+// where lane `lane` has its numbers after that: place of the first one of a row's 2 NP, and whether they are another lane's too
+template <int NP>
+__device__ inline int place_of(int lane) {
+  constexpr int LPC = NP / 4;
+  int m = (lane & 32 ? 4 : 0) + (lane & 16 ? 2 : 0);
+  if (LPC <= 8) m += lane & 8 ? 1 : 0;
+  return (m >= 4 ? NP : 0) + 4 * (lane % LPC) + (m & 3);
+}
+template <int NP>
+__device__ inline void sum_elements(float (&v)[8], float *to, bool up8, bool give) {
+  constexpr int LPC = NP / 4;
+  halve32<4>(v);
+  halve16<2>(v);
+  if constexpr (LPC <= 8) {
+    const float keep = up8 ? v[1] : v[0], send = up8 ? v[0] : v[1];
+    v[0] = keep + moved<kTurn8>(send);
+    if constexpr (LPC == 4) v[0] += moved<kAhead4>(v[0]);  // in the lanes that give
+    if (give) to[0] = v[0];
+  } else {
+    to[0] = v[0];
+    to[1] = v[1];
   }
 }
 
-// Backward of a unit's rows: a lane has states 4 q .. 4 q + 3 of an element; a workgroup's wavefronts have elements side by side.
+// Backward of a unit's rows: a lane has states 4 q .. 4 q + 3 of an element; a workgroup's wavefronts have elements side by side.  Rows are gone
+// through in blocks of kSaved, last block first, each bag's rows of a block at a time: forward from the state before them, w and
+// the decays kept in registers, and back.
 template <class E, int NP>
-__global__ __launch_bounds__(64 * kGradWaves) void ssm_grad_kernel(SsmArgs a, int waves) {
-  constexpr int LPC = NP / 4, CPW = 64 / LPC, OWN = kBlock / LPC;  // lanes of an element, elements of a wavefront, rows whose scalars a lane finds
+__global__ __launch_bounds__(64 * kGradWaves, 2) void ssm_grad_kernel(SsmArgs a, int waves) {
+  constexpr int S = kSaved, LPC = NP / 4, CPW = 64 / LPC, OWN = (S + LPC - 1) / LPC;  // lanes of an element, elements of a wavefront, rows whose scalars a lane finds
   extern __shared__ float4 lds[];
-  float(*bc)[2 * NP] = (float(*)[2 * NP])lds;                                // [kBlock][2 NP]
-  float *part = (float *)lds + kBlock * 2 * NP;                              // [waves][kBlock][2 NP]
+  float(*bc)[2 * NP] = (float(*)[2 * NP])lds;                           // [S][2 NP]
+  float *part = (float *)lds + S * 2 * NP;                              // [waves][S][2 NP]
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, q = lane % LPC, e = lane / LPC, N = a.states;
-  float4(*row)[CPW] = (float4(*)[CPW])(part + waves * kBlock * 2 * NP) + wave * kBlock;  // [kBlock][CPW] of each wavefront: D, D x, dv
+  float4(*row)[CPW] = (float4(*)[CPW])(part + waves * S * 2 * NP) + wave * S;  // [S][CPW] of each wavefront: D, D x, dv, x
+  float *mine = part + wave * S * 2 * NP + place_of<NP>(lane);
+  const bool up8 = lane & 8, give = LPC != 4 || !(lane & 4);
   const int64_t worker = blockIdx.x / a.blocks;
   const int block = (int)(blockIdx.x % a.blocks), d = (block * waves + wave) * CPW + e, dc = min(d, a.dim - 1);
   const bool in = d < a.dim;
   const int group = a.groups > 1 ? block * waves * CPW / (a.dim / a.groups) : 0;
-  float av[4], a2[4], da[4] = {0.0f, 0.0f, 0.0f, 0.0f}, dskip = 0.0f, dbias = 0.0f;
+  float av[4], da[4] = {0.0f, 0.0f, 0.0f, 0.0f}, dskip = 0.0f, dbias = 0.0f;
 #pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    av[j] = 4 * q + j < N ? a.a[(int64_t)dc * N + 4 * q + j] : 0.0f;
-    a2[j] = av[j] * kLog2e;
-  }
+  for (int j = 0; j < 4; ++j) av[j] = 4 * q + j < N ? a.a[(int64_t)dc * N + 4 * q + j] : 0.0f;
   const float bias = a.bias ? a.bias[dc] : 0.0f, skip = a.skip ? a.skip[dc] : 0.0f;
+  const bool gated = a.z;
+  // four states of [.., dim, states] numbers; nothing beyond the states
+  auto four = [&](const float *p, float (&to)[4]) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) to[j] = p && 4 * q + j < N ? p[(int64_t)dc * N + 4 * q + j] : 0.0f;
+  };
   for (int64_t k = worker; k < a.count; k += a.workers) {
     const int64_t begin = a.units[k].begin, end = a.units[k + 1].begin;
     if (begin >= end) continue;
-    float carry[4];  // exp(D a) g of the row behind
+    float carry[4] = {0.0f, 0.0f, 0.0f, 0.0f};  // exp(D a) g of the row behind
+    if (a.units[k + 1].cut) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) carry[j] = a.units[k + 1].cut && 4 * q + j < N ? start_of<NP>(a, k, dc, 4 * q + j, a2[j]) : 0.0f;
-    for (int64_t row0 = (end - 1) & ~(int64_t)(kBlock - 1); row0 + kBlock > begin; row0 -= kBlock) {
-      const int lo = (int)max(begin - row0, (int64_t)0), hi = (int)min(end - row0, (int64_t)kBlock);
-      __syncthreads();
-      for (int i = threadIdx.x; i < kBlock * 2 * NP; i += 64 * waves) {
-        const int t = i / (2 * NP), n = i % (2 * NP), s = n % NP;
-        const bool have = t >= lo && t < hi && s < N;
-        const int64_t r = row0 + t;
-        bc[t][n] = have ? (float)(n < NP ? ((const E *)a.b)[r * a.bs + group * N + s] : ((const E *)a.c)[r * a.cs + group * N + s]) : 0.0f;
-      }
+      for (int j = 0; j < 4; ++j) carry[j] = 4 * q + j < N ? start_of<NP>(a, k, dc, 4 * q + j, av[j] * kLog2e) : 0.0f;
+    }
+    for (int64_t row0 = (end - 1) & ~(int64_t)(S - 1); row0 + S > begin; row0 -= S) {
+      const int lo = (int)max(begin - row0, (int64_t)0), hi = (int)min(end - row0, (int64_t)S);
       const Marks m = marks_of(a, row0, lo, hi);
+      float saved[4] = {0.0f, 0.0f, 0.0f, 0.0f};  // (a unit that begins within a block begins with a bag)
+      if (lo == 0) {
+        const float4 s = *(const float4 *)(a.saved + (row0 / S * a.dim + dc) * NP + 4 * q);
+        saved[0] = s.x, saved[1] = s.y, saved[2] = s.z, saved[3] = s.w;
+      }
       // scalars of the rows t with t % LPC = q
-      float xv[OWN], step[OWN], slope[OWN], dv[OWN], gate[OWN], own_v[OWN], own_b[OWN], own_w[OWN];
+      float slope[OWN], gate[OWN], own_v[OWN], own_b[OWN], own_w[OWN];
+      E in_x[OWN], in_u[OWN], in_y[OWN], in_z[OWN];
 #pragma unroll
       for (int i = 0; i < OWN; ++i) {
-        const int t = i * LPC + q;
+        const int t = min(i * LPC + q, S - 1);
         const int64_t r = row0 + min(max(t, lo), hi - 1);
-        xv[i] = (float)((const E *)a.x)[r * a.xs + dc];
-        const float u = (float)((const E *)a.delta)[r * a.ts + dc] + bias, dy = (float)((const E *)a.dy)[r * a.dys + dc];
-        step[i] = soft(u);
+        in_x[i] = ((const E *)a.x)[r * a.xs + dc];
+        in_u[i] = ((const E *)a.delta)[r * a.ts + dc];
+        in_y[i] = ((const E *)a.dy)[r * a.dys + dc];
+        in_z[i] = gated ? ((const E *)a.z)[r * a.zs + dc] : (E)0.0f;
+      }
+      __syncthreads();  // what the block before has left in LDS has been read
+      for (int i = threadIdx.x; i < S * 2 * NP; i += 64 * waves) {
+        const int t = i / (2 * NP), n = i % (2 * NP);
+        const int64_t r = row0 + min(max(t, lo), hi - 1);
+        const int at = group * N + min(n % NP, N - 1);
+        const float v = (float)(n < NP ? ((const E *)a.b)[r * a.bs + at] : ((const E *)a.c)[r * a.cs + at]);
+        bc[t][n] = n % NP < N ? v : 0.0f;
+      }
+#pragma unroll
+      for (int i = 0; i < OWN; ++i) {
+        const float u = (float)in_u[i] + bias, dy = (float)in_y[i], step = soft(u), x = in ? (float)in_x[i] : 0.0f;
+        float dv = dy;
         slope[i] = sigmoid(u);
-        dv[i] = dy;
         gate[i] = 0.0f;
-        if (a.z) {
-          const float z = (float)((const E *)a.z)[r * a.zs + dc], f = sigmoid(z);
-          dv[i] = dy * z * f;
+        if (gated) {
+          const float z = (float)in_z[i], f = sigmoid(z);
+          dv = dy * z * f;
           gate[i] = dy * (f * (1.0f + z * (1.0f - f)));
         }
-        if (!in) dv[i] = xv[i] = 0.0f;  // elements beyond the row have no part of db and dc
+        if (!in) dv = 0.0f;  // elements beyond the row have no part of db and dc
         own_v[i] = own_b[i] = own_w[i] = 0.0f;
-        row[t][e] = make_float4(step[i], step[i] * xv[i], dv[i], 0.0f);
+        if (i * LPC + q < S) row[i * LPC + q][e] = make_float4(step, step * x, dv, x);
       }
       __syncthreads();
-      // forward: w and the decays of the block's rows
-      float h[4], w[kBlock][4], decay[kBlock][4];
-      if (lo == 0) {
-        const float4 s = *(const float4 *)(a.saved + (row0 / kBlock * a.dim + dc) * NP + 4 * q);
-        h[0] = s.x, h[1] = s.y, h[2] = s.z, h[3] = s.w;
-      } else {
+      // the bags' rows [from, to) of the block, from the last
+      for (int to = hi; to > lo;) {
+        const uint32_t before = m.starts & ((1u << to) - 1);
+        const bool starts = before != 0;
+        const int from = starts ? 31 - __builtin_clz(before) : lo;
+        float h[4], w[S][4], decay[S][4];
+        if (starts) {
+          four(a.h0 ? a.h0 + (int64_t)__builtin_amdgcn_readlane(m.bag.x, from) * a.h0s : nullptr, h);
+        } else {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) h[j] = 0.0f;
-      }
-#pragma unroll
-      for (int t = 0; t < kBlock; ++t) {
-        if (t < lo || t >= hi) continue;
-        if (m.starts >> t & 1) {
-          const int64_t bag = __builtin_amdgcn_readlane(m.bag.x, t);
-#pragma unroll
-          for (int j = 0; j < 4; ++j) h[j] = a.h0 && 4 * q + j < N ? a.h0[bag * a.h0s + (int64_t)dc * N + 4 * q + j] : 0.0f;
+          for (int j = 0; j < 4; ++j) h[j] = saved[j];
         }
-        const float4 s = row[t][e], b = *(const float4 *)&bc[t][4 * q];
-        const float bj[4] = {b.x, b.y, b.z, b.w};
+        if (m.ends >> (to - 1) & 1) four(a.dlast ? a.dlast + (int64_t)__builtin_amdgcn_readlane(m.bag.y, to - 1) * a.dim * N : nullptr, carry);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          decay[t][j] = __builtin_amdgcn_exp2f(s.x * a2[j]);
-          w[t][j] = decay[t][j] * h[j];
-          h[j] = w[t][j] + s.y * bj[j];
-        }
-        if (a.z) {
-          const float4 c = *(const float4 *)&bc[t][NP + 4 * q];
-          const float v = lane_sum<LPC>((c.x * h[0] + c.y * h[1]) + (c.z * h[2] + c.w * h[3]));
-          own_v[t / LPC] = t % LPC == q ? v : own_v[t / LPC];
-        }
-      }
-      // and back
+        for (int t = 0; t < S; ++t) {
+          if (t < from || t >= to) continue;
+          const float4 s = row[t][e], b = *(const float4 *)&bc[t][4 * q];
+          const float bj[4] = {b.x, b.y, b.z, b.w};
+          const float s2 = s.x * kLog2e;
 #pragma unroll
-      for (int t = kBlock - 1; t >= 0; --t) {
-        if (t < lo || t >= hi) continue;
-        if (m.ends >> t & 1) {
-          const int64_t bag = __builtin_amdgcn_readlane(m.bag.y, t);
-#pragma unroll
-          for (int j = 0; j < 4; ++j) carry[j] = a.dlast && 4 * q + j < N ? a.dlast[(bag * a.dim + dc) * N + 4 * q + j] : 0.0f;
+          for (int j = 0; j < 4; ++j) {
+            decay[t][j] = __builtin_amdgcn_exp2f(s2 * av[j]);
+            w[t][j] = decay[t][j] * h[j];
+            h[j] = w[t][j] + s.y * bj[j];
+          }
+          if (gated) {
+            const float4 c = *(const float4 *)&bc[t][NP + 4 * q];
+            const float v = lane_sum<LPC>((c.x * h[0] + c.y * h[1]) + (c.z * h[2] + c.w * h[3]));
+            own_v[t / LPC] = t % LPC == q ? v : own_v[t / LPC];
+          }
         }
-        const float4 s = row[t][e], b = *(const float4 *)&bc[t][4 * q], c = *(const float4 *)&bc[t][NP + 4 * q];
-        const float bj[4] = {b.x, b.y, b.z, b.w}, cj[4] = {c.x, c.y, c.z, c.w};
-        float gb = 0.0f, gwa = 0.0f, both[8];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const float g = cj[j] * s.z + carry[j], gw = g * w[t][j];
-          gb += g * bj[j];
-          gwa += gw * av[j];
-          da[j] += gw * s.x;
-          both[j] = g * s.y;
-          both[4 + j] = s.z * (w[t][j] + s.y * bj[j]);
-          carry[j] = decay[t][j] * g;
+        for (int t = S - 1; t >= 0; --t) {
+          if (t < from || t >= to) continue;
+          const float4 s = row[t][e], b = *(const float4 *)&bc[t][4 * q], c = *(const float4 *)&bc[t][NP + 4 * q];
+          const float bj[4] = {b.x, b.y, b.z, b.w}, cj[4] = {c.x, c.y, c.z, c.w};
+          float gb = 0.0f, gwa = 0.0f, both[8];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const float g = cj[j] * s.z + carry[j], gw = g * w[t][j];
+            gb += g * bj[j];
+            gwa += gw * av[j];
+            da[j] += gw * s.x;
+            both[j] = g * s.y;
+            both[4 + j] = s.z * (w[t][j] + s.y * bj[j]);
+            carry[j] = decay[t][j] * g;
+          }
+          gb = lane_sum<LPC>(gb);
+          gwa = lane_sum<LPC>(gwa);
+          own_b[t / LPC] = t % LPC == q ? gb : own_b[t / LPC];
+          own_w[t / LPC] = t % LPC == q ? gwa : own_w[t / LPC];
+          sum_elements<NP>(both, mine + t * 2 * NP, up8, give);
         }
-        gb = lane_sum<LPC>(gb);
-        gwa = lane_sum<LPC>(gwa);
-        own_b[t / LPC] = t % LPC == q ? gb : own_b[t / LPC];
-        own_w[t / LPC] = t % LPC == q ? gwa : own_w[t / LPC];
-        sum_elements<NP>(both, part + (wave * kBlock + t) * 2 * NP);
-        if ((m.starts >> t & 1) && a.dh0 && in) {
-          const int64_t bag = __builtin_amdgcn_readlane(m.bag.x, t);
+        if (starts && a.dh0 && in) {
+          float *p = a.dh0 + ((int64_t)__builtin_amdgcn_readlane(m.bag.x, from) * a.dim + d) * N + 4 * q;
 #pragma unroll
           for (int j = 0; j < 4; ++j)
-            if (4 * q + j < N) a.dh0[(bag * a.dim + d) * N + 4 * q + j] = carry[j];
+            if (4 * q + j < N) p[j] = carry[j];
         }
+        to = from;
       }
 #pragma unroll
       for (int i = 0; i < OWN; ++i) {
         const int t = i * LPC + q;
         if (t < lo || t >= hi || !in) continue;
         const int64_t at = (row0 + t) * a.dim + d;
-        const float du = (own_w[i] + xv[i] * own_b[i]) * slope[i];
-        ((E *)a.dx)[at] = (E)(skip * dv[i] + step[i] * own_b[i]);
+        const float4 s = row[t][e];  // D, D x, dv, x
+        const float du = (own_w[i] + s.w * own_b[i]) * slope[i];
+        ((E *)a.dx)[at] = (E)(skip * s.z + s.x * own_b[i]);
         ((E *)a.ddelta)[at] = (E)du;
-        if (a.z) ((E *)a.dz)[at] = (E)(gate[i] * (own_v[i] + skip * xv[i]));
-        dskip += dv[i] * xv[i];
+        if (gated) ((E *)a.dz)[at] = (E)(gate[i] * (own_v[i] + skip * s.w));
+        dskip += s.z * s.w;
         dbias += du;
       }
       __syncthreads();
-      for (int i = threadIdx.x; i < kBlock * 2 * NP; i += 64 * waves) {
+      for (int i = threadIdx.x; i < S * 2 * NP; i += 64 * waves) {
         const int t = i / (2 * NP), n = i % (2 * NP), s = n % NP;
         if (t < lo || t >= hi || s >= N) continue;
         float v = 0.0f;
-        for (int j = 0; j < waves; ++j) v += part[j * kBlock * 2 * NP + i];
+        for (int j = 0; j < waves; ++j) v += part[j * S * 2 * NP + i];
         const int64_t r = row0 + t;
         if (a.shared) a.shared[((int64_t)block * a.rows + r) * 2 * N + (n < NP ? 0 : N) + s] = v;
         else ((E *)(n < NP ? a.db : a.dc))[r * a.groups * N + group * N + s] = (E)v;
@@ -685,7 +767,7 @@ struct GradLay {
 };
 GradLay grad_lay(int dim, int groups, int np) {
   const int each = 64 / (np / 4);  // elements of a wavefront
-  int waves = np == 64 ? 4 : kGradWaves;  // up to 52 KB of LDS
+  int waves = kGradWaves;
   if (groups > 1) waves = std::min(waves, 64 / each);  // a workgroup's elements are of one group
   else waves = (int)std::min<int64_t>(waves, divide_up(dim, each));
   return {waves, (int)divide_up(dim, waves * each)};
@@ -716,7 +798,7 @@ void join(const SsmArgs &a, hipStream_t st) {
 }
 
 void prepare(const SsmArgs &a, float *empty_to, const float *empty_from, int64_t stride, hipStream_t st) {
-  const int64_t bag_groups = divide_up(a.bags, kThreads), groups = bag_groups + divide_up(a.count + 1, kThreads / 64);
+  const int64_t bag_groups = divide_up(a.bags, kThreads), groups = bag_groups + divide_up(a.count + 1, kThreads / 64);  // (the unit behind the last: an end)
   ssm_prepare_kernel<<<dim3((unsigned)groups), kThreads, 0, st>>>(a, bag_groups, empty_to, empty_from, stride);
 }
 
@@ -746,7 +828,7 @@ int backward(SsmArgs a, const tbe_ssm_grads *g, hipStream_t st) {
     ssm_grad_ends_kernel<E, NP><<<dim3((unsigned)(a.count * a.waves)), 64, 0, st>>>(a);
     join<NP, true>(a, st);
   }
-  const size_t lds = (size_t)kBlock * 2 * NP * 4 * (1 + l.waves) + (size_t)l.waves * kBlock * (64 / (NP / 4)) * 16;
+  const size_t lds = (size_t)kSaved * 2 * NP * 4 * (1 + l.waves) + (size_t)l.waves * kSaved * (64 / (NP / 4)) * 16;
   ssm_grad_kernel<E, NP><<<dim3((unsigned)(a.workers * l.blocks)), 64 * l.waves, lds, st>>>(a, l.waves);
   if (a.shared) {
     const int64_t groups = divide_up(a.rows * a.groups * 2 * a.states, kThreads);
@@ -884,7 +966,7 @@ int tbe_ssm_destroy(tbe_ssm_handle s) {
 
 int64_t tbe_ssm_saved_floats(tbe_ssm_handle s, int64_t rows) {
   if (!s || rows < 0) return report(TBE_EINVAL, "null handle or a negative number of rows");
-  return divide_up(rows, kBlock) * s->dim * s->np;
+  return divide_up(rows, kSaved) * s->dim * s->np;
 }
 
 int tbe_ssm_forward(tbe_ssm_handle s, const tbe_ssm_batch *b, void *d_y, int64_t y_stride, float *d_last, float *d_saved, void *stream) {
