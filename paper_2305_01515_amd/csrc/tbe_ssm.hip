@@ -17,6 +17,7 @@
 // element, so that 8 rows' w and decays stay in registers on the way back; states before every 8th row were saved by the forward.
 #include <algorithm>
 #include <new>
+#include <type_traits>
 
 #include "tbe_rows.h"
 
@@ -24,13 +25,12 @@ using namespace tbe;
 
 namespace {
 
-constexpr int kBlock = 16;       // rows that the forward stages at once
+constexpr int kBlock = 16;       // rows whose b or c the kernels of the ends stage at once
 constexpr int kSaved = 8;        // states before every so many rows are what the backward goes from: that many rows' w and decays fit its registers
 constexpr int kSegment = 64;     // units that a lane of `join` goes through
 constexpr int kMostStates = 64;
 constexpr int kThreads = 256;
 constexpr int kGradWorkers = 1024;  // workgroups of the backward, together
-constexpr int kGradWaves = 8;       // wavefronts of one, at most
 
 struct Unit {
   int64_t begin;  // first row
@@ -140,11 +140,18 @@ __device__ inline float soft(float u) {
 // a decay's product with a state that may be zero beside an infinite one
 __device__ inline float carried(float a2, float span, float h) { return h == 0.0f ? 0.0f : __builtin_amdgcn_exp2f(a2 * span) * h; }
 
-// State n of element d before unit k, as `join` left it
-template <int NP>
-__device__ inline float start_of(const SsmArgs &a, int64_t k, int d, int n, float a2) {
-  const float r = a.reach[k * a.dim + d], h = a.ends[(k * a.dim + d) * NP + n];
-  return r < 0.0f ? h : h + carried(a2, r, a.seg_start[(k / kSegment * a.dim + d) * NP + n]);
+// States n .. n + COUNT - 1 of element d before unit k, as `join` left them
+template <int NP, int COUNT>
+__device__ inline void start_of(const SsmArgs &a, int64_t k, int d, int n, const float *a2, float (&to)[COUNT]) {
+  const float r = a.reach[k * a.dim + d], *h = a.ends + (k * a.dim + d) * NP + n;
+  float far[COUNT];
+#pragma unroll
+  for (int j = 0; j < COUNT; ++j) to[j] = h[j];
+  const float *p = a.seg_start + (k / kSegment * a.dim + d) * NP + n;  // (of no meaning where nothing of the segment before gets here)
+#pragma unroll
+  for (int j = 0; j < COUNT; ++j) far[j] = p[j];
+#pragma unroll
+  for (int j = 0; j < COUNT; ++j) to[j] += r < 0.0f ? 0.0f : carried(a2[j], r, far[j]);
 }
 
 // b and c (or only one) of the rows row0 + [lo, hi) to LDS, zero beyond the states: to[row][n], to[row][NP + n]
@@ -159,27 +166,40 @@ __device__ inline void stage(const SsmArgs &a, int64_t row0, int lo, int hi, int
   }
 }
 
-// the bags that start and end in the rows row0 + [lo, hi), as masks of rows; `bag` of lane t: that of row t
-struct Marks {
-  uint32_t starts, ends;
-  int2 bag;
-};
-__device__ inline Marks marks_of(const SsmArgs &a, int64_t row0, int lo, int hi) {
-  const int t = threadIdx.x & 63;
-  int2 m = {-1, -1};
-  if (t >= lo && t < hi) m = a.marks[row0 + t];
-  return {(uint32_t)__ballot(m.x >= 0), (uint32_t)__ballot(m.y >= 0), m};
+// Waits for loaded numbers here.  Behind a branch that loads, the compiler would wait where they are used first, on the way that has loaded nothing
+// too, and for all loads and stores under way: a store's time for each row.
+template <int COUNT>
+__device__ inline void settle(float (&v)[COUNT]) {
+#pragma unroll
+  for (int i = 0; i < COUNT; ++i) asm volatile("" : "+v"(v[i]));
 }
 
-// What a lane's element has of a row, read ahead
-template <class E>
-struct Raw {
-  E x, u, z;
-};
+// The lane's number, found again: what follows from it would be kept from block to block in registers that there are not.
+__device__ inline int lane_again() {
+  int me = threadIdx.x;
+  asm volatile("" : "+v"(me));
+  return me;
+}
 
+// V elements of a row, or the first n of them
+template <class E, int V>
+__device__ inline void load_some(const E *p, int n, Pack<E, V> &to) {
+  if (n >= V) {
+    __builtin_memcpy(&to, p, sizeof to);
+  } else {
+#pragma unroll
+    for (int i = 0; i < V; ++i)
+      if (i < n) to.e[i] = p[i];
+  }
+}
+
+// A wavefront goes down a unit's rows in tiles of 2 V rows of 64 elements: x, delta and z are read in packs of 16 bytes a tile ahead, b, c
+// and marks too, and lie in LDS while the tile is gone through.
 template <class E, int NP, bool FULL>
-__global__ __launch_bounds__(64) void ssm_kernel(SsmArgs a) {
-  __shared__ float bc[kBlock][2 * NP];
+__global__ __launch_bounds__(64, NP == 16 && FULL ? 3 : 1) void ssm_kernel(SsmArgs a) {
+  constexpr int V = 16 / sizeof(E), T = 2 * V, PACKS = 64 / V;
+  __shared__ float bc[T][2 * NP];
+  __shared__ Pack<E, V> tile[3][T][PACKS];
   const int64_t k = blockIdx.x / a.waves;
   const int wave = (int)(blockIdx.x % a.waves), lane = threadIdx.x;
   const Unit u = a.units[k];
@@ -188,6 +208,32 @@ __global__ __launch_bounds__(64) void ssm_kernel(SsmArgs a) {
   const int d = wave * 64 + lane, dc = min(d, a.dim - 1);
   const bool in = d < a.dim;
   const int group = a.groups > 1 ? wave * 64 / (a.dim / a.groups) : 0, N = a.states;
+  const bool gated = a.z;
+  Pack<E, V> raw[3][2];
+  constexpr int PIECES = T * 2 * NP / 64;  // of a tile's b and c
+  constexpr int ROWS = 64 / (2 * NP) > 0 ? 64 / (2 * NP) : 1, PARTS = 2 * NP > 64 ? 2 * NP / 64 : 1;
+  E shared[PIECES];
+  int2 mark;
+  auto fetch = [&](int64_t row0) {
+    const int me = lane_again(), pack = wave * 64 + me % PACKS * V, have = a.dim - pack;  // of a row, that this lane brings
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int64_t r = min(max(row0 + i * V + me / PACKS, begin), end - 1);
+      load_some<E, V>((const E *)a.x + r * a.xs + pack, have, raw[0][i]);
+      load_some<E, V>((const E *)a.delta + r * a.ts + pack, have, raw[1][i]);
+      if (gated) load_some<E, V>((const E *)a.z + r * a.zs + pack, have, raw[2][i]);
+    }
+#pragma unroll
+    for (int p = 0; p < PIECES; ++p) {
+      const int n = PARTS > 1 ? p % PARTS * 64 + me : me % (2 * NP), t = PARTS > 1 ? p / PARTS : p * ROWS + me / (2 * NP);
+      const int64_t r = min(max(row0 + t, begin), end - 1);
+      const int at = group * N + min(n % NP, N - 1);
+      shared[p] = n < NP ? ((const E *)a.b)[r * a.bs + at] : ((const E *)a.c)[r * a.cs + at];
+    }
+    mark = a.marks[min(max(row0 + (lane & (T - 1)), begin), end - 1)];
+  };
+  const int64_t from = begin & ~(int64_t)(T - 1);
+  fetch(from);
   float h[NP], a2[NP];
 #pragma unroll
   for (int n = 0; n < NP; ++n) {
@@ -195,45 +241,18 @@ __global__ __launch_bounds__(64) void ssm_kernel(SsmArgs a) {
     h[n] = 0.0f;
   }
   if (u.cut) {
-#pragma unroll
-    for (int n = 0; n < NP; ++n) h[n] = FULL || n < N ? start_of<NP>(a, k, dc, n, a2[n]) : 0.0f;
+    start_of<NP>(a, k, dc, 0, a2, h);
+    settle(h);
   }
   const float bias = a.bias ? a.bias[dc] : 0.0f, skip = a.skip ? a.skip[dc] : 0.0f;
-  const bool gated = a.z;
-  const E *x = (const E *)a.x + dc, *delta = (const E *)a.delta + dc, *z = (const E *)(gated ? a.z : a.x) + dc;
-  const int64_t zs = gated ? a.zs : a.xs;
-  E *y = (E *)a.y + d;
-  // Four rows are read ahead of those that are gone through, b, c and marks a block ahead.
-  Raw<E> ahead[4];
-  auto read = [&](int64_t r0) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int64_t r = min(max(r0 + i, begin), end - 1);
-      ahead[i].x = x[r * a.xs];
-      ahead[i].u = delta[r * a.ts];
-      ahead[i].z = z[r * zs];
-    }
-  };
-  constexpr int PIECES = kBlock * 2 * NP / 64;  // of a block's b and c that a lane brings: number `mine` of rows `mine_row`, + ROWS, ...
-  constexpr int ROWS = 64 / (2 * NP) > 0 ? 64 / (2 * NP) : 1, PARTS = 2 * NP > 64 ? 2 * NP / 64 : 1;
-  E shared[PIECES];
-  int2 mark;
-  auto bring = [&](int64_t row0) {
-#pragma unroll
-    for (int p = 0; p < PIECES; ++p) {
-      const int n = PARTS > 1 ? p % PARTS * 64 + lane : lane % (2 * NP), t = PARTS > 1 ? p / PARTS : p * ROWS + lane / (2 * NP);
-      const int64_t r = min(max(row0 + t, begin), end - 1);
-      const int at = group * N + min(n % NP, N - 1);
-      shared[p] = n < NP ? ((const E *)a.b)[r * a.bs + at] : ((const E *)a.c)[r * a.cs + at];
-    }
-    mark = a.marks[min(max(row0 + (lane & (kBlock - 1)), begin), end - 1)];
-  };
-  const int64_t from = begin & ~(int64_t)(kBlock - 1);
-  bring(from);
-  read(begin & ~3ll);
-  for (int64_t row0 = from; row0 < end; row0 += kBlock) {
-    const int lo = (int)max(begin - row0, (int64_t)0), hi = (int)min(end - row0, (int64_t)kBlock);
+  for (int64_t row0 = from; row0 < end; row0 += T) {
+    const int lo = (int)max(begin - row0, (int64_t)0), hi = (int)min(end - row0, (int64_t)T);
     __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int j = 0; j < 3; ++j)
+        if (j < 2 || gated) tile[j][i * V + lane / PACKS][lane % PACKS] = raw[j][i];
 #pragma unroll
     for (int p = 0; p < PIECES; ++p) {
       const int n = PARTS > 1 ? p % PARTS * 64 + lane : lane % (2 * NP), t = PARTS > 1 ? p / PARTS : p * ROWS + lane / (2 * NP);
@@ -242,54 +261,80 @@ __global__ __launch_bounds__(64) void ssm_kernel(SsmArgs a) {
     const int2 bag_of = mark;
     const bool mine = lane >= lo && lane < hi;
     const uint32_t starts = (uint32_t)__ballot(mine && mark.x >= 0), ends = (uint32_t)__ballot(mine && mark.y >= 0);
-    bring(row0 + kBlock);
+    if (row0 + T < end) fetch(row0 + T);
     __syncthreads();
-    for (int t0 = lo & ~3; t0 < hi; t0 += 4) {
-      Raw<E> now[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) now[i] = ahead[i];
-      read(row0 + t0 + 4);
-      if (a.saved && (t0 & (kSaved - 1)) == 0 && t0 >= lo && in) {
-        float *to = a.saved + ((row0 + t0) / kSaved * a.dim + d) * NP;
+    const E *xt = (const E *)tile[0] + lane, *ut = (const E *)tile[1] + lane, *zt = (const E *)tile[2] + lane;
+    E *y = (E *)a.y + (row0 + lo) * a.ys + d;
+    auto put = [&](int t) {  // the state before row t, for the backward
+      if (a.saved && (t & (kSaved - 1)) == 0 && in) {
+        float *to = a.saved + ((row0 + t) / kSaved * a.dim + d) * NP;
 #pragma unroll
         for (int n = 0; n < NP; n += 4) *(float4 *)(to + n) = make_float4(h[n], h[n + 1], h[n + 2], h[n + 3]);
       }
+    };
+    auto go = [&](int t, E xe, E ue, E ze) {
+      const float xv = (float)xe, step = soft((float)ue + bias), sx = step * xv;
+      float v = skip * xv, v2 = 0.0f;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int t = t0 + i;
-        if (t < lo || t >= hi) continue;
-        if (starts >> t & 1) {
-          const int64_t bag = __builtin_amdgcn_readlane(bag_of.x, t);
-          if (a.h0) {
-            const float *p = a.h0 + bag * a.h0s + (int64_t)dc * N;
+      for (int n = 0; n < NP; ++n) {
+        const float g = __builtin_amdgcn_exp2f(step * a2[n]) * h[n] + sx * bc[t][n];
+        h[n] = FULL || n < N ? g : 0.0f;
+        (n & 1 ? v2 : v) += bc[t][NP + n] * h[n];
+      }
+      v += v2;
+      if (gated) {
+        const float zv = (float)ze;
+        v *= zv * sigmoid(zv);
+      }
+      return v;
+    };
+    for (int t = lo; t < hi;) {
+      constexpr int R = sizeof(E) == 2 ? 2 : 4;
+      if (t + R <= hi && (t & (R - 1)) == 0 && !((starts | ends) >> t & ((1 << R) - 1))) {  // without branches between the rows
+        put(t);
+        float v[R];
 #pragma unroll
-            for (int n = 0; n < NP; ++n) h[n] = FULL || n < N ? p[n] : 0.0f;
-          } else {
+        for (int i = 0; i < R; ++i) v[i] = go(t + i, xt[(t + i) * 64], ut[(t + i) * 64], zt[(t + i) * 64]);
+        if (in) {
 #pragma unroll
-            for (int n = 0; n < NP; ++n) h[n] = 0.0f;
+          for (int i = 0; i < R; ++i) y[i * a.ys] = (E)v[i];
+        }
+        y += R * a.ys;
+        t += R;
+        continue;
+      }
+      const E xe = xt[t * 64], ue = ut[t * 64], ze = zt[t * 64];
+      if (starts >> t & 1) {
+        const int64_t bag = __builtin_amdgcn_readlane(bag_of.x, t);
+        if (a.h0) {
+          const float *p = a.h0 + bag * a.h0s + (int64_t)dc * N;
+#pragma unroll
+          for (int n = 0; n < NP; n += 4) {
+            float v[4];
+            load_floats<float, 4>(p + n, FULL ? 4 : N - n, v);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) h[n + j] = v[j];
           }
-        }
-        const float xv = (float)now[i].x, step = soft((float)now[i].u + bias), sx = step * xv;
-        float v = skip * xv;
+          settle(h);
+        } else {
 #pragma unroll
-        for (int n = 0; n < NP; ++n) {
-          const float g = __builtin_amdgcn_exp2f(step * a2[n]) * h[n] + sx * bc[t][n];
-          h[n] = FULL || n < N ? g : 0.0f;
-          v += bc[t][NP + n] * h[n];
-        }
-        if (gated) {
-          const float zv = (float)now[i].z;
-          v *= zv * sigmoid(zv);
-        }
-        if (in) y[(row0 + t) * a.ys] = (E)v;
-        if ((ends >> t & 1) && a.last && in) {
-          const int64_t bag = __builtin_amdgcn_readlane(bag_of.y, t);
-          float *to = a.last + (bag * a.dim + d) * N;
-#pragma unroll
-          for (int n = 0; n < NP; ++n)
-            if (FULL || n < N) to[n] = h[n];
+          for (int n = 0; n < NP; ++n) h[n] = 0.0f;
         }
       }
+      put(t);
+      const float v = go(t, xe, ue, ze);
+      if (in) *y = (E)v;
+      y += a.ys;
+      if ((ends >> t & 1) && a.last && in) {
+        const int64_t bag = __builtin_amdgcn_readlane(bag_of.y, t);
+        float *to = a.last + (bag * a.dim + d) * N;
+#pragma unroll
+        for (int n = 0; n < NP; n += 4) {
+          const float v[4] = {h[n], h[n + 1], h[n + 2], h[n + 3]};
+          store_floats<float, 4>(to + n, FULL ? 4 : N - n, v);
+        }
+      }
+      ++t;
     }
   }
 }
@@ -528,149 +573,272 @@ __device__ inline void sum_elements(float (&v)[8], float *to, bool up8, bool giv
 // Backward of a unit's rows: a lane has states 4 q .. 4 q + 3 of an element; a workgroup's wavefronts have elements side by side.  Rows are gone
 // through in blocks of kSaved, last block first, each bag's rows of a block at a time: forward from the state before them, w and
 // the decays kept in registers, and back.
-template <class E, int NP>
-__global__ __launch_bounds__(64 * kGradWaves, 2) void ssm_grad_kernel(SsmArgs a, int waves) {
+template <class E, int NP, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, 2) void ssm_grad_kernel(SsmArgs a) {
   constexpr int S = kSaved, LPC = NP / 4, CPW = 64 / LPC, OWN = (S + LPC - 1) / LPC;  // lanes of an element, elements of a wavefront, rows whose scalars a lane finds
-  extern __shared__ float4 lds[];
-  float(*bc)[2 * NP] = (float(*)[2 * NP])lds;                           // [S][2 NP]
-  float *part = (float *)lds + S * 2 * NP;                              // [waves][S][2 NP]
+  constexpr int V = 16 / sizeof(E), CH = CPW * WAVES, THREADS = 64 * WAVES;           // elements and lanes of a workgroup
+  constexpr int PACKS = CH / V, BRINGS = (4 * S * PACKS + THREADS - 1) / THREADS;     // of a row; of x, delta, dy and z of a block that a lane brings
+  constexpr int NUMBERS = (S * 2 * NP + THREADS - 1) / THREADS;                       // of b and c
+  __shared__ Pack<E, V> tile[2][4][S][PACKS];
+  __shared__ float bc[2][S][2 * NP], part[2][WAVES][S][2 * NP];
+  __shared__ float4 rows_of[WAVES][S][CPW];  // D, D x, dv, x
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, q = lane % LPC, e = lane / LPC, N = a.states;
-  float4(*row)[CPW] = (float4(*)[CPW])(part + waves * S * 2 * NP) + wave * S;  // [S][CPW] of each wavefront: D, D x, dv, x
-  float *mine = part + wave * S * 2 * NP + place_of<NP>(lane);
+  float4(*row)[CPW] = rows_of[wave];
+  const int place = place_of<NP>(lane);
   const bool up8 = lane & 8, give = LPC != 4 || !(lane & 4);
   const int64_t worker = blockIdx.x / a.blocks;
-  const int block = (int)(blockIdx.x % a.blocks), d = (block * waves + wave) * CPW + e, dc = min(d, a.dim - 1);
-  const bool in = d < a.dim;
-  const int group = a.groups > 1 ? block * waves * CPW / (a.dim / a.groups) : 0;
+  const int block = (int)(blockIdx.x % a.blocks), d = block * CH + wave * CPW + e, dc = min(d, a.dim - 1);
+  const bool in = d < a.dim, gated = a.z;
+  const int group = a.groups > 1 ? block * CH / (a.dim / a.groups) : 0;
   float av[4], da[4] = {0.0f, 0.0f, 0.0f, 0.0f}, dskip = 0.0f, dbias = 0.0f;
 #pragma unroll
   for (int j = 0; j < 4; ++j) av[j] = 4 * q + j < N ? a.a[(int64_t)dc * N + 4 * q + j] : 0.0f;
   const float bias = a.bias ? a.bias[dc] : 0.0f, skip = a.skip ? a.skip[dc] : 0.0f;
-  const bool gated = a.z;
-  // four states of [.., dim, states] numbers; nothing beyond the states
+  const bool even = N % 4 == 0;  // the states of a lane are all there, or none
+  // four states of [.., dim, states] numbers, to be waited for; nothing beyond the states
   auto four = [&](const float *p, float (&to)[4]) {
+    if (even) {
+      const int at = 4 * q < N ? 4 * q : 0;
+      load_floats<float, 4>(p + (int64_t)dc * N + at, 4, to);
+    } else {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) to[j] = p && 4 * q + j < N ? p[(int64_t)dc * N + 4 * q + j] : 0.0f;
-  };
-  for (int64_t k = worker; k < a.count; k += a.workers) {
-    const int64_t begin = a.units[k].begin, end = a.units[k + 1].begin;
-    if (begin >= end) continue;
-    float carry[4] = {0.0f, 0.0f, 0.0f, 0.0f};  // exp(D a) g of the row behind
-    if (a.units[k + 1].cut) {
-#pragma unroll
-      for (int j = 0; j < 4; ++j) carry[j] = 4 * q + j < N ? start_of<NP>(a, k, dc, 4 * q + j, av[j] * kLog2e) : 0.0f;
+      for (int j = 0; j < 4; ++j) to[j] = p[(int64_t)dc * N + min(4 * q + j, N - 1)];
     }
-    for (int64_t row0 = (end - 1) & ~(int64_t)(S - 1); row0 + S > begin; row0 -= S) {
-      const int lo = (int)max(begin - row0, (int64_t)0), hi = (int)min(end - row0, (int64_t)S);
-      const Marks m = marks_of(a, row0, lo, hi);
-      float saved[4] = {0.0f, 0.0f, 0.0f, 0.0f};  // (a unit that begins within a block begins with a bag)
-      if (lo == 0) {
-        const float4 s = *(const float4 *)(a.saved + (row0 / S * a.dim + dc) * NP + 4 * q);
-        saved[0] = s.x, saved[1] = s.y, saved[2] = s.z, saved[3] = s.w;
+  };
+  auto known = [&](bool there, const float (&from)[4], float (&to)[4]) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) to[j] = there && 4 * q + j < N ? from[j] : 0.0f;
+  };
+
+  // The blocks of this workgroup's units one after the other.
+  struct Place {
+    int64_t row0, begin, end, k;
+    bool there;
+  };
+  auto enter = [&](int64_t k) {
+    for (; k < a.count; k += a.workers) {
+      const int64_t begin = a.units[k].begin, end = a.units[k + 1].begin;
+      if (begin < end) return Place{(end - 1) & ~(int64_t)(S - 1), begin, end, k, true};
+    }
+    return Place{0, 0, 1, k, false};  // (what is read ahead of it is not used)
+  };
+  auto after = [&](Place p) {
+    if (p.there && p.row0 <= p.begin) return enter(p.k + a.workers);
+    p.row0 = max(p.row0 - S, (int64_t)0);
+    return p;
+  };
+  // What a lane brings of a block, one block ahead: packs of the inputs (this lane's are all of one kind), numbers of b and c, the states before it; marks two
+  // blocks ahead, so that the states at the end of its last bag are there too.
+  Pack<E, V> raw[BRINGS];
+  E shared[NUMBERS];
+  float4 before;
+  auto fetch = [&](const Place &p) {
+    const int me = lane_again();
+#pragma unroll
+    for (int i = 0; i < BRINGS; ++i) {
+      const int n = me + i * THREADS, kind = n / (S * PACKS) & 3, t = n / PACKS % S, at = block * CH + n % PACKS * V;
+      const E *from = (const E *)(kind == 0 || (kind == 3 && !gated) ? a.x : kind == 1 ? a.delta : kind == 2 ? a.dy : a.z);
+      const int64_t stride = kind == 0 || (kind == 3 && !gated) ? a.xs : kind == 1 ? a.ts : kind == 2 ? a.dys : a.zs;
+      const E *r = from + min(max(p.row0 + t, p.begin), p.end - 1) * stride;
+      if (a.dim % V == 0) __builtin_memcpy(&raw[i], r + min(at, a.dim - V), sizeof raw[i]);
+      else load_some<E, V>(r + at, a.dim - at, raw[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < NUMBERS; ++i) {
+      const int n = me + i * THREADS, t = n / (2 * NP) % S, m = n % (2 * NP);
+      const int64_t r = min(max(p.row0 + t, p.begin), p.end - 1);
+      const E *from = m < NP ? (const E *)a.b + r * a.bs : (const E *)a.c + r * a.cs;
+      shared[i] = from[group * N + min(m % NP, N - 1)];
+    }
+    before = *(const float4 *)(a.saved + (p.row0 / S * a.dim + dc) * NP + 4 * q);
+  };
+  auto mark_at = [&](const Place &p) { return a.marks[min(max(p.row0 + (lane & (S - 1)), p.begin), p.end - 1)]; };
+  // a block's rows that are this unit's, and the bags that start and end in them
+  struct Seen {
+    int lo, hi;
+    uint32_t starts, ends;
+  };
+  auto look = [&](const Place &p, int2 mark) {
+    Seen s;
+    s.lo = (int)max(p.begin - p.row0, (int64_t)0), s.hi = (int)min(p.end - p.row0, (int64_t)S);
+    const bool mine = lane >= s.lo && lane < s.hi;
+    s.starts = (uint32_t)__ballot(mine && mark.x >= 0), s.ends = (uint32_t)__ballot(mine && mark.y >= 0);
+    return s;
+  };
+  // states that the last bag's rows [from, to) of [.., to) begin with, and gradients that they end with, if it starts and ends there
+  struct Bag {
+    int from;
+    bool starts, ends;
+  };
+  auto last_bag = [&](const Seen &s, int to) {
+    const uint32_t b = s.starts & ((1u << to) - 1);
+    return Bag{b ? 31 - __builtin_clz(b) : s.lo, b != 0, (s.ends >> (to - 1) & 1) != 0};
+  };
+  auto ask = [&](const Bag &b, int to, int2 mark, float (&h)[4], float (&g)[4]) {
+    if (b.starts && a.h0) four(a.h0 + (int64_t)__builtin_amdgcn_readlane(mark.x, b.from) * a.h0s, h);
+    if (b.ends && a.dlast) four(a.dlast + (int64_t)__builtin_amdgcn_readlane(mark.y, to - 1) * a.dim * N, g);
+  };
+  // db and dc of a block, from the wavefronts' sums
+  auto give_shared = [&](const Place &p, int buffer) {
+    const int me = lane_again();
+#pragma unroll
+    for (int i = 0; i < NUMBERS; ++i) {
+      const int n = me + i * THREADS, t = n / (2 * NP), m = n % (2 * NP), s = m % NP;
+      const int64_t r = p.row0 + t;
+      if (t >= S || r < p.begin || r >= p.end || s >= N) continue;
+      float v = 0.0f;
+#pragma unroll
+      for (int j = 0; j < WAVES; ++j) v += part[buffer][j][t][m];
+      if (a.shared) a.shared[((int64_t)block * a.rows + r) * 2 * N + (m < NP ? 0 : N) + s] = v;
+      else ((E *)(m < NP ? a.db : a.dc))[r * a.groups * N + group * N + s] = (E)v;
+    }
+  };
+
+  Place now = enter(worker), done{0, 0, 0, 0, false};
+  if (now.there) {
+    Place next = after(now);
+    int2 mark = mark_at(now), mark_next = mark_at(next);
+    fetch(now);
+    Seen seen = look(now, mark);
+    Bag bag = last_bag(seen, seen.hi);
+    float carry[4] = {0.0f, 0.0f, 0.0f, 0.0f};  // exp(D a) g of the row behind
+    float asked_h[4] = {0.0f, 0.0f, 0.0f, 0.0f}, asked_g[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    ask(bag, seen.hi, mark, asked_h, asked_g);
+    int64_t unit = -1;
+    int buffer = 0;
+    do {
+      const Place then = after(next);
+#pragma unroll
+      for (int i = 0; i < BRINGS; ++i) {
+        const int n = threadIdx.x + i * THREADS;
+        if (4 * S * PACKS % THREADS == 0 || n < 4 * S * PACKS) (&tile[buffer][0][0][0])[n] = raw[i];
+      }
+#pragma unroll
+      for (int i = 0; i < NUMBERS; ++i) {
+        const int n = threadIdx.x + i * THREADS;
+        if (S * 2 * NP % THREADS == 0 || n < S * 2 * NP) (&bc[buffer][0][0])[n] = n % NP < N ? (float)shared[i] : 0.0f;
+      }
+      const float saved[4] = {before.x, before.y, before.z, before.w};
+      const Seen here = seen;
+      const int2 bag_of = mark;
+      const Bag first = bag;
+      fetch(next);
+      mark = mark_next;
+      mark_next = mark_at(then);
+      seen = look(next, mark);
+      bag = last_bag(seen, seen.hi);
+      __syncthreads();
+      if (done.there) give_shared(done, buffer ^ 1);
+      if (now.k != unit) {
+        unit = now.k;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) carry[j] = 0.0f;
+        if (a.units[unit + 1].cut) {
+          const float a2[4] = {av[0] * kLog2e, av[1] * kLog2e, av[2] * kLog2e, av[3] * kLog2e};
+          start_of<NP>(a, unit, dc, 4 * q, a2, carry);
+          settle(carry);
+        }
       }
       // scalars of the rows t with t % LPC = q
       float slope[OWN], gate[OWN], own_v[OWN], own_b[OWN], own_w[OWN];
-      E in_x[OWN], in_u[OWN], in_y[OWN], in_z[OWN];
 #pragma unroll
       for (int i = 0; i < OWN; ++i) {
-        const int t = min(i * LPC + q, S - 1);
-        const int64_t r = row0 + min(max(t, lo), hi - 1);
-        in_x[i] = ((const E *)a.x)[r * a.xs + dc];
-        in_u[i] = ((const E *)a.delta)[r * a.ts + dc];
-        in_y[i] = ((const E *)a.dy)[r * a.dys + dc];
-        in_z[i] = gated ? ((const E *)a.z)[r * a.zs + dc] : (E)0.0f;
-      }
-      __syncthreads();  // what the block before has left in LDS has been read
-      for (int i = threadIdx.x; i < S * 2 * NP; i += 64 * waves) {
-        const int t = i / (2 * NP), n = i % (2 * NP);
-        const int64_t r = row0 + min(max(t, lo), hi - 1);
-        const int at = group * N + min(n % NP, N - 1);
-        const float v = (float)(n < NP ? ((const E *)a.b)[r * a.bs + at] : ((const E *)a.c)[r * a.cs + at]);
-        bc[t][n] = n % NP < N ? v : 0.0f;
-      }
-#pragma unroll
-      for (int i = 0; i < OWN; ++i) {
-        const float u = (float)in_u[i] + bias, dy = (float)in_y[i], step = soft(u), x = in ? (float)in_x[i] : 0.0f;
+        const int t = min(i * LPC + q, S - 1), at = t * CH + wave * CPW + e;
+        const E *in_x = (const E *)tile[buffer] + at;
+        constexpr int of = S * CH;
+        // elements beyond the row (of which there is nothing in the tile) have no part of db and dc
+        const float u = (in ? (float)in_x[of] : 0.0f) + bias, dy = in ? (float)in_x[2 * of] : 0.0f, step = soft(u), x = in ? (float)in_x[0] : 0.0f;
         float dv = dy;
         slope[i] = sigmoid(u);
         gate[i] = 0.0f;
         if (gated) {
-          const float z = (float)in_z[i], f = sigmoid(z);
+          const float z = in ? (float)in_x[3 * of] : 0.0f, f = sigmoid(z);
           dv = dy * z * f;
           gate[i] = dy * (f * (1.0f + z * (1.0f - f)));
         }
-        if (!in) dv = 0.0f;  // elements beyond the row have no part of db and dc
         own_v[i] = own_b[i] = own_w[i] = 0.0f;
         if (i * LPC + q < S) row[i * LPC + q][e] = make_float4(step, step * x, dv, x);
       }
-      __syncthreads();
       // the bags' rows [from, to) of the block, from the last
-      for (int to = hi; to > lo;) {
-        const uint32_t before = m.starts & ((1u << to) - 1);
-        const bool starts = before != 0;
-        const int from = starts ? 31 - __builtin_clz(before) : lo;
+      Bag rows = first;
+      for (int to = here.hi; to > here.lo;) {
         float h[4], w[S][4], decay[S][4];
-        if (starts) {
-          four(a.h0 ? a.h0 + (int64_t)__builtin_amdgcn_readlane(m.bag.x, from) * a.h0s : nullptr, h);
-        } else {
-#pragma unroll
-          for (int j = 0; j < 4; ++j) h[j] = saved[j];
+        if (to != here.hi) {
+          rows = last_bag(here, to);
+          ask(rows, to, bag_of, asked_h, asked_g);
         }
-        if (m.ends >> (to - 1) & 1) four(a.dlast ? a.dlast + (int64_t)__builtin_amdgcn_readlane(m.bag.y, to - 1) * a.dim * N : nullptr, carry);
+        const int from = rows.from;
+        float start[4], finish[4];
+        known(a.h0, asked_h, start);
+        known(a.dlast, asked_g, finish);
 #pragma unroll
-        for (int t = 0; t < S; ++t) {
-          if (t < from || t >= to) continue;
-          const float4 s = row[t][e], b = *(const float4 *)&bc[t][4 * q];
-          const float bj[4] = {b.x, b.y, b.z, b.w};
-          const float s2 = s.x * kLog2e;
+        for (int j = 0; j < 4; ++j) h[j] = rows.starts ? start[j] : saved[j];  // (a unit that begins within a block begins with a bag)
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            decay[t][j] = __builtin_amdgcn_exp2f(s2 * av[j]);
-            w[t][j] = decay[t][j] * h[j];
-            h[j] = w[t][j] + s.y * bj[j];
+        for (int j = 0; j < 4; ++j) carry[j] = rows.ends ? finish[j] : carry[j];
+        settle(h);
+        settle(carry);
+        if (from <= here.lo) ask(bag, seen.hi, mark, asked_h, asked_g);  // the next block's, while this one's last rows are gone through
+        // Whole blocks apart: without branches between them, rows are interleaved, which hides the way through LDS and the chains of exchanges.
+        auto walk = [&](auto whole) {
+          constexpr bool WHOLE = decltype(whole)::value;
+#pragma unroll
+          for (int t = 0; t < S; ++t) {
+            if (!WHOLE && (t < from || t >= to)) continue;
+            if (WHOLE) __builtin_amdgcn_sched_barrier(0);  // more rows at once do not fit the registers
+            const float4 s = row[t][e], b = *(const float4 *)&bc[buffer][t][4 * q];
+            const float bj[4] = {b.x, b.y, b.z, b.w};
+            const float s2 = s.x * kLog2e;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              decay[t][j] = __builtin_amdgcn_exp2f(s2 * av[j]);
+              w[t][j] = decay[t][j] * h[j];
+              h[j] = w[t][j] + s.y * bj[j];
+            }
+            if (gated) {
+              const float4 c = *(const float4 *)&bc[buffer][t][NP + 4 * q];
+              const float v = lane_sum<LPC>((c.x * h[0] + c.y * h[1]) + (c.z * h[2] + c.w * h[3]));
+              own_v[t / LPC] = t % LPC == q ? v : own_v[t / LPC];
+            }
           }
-          if (gated) {
-            const float4 c = *(const float4 *)&bc[t][NP + 4 * q];
-            const float v = lane_sum<LPC>((c.x * h[0] + c.y * h[1]) + (c.z * h[2] + c.w * h[3]));
-            own_v[t / LPC] = t % LPC == q ? v : own_v[t / LPC];
+#pragma unroll
+          for (int t = S - 1; t >= 0; --t) {
+            if (!WHOLE && (t < from || t >= to)) continue;
+            if (WHOLE) __builtin_amdgcn_sched_barrier(0);
+            const float4 s = row[t][e], b = *(const float4 *)&bc[buffer][t][4 * q], c = *(const float4 *)&bc[buffer][t][NP + 4 * q];
+            const float bj[4] = {b.x, b.y, b.z, b.w}, cj[4] = {c.x, c.y, c.z, c.w};
+            float gb = 0.0f, gwa = 0.0f, both[8];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              const float g = cj[j] * s.z + carry[j], gw = g * w[t][j];
+              gb += g * bj[j];
+              gwa += gw * av[j];
+              da[j] += gw * s.x;
+              both[j] = g * s.y;
+              both[4 + j] = s.z * (w[t][j] + s.y * bj[j]);
+              carry[j] = decay[t][j] * g;
+            }
+            gb = lane_sum<LPC>(gb);
+            gwa = lane_sum<LPC>(gwa);
+            own_b[t / LPC] = t % LPC == q ? gb : own_b[t / LPC];
+            own_w[t / LPC] = t % LPC == q ? gwa : own_w[t / LPC];
+            sum_elements<NP>(both, &part[buffer][wave][t][0] + place, up8, give);
           }
-        }
-#pragma unroll
-        for (int t = S - 1; t >= 0; --t) {
-          if (t < from || t >= to) continue;
-          const float4 s = row[t][e], b = *(const float4 *)&bc[t][4 * q], c = *(const float4 *)&bc[t][NP + 4 * q];
-          const float bj[4] = {b.x, b.y, b.z, b.w}, cj[4] = {c.x, c.y, c.z, c.w};
-          float gb = 0.0f, gwa = 0.0f, both[8];
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const float g = cj[j] * s.z + carry[j], gw = g * w[t][j];
-            gb += g * bj[j];
-            gwa += gw * av[j];
-            da[j] += gw * s.x;
-            both[j] = g * s.y;
-            both[4 + j] = s.z * (w[t][j] + s.y * bj[j]);
-            carry[j] = decay[t][j] * g;
-          }
-          gb = lane_sum<LPC>(gb);
-          gwa = lane_sum<LPC>(gwa);
-          own_b[t / LPC] = t % LPC == q ? gb : own_b[t / LPC];
-          own_w[t / LPC] = t % LPC == q ? gwa : own_w[t / LPC];
-          sum_elements<NP>(both, mine + t * 2 * NP, up8, give);
-        }
-        if (starts && a.dh0 && in) {
-          float *p = a.dh0 + ((int64_t)__builtin_amdgcn_readlane(m.bag.x, from) * a.dim + d) * N + 4 * q;
-#pragma unroll
-          for (int j = 0; j < 4; ++j)
-            if (4 * q + j < N) p[j] = carry[j];
+        };
+        if (from == 0 && to == S) walk(std::true_type{});
+        else walk(std::false_type{});
+        if (rows.starts && a.dh0 && in) {
+          float *p = a.dh0 + ((int64_t)__builtin_amdgcn_readlane(bag_of.x, from) * a.dim + d) * N + 4 * q;
+          store_floats<float, 4>(p, N - 4 * q, carry);
         }
         to = from;
       }
+      const int me = lane_again() & 63;
 #pragma unroll
       for (int i = 0; i < OWN; ++i) {
-        const int t = i * LPC + q;
-        if (t < lo || t >= hi || !in) continue;
-        const int64_t at = (row0 + t) * a.dim + d;
-        const float4 s = row[t][e];  // D, D x, dv, x
+        const int t = i * LPC + me % LPC, of = block * CH + wave * CPW + me / LPC;
+        if (t < here.lo || t >= here.hi || of >= a.dim) continue;
+        const int64_t at = (now.row0 + t) * a.dim + of;
+        const float4 s = row[t][me / LPC];
         const float du = (own_w[i] + s.w * own_b[i]) * slope[i];
         ((E *)a.dx)[at] = (E)(skip * s.z + s.x * own_b[i]);
         ((E *)a.ddelta)[at] = (E)du;
@@ -678,25 +846,19 @@ __global__ __launch_bounds__(64 * kGradWaves, 2) void ssm_grad_kernel(SsmArgs a,
         dskip += s.z * s.w;
         dbias += du;
       }
-      __syncthreads();
-      for (int i = threadIdx.x; i < S * 2 * NP; i += 64 * waves) {
-        const int t = i / (2 * NP), n = i % (2 * NP), s = n % NP;
-        if (t < lo || t >= hi || s >= N) continue;
-        float v = 0.0f;
-        for (int j = 0; j < waves; ++j) v += part[j * S * 2 * NP + i];
-        const int64_t r = row0 + t;
-        if (a.shared) a.shared[((int64_t)block * a.rows + r) * 2 * N + (n < NP ? 0 : N) + s] = v;
-        else ((E *)(n < NP ? a.db : a.dc))[r * a.groups * N + group * N + s] = (E)v;
-      }
-    }
+      done = now;
+      now = next;
+      next = then;
+      buffer ^= 1;
+    } while (now.there);
+    __syncthreads();
+    give_shared(done, buffer ^ 1);
   }
   dskip = lane_sum<LPC>(dskip);
   dbias = lane_sum<LPC>(dbias);
   if (!in) return;
   float *to = a.parts + (worker * a.dim + d) * (N + 2);
-#pragma unroll
-  for (int j = 0; j < 4; ++j)
-    if (4 * q + j < N) to[4 * q + j] = da[j];
+  store_floats<float, 4>(to + 4 * q, N - 4 * q, da);
   if (q == 0) to[N] = dskip, to[N + 1] = dbias;
 }
 
@@ -767,9 +929,8 @@ struct GradLay {
 };
 GradLay grad_lay(int dim, int groups, int np) {
   const int each = 64 / (np / 4);  // elements of a wavefront
-  int waves = kGradWaves;
-  if (groups > 1) waves = std::min(waves, 64 / each);  // a workgroup's elements are of one group
-  else waves = (int)std::min<int64_t>(waves, divide_up(dim, each));
+  const bool eight = groups > 1 ? dim / groups % (8 * each) == 0 : dim > 4 * each;  // a workgroup's elements are of one group
+  const int waves = eight ? 8 : 4;
   return {waves, (int)divide_up(dim, waves * each)};
 }
 int64_t workers_of(int64_t units, int blocks) { return std::max<int64_t>(1, std::min<int64_t>(units, kGradWorkers / blocks)); }
@@ -828,8 +989,9 @@ int backward(SsmArgs a, const tbe_ssm_grads *g, hipStream_t st) {
     ssm_grad_ends_kernel<E, NP><<<dim3((unsigned)(a.count * a.waves)), 64, 0, st>>>(a);
     join<NP, true>(a, st);
   }
-  const size_t lds = (size_t)kSaved * 2 * NP * 4 * (1 + l.waves) + (size_t)l.waves * kSaved * (64 / (NP / 4)) * 16;
-  ssm_grad_kernel<E, NP><<<dim3((unsigned)(a.workers * l.blocks)), 64 * l.waves, lds, st>>>(a, l.waves);
+  const dim3 grid((unsigned)(a.workers * l.blocks));
+  if (l.waves == 8) ssm_grad_kernel<E, NP, 8><<<grid, 512, 0, st>>>(a);
+  else ssm_grad_kernel<E, NP, 4><<<grid, 256, 0, st>>>(a);
   if (a.shared) {
     const int64_t groups = divide_up(a.rows * a.groups * 2 * a.states, kThreads);
     for (int64_t done = 0; done < groups; done += most_groups(kThreads))
