@@ -570,6 +570,15 @@ __device__ inline void sum_elements(float (&v)[8], float *to, bool up8, bool giv
   }
 }
 
+// The kernel's arguments, read again: kept in scalar registers through a loop there would be more of them than there are, and each use of one that has
+// been moved to a vector register's lane is a vector instruction.
+using ArgsInPlace = const __attribute__((address_space(4))) SsmArgs;
+__device__ inline ArgsInPlace *args_again() {
+  ArgsInPlace *p = (ArgsInPlace *)__builtin_amdgcn_kernarg_segment_ptr();
+  asm volatile("" : "+s"(p));
+  return p;
+}
+
 // Backward of a unit's rows: a lane has states 4 q .. 4 q + 3 of an element; a workgroup's wavefronts have elements side by side.  Rows are gone
 // through in blocks of kSaved, last block first, each bag's rows of a block at a time: forward from the state before them, w and
 // the decays kept in registers, and back.
@@ -588,7 +597,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void ssm_grad_kernel(SsmArgs a) {
   const bool up8 = lane & 8, give = LPC != 4 || !(lane & 4);
   const int64_t worker = blockIdx.x / a.blocks;
   const int block = (int)(blockIdx.x % a.blocks), d = block * CH + wave * CPW + e, dc = min(d, a.dim - 1);
-  const bool in = d < a.dim, gated = a.z;
+  const bool in = d < a.dim, gated = a.z, with_h0 = a.h0, with_dlast = a.dlast;
   const int group = a.groups > 1 ? block * CH / (a.dim / a.groups) : 0;
   float av[4], da[4] = {0.0f, 0.0f, 0.0f, 0.0f}, dskip = 0.0f, dbias = 0.0f;
 #pragma unroll
@@ -616,6 +625,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void ssm_grad_kernel(SsmArgs a) {
     bool there;
   };
   auto enter = [&](int64_t k) {
+    const auto &a = *args_again();
     for (; k < a.count; k += a.workers) {
       const int64_t begin = a.units[k].begin, end = a.units[k + 1].begin;
       if (begin < end) return Place{(end - 1) & ~(int64_t)(S - 1), begin, end, k, true};
@@ -623,7 +633,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void ssm_grad_kernel(SsmArgs a) {
     return Place{0, 0, 1, k, false};  // (what is read ahead of it is not used)
   };
   auto after = [&](Place p) {
-    if (p.there && p.row0 <= p.begin) return enter(p.k + a.workers);
+    if (p.there && p.row0 <= p.begin) return enter(p.k + args_again()->workers);
     p.row0 = max(p.row0 - S, (int64_t)0);
     return p;
   };
@@ -634,6 +644,8 @@ __global__ __launch_bounds__(64 * WAVES, 2) void ssm_grad_kernel(SsmArgs a) {
   float4 before;
   auto fetch = [&](const Place &p) {
     const int me = lane_again();
+    const auto &a = *args_again();
+    const bool gated = a.z;
 #pragma unroll
     for (int i = 0; i < BRINGS; ++i) {
       const int n = me + i * THREADS, kind = n / (S * PACKS) & 3, t = n / PACKS % S, at = block * CH + n % PACKS * V;
@@ -652,7 +664,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void ssm_grad_kernel(SsmArgs a) {
     }
     before = *(const float4 *)(a.saved + (p.row0 / S * a.dim + dc) * NP + 4 * q);
   };
-  auto mark_at = [&](const Place &p) { return a.marks[min(max(p.row0 + (lane & (S - 1)), p.begin), p.end - 1)]; };
+  auto mark_at = [&](const Place &p) { return args_again()->marks[min(max(p.row0 + (lane & (S - 1)), p.begin), p.end - 1)]; };
   // a block's rows that are this unit's, and the bags that start and end in them
   struct Seen {
     int lo, hi;
@@ -675,12 +687,14 @@ __global__ __launch_bounds__(64 * WAVES, 2) void ssm_grad_kernel(SsmArgs a) {
     return Bag{b ? 31 - __builtin_clz(b) : s.lo, b != 0, (s.ends >> (to - 1) & 1) != 0};
   };
   auto ask = [&](const Bag &b, int to, int2 mark, float (&h)[4], float (&g)[4]) {
+    const auto &a = *args_again();
     if (b.starts && a.h0) four(a.h0 + (int64_t)__builtin_amdgcn_readlane(mark.x, b.from) * a.h0s, h);
     if (b.ends && a.dlast) four(a.dlast + (int64_t)__builtin_amdgcn_readlane(mark.y, to - 1) * a.dim * N, g);
   };
   // db and dc of a block, from the wavefronts' sums
   auto give_shared = [&](const Place &p, int buffer) {
     const int me = lane_again();
+    const auto &a = *args_again();
 #pragma unroll
     for (int i = 0; i < NUMBERS; ++i) {
       const int n = me + i * THREADS, t = n / (2 * NP), m = n % (2 * NP), s = m % NP;
@@ -733,7 +747,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void ssm_grad_kernel(SsmArgs a) {
         unit = now.k;
 #pragma unroll
         for (int j = 0; j < 4; ++j) carry[j] = 0.0f;
-        if (a.units[unit + 1].cut) {
+        if (args_again()->units[unit + 1].cut) {
           const float a2[4] = {av[0] * kLog2e, av[1] * kLog2e, av[2] * kLog2e, av[3] * kLog2e};
           start_of<NP>(a, unit, dc, 4 * q, a2, carry);
           settle(carry);
@@ -769,8 +783,8 @@ __global__ __launch_bounds__(64 * WAVES, 2) void ssm_grad_kernel(SsmArgs a) {
         }
         const int from = rows.from;
         float start[4], finish[4];
-        known(a.h0, asked_h, start);
-        known(a.dlast, asked_g, finish);
+        known(with_h0, asked_h, start);
+        known(with_dlast, asked_g, finish);
 #pragma unroll
         for (int j = 0; j < 4; ++j) h[j] = rows.starts ? start[j] : saved[j];  // (a unit that begins within a block begins with a bag)
 #pragma unroll
@@ -826,23 +840,24 @@ __global__ __launch_bounds__(64 * WAVES, 2) void ssm_grad_kernel(SsmArgs a) {
         };
         if (from == 0 && to == S) walk(std::true_type{});
         else walk(std::false_type{});
-        if (rows.starts && a.dh0 && in) {
-          float *p = a.dh0 + ((int64_t)__builtin_amdgcn_readlane(bag_of.x, from) * a.dim + d) * N + 4 * q;
+        if (rows.starts && args_again()->dh0 && in) {
+          float *p = args_again()->dh0 + ((int64_t)__builtin_amdgcn_readlane(bag_of.x, from) * args_again()->dim + d) * N + 4 * q;
           store_floats<float, 4>(p, N - 4 * q, carry);
         }
         to = from;
       }
       const int me = lane_again() & 63;
+      const auto &again = *args_again();
 #pragma unroll
       for (int i = 0; i < OWN; ++i) {
         const int t = i * LPC + me % LPC, of = block * CH + wave * CPW + me / LPC;
-        if (t < here.lo || t >= here.hi || of >= a.dim) continue;
-        const int64_t at = (now.row0 + t) * a.dim + of;
+        if (t < here.lo || t >= here.hi || of >= again.dim) continue;
+        const int64_t at = (now.row0 + t) * again.dim + of;
         const float4 s = row[t][me / LPC];
         const float du = (own_w[i] + s.w * own_b[i]) * slope[i];
-        ((E *)a.dx)[at] = (E)(skip * s.z + s.x * own_b[i]);
-        ((E *)a.ddelta)[at] = (E)du;
-        if (gated) ((E *)a.dz)[at] = (E)(gate[i] * (own_v[i] + skip * s.w));
+        ((E *)again.dx)[at] = (E)(skip * s.z + s.x * own_b[i]);
+        ((E *)again.ddelta)[at] = (E)du;
+        if (gated) ((E *)again.dz)[at] = (E)(gate[i] * (own_v[i] + skip * s.w));
         dskip += s.z * s.w;
         dbias += du;
       }
