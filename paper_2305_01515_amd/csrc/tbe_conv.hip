@@ -4,10 +4,10 @@
 //   v_t = bias + sum over j < W of w_j e_{t-W+1+j},  e: a bag's earlier rows and its rows;  y = v or silu(v).
 //   With g = dy silu'(v):  de_i = sum over k < W of w_{W-1-k} g_{i+k} (rows of the bag),  dw_j = sum over t of g_t e_{t-W+1+j},  dbias = sum of g.
 //
-// Bound by memory.  A workgroup takes a tile of rows wherever bags begin; a lane walks V elements of kRows rows in a row down, with the
-// last W - 1 rows in registers, after up to W - 1 rows in front of its own that it reads once more (from the caches).  Where bags start within the
-// tile is written to LDS first.  The backward walks the same way and W - 1 rows on: it finds v again, has the sums of the last W - 1
-// rows' gradients in registers and gives a row up when the last result that sees it is done, or where the bag ends.
+// Bound by memory.  A workgroup takes a tile of rows wherever bags begin; a lane walks V elements of so many rows in a row down, all of which it reads
+// at first, and W - 1 in front of them once more (from the caches).  Where bags start within the tile is written to LDS meanwhile.  Rows
+// near a bag's start, which do not see all of the rows in front of them, take a way of their own.  The backward walks the same way and
+// W - 1 rows on: it finds v again, keeps the sums of the last W rows' gradients and gives a row up when the last result that sees it is done.
 #include <algorithm>
 #include <new>
 
@@ -18,7 +18,8 @@ using namespace tbe;
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kRows = 16;                  // of a lane in a tile
+constexpr int kRows = 8;                   // of a lane in a tile
+constexpr int grad_rows(int width) { return width <= 4 ? 8 : 4; }  // ... in the backward: its lanes hold those that see them too
 constexpr int kMostWidth = 8;
 constexpr int64_t kMostParts = 1024;       // workgroups of the backward, each with partial sums of dw and dbias
 
@@ -34,8 +35,8 @@ struct ConvArgs {
   bool silu;
 };
 
-template <class E> constexpr int kPack = 16 / sizeof(E) < 8 ? 4 : 8;
-constexpr int kGradPack = 4;
+template <class E> constexpr int kPack = 16 / sizeof(E);
+template <class E> constexpr int kGradPack = 8 / sizeof(E);
 
 // how many of the ascending offsets[0 .. n) are at most `row`, the same in all lanes of a wavefront: 64 places are looked at at once
 __device__ inline int64_t count_up_to(const int64_t *off, int64_t n, int64_t row) {
@@ -68,55 +69,36 @@ __device__ inline Head mark_tile(const ConvArgs &a, int64_t r0, int64_t r1, int 
   return {head, min(a.off[head], r0)};
 }
 
-// The state of a walk: the last W - 1 rows of e (the latest last)
-template <int W, int V>
-struct Ring {
-  float e[W > 1 ? W - 1 : 1][V];
-};
-
-template <class E, int W, int V>
-__device__ inline void fill_before(Ring<W, V> &ring, const ConvArgs &a, int64_t bag, int at, int n) {
+// how many rows of its bag row r, the first of a walk, has in front of it, W - 1 or more as W - 1, and its bag if there are fewer
+template <int W>
+__device__ inline int age_of(const int *marks, int64_t r0, int64_t r, Head head, int64_t &bag) {
+  bag = head.bag;
 #pragma unroll
   for (int k = 0; k < W - 1; ++k) {
-    if (a.before) load_floats<E, V>((const E *)a.before + (bag * (W - 1) + k) * a.dim + at, n, ring.e[k]);
-    else
-#pragma unroll
-      for (int j = 0; j < V; ++j) ring.e[k][j] = 0.0f;
-  }
-}
-
-// the rows in front of row r (which does not start a bag, or the ring is filled again): those of its bag, and the earlier ones of that bag
-template <class E, int W, int V>
-__device__ inline void fill_ring(Ring<W, V> &ring, const ConvArgs &a, const int *marks, int64_t r0, int64_t r, Head head, int at, int n) {
-  if constexpr (W > 1) {
-    int64_t start = head.start, bag = head.bag;
-    int k = 1;
-    for (; k < W && r - k >= r0; ++k)
-      if (marks[r - k - r0] >= 0) {
-        start = r - k, bag = marks[r - k - r0];
-        break;
-      }
-#pragma unroll
-    for (int k = 0; k < W - 1; ++k) {
-      const int64_t i = r - (W - 1) + k;
-      if (i >= start && i >= 0) load_floats<E, V>((const E *)a.x + i * a.xs + at, n, ring.e[k]);
-      else if (a.before && i - start + (W - 1) >= 0) load_floats<E, V>((const E *)a.before + (bag * (W - 1) + (i - start + W - 1)) * a.dim + at, n, ring.e[k]);
-      else
-#pragma unroll
-        for (int j = 0; j < V; ++j) ring.e[k][j] = 0.0f;
+    if (r - k < r0) break;
+    if (marks[r - k - r0] >= 0) {
+      bag = marks[r - k - r0];
+      return k;
     }
   }
+  return (int)min(max(r - head.start, (int64_t)0), (int64_t)(W - 1));
 }
 
-template <int W, int V>
-__device__ inline void push(Ring<W, V> &ring, const float (&x)[V]) {
+// The rows that a result sees, oldest first, where its bag has only `age` < W - 1 rows in front of it: the others are earlier ones, or zero
+template <class E, int W, int V>
+__device__ inline void young(const ConvArgs &a, int age, int64_t bag, int at, int n, float (&e)[W][V]) {
 #pragma unroll
-  for (int k = 0; k + 1 < W - 1; ++k)
+  for (int k = 0; k < W - 1; ++k)  // e[k]: W - 1 - k rows back
+    if (W - 1 - k > age) {
+      if (a.before) {
+        load_floats<E, V>((const E *)a.before + (bag * (W - 1) + k + age) * a.dim + at, n, e[k]);
+      } else {
 #pragma unroll
-    for (int j = 0; j < V; ++j) ring.e[k][j] = ring.e[k + 1][j];
-  if constexpr (W > 1)
+        for (int j = 0; j < V; ++j) e[k][j] = 0.0f;
+      }
 #pragma unroll
-    for (int j = 0; j < V; ++j) ring.e[W - 2][j] = x[j];
+      for (int j = 0; j < V; ++j) asm volatile("" : "+v"(e[k][j]));  // waited for here, and not by the rows that load nothing
+    }
 }
 
 template <int W, int V>
@@ -131,42 +113,71 @@ __device__ inline void load_weights(const ConvArgs &a, int at, float (&w)[W][V],
 }
 
 template <int W, int V>
-__device__ inline void result(const Ring<W, V> &ring, const float (&x)[V], const float (&w)[W][V], const float (&bias)[V], float (&v)[V]) {
+__device__ inline void result(const float (&e)[W][V], const float (&w)[W][V], const float (&bias)[V], float (&v)[V]) {
 #pragma unroll
   for (int j = 0; j < V; ++j) {
     v[j] = bias[j];
 #pragma unroll
-    for (int k = 0; k < W - 1; ++k) v[j] += w[k][j] * ring.e[k][j];
-    v[j] += w[W - 1][j] * x[j];
+    for (int k = 0; k < W; ++k) v[j] += w[k][j] * e[k][j];
   }
 }
 
-// Row m of the bag's last W - 1 ones, for the lanes behind the tiles: from the rows or the earlier ones.  GRAD: an empty bag's dbefore, which is its dlast.
-template <class E, int W, bool GRAD>
-__device__ inline void bag_ends(const ConvArgs &a, int64_t i) {
+// whether bag b has offsets that do not ascend from 0 to rows, which are reported
+__device__ inline bool refused(const ConvArgs &a, int64_t b, int64_t s, int64_t e, bool say) {
+  const bool bad = s > e || s < 0 || e > a.rows || (b == 0 && s != 0) || (b == a.bags - 1 && e != a.rows);
+  if (bad && say) *a.err = 1;
+  return bad;
+}
+// The lanes behind the tiles have a pack each of a row m of what is a bag's own: of its last W - 1 rows, from the rows or the earlier ones
+template <class E, int W>
+__device__ inline void last_rows(const ConvArgs &a, int64_t i) {
   if constexpr (W > 1) {
-    const int64_t per_bag = (int64_t)(W - 1) * a.dim, b = i / per_bag;
+    constexpr int V = kPack<E>;
+    const int packs = (a.dim + V - 1) / V;
+    const int64_t row = quotient(i, packs), b = quotient(row, W - 1);
     if (b >= a.bags) return;
+    const int m = (int)(row - b * (W - 1)), at = (int)(i - row * packs) * V;
     const int64_t s = a.off[b], e = a.off[b + 1];
-    const int64_t in = i - b * per_bag;
-    if (s > e || s < 0 || e > a.rows || (b == 0 && s != 0) || (b == a.bags - 1 && e != a.rows)) {
-      if (in == 0) *a.err = 1;
-      return;
-    }
-    if (GRAD) {
-      if (s == e) ((E *)a.dbefore)[i] = a.dlast ? ((const E *)a.dlast)[i] : (E)0.0f;
-      return;
-    }
-    const int m = (int)(in / a.dim), d = (int)(in - (int64_t)m * a.dim);
+    if (refused(a, b, s, e, m == 0 && at == 0)) return;
     const int64_t r = e - (W - 1) + m;
-    ((E *)a.last)[i] = r >= s ? ((const E *)a.x)[r * a.xs + d] : a.before ? ((const E *)a.before)[b * per_bag + (r - s + W - 1) * a.dim + d] : (E)0.0f;
+    Words<E, V> v;
+    if (r >= s) load_words<E, V>((const E *)a.x + r * a.xs + at, a.dim - at, v);
+    else if (a.before) load_words<E, V>((const E *)a.before + (b * (W - 1) + r - s + W - 1) * a.dim + at, a.dim - at, v);
+    else v = {};
+    store_words<E, V>((E *)a.last + row * a.dim + at, a.dim - at, v);
+  }
+}
+// or, in the backward, an element of the gradient of the earlier rows: sum over t <= m of w_{m-t} g_t, and what of dlast goes past the bag's rows
+template <class E, int W>
+__device__ inline void earlier_rows(const ConvArgs &a, int64_t i) {
+  if constexpr (W > 1) {
+    const int64_t row = quotient(i, a.dim), b = quotient(row, W - 1);
+    if (b >= a.bags) return;
+    const int m = (int)(row - b * (W - 1)), d = (int)(i - row * a.dim);
+    const int64_t s = a.off[b], e = a.off[b + 1], size = e - s;
+    if (refused(a, b, s, e, m == 0 && d == 0)) return;
+    float sum = a.dlast && m >= size ? (float)((const E *)a.dlast)[(row - size) * a.dim + d] : 0.0f;
+    for (int t = 0; t <= m && t < size; ++t) {
+      float g = (float)((const E *)a.dy)[(s + t) * a.dys + d];
+      if (a.silu) {
+        float v = a.bias ? load_param(a.bias, a.weight_dtype, d) : 0.0f;
+        for (int k = 0; k < W; ++k) {
+          const int back = W - 1 - k;
+          const float x = back <= t ? (float)((const E *)a.x)[(s + t - back) * a.xs + d]
+                                    : a.before ? (float)((const E *)a.before)[(b * (W - 1) + t + k) * a.dim + d] : 0.0f;
+          v += load_param(a.weight, a.weight_dtype, (int64_t)d * W + k) * x;
+        }
+        const float f = sigmoid(v);
+        g *= f * (1.0f + v * (1.0f - f));
+      }
+      sum += load_param(a.weight, a.weight_dtype, (int64_t)d * W + m - t) * g;
+    }
+    ((E *)a.dbefore)[i] = (E)sum;
   }
 }
 // the same look at the offsets where there are no such lanes
 __device__ inline void look_over(const ConvArgs &a, int64_t b) {
-  if (b >= a.bags) return;
-  const int64_t s = a.off[b], e = a.off[b + 1];
-  if (s > e || s < 0 || e > a.rows || (b == 0 && s != 0) || (b == a.bags - 1 && e != a.rows)) *a.err = 1;
+  if (b < a.bags) refused(a, b, a.off[b], a.off[b + 1], true);
 }
 
 template <class E, int W>
@@ -176,49 +187,66 @@ __global__ __launch_bounds__(kThreads) void conv_kernel(ConvArgs a) {
   const int64_t group = a.first_group + blockIdx.x;
   if (group >= a.tiles * a.passes) {
     const int64_t i = (group - a.tiles * a.passes) * kThreads + threadIdx.x;
-    if (W > 1 && a.last) bag_ends<E, W, false>(a, i);
+    if (W > 1 && a.last) last_rows<E, W>(a, i);
     else look_over(a, i);
     return;
   }
   const int64_t tile = group / a.passes;
   const int walks = kThreads / a.lanes, tile_rows = walks * kRows;
   const int64_t r0 = tile * tile_rows, r1 = min(r0 + tile_rows, a.rows);
-  const Head head = mark_tile(a, r0, r1, marks, tile_rows);
   const int at = ((int)(group % a.passes) * a.lanes + (threadIdx.x & (a.lanes - 1))) * V, n = a.dim - at;
   const int64_t first = r0 + threadIdx.x / a.lanes * kRows;
-  if (n <= 0 || first >= r1) return;
+  const bool some = n > 0 && first < r1;
+  Words<E, V> raw[W - 1 + kRows];  // rows first - (W - 1) and on
+  if (some) {
+#pragma unroll
+    for (int i = 0; i < W - 1 + kRows; ++i) load_words<E, V>((const E *)a.x + min(max(first - (W - 1) + i, (int64_t)0), r1 - 1) * a.xs + at, n, raw[i]);
+  }
+  const Head head = mark_tile(a, r0, r1, marks, tile_rows);
+  if (!some) return;
   float w[W][V], bias[V];
   load_weights<W, V>(a, at, w, bias);
-  Ring<W, V> ring;
-  fill_ring<E, W, V>(ring, a, marks, r0, first, head, at, n);
-  const int64_t end = min(first + kRows, r1);
-#pragma unroll 4
-  for (int64_t r = first; r < end; ++r) {
-    float x[V], v[V];
-    load_floats<E, V>((const E *)a.x + r * a.xs + at, n, x);
-    const int b = marks[r - r0];
-    if (b >= 0) fill_before<E, W, V>(ring, a, b, at, n);
-    result<W, V>(ring, x, w, bias, v);
+  int64_t bag;
+  int age = age_of<W>(marks, r0, first, head, bag);
+  E *y = (E *)a.y + first * a.ys + at;
+  const int rows = (int)min((int64_t)kRows, r1 - first);
+  const int *mark = marks + (first - r0);
+#pragma unroll
+  for (int i = 0; i < kRows; ++i) {
+    if (i >= rows) continue;
+    __builtin_amdgcn_sched_barrier(0);  // rows become fp32 one by one: all at once they do not fit the registers
+    if (i > 0) {
+      const int b = mark[i];
+      age = b >= 0 ? 0 : min(age + 1, W - 1);
+      bag = b >= 0 ? b : bag;
+    }
+    float e[W][V], v[V];
+#pragma unroll
+    for (int k = 0; k < W; ++k)
+#pragma unroll
+      for (int j = 0; j < V; ++j) e[k][j] = raw[i + k].get(j);
+    if (age < W - 1) young<E, W, V>(a, age, bag, at, n, e);
+    result<W, V>(e, w, bias, v);
     if (a.silu) {
 #pragma unroll
       for (int j = 0; j < V; ++j) v[j] *= sigmoid(v[j]);
     }
-    store_floats<E, V>((E *)a.y + r * a.ys + at, n, v);
-    push<W, V>(ring, x);
+    store_floats<E, V>(y, n, v);
+    y += a.ys;
   }
 }
 
 template <class E, int W>
 __global__ __launch_bounds__(kThreads) void conv_grad_kernel(ConvArgs a, int64_t workers) {
-  constexpr int V = kGradPack, K = W + 1;  // sums of an element: W of dw, one of dbias
-  extern __shared__ int marks[];           // tile_rows + W - 1 of them, and then the sums of the walks
+  constexpr int V = kGradPack<E>, R = grad_rows(W), K = W + 1;  // sums of an element: W of dw, one of dbias
+  extern __shared__ int marks[];                             // tile_rows + W - 1 of them, and then the sums of the walks
   if ((int64_t)blockIdx.x >= workers * a.passes) {
     const int64_t i = ((int64_t)blockIdx.x - workers * a.passes) * kThreads + threadIdx.x;
-    if (W > 1 && a.dbefore) bag_ends<E, W, true>(a, i);
+    if (W > 1 && a.dbefore) earlier_rows<E, W>(a, i);
     else look_over(a, i);
     return;
   }
-  const int lane = threadIdx.x & (a.lanes - 1), walk = threadIdx.x / a.lanes, walks = kThreads / a.lanes, tile_rows = walks * kRows;
+  const int lane = threadIdx.x & (a.lanes - 1), walk = threadIdx.x / a.lanes, walks = kThreads / a.lanes, tile_rows = walks * R;
   const int64_t worker = blockIdx.x / a.passes;
   const int at = ((int)(blockIdx.x % a.passes) * a.lanes + lane) * V, n = a.dim - at;
   float w[W][V], bias[V], dw[K][V];
@@ -229,106 +257,99 @@ __global__ __launch_bounds__(kThreads) void conv_grad_kernel(ConvArgs a, int64_t
     for (int j = 0; j < V; ++j) dw[k][j] = 0.0f;
   for (int64_t tile = worker; tile < a.tiles; tile += workers) {
     const int64_t r0 = tile * tile_rows, r1 = min(r0 + tile_rows, a.rows);
+    const int64_t first = r0 + walk * R, stop = min(r1 + W - 1, a.rows);
+    const bool some = n > 0 && first < r1;
+    Words<E, V> raw[2 * (W - 1) + R], raw_dy[W - 1 + R];  // rows first - (W - 1) and on, rows first and on
+    if (some) {
+#pragma unroll
+      for (int i = 0; i < 2 * (W - 1) + R; ++i) load_words<E, V>((const E *)a.x + min(max(first - (W - 1) + i, (int64_t)0), stop - 1) * a.xs + at, n, raw[i]);
+#pragma unroll
+      for (int i = 0; i < W - 1 + R; ++i) load_words<E, V>((const E *)a.dy + min(first + i, stop - 1) * a.dys + at, n, raw_dy[i]);
+    }
     __syncthreads();  // the marks of the tile before
-    const Head head = mark_tile(a, r0, min(r1 + W - 1, a.rows), marks, tile_rows + W - 1);
-    const int64_t first = r0 + walk * kRows, end = min(first + kRows, r1);
-    if (n <= 0 || first >= r1) continue;
-    Ring<W, V> ring;
-    fill_ring<E, W, V>(ring, a, marks, r0, first, head, at, n);
-    float acc[W][V];  // acc[k]: what rows r - k have had so far
+    const Head head = mark_tile(a, r0, stop, marks, tile_rows + W - 1);
+    if (!some) continue;
+    int64_t bag;
+    int age = age_of<W>(marks, r0, first, head, bag);
+    const int *mark = marks + (first - r0);
+    float acc[W][V];  // acc[k]: what row t - k has had so far
 #pragma unroll
     for (int k = 0; k < W; ++k)
 #pragma unroll
       for (int j = 0; j < V; ++j) acc[k][j] = 0.0f;
-    int64_t bag = -1, start = -1;  // of the bag that started within these rows
-    // Row p has all of its gradient, d.  `ends`: the bag, `of`, ends in front of row e, so its last rows have a part of dlast.
-    auto give = [&](int64_t p, const float(&d)[V], bool ends, int64_t e, int64_t of) {
-      float o[V];
 #pragma unroll
-      for (int j = 0; j < V; ++j) o[j] = d[j];
-      if (ends && a.dlast && p >= e - (W - 1)) {
-        float t[V];
-        load_floats<E, V>((const E *)a.dlast + (of * (W - 1) + (p - e + W - 1)) * a.dim + at, n, t);
+    for (int i = 0; i < R + W - 1; ++i) {
+      __builtin_amdgcn_sched_barrier(0);
+      const int64_t t = first + i;
+      const bool there = t < a.rows;  // behind the last row nothing sees anything, like behind the end of a bag
+      const int b = there ? mark[i] : 0;
+      if (i > 0) {
+        age = b >= 0 ? 0 : min(age + 1, W - 1);
+        bag = b >= 0 ? b : bag;
+      }
+      if (!there) age = 0;
+      if (there) {
+        float e[W][V], g[V], v[V];
 #pragma unroll
-        for (int j = 0; j < V; ++j) o[j] += t[j];
-      }
-      if (start >= 0 && p < start) {  // an earlier row of a bag that starts here
-        if (a.dbefore && p >= start - (W - 1)) store_floats<E, V>((E *)a.dbefore + (of * (W - 1) + (p - start + W - 1)) * a.dim + at, n, o);
-      } else if (p >= first && p < end) {
-        store_floats<E, V>((E *)a.dx + p * a.dxs + at, n, o);
-      }
-    };
-    auto finish = [&](int64_t e) {  // the bag ends in front of row e: its rows e - 1 .. e - W + 1 (and earlier ones) are done
-      int64_t of = bag >= 0 ? bag : head.bag;
-      if (bag < 0 && a.dlast)  // it started in front of these rows, in this tile or before
-        for (int64_t q = first - 1; q >= r0; --q)
-          if (marks[q - r0] >= 0) {
-            of = marks[q - r0];
-            break;
+        for (int k = 0; k < W; ++k)
+#pragma unroll
+          for (int j = 0; j < V; ++j) e[k][j] = raw[i + k].get(j);
+#pragma unroll
+        for (int j = 0; j < V; ++j) g[j] = raw_dy[i].get(j);
+        if (age < W - 1) young<E, W, V>(a, age, bag, at, n, e);
+        if (a.silu) {
+          result<W, V>(e, w, bias, v);
+#pragma unroll
+          for (int j = 0; j < V; ++j) {
+            const float f = sigmoid(v[j]);
+            g[j] *= f * (1.0f + v[j] * (1.0f - f));
           }
+        }
+        if (i < R && t < r1) {
 #pragma unroll
-      for (int k = W - 1; k >= 1; --k) give(e - k, acc[k], true, e, of);
-    };
-    const int64_t stop = min(end + W - 1, a.rows);
-    int64_t r = first;
-    bool open = false;  // rows of `first` and after have something in acc
-    for (; r < stop; ++r) {
-      const int b = marks[r - r0];
-      // acc[k] belongs to row r - k from here on
+          for (int j = 0; j < V; ++j) {
+#pragma unroll
+            for (int k = 0; k < W; ++k) dw[k][j] += g[j] * e[k][j];
+            dw[W][j] += g[j];
+          }
+        }
+        if (age < W - 1) {  // only rows of its bag
+#pragma unroll
+          for (int k = 0; k < W; ++k)
+#pragma unroll
+            for (int j = 0; j < V; ++j) acc[k][j] += k <= age ? w[W - 1 - k][j] * g[j] : 0.0f;
+        } else {
+#pragma unroll
+          for (int k = 0; k < W; ++k)
+#pragma unroll
+            for (int j = 0; j < V; ++j) acc[k][j] += w[W - 1 - k][j] * g[j];
+        }
+      }
+      // row t - (W - 1) has all of its gradient but dlast's part, which rows W - 1 or less before the bag's end have
+      const int64_t p = t - (W - 1);
+      if (i >= W - 1 && p < r1) {
+        if (age < W - 1 && a.dlast) {
+          int64_t ends = stop, of = head.bag;  // (stop: all rows there are, or p is not near the end)
+          for (int k = W - 1; k >= 1; --k)
+            if (p + k < stop && marks[p + k - r0] >= 0) ends = p + k;
+          for (int64_t r = p; r >= r0; --r)
+            if (marks[r - r0] >= 0) {
+              of = marks[r - r0];
+              break;
+            }
+          float d[V];
+          load_floats<E, V>((const E *)a.dlast + (of * (W - 1) + max(p - ends + W - 1, (int64_t)0)) * a.dim + at, n, d);
+#pragma unroll
+          for (int j = 0; j < V; ++j) acc[W - 1][j] += d[j];
+        }
+        store_floats<E, V>((E *)a.dx + p * a.dxs + at, n, acc[W - 1]);
+      }
 #pragma unroll
       for (int k = W - 1; k >= 1; --k)
 #pragma unroll
         for (int j = 0; j < V; ++j) acc[k][j] = acc[k - 1][j];
 #pragma unroll
       for (int j = 0; j < V; ++j) acc[0][j] = 0.0f;
-      if (b >= 0) {
-        if (open) finish(r);
-        if (r >= end) {  // the next walk's
-          open = false;
-          break;
-        }
-        fill_before<E, W, V>(ring, a, b, at, n);
-        bag = b, start = r;
-#pragma unroll
-        for (int k = 1; k < W; ++k)
-#pragma unroll
-          for (int j = 0; j < V; ++j) acc[k][j] = 0.0f;
-      }
-      open = true;
-      float x[V], g[V], v[V];
-      load_floats<E, V>((const E *)a.x + r * a.xs + at, n, x);
-      load_floats<E, V>((const E *)a.dy + r * a.dys + at, n, g);
-      if (a.silu) {
-        result<W, V>(ring, x, w, bias, v);
-#pragma unroll
-        for (int j = 0; j < V; ++j) {
-          const float f = sigmoid(v[j]);
-          g[j] *= f * (1.0f + v[j] * (1.0f - f));
-        }
-      }
-      if (r < end) {
-#pragma unroll
-        for (int j = 0; j < V; ++j) {
-#pragma unroll
-          for (int k = 0; k < W - 1; ++k) dw[k][j] += g[j] * ring.e[k][j];
-          dw[W - 1][j] += g[j] * x[j];
-          dw[W][j] += g[j];
-        }
-      }
-#pragma unroll
-      for (int k = 0; k < W; ++k)
-#pragma unroll
-        for (int j = 0; j < V; ++j) acc[k][j] += w[W - 1 - k][j] * g[j];
-      give(r - (W - 1), acc[W - 1], false, 0, bag);
-      push<W, V>(ring, x);
-    }
-    // Rows of the walk that are still open: the data end, so does their bag.  (Otherwise the walk has gone W - 1 rows on and given up all of its own.)
-    if (open && r == a.rows) {
-#pragma unroll
-      for (int k = W - 1; k >= 1; --k)
-#pragma unroll
-        for (int j = 0; j < V; ++j) acc[k][j] = acc[k - 1][j];
-      finish(r);
     }
   }
   if (!a.parts) return;
@@ -363,21 +384,19 @@ __global__ __launch_bounds__(kThreads) void conv_step_kernel(ConvArgs a, E *stat
 #pragma unroll
     for (int j = 0; j < V; ++j) v[j] = 0.0f;
   } else {
-    float w[W][V], bias[V], x[V];
-    Ring<W, V> ring;
+    float w[W][V], bias[V], e[W][V];
     E *s = state + slot * (W - 1) * a.dim + at;
 #pragma unroll
-    for (int k = 0; k < W - 1; ++k) load_floats<E, V>(s + (int64_t)k * a.dim, n, ring.e[k]);
-    load_floats<E, V>((const E *)a.x + r * a.xs + at, n, x);
+    for (int k = 0; k < W - 1; ++k) load_floats<E, V>(s + (int64_t)k * a.dim, n, e[k]);
+    load_floats<E, V>((const E *)a.x + r * a.xs + at, n, e[W - 1]);
     load_weights<W, V>(a, at, w, bias);
-    result<W, V>(ring, x, w, bias, v);
+    result<W, V>(e, w, bias, v);
     if (a.silu) {
 #pragma unroll
       for (int j = 0; j < V; ++j) v[j] *= sigmoid(v[j]);
     }
-    push<W, V>(ring, x);
 #pragma unroll
-    for (int k = 0; k < W - 1; ++k) store_floats<E, V>(s + (int64_t)k * a.dim, n, ring.e[k]);
+    for (int k = 0; k < W - 1; ++k) store_floats<E, V>(s + (int64_t)k * a.dim, n, e[k + 1]);
   }
   if (a.y) store_floats<E, V>((E *)a.y + r * a.ys + at, n, v);
 }
@@ -395,21 +414,21 @@ struct tbe_conv_t : DenseBase {
 namespace {
 
 // Lanes of a row (a power of two up to kThreads), and how often so many lanes' elements go into one
-void lanes_of(ConvArgs &a, int V) {
+void lanes_of(ConvArgs &a, int V, int walk) {
   const int packs = (a.dim + V - 1) / V;
   a.lanes = 1;
   while (a.lanes < packs && a.lanes < kThreads) a.lanes *= 2;
   a.passes = (packs + a.lanes - 1) / a.lanes;
-  a.tiles = divide_up(a.rows, (int64_t)kThreads / a.lanes * kRows);
+  a.tiles = divide_up(a.rows, (int64_t)kThreads / a.lanes * walk);
 }
-int64_t tail_groups(const ConvArgs &a, int width) {  // of lanes behind the tiles, for what is a bag's own
-  return divide_up(width > 1 && (a.last || a.dbefore) ? a.bags * (width - 1) * a.dim : a.bags, kThreads);
+int64_t tail_groups(const ConvArgs &a, int width, int pack) {  // of lanes behind the tiles, for what is a bag's own
+  return divide_up(width > 1 && (a.last || a.dbefore) ? a.bags * (width - 1) * divide_up(a.dim, pack) : a.bags, kThreads);
 }
 
 template <class E, int W>
 int forward(ConvArgs a, hipStream_t st) {
-  lanes_of(a, kPack<E>);
-  const int64_t groups = a.tiles * a.passes + tail_groups(a, W);
+  lanes_of(a, kPack<E>, kRows);
+  const int64_t groups = a.tiles * a.passes + tail_groups(a, W, kPack<E>);
   const size_t lds = (size_t)kThreads / a.lanes * kRows * sizeof(int);
   for (int64_t done = 0; done < groups; done += most_groups(kThreads)) {
     a.first_group = done;
@@ -422,10 +441,10 @@ int64_t workers_of(const ConvArgs &a) { return std::max<int64_t>(1, std::min(a.t
 
 template <class E, int W>
 int backward(ConvArgs a, float *dweight, float *dbias, hipStream_t st) {
-  lanes_of(a, kGradPack);
-  const int64_t workers = workers_of(a), groups = workers * a.passes + tail_groups(a, W);
+  lanes_of(a, kGradPack<E>, grad_rows(W));
+  const int64_t workers = workers_of(a), groups = workers * a.passes + tail_groups(a, W, 1);
   if (groups > most_groups(kThreads)) return report(TBE_ELIMIT, "more bags than one launch can take");
-  const size_t lds = std::max((size_t)(kThreads / a.lanes * kRows + W - 1) * sizeof(int), (size_t)kThreads * kGradPack * (W + 1) * sizeof(float));
+  const size_t lds = std::max((size_t)(kThreads / a.lanes * grad_rows(W) + W - 1) * sizeof(int), (size_t)kThreads * kGradPack<E> * (W + 1) * sizeof(float));
   conv_grad_kernel<E, W><<<dim3((unsigned)groups), kThreads, lds, st>>>(a, workers);
   if (a.parts) sum_parts(a.parts, workers, (int64_t)a.dim * (W + 1), W + 1, W, dweight, dbias, nullptr, st);
   return check_launch();
@@ -518,7 +537,7 @@ int tbe_conv_create(tbe_conv_handle *out, int32_t dim, int32_t width, int32_t dt
   s->dim = dim, s->width = width, s->dtype = dtype, s->silu = silu != 0, s->max_bags = max_bags, s->max_rows = max_rows;
   ConvArgs a{};
   a.dim = dim, a.rows = max_rows;
-  lanes_of(a, kGradPack);
+  lanes_of(a, dtype == TBE_FP32 ? kGradPack<float> : kGradPack<_Float16>, grad_rows(width));
   const size_t floats = (size_t)workers_of(a) * dim * (width + 1);
   char *block = nullptr;
   hipError_t e = hipGetDevice(&s->device);

@@ -32,6 +32,52 @@ __device__ inline void store_floats(E *p, int n, const float (&from)[V]) {
   }
 }
 
+// V elements as they lie in memory.  (As elements, each of 16 bits would have a register of its own.)
+template <class E, int V> struct alignas(sizeof(E) * V) Words {
+  uint32_t w[sizeof(E) * V / 4];
+  __device__ float get(int i) const {
+    if constexpr (sizeof(E) == 4) {
+      return __builtin_bit_cast(float, w[i]);
+    } else {
+      const uint16_t b = (uint16_t)(w[i / 2] >> (i % 2 * 16));
+      return (float)__builtin_bit_cast(E, b);
+    }
+  }
+};
+// the first n of them, if fewer: zero beyond
+template <class E, int V>
+__device__ inline void load_words(const E *p, int n, Words<E, V> &to) {
+  if (n >= V) {
+    __builtin_memcpy(to.w, p, sizeof to.w);
+  } else {
+#pragma unroll
+    for (unsigned i = 0; i < sizeof to.w / 4; ++i) to.w[i] = 0;
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      if (i >= n) continue;
+      if constexpr (sizeof(E) == 4) to.w[i] = ((const uint32_t *)p)[i];
+      else to.w[i / 2] |= (uint32_t)((const uint16_t *)p)[i] << (i % 2 * 16);
+    }
+  }
+}
+
+template <class E, int V>
+__device__ inline void store_words(E *p, int n, const Words<E, V> &from) {
+  if (n >= V) {
+    __builtin_memcpy(p, from.w, sizeof from.w);
+  } else {
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      if (i >= n) continue;
+      if constexpr (sizeof(E) == 4) ((uint32_t *)p)[i] = from.w[i];
+      else ((uint16_t *)p)[i] = (uint16_t)(from.w[i / 2] >> (i % 2 * 16));
+    }
+  }
+}
+
+// quotient of numbers that mostly have 32 bits
+__device__ inline int64_t quotient(int64_t a, int64_t b) { return ((a | b) >> 32) == 0 ? (int64_t)((uint32_t)a / (uint32_t)b) : a / b; }
+
 // parameters of a type that is known at run time only
 __device__ inline float load_param(const void *p, int dtype, int64_t i) {
   return dtype == TBE_FP32 ? ((const float *)p)[i] : dtype == TBE_FP16 ? (float)((const _Float16 *)p)[i] : (float)((const __bf16 *)p)[i];

@@ -57,6 +57,7 @@ struct SsmArgs {
   float *seg_state; // [segments][dim][NP]
   float *seg_reach; // [segments][dim]
   float *seg_start; // [segments][dim][NP]
+  int32_t *seg_says; // [segments]: whether a unit of it says anything
   float *parts, *shared;
   int32_t *err;
   int64_t count;    // units
@@ -181,25 +182,13 @@ __device__ inline int lane_again() {
   return me;
 }
 
-// V elements of a row, or the first n of them
-template <class E, int V>
-__device__ inline void load_some(const E *p, int n, Pack<E, V> &to) {
-  if (n >= V) {
-    __builtin_memcpy(&to, p, sizeof to);
-  } else {
-#pragma unroll
-    for (int i = 0; i < V; ++i)
-      if (i < n) to.e[i] = p[i];
-  }
-}
-
 // A wavefront goes down a unit's rows in tiles of 2 V rows of 64 elements: x, delta and z are read in packs of 16 bytes a tile ahead, b, c
 // and marks too, and lie in LDS while the tile is gone through.
 template <class E, int NP, bool FULL>
 __global__ __launch_bounds__(64, NP == 16 && FULL ? 3 : 1) void ssm_kernel(SsmArgs a) {
   constexpr int V = 16 / sizeof(E), T = 2 * V, PACKS = 64 / V;
   __shared__ float bc[T][2 * NP];
-  __shared__ Pack<E, V> tile[3][T][PACKS];
+  __shared__ Words<E, V> tile[3][T][PACKS];
   const int64_t k = blockIdx.x / a.waves;
   const int wave = (int)(blockIdx.x % a.waves), lane = threadIdx.x;
   const Unit u = a.units[k];
@@ -209,7 +198,7 @@ __global__ __launch_bounds__(64, NP == 16 && FULL ? 3 : 1) void ssm_kernel(SsmAr
   const bool in = d < a.dim;
   const int group = a.groups > 1 ? wave * 64 / (a.dim / a.groups) : 0, N = a.states;
   const bool gated = a.z;
-  Pack<E, V> raw[3][2];
+  Words<E, V> raw[3][2];
   constexpr int PIECES = T * 2 * NP / 64;  // of a tile's b and c
   constexpr int ROWS = 64 / (2 * NP) > 0 ? 64 / (2 * NP) : 1, PARTS = 2 * NP > 64 ? 2 * NP / 64 : 1;
   E shared[PIECES];
@@ -219,9 +208,9 @@ __global__ __launch_bounds__(64, NP == 16 && FULL ? 3 : 1) void ssm_kernel(SsmAr
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       const int64_t r = min(max(row0 + i * V + me / PACKS, begin), end - 1);
-      load_some<E, V>((const E *)a.x + r * a.xs + pack, have, raw[0][i]);
-      load_some<E, V>((const E *)a.delta + r * a.ts + pack, have, raw[1][i]);
-      if (gated) load_some<E, V>((const E *)a.z + r * a.zs + pack, have, raw[2][i]);
+      load_words<E, V>((const E *)a.x + r * a.xs + pack, have, raw[0][i]);
+      load_words<E, V>((const E *)a.delta + r * a.ts + pack, have, raw[1][i]);
+      if (gated) load_words<E, V>((const E *)a.z + r * a.zs + pack, have, raw[2][i]);
     }
 #pragma unroll
     for (int p = 0; p < PIECES; ++p) {
@@ -441,6 +430,7 @@ __global__ __launch_bounds__(kThreads) void ssm_join_kernel(SsmArgs a, int64_t s
   const bool in = i < n_all;
   const int64_t ic = in ? i : n_all - 1;
   const int d = (int)(ic / NP), n = (int)(ic % NP);
+  if (blockIdx.x % groups == 0 && threadIdx.x == 0) a.seg_says[seg] = speak != 0;
   if (!speak) {  // no cut bag: nothing to be written but that nothing gets through
     if (in && n == 0) a.seg_reach[seg * a.dim + d] = -1.0f;
     if (in) a.seg_state[seg * n_all + i] = 0.0f;
@@ -487,7 +477,9 @@ __global__ __launch_bounds__(kThreads) void ssm_join_kernel(SsmArgs a, int64_t s
 template <int NP, bool BACK>
 __global__ __launch_bounds__(64) void ssm_segments_kernel(SsmArgs a, int64_t segments) {
   const int64_t i = (int64_t)blockIdx.x * 64 + threadIdx.x, n_all = (int64_t)a.dim * NP;
-  if (i >= n_all) return;
+  bool any = false;  // else nobody asks
+  for (int64_t k = threadIdx.x; k < segments; k += 64) any = any || a.seg_says[k] != 0;
+  if (!__any(any) || i >= n_all) return;
   const int d = (int)(i / NP), n = (int)(i % NP);
   const float a2 = n < a.states ? a.a[(int64_t)d * a.states + n] * kLog2e : 0.0f;
   float st = 0.0f;
@@ -555,7 +547,7 @@ __device__ inline int place_of(int lane) {
   return (m >= 4 ? NP : 0) + 4 * (lane % LPC) + (m & 3);
 }
 template <int NP>
-__device__ inline void sum_elements(float (&v)[8], float *to, bool up8, bool give) {
+__device__ inline void sum_elements(float (&v)[8], float *to, bool up8) {
   constexpr int LPC = NP / 4;
   halve32<4>(v);
   halve16<2>(v);
@@ -563,7 +555,7 @@ __device__ inline void sum_elements(float (&v)[8], float *to, bool up8, bool giv
     const float keep = up8 ? v[1] : v[0], send = up8 ? v[0] : v[1];
     v[0] = keep + moved<kTurn8>(send);
     if constexpr (LPC == 4) v[0] += moved<kAhead4>(v[0]);  // in the lanes that give
-    if (give) to[0] = v[0];
+    to[0] = v[0];
   } else {
     to[0] = v[0];
     to[1] = v[1];
@@ -582,22 +574,23 @@ __device__ inline ArgsInPlace *args_again() {
 // Backward of a unit's rows: a lane has states 4 q .. 4 q + 3 of an element; a workgroup's wavefronts have elements side by side.  Rows are gone
 // through in blocks of kSaved, last block first, each bag's rows of a block at a time: forward from the state before them, w and
 // the decays kept in registers, and back.
-template <class E, int NP, int WAVES>
+template <class E, int NP, int WAVES, bool GATED>
 __global__ __launch_bounds__(64 * WAVES, 2) void ssm_grad_kernel(SsmArgs a) {
   constexpr int S = kSaved, LPC = NP / 4, CPW = 64 / LPC, OWN = (S + LPC - 1) / LPC;  // lanes of an element, elements of a wavefront, rows whose scalars a lane finds
   constexpr int V = 16 / sizeof(E), CH = CPW * WAVES, THREADS = 64 * WAVES;           // elements and lanes of a workgroup
   constexpr int PACKS = CH / V, BRINGS = (4 * S * PACKS + THREADS - 1) / THREADS;     // of a row; of x, delta, dy and z of a block that a lane brings
   constexpr int NUMBERS = (S * 2 * NP + THREADS - 1) / THREADS;                       // of b and c
-  __shared__ Pack<E, V> tile[2][4][S][PACKS];
+  __shared__ Words<E, V> tile[2][4][S][PACKS];
   __shared__ float bc[2][S][2 * NP], part[2][WAVES][S][2 * NP];
   __shared__ float4 rows_of[WAVES][S][CPW];  // D, D x, dv, x
+  __shared__ float spare[S][2 * NP];         // for the lanes whose sums are another lane's: a store that all lanes make needs no branch
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, q = lane % LPC, e = lane / LPC, N = a.states;
   float4(*row)[CPW] = rows_of[wave];
   const int place = place_of<NP>(lane);
   const bool up8 = lane & 8, give = LPC != 4 || !(lane & 4);
   const int64_t worker = blockIdx.x / a.blocks;
   const int block = (int)(blockIdx.x % a.blocks), d = block * CH + wave * CPW + e, dc = min(d, a.dim - 1);
-  const bool in = d < a.dim, gated = a.z, with_h0 = a.h0, with_dlast = a.dlast;
+  const bool in = d < a.dim, with_h0 = a.h0, with_dlast = a.dlast;
   const int group = a.groups > 1 ? block * CH / (a.dim / a.groups) : 0;
   float av[4], da[4] = {0.0f, 0.0f, 0.0f, 0.0f}, dskip = 0.0f, dbias = 0.0f;
 #pragma unroll
@@ -639,21 +632,20 @@ __global__ __launch_bounds__(64 * WAVES, 2) void ssm_grad_kernel(SsmArgs a) {
   };
   // What a lane brings of a block, one block ahead: packs of the inputs (this lane's are all of one kind), numbers of b and c, the states before it; marks two
   // blocks ahead, so that the states at the end of its last bag are there too.
-  Pack<E, V> raw[BRINGS];
+  Words<E, V> raw[BRINGS];
   E shared[NUMBERS];
   float4 before;
   auto fetch = [&](const Place &p) {
     const int me = lane_again();
     const auto &a = *args_again();
-    const bool gated = a.z;
 #pragma unroll
     for (int i = 0; i < BRINGS; ++i) {
       const int n = me + i * THREADS, kind = n / (S * PACKS) & 3, t = n / PACKS % S, at = block * CH + n % PACKS * V;
-      const E *from = (const E *)(kind == 0 || (kind == 3 && !gated) ? a.x : kind == 1 ? a.delta : kind == 2 ? a.dy : a.z);
-      const int64_t stride = kind == 0 || (kind == 3 && !gated) ? a.xs : kind == 1 ? a.ts : kind == 2 ? a.dys : a.zs;
+      const E *from = (const E *)(kind == 0 || (kind == 3 && !GATED) ? a.x : kind == 1 ? a.delta : kind == 2 ? a.dy : a.z);
+      const int64_t stride = kind == 0 || (kind == 3 && !GATED) ? a.xs : kind == 1 ? a.ts : kind == 2 ? a.dys : a.zs;
       const E *r = from + min(max(p.row0 + t, p.begin), p.end - 1) * stride;
       if (a.dim % V == 0) __builtin_memcpy(&raw[i], r + min(at, a.dim - V), sizeof raw[i]);
-      else load_some<E, V>(r + at, a.dim - at, raw[i]);
+      else load_words<E, V>(r + at, a.dim - at, raw[i]);
     }
 #pragma unroll
     for (int i = 0; i < NUMBERS; ++i) {
@@ -765,7 +757,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void ssm_grad_kernel(SsmArgs a) {
         float dv = dy;
         slope[i] = sigmoid(u);
         gate[i] = 0.0f;
-        if (gated) {
+        if (GATED) {
           const float z = in ? (float)in_x[3 * of] : 0.0f, f = sigmoid(z);
           dv = dy * z * f;
           gate[i] = dy * (f * (1.0f + z * (1.0f - f)));
@@ -773,6 +765,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void ssm_grad_kernel(SsmArgs a) {
         own_v[i] = own_b[i] = own_w[i] = 0.0f;
         if (i * LPC + q < S) row[i * LPC + q][e] = make_float4(step, step * x, dv, x);
       }
+      float *sums = (give ? &part[buffer][wave][0][0] : &spare[0][0]) + place;
       // the bags' rows [from, to) of the block, from the last
       Bag rows = first;
       for (int to = here.hi; to > here.lo;) {
@@ -798,7 +791,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void ssm_grad_kernel(SsmArgs a) {
 #pragma unroll
           for (int t = 0; t < S; ++t) {
             if (!WHOLE && (t < from || t >= to)) continue;
-            if (WHOLE) __builtin_amdgcn_sched_barrier(0);  // more rows at once do not fit the registers
+            if (WHOLE && t % 2 == 0) __builtin_amdgcn_sched_barrier(0);  // more rows at once do not fit the registers
             const float4 s = row[t][e], b = *(const float4 *)&bc[buffer][t][4 * q];
             const float bj[4] = {b.x, b.y, b.z, b.w};
             const float s2 = s.x * kLog2e;
@@ -808,7 +801,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void ssm_grad_kernel(SsmArgs a) {
               w[t][j] = decay[t][j] * h[j];
               h[j] = w[t][j] + s.y * bj[j];
             }
-            if (gated) {
+            if (GATED) {
               const float4 c = *(const float4 *)&bc[buffer][t][NP + 4 * q];
               const float v = lane_sum<LPC>((c.x * h[0] + c.y * h[1]) + (c.z * h[2] + c.w * h[3]));
               own_v[t / LPC] = t % LPC == q ? v : own_v[t / LPC];
@@ -817,7 +810,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void ssm_grad_kernel(SsmArgs a) {
 #pragma unroll
           for (int t = S - 1; t >= 0; --t) {
             if (!WHOLE && (t < from || t >= to)) continue;
-            if (WHOLE) __builtin_amdgcn_sched_barrier(0);
+            if (WHOLE && t % 2 == 1) __builtin_amdgcn_sched_barrier(0);
             const float4 s = row[t][e], b = *(const float4 *)&bc[buffer][t][4 * q], c = *(const float4 *)&bc[buffer][t][NP + 4 * q];
             const float bj[4] = {b.x, b.y, b.z, b.w}, cj[4] = {c.x, c.y, c.z, c.w};
             float gb = 0.0f, gwa = 0.0f, both[8];
@@ -835,7 +828,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void ssm_grad_kernel(SsmArgs a) {
             gwa = lane_sum<LPC>(gwa);
             own_b[t / LPC] = t % LPC == q ? gb : own_b[t / LPC];
             own_w[t / LPC] = t % LPC == q ? gwa : own_w[t / LPC];
-            sum_elements<NP>(both, &part[buffer][wave][t][0] + place, up8, give);
+            sum_elements<NP>(both, sums + t * 2 * NP, up8);
           }
         };
         if (from == 0 && to == S) walk(std::true_type{});
@@ -857,7 +850,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void ssm_grad_kernel(SsmArgs a) {
         const float du = (own_w[i] + s.w * own_b[i]) * slope[i];
         ((E *)again.dx)[at] = (E)(skip * s.z + s.x * own_b[i]);
         ((E *)again.ddelta)[at] = (E)du;
-        if (gated) ((E *)again.dz)[at] = (E)(gate[i] * (own_v[i] + skip * s.w));
+        if (GATED) ((E *)again.dz)[at] = (E)(gate[i] * (own_v[i] + skip * s.w));
         dskip += s.z * s.w;
         dbias += du;
       }
@@ -1005,8 +998,8 @@ int backward(SsmArgs a, const tbe_ssm_grads *g, hipStream_t st) {
     join<NP, true>(a, st);
   }
   const dim3 grid((unsigned)(a.workers * l.blocks));
-  if (l.waves == 8) ssm_grad_kernel<E, NP, 8><<<grid, 512, 0, st>>>(a);
-  else ssm_grad_kernel<E, NP, 4><<<grid, 256, 0, st>>>(a);
+  if (l.waves == 8) a.z ? ssm_grad_kernel<E, NP, 8, true><<<grid, 512, 0, st>>>(a) : ssm_grad_kernel<E, NP, 8, false><<<grid, 512, 0, st>>>(a);
+  else a.z ? ssm_grad_kernel<E, NP, 4, true><<<grid, 256, 0, st>>>(a) : ssm_grad_kernel<E, NP, 4, false><<<grid, 256, 0, st>>>(a);
   if (a.shared) {
     const int64_t groups = divide_up(a.rows * a.groups * 2 * a.states, kThreads);
     for (int64_t done = 0; done < groups; done += most_groups(kThreads))
@@ -1113,7 +1106,7 @@ int tbe_ssm_create(tbe_ssm_handle *out, int32_t dim, int32_t states, int32_t gro
   };
   const int64_t o_units = take((units + 1) * sizeof(Unit)), o_marks = take(max_rows * sizeof(int2)), o_ends = take(units * dim * np * 4),
                 o_spans = take(units * dim * 4), o_reach = take(units * dim * 4), o_state = take(segments * dim * np * 4),
-                o_sreach = take(segments * dim * 4), o_start = take(segments * dim * np * 4),
+                o_sreach = take(segments * dim * 4), o_start = take(segments * dim * np * 4), o_says = take(segments * 4),
                 o_parts = take(workers_of(units, l.blocks) * dim * (states + 2) * 4),
                 o_shared = take(l.blocks / groups > 1 ? (int64_t)l.blocks * max_rows * 2 * states * 4 : 0);
   hipError_t e = hipGetDevice(&s->device);
@@ -1128,6 +1121,7 @@ int tbe_ssm_create(tbe_ssm_handle *out, int32_t dim, int32_t states, int32_t gro
   SsmArgs &a = s->scratch;
   a.units = (Unit *)(s->block + o_units), a.marks = (int2 *)(s->block + o_marks), a.ends = (float *)(s->block + o_ends);
   a.spans = (float *)(s->block + o_spans), a.reach = (float *)(s->block + o_reach), a.seg_state = (float *)(s->block + o_state);
+  a.seg_says = (int32_t *)(s->block + o_says);
   a.seg_reach = (float *)(s->block + o_sreach), a.seg_start = (float *)(s->block + o_start), a.parts = (float *)(s->block + o_parts);
   a.shared = (float *)(s->block + o_shared);
   *out = s;
