@@ -30,7 +30,7 @@ constexpr int kSaved = 8;        // states before every so many rows are what th
 constexpr int kSegment = 64;     // units that a lane of `join` goes through
 constexpr int kMostStates = 64;
 constexpr int kThreads = 256;
-constexpr int kGradWorkers = 1024;  // workgroups of the backward, together
+constexpr int kGradWaves = 2048;    // wavefronts of the backward, as many as the GPU holds at once
 
 struct Unit {
   int64_t begin;  // first row
@@ -612,21 +612,22 @@ __global__ __launch_bounds__(64 * WAVES, 2) void ssm_grad_kernel(SsmArgs a) {
     for (int j = 0; j < 4; ++j) to[j] = there && 4 * q + j < N ? from[j] : 0.0f;
   };
 
-  // The blocks of this workgroup's units one after the other.
+  // The blocks of this workgroup's units one after the other: units side by side, because what one of them has more its neighbour has less.
+  const int64_t past = (worker + 1) * a.count / a.workers;
   struct Place {
     int64_t row0, begin, end, k;
     bool there;
   };
   auto enter = [&](int64_t k) {
     const auto &a = *args_again();
-    for (; k < a.count; k += a.workers) {
+    for (; k < past; ++k) {
       const int64_t begin = a.units[k].begin, end = a.units[k + 1].begin;
       if (begin < end) return Place{(end - 1) & ~(int64_t)(S - 1), begin, end, k, true};
     }
     return Place{0, 0, 1, k, false};  // (what is read ahead of it is not used)
   };
   auto after = [&](Place p) {
-    if (p.there && p.row0 <= p.begin) return enter(p.k + args_again()->workers);
+    if (p.there && p.row0 <= p.begin) return enter(p.k + 1);
     p.row0 = max(p.row0 - S, (int64_t)0);
     return p;
   };
@@ -700,7 +701,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void ssm_grad_kernel(SsmArgs a) {
     }
   };
 
-  Place now = enter(worker), done{0, 0, 0, 0, false};
+  Place now = enter(worker * a.count / a.workers), done{0, 0, 0, 0, false};
   if (now.there) {
     Place next = after(now);
     int2 mark = mark_at(now), mark_next = mark_at(next);
@@ -941,7 +942,7 @@ GradLay grad_lay(int dim, int groups, int np) {
   const int waves = eight ? 8 : 4;
   return {waves, (int)divide_up(dim, waves * each)};
 }
-int64_t workers_of(int64_t units, int blocks) { return std::max<int64_t>(1, std::min<int64_t>(units, kGradWorkers / blocks)); }
+int64_t workers_of(int64_t units, GradLay l) { return std::max<int64_t>(1, std::min<int64_t>(units, kGradWaves / l.waves / l.blocks)); }
 
 }  // namespace
 
@@ -991,7 +992,7 @@ int backward(SsmArgs a, const tbe_ssm_grads *g, hipStream_t st) {
   prepare(a, a.dh0, a.dlast, (int64_t)a.dim * a.states, st);
   const GradLay l = grad_lay(a.dim, a.groups, NP);
   a.blocks = l.blocks;
-  a.workers = workers_of(a.count, l.blocks);
+  a.workers = workers_of(a.count, l);
   if (l.blocks / a.groups <= 1) a.shared = nullptr;
   if (a.rows > 2 * a.unit) {
     ssm_grad_ends_kernel<E, NP><<<dim3((unsigned)(a.count * a.waves)), 64, 0, st>>>(a);
@@ -1107,7 +1108,7 @@ int tbe_ssm_create(tbe_ssm_handle *out, int32_t dim, int32_t states, int32_t gro
   const int64_t o_units = take((units + 1) * sizeof(Unit)), o_marks = take(max_rows * sizeof(int2)), o_ends = take(units * dim * np * 4),
                 o_spans = take(units * dim * 4), o_reach = take(units * dim * 4), o_state = take(segments * dim * np * 4),
                 o_sreach = take(segments * dim * 4), o_start = take(segments * dim * np * 4), o_says = take(segments * 4),
-                o_parts = take(workers_of(units, l.blocks) * dim * (states + 2) * 4),
+                o_parts = take(workers_of(units, l) * dim * (states + 2) * 4),
                 o_shared = take(l.blocks / groups > 1 ? (int64_t)l.blocks * max_rows * 2 * states * 4 : 0);
   hipError_t e = hipGetDevice(&s->device);
   if (e == hipSuccess) e = hipMalloc((void **)&s->block, (size_t)at);
