@@ -9,7 +9,7 @@
 // for 8 to 14 bytes of rows in 16 bits.  So the rows are gone through once where that can be, and no lane idles:
 //   units    The rows are cut every `unit` rows.  A bag of up to two units is not cut: the unit it starts in goes on to its end.
 //   ends     Units whose end cuts a bag find the state there from a zero one (or the bag's start), and the sum of the D: the
-//            product of the decays is the exponential of a times that                          (ssm_ends_kernel, ssm_grad_ends_kernel)
+//            product of the decays is the exponential of a times that                          (ssm_ends_kernel)
 //   join     states at the cuts, by a scan over the units in segments and one over the segments (ssm_join_kernel, ssm_segments_kernel)
 //   rows     every unit from the state before it                                                (ssm_kernel, ssm_grad_kernel)
 // Where no bag is longer than two units, `ends` and `join` find nothing to do.
@@ -25,7 +25,6 @@ using namespace tbe;
 
 namespace {
 
-constexpr int kBlock = 16;       // rows whose b or c the kernels of the ends stage at once
 constexpr int kSaved = 8;        // states before every so many rows are what the backward goes from: that many rows' w and decays fit its registers
 constexpr int kSegment = 64;     // units that a lane of `join` goes through
 constexpr int kMostStates = 64;
@@ -153,18 +152,6 @@ __device__ inline void start_of(const SsmArgs &a, int64_t k, int d, int n, const
   for (int j = 0; j < COUNT; ++j) far[j] = p[j];
 #pragma unroll
   for (int j = 0; j < COUNT; ++j) to[j] += r < 0.0f ? 0.0f : carried(a2[j], r, far[j]);
-}
-
-// b and c (or only one) of the rows row0 + [lo, hi) to LDS, zero beyond the states: to[row][n], to[row][NP + n]
-template <class E, int NP, int THREADS>
-__device__ inline void stage(const SsmArgs &a, int64_t row0, int lo, int hi, int group, float (*to)[2 * NP], bool with_b, bool with_c) {
-  for (int k = threadIdx.x; k < kBlock * 2 * NP; k += THREADS) {
-    const int t = k / (2 * NP), n = k % (2 * NP), s = n % NP;
-    const bool of_b = n < NP, in = t >= lo && t < hi && s < a.states && (of_b ? with_b : with_c);
-    const int64_t r = row0 + t;
-    const int at = group * a.states + s;
-    to[t][n] = in ? (float)(of_b ? ((const E *)a.b)[r * a.bs + at] : ((const E *)a.c)[r * a.cs + at]) : 0.0f;
-  }
 }
 
 // Waits for loaded numbers here.  Behind a branch that loads, the compiler would wait where they are used first, on the way that has loaded nothing
@@ -328,85 +315,94 @@ __global__ __launch_bounds__(64, NP == 16 && FULL ? 3 : 1) void ssm_kernel(SsmAr
   }
 }
 
-// The state at the end of a unit that the next one goes on from within a bag, from zero (the bag began before) or from the bag's start
-template <class E, int NP>
+// gradient of v = sum c h + skip x, from that of y
+__device__ inline float before_gate(float dy, bool gated, float z) { return gated ? dy * z * sigmoid(z) : dy; }
+
+// What a unit says.  Forward, one whose end is within a bag: the state there, from zero (the bag began before) or from the bag's start.  BACK, one that begins
+// within a bag: exp(D a) g of its first row, from the bag's end or from zero.  Rows are read in tiles as in ssm_kernel.
+template <class E, int NP, bool BACK>
 __global__ __launch_bounds__(64) void ssm_ends_kernel(SsmArgs a) {
-  __shared__ float bc[kBlock][2 * NP];
+  constexpr int V = 16 / sizeof(E), T = 2 * V, PACKS = 64 / V, R = sizeof(E) == 2 ? 2 : 4;
+  __shared__ float bc[T][NP];  // b, or c
+  __shared__ Words<E, V> tile[3][T][PACKS];
   const int64_t k = blockIdx.x / a.waves;
   const Unit u = a.units[k], next = a.units[k + 1];
-  if (!next.cut) return;
+  if (!(BACK ? u.cut : next.cut)) return;
+  const bool whole = u.cut && next.cut && u.bag == next.bag, gated = BACK && a.z;
+  const int64_t begin = BACK ? u.begin : max(u.begin, a.off[next.bag]);
+  const int64_t end = BACK && !whole ? min(next.begin, max(a.off[u.bag + 1], begin)) : next.begin;
   const int wave = (int)(blockIdx.x % a.waves), lane = threadIdx.x, N = a.states;
-  const int64_t start = a.off[next.bag], begin = max(u.begin, start), end = next.begin;
-  const bool whole = u.cut && u.bag == next.bag;
   const int d = wave * 64 + lane, dc = min(d, a.dim - 1), group = a.groups > 1 ? wave * 64 / (a.dim / a.groups) : 0;
-  float h[NP], a2[NP], span = 0.0f;
+  Words<E, V> raw[3][2];
+  constexpr int NUMBERS = T * NP / 64;
+  E shared[NUMBERS];
+  auto fetch = [&](int64_t row0) {
+    const int me = lane_again(), pack = wave * 64 + me % PACKS * V, have = a.dim - pack;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int64_t r = min(max(row0 + i * V + me / PACKS, begin), end - 1);
+      load_words<E, V>(BACK ? (const E *)a.dy + r * a.dys + pack : (const E *)a.x + r * a.xs + pack, have, raw[0][i]);
+      load_words<E, V>((const E *)a.delta + r * a.ts + pack, have, raw[1][i]);
+      if (gated) load_words<E, V>((const E *)a.z + r * a.zs + pack, have, raw[2][i]);
+    }
+#pragma unroll
+    for (int i = 0; i < NUMBERS; ++i) {
+      const int n = me + i * 64;
+      const int64_t r = min(max(row0 + n / NP, begin), end - 1);
+      const E *from = BACK ? (const E *)a.c + r * a.cs : (const E *)a.b + r * a.bs;
+      shared[i] = from[group * N + min(n % NP, N - 1)];
+    }
+  };
+  const int64_t first = (BACK ? end - 1 : begin) & ~(int64_t)(T - 1);
+  if (begin < end) fetch(first);
+  float h[NP], a2[NP], span = 0.0f;  // BACK, h: what the row before the last one seen gets
+  const float *from = BACK ? a.dlast : a.h0;
+  const int64_t at = BACK ? (int64_t)u.bag * a.dim * N : next.bag * a.h0s;
 #pragma unroll
   for (int n = 0; n < NP; ++n) {
     a2[n] = n < N ? a.a[(int64_t)dc * N + n] * kLog2e : 0.0f;
-    h[n] = !whole && a.h0 && n < N ? a.h0[next.bag * a.h0s + (int64_t)dc * N + n] : 0.0f;
+    h[n] = !whole && from && n < N ? from[at + (int64_t)dc * N + n] : 0.0f;
   }
   const float bias = a.bias ? a.bias[dc] : 0.0f;
-  const E *x = (const E *)a.x + dc, *delta = (const E *)a.delta + dc;
-  for (int64_t row0 = begin & ~(int64_t)(kBlock - 1); row0 < end; row0 += kBlock) {
-    const int lo = (int)max(begin - row0, (int64_t)0), hi = (int)min(end - row0, (int64_t)kBlock);
+  for (int64_t row0 = first; BACK ? row0 + T > begin : row0 < end; row0 += BACK ? -T : T) {
+    const int lo = (int)max(begin - row0, (int64_t)0), hi = (int)min(end - row0, (int64_t)T);
     __syncthreads();
-    stage<E, NP, 64>(a, row0, lo, hi, group, bc, true, false);
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int j = 0; j < 3; ++j)
+        if (j < 2 || gated) tile[j][i * V + lane / PACKS][lane % PACKS] = raw[j][i];
+#pragma unroll
+    for (int i = 0; i < NUMBERS; ++i) (&bc[0][0])[lane + i * 64] = (lane + i * 64) % NP < N ? (float)shared[i] : 0.0f;
+    if (BACK ? row0 > begin : row0 + T < end) fetch(row0 + (BACK ? -T : T));
     __syncthreads();
-#pragma unroll 4
-    for (int t = lo; t < hi; ++t) {
-      const float step = soft((float)delta[(row0 + t) * a.ts] + bias), sx = step * (float)x[(row0 + t) * a.xs];
+    const E *xt = (const E *)tile[0] + lane, *ut = (const E *)tile[1] + lane, *zt = (const E *)tile[2] + lane;
+    auto go = [&](int t) {
+      const float step = soft((float)ut[t * 64] + bias), x = (float)xt[t * 64];
+      const float s = BACK ? before_gate(x, gated, gated ? (float)zt[t * 64] : 0.0f) : step * x;
       span += step;
 #pragma unroll
-      for (int n = 0; n < NP; ++n) h[n] = __builtin_amdgcn_exp2f(step * a2[n]) * h[n] + sx * bc[t][n];
+      for (int n = 0; n < NP; ++n) {
+        const float decay = __builtin_amdgcn_exp2f(step * a2[n]);
+        h[n] = BACK ? decay * (bc[t][n] * s + h[n]) : decay * h[n] + s * bc[t][n];
+      }
+    };
+    for (int n = 0; n < hi - lo;) {  // rows done
+      const int t = BACK ? hi - 1 - n : lo + n;
+      if (n + R <= hi - lo) {
+#pragma unroll
+        for (int i = 0; i < R; ++i) go(BACK ? t - i : t + i);
+        n += R;
+      } else {
+        go(t);
+        ++n;
+      }
     }
   }
   if (d >= a.dim) return;
   float *to = a.ends + (k * a.dim + d) * NP;
 #pragma unroll
   for (int n = 0; n < NP; n += 4) *(float4 *)(to + n) = make_float4(h[n], h[n + 1], h[n + 2], h[n + 3]);
-  a.spans[k * a.dim + d] = span;
-}
-
-// gradient of v = sum c h + skip x, from that of y
-__device__ inline float before_gate(float dy, bool gated, float z) { return gated ? dy * z * sigmoid(z) : dy; }
-
-// What a unit that begins within a bag tells the one before: exp(D a) g of its first row, from the bag's end or from zero
-template <class E, int NP>
-__global__ __launch_bounds__(64) void ssm_grad_ends_kernel(SsmArgs a) {
-  __shared__ float bc[kBlock][2 * NP];
-  const int64_t k = blockIdx.x / a.waves;
-  const Unit u = a.units[k], next = a.units[k + 1];
-  if (!u.cut) return;
-  const int wave = (int)(blockIdx.x % a.waves), lane = threadIdx.x, N = a.states;
-  const bool whole = next.cut && u.bag == next.bag;
-  const int64_t begin = u.begin, end = whole ? next.begin : min(next.begin, max(a.off[u.bag + 1], begin));
-  const int d = wave * 64 + lane, dc = min(d, a.dim - 1), group = a.groups > 1 ? wave * 64 / (a.dim / a.groups) : 0;
-  float g[NP], a2[NP], span = 0.0f;  // g: what the row before the last one seen gets
-#pragma unroll
-  for (int n = 0; n < NP; ++n) {
-    a2[n] = n < N ? a.a[(int64_t)dc * N + n] * kLog2e : 0.0f;
-    g[n] = !whole && a.dlast && n < N ? a.dlast[((int64_t)u.bag * a.dim + dc) * N + n] : 0.0f;
-  }
-  const float bias = a.bias ? a.bias[dc] : 0.0f;
-  const E *delta = (const E *)a.delta + dc, *dy = (const E *)a.dy + dc, *z = a.z ? (const E *)a.z + dc : nullptr;
-  for (int64_t row0 = (end - 1) & ~(int64_t)(kBlock - 1); row0 + kBlock > begin; row0 -= kBlock) {
-    const int lo = (int)max(begin - row0, (int64_t)0), hi = (int)min(end - row0, (int64_t)kBlock);
-    __syncthreads();
-    stage<E, NP, 64>(a, row0, lo, hi, group, bc, false, true);
-    __syncthreads();
-#pragma unroll 4
-    for (int t = hi - 1; t >= lo; --t) {
-      const int64_t r = row0 + t;
-      const float step = soft((float)delta[r * a.ts] + bias), dv = before_gate((float)dy[r * a.dys], z, z ? (float)z[r * a.zs] : 0.0f);
-      span += step;
-#pragma unroll
-      for (int n = 0; n < NP; ++n) g[n] = __builtin_amdgcn_exp2f(step * a2[n]) * (bc[t][NP + n] * dv + g[n]);
-    }
-  }
-  if (d >= a.dim) return;
-  float *to = a.ends + (k * a.dim + d) * NP;
-#pragma unroll
-  for (int n = 0; n < NP; n += 4) *(float4 *)(to + n) = make_float4(g[n], g[n + 1], g[n + 2], g[n + 3]);
   a.spans[k * a.dim + d] = span;
 }
 
@@ -442,7 +438,7 @@ __global__ __launch_bounds__(kThreads) void ssm_join_kernel(SsmArgs a, int64_t s
   }
   const float a2 = n < a.states ? a.a[(int64_t)d * a.states + n] * kLog2e : 0.0f;
   float st = 0.0f, sum = 0.0f;  // sum < 0: nothing of what comes before the segment gets here
-  constexpr int R = 8;
+  constexpr int R = 16;  // loads under way
   for (int64_t j0 = 0; j0 < k1 - k0; j0 += R) {
     float e[R], s[R];
 #pragma unroll
@@ -455,7 +451,7 @@ __global__ __launch_bounds__(kThreads) void ssm_join_kernel(SsmArgs a, int64_t s
 #pragma unroll
     for (int r = 0; r < R; ++r) {
       const int64_t j = j0 + r, k = BACK ? k1 - 1 - j : k0 + j;
-      if (j >= k1 - k0) break;
+      if (j >= k1 - k0) continue;
       if (in) a.ends[k * n_all + i] = st;
       if (in && n == 0) a.reach[k * a.dim + d] = sum;
       const int64_t bit = k - k0;
@@ -483,7 +479,7 @@ __global__ __launch_bounds__(64) void ssm_segments_kernel(SsmArgs a, int64_t seg
   const int d = (int)(i / NP), n = (int)(i % NP);
   const float a2 = n < a.states ? a.a[(int64_t)d * a.states + n] * kLog2e : 0.0f;
   float st = 0.0f;
-  constexpr int R = 8;
+  constexpr int R = 16;  // loads under way
   for (int64_t j0 = 0; j0 < segments; j0 += R) {
     float e[R], s[R];
 #pragma unroll
@@ -495,7 +491,7 @@ __global__ __launch_bounds__(64) void ssm_segments_kernel(SsmArgs a, int64_t seg
 #pragma unroll
     for (int r = 0; r < R; ++r) {
       const int64_t j = j0 + r, k = BACK ? segments - 1 - j : j;
-      if (j >= segments) break;
+      if (j >= segments) continue;
       a.seg_start[k * n_all + i] = st;
       st = s[r] < 0.0f ? e[r] : carried(a2, s[r], st) + e[r];
     }
@@ -978,7 +974,7 @@ int forward(const SsmArgs &a, hipStream_t st) {
   if (a.rows > 0) {
     const dim3 grid((unsigned)(a.count * a.waves));
     if (a.rows > 2 * a.unit) {  // else no bag is cut
-      ssm_ends_kernel<E, NP><<<grid, 64, 0, st>>>(a);
+      ssm_ends_kernel<E, NP, false><<<grid, 64, 0, st>>>(a);
       join<NP, false>(a, st);
     }
     if (a.states == NP) ssm_kernel<E, NP, true><<<grid, 64, 0, st>>>(a);
@@ -995,7 +991,7 @@ int backward(SsmArgs a, const tbe_ssm_grads *g, hipStream_t st) {
   a.workers = workers_of(a.count, l);
   if (l.blocks / a.groups <= 1) a.shared = nullptr;
   if (a.rows > 2 * a.unit) {
-    ssm_grad_ends_kernel<E, NP><<<dim3((unsigned)(a.count * a.waves)), 64, 0, st>>>(a);
+    ssm_ends_kernel<E, NP, true><<<dim3((unsigned)(a.count * a.waves)), 64, 0, st>>>(a);
     join<NP, true>(a, st);
   }
   const dim3 grid((unsigned)(a.workers * l.blocks));
