@@ -84,7 +84,7 @@ __device__ inline int age_of(const int *marks, int64_t r0, int64_t r, Head head,
   return (int)min(max(r - head.start, (int64_t)0), (int64_t)(W - 1));
 }
 
-// The rows that a result sees, oldest first, where its bag has only `age` < W - 1 rows in front of it: the others are earlier ones, or zero
+// Where a bag has only `age` < W - 1 rows in front of one, the others that its result and those after it see are earlier ones, or zero.
 template <class E, int W, int V>
 __device__ inline void young(const ConvArgs &a, int age, int64_t bag, int at, int n, float (&e)[W][V]) {
 #pragma unroll
@@ -112,6 +112,15 @@ __device__ inline void load_weights(const ConvArgs &a, int at, float (&w)[W][V],
   }
 }
 
+template <int W, int V, class R>
+__device__ inline void next_row(float (&e)[W][V], const R &x) {
+#pragma unroll
+  for (int j = 0; j < V; ++j) {
+#pragma unroll
+    for (int k = 0; k < W - 1; ++k) e[k][j] = e[k + 1][j];
+    e[W - 1][j] = x.get(j);
+  }
+}
 template <int W, int V>
 __device__ inline void result(const float (&e)[W][V], const float (&w)[W][V], const float (&bias)[V], float (&v)[V]) {
 #pragma unroll
@@ -211,21 +220,19 @@ __global__ __launch_bounds__(kThreads) void conv_kernel(ConvArgs a) {
   E *y = (E *)a.y + first * a.ys + at;
   const int rows = (int)min((int64_t)kRows, r1 - first);
   const int *mark = marks + (first - r0);
+  float e[W][V];  // what a result sees, oldest first
+#pragma unroll
+  for (int k = 0; k < W - 1; ++k)
+#pragma unroll
+    for (int j = 0; j < V; ++j) e[k + 1][j] = raw[k].get(j);
 #pragma unroll
   for (int i = 0; i < kRows; ++i) {
     if (i >= rows) continue;
     __builtin_amdgcn_sched_barrier(0);  // rows become fp32 one by one: all at once they do not fit the registers
-    if (i > 0) {
-      const int b = mark[i];
-      age = b >= 0 ? 0 : min(age + 1, W - 1);
-      bag = b >= 0 ? b : bag;
-    }
-    float e[W][V], v[V];
-#pragma unroll
-    for (int k = 0; k < W; ++k)
-#pragma unroll
-      for (int j = 0; j < V; ++j) e[k][j] = raw[i + k].get(j);
-    if (age < W - 1) young<E, W, V>(a, age, bag, at, n, e);
+    next_row<W, V>(e, raw[W - 1 + i]);
+    if (i > 0 && mark[i] >= 0) age = 0, bag = mark[i];
+    if (i > 0 ? mark[i] >= 0 : age < W - 1) young<E, W, V>(a, age, bag, at, n, e);
+    float v[V];
     result<W, V>(e, w, bias, v);
     if (a.silu) {
 #pragma unroll
@@ -272,6 +279,11 @@ __global__ __launch_bounds__(kThreads) void conv_grad_kernel(ConvArgs a, int64_t
     int64_t bag;
     int age = age_of<W>(marks, r0, first, head, bag);
     const int *mark = marks + (first - r0);
+    float e[W][V];    // what a result sees, oldest first
+#pragma unroll
+    for (int k = 0; k < W - 1; ++k)
+#pragma unroll
+      for (int j = 0; j < V; ++j) e[k + 1][j] = raw[k].get(j);
     float acc[W][V];  // acc[k]: what row t - k has had so far
 #pragma unroll
     for (int k = 0; k < W; ++k)
@@ -287,16 +299,13 @@ __global__ __launch_bounds__(kThreads) void conv_grad_kernel(ConvArgs a, int64_t
         age = b >= 0 ? 0 : min(age + 1, W - 1);
         bag = b >= 0 ? b : bag;
       }
+      next_row<W, V>(e, raw[W - 1 + i]);
       if (!there) age = 0;
       if (there) {
-        float e[W][V], g[V], v[V];
-#pragma unroll
-        for (int k = 0; k < W; ++k)
-#pragma unroll
-          for (int j = 0; j < V; ++j) e[k][j] = raw[i + k].get(j);
+        float g[V], v[V];
 #pragma unroll
         for (int j = 0; j < V; ++j) g[j] = raw_dy[i].get(j);
-        if (age < W - 1) young<E, W, V>(a, age, bag, at, n, e);
+        if (i > 0 ? b >= 0 : age < W - 1) young<E, W, V>(a, age, bag, at, n, e);
         if (a.silu) {
           result<W, V>(e, w, bias, v);
 #pragma unroll

@@ -67,15 +67,22 @@ __device__ inline uint32_t row_max(uint32_t v, int lanes, uint32_t *lds) {
 // group with an infinity or a NaN has such a scale and reads back as NaN: its finite numbers' codes are zero, and zero times that is NaN.
 template <int V>
 __device__ inline void store_codes(uint8_t *p, int n, const float (&v)[V], float top) {
-  const float up = top < 0x1p-100f ? 0x1p100f : 1.0f;  // 448 over a very small number would be infinite
-  const float f = top > 0.0f ? 448.0f / (top * up) : 0.0f;
-  const bool zero = top / 448.0f == 0.0f;
   uint32_t w[V / 4];
+  auto codes = [&](float up, float f) {
 #pragma unroll
-  for (int i = 0; i < V; i += 4) {
-    int c = __builtin_amdgcn_cvt_pk_fp8_f32(v[i] * up * f, v[i + 1] * up * f, 0, false);
-    c = __builtin_amdgcn_cvt_pk_fp8_f32(v[i + 2] * up * f, v[i + 3] * up * f, c, true);
-    w[i / 4] = zero ? 0u : (uint32_t)c;
+    for (int i = 0; i < V; i += 4) {
+      int c = __builtin_amdgcn_cvt_pk_fp8_f32(v[i] * up * f, v[i + 1] * up * f, 0, false);
+      c = __builtin_amdgcn_cvt_pk_fp8_f32(v[i + 2] * up * f, v[i + 3] * up * f, c, true);
+      w[i / 4] = (uint32_t)c;
+    }
+  };
+  if (top < 0x1p-100f) {  // 448 over a very small number would be infinite
+    codes(0x1p100f, top > 0.0f ? 448.0f / (top * 0x1p100f) : 0.0f);
+    if (top / 448.0f == 0.0f)
+#pragma unroll
+      for (int i = 0; i < V / 4; ++i) w[i] = 0;
+  } else {
+    codes(1.0f, 448.0f / top);
   }
   if (n >= V) {
     __builtin_memcpy(p, w, V);
@@ -131,7 +138,11 @@ __global__ __launch_bounds__(ROW_THREADS > 64 ? ROW_THREADS : kThreads) void nor
     float w[V];
     load_params<V>(a.weight, a.weight_dtype, at, a.dim - at, w);
 #pragma unroll
-    for (int j = 0; j < V; ++j) v[i][j] = at + j < a.dim ? v[i][j] * rstd * w[j] : 0.0f;  // (an infinite rstd has no part beyond the row)
+    for (int j = 0; j < V; ++j) v[i][j] = v[i][j] * rstd * w[j];
+    if (at + V > a.dim) {
+#pragma unroll
+      for (int j = 0; j < V; ++j) v[i][j] = at + j < a.dim ? v[i][j] : 0.0f;  // (an infinite rstd has no part beyond the row)
+    }
   }
   if constexpr (!BITS8) {
 #pragma unroll
@@ -314,13 +325,14 @@ __global__ __launch_bounds__(kWideThreads) void norm_grad_wide_kernel(NormGrad a
 
 // How a row lies on lanes: on a part of a wavefront or a whole one (threads 64, up to two packs a lane), on 256 or on 1024 lanes of up to 32 elements
 constexpr int kElements = 32, kMostDim = 1024 * kElements;
+template <class E> constexpr int kHalf = kElements / kPack<E> / 2;
 struct Lay {
   int threads, lanes, packs;
 };
 Lay lay_of(int dim, int V) {
   const int64_t n = divide_up(dim, V);
   if (dim > 256 * kElements) return {1024, 1024, kElements / V};
-  if (n > 128) return {256, 256, kElements / V};
+  if (n > 128) return {256, 256, dim > 128 * kElements ? kElements / V : kElements / V / 2};  // up to 16 elements, or up to 32
   int lanes = 1;
   while (lanes < n && lanes < 64) lanes *= 2;
   return {64, lanes, n > 64 ? 2 : 1};
@@ -337,8 +349,9 @@ void launch_norm(NormArgs a, hipStream_t st) {
     a.row0 = done * at_once;
     if (l.threads == 64 && l.packs == 1) norm_kernel<E, R, BITS8, 64, 1><<<grid, threads, 0, st>>>(a);
     else if (l.threads == 64) norm_kernel<E, R, BITS8, 64, 2><<<grid, threads, 0, st>>>(a);
-    else if (l.threads == 256) norm_kernel<E, R, BITS8, 256, kElements / kPack<E>><<<grid, threads, 0, st>>>(a);
-    else norm_kernel<E, R, BITS8, 1024, kElements / kPack<E>><<<grid, threads, 0, st>>>(a);
+    else if (l.threads == 256 && l.packs == kHalf<E>) norm_kernel<E, R, BITS8, 256, kHalf<E>><<<grid, threads, 0, st>>>(a);
+    else if (l.threads == 256) norm_kernel<E, R, BITS8, 256, 2 * kHalf<E>><<<grid, threads, 0, st>>>(a);
+    else norm_kernel<E, R, BITS8, 1024, 2 * kHalf<E>><<<grid, threads, 0, st>>>(a);
   }
 }
 
@@ -356,7 +369,8 @@ void launch_grad(NormGrad a, float *dweight, hipStream_t st) {
   const size_t lds = (size_t)kThreads * kPack<E> * l.packs * sizeof(float);
   if (l.threads == 64 && l.packs == 1) norm_grad_kernel<E, S, 64, 1><<<grid, kThreads, lds, st>>>(a);
   else if (l.threads == 64) norm_grad_kernel<E, S, 64, 2><<<grid, kThreads, lds, st>>>(a);
-  else if (l.threads == 256) norm_grad_kernel<E, S, 256, kElements / kPack<E>><<<grid, kThreads, 0, st>>>(a);
+  else if (l.threads == 256 && l.packs == kHalf<E>) norm_grad_kernel<E, S, 256, kHalf<E>><<<grid, kThreads, 0, st>>>(a);
+  else if (l.threads == 256) norm_grad_kernel<E, S, 256, 2 * kHalf<E>><<<grid, kThreads, 0, st>>>(a);
   else norm_grad_wide_kernel<E, S><<<grid, kWideThreads, 0, st>>>(a);
   if (dweight) sum_parts(a.parts, groups, a.dim, a.dim, a.dim, dweight, nullptr, nullptr, st);
 }

@@ -91,11 +91,8 @@ __device__ inline void load_params(const void *p, int dtype, int64_t at, int n, 
 
 constexpr float kLog2e = 1.44269504f, kLn2 = 0.693147181f;
 
-// The exponential is the hardware's power of two of the rounded v log2(e), so a sigmoid is off by up to (|v| + 8) 2^-24 of itself.
-__device__ inline float sigmoid(float v) {
-  const float e = __builtin_amdgcn_exp2f(fabsf(v) * -kLog2e), r = __builtin_amdgcn_rcpf(1.0f + e);
-  return v >= 0.0f ? r : e * r;
-}
+// The exponential is the hardware's power of two of the rounded v log2(e), so a sigmoid is off by up to (|v| + 8) 2^-24 of itself; below -87 it is zero.
+__device__ inline float sigmoid(float v) { return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(v * -kLog2e)); }
 
 // Sums over the parts of [parts][n] fp32 numbers, in a fixed order: 32 columns a workgroup, 32 lanes a column with every 32nd part each.
 // A row of `width` columns has `cut` columns that go to `to`, one that goes to `next`, one that goes to `other` (each unless null).

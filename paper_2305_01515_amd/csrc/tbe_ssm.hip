@@ -169,6 +169,25 @@ __device__ inline int lane_again() {
   return me;
 }
 
+// Elements at .. at + V - 1 of a row, those beyond its end being other ones of it.  All lanes go one way: with registers as scarce as here, branches that part them
+// gave results of other registers (64 states of rows that end within a wavefront, ROCm 7.2).
+template <class E, int V>
+__device__ inline void load_pack_of(const E *row, int dim, int at, Words<E, V> &to) {
+  if (dim % V == 0) {
+    __builtin_memcpy(to.w, row + min(at, dim - V), sizeof to.w);
+  } else {
+#pragma unroll
+    for (unsigned i = 0; i < sizeof to.w / 4; ++i) {
+      if constexpr (sizeof(E) == 4) {
+        to.w[i] = ((const uint32_t *)row)[min(at + (int)i, dim - 1)];
+      } else {
+        const uint16_t *p = (const uint16_t *)row;
+        to.w[i] = p[min(at + 2 * (int)i, dim - 1)] | (uint32_t)p[min(at + 2 * (int)i + 1, dim - 1)] << 16;
+      }
+    }
+  }
+}
+
 // A wavefront goes down a unit's rows in tiles of 2 V rows of 64 elements: x, delta and z are read in packs of 16 bytes a tile ahead, b, c
 // and marks too, and lie in LDS while the tile is gone through.
 template <class E, int NP, bool FULL>
@@ -181,8 +200,8 @@ __global__ __launch_bounds__(64, NP == 16 && FULL ? 3 : 1) void ssm_kernel(SsmAr
   const Unit u = a.units[k];
   const int64_t begin = u.begin, end = a.units[k + 1].begin;
   if (begin >= end) return;
-  const int d = wave * 64 + lane, dc = min(d, a.dim - 1);
-  const bool in = d < a.dim;
+  // Lanes beyond the row's end do what the last element's lane does, and write what it writes.
+  const int column = min(lane, a.dim - 1 - wave * 64), dc = wave * 64 + column;
   const int group = a.groups > 1 ? wave * 64 / (a.dim / a.groups) : 0, N = a.states;
   const bool gated = a.z;
   Words<E, V> raw[3][2];
@@ -191,13 +210,13 @@ __global__ __launch_bounds__(64, NP == 16 && FULL ? 3 : 1) void ssm_kernel(SsmAr
   E shared[PIECES];
   int2 mark;
   auto fetch = [&](int64_t row0) {
-    const int me = lane_again(), pack = wave * 64 + me % PACKS * V, have = a.dim - pack;  // of a row, that this lane brings
+    const int me = lane_again(), pack = wave * 64 + me % PACKS * V;  // of a row, that this lane brings
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       const int64_t r = min(max(row0 + i * V + me / PACKS, begin), end - 1);
-      load_words<E, V>((const E *)a.x + r * a.xs + pack, have, raw[0][i]);
-      load_words<E, V>((const E *)a.delta + r * a.ts + pack, have, raw[1][i]);
-      if (gated) load_words<E, V>((const E *)a.z + r * a.zs + pack, have, raw[2][i]);
+      load_pack_of<E, V>((const E *)a.x + r * a.xs, a.dim, pack, raw[0][i]);
+      load_pack_of<E, V>((const E *)a.delta + r * a.ts, a.dim, pack, raw[1][i]);
+      if (gated) load_pack_of<E, V>((const E *)a.z + r * a.zs, a.dim, pack, raw[2][i]);
     }
 #pragma unroll
     for (int p = 0; p < PIECES; ++p) {
@@ -239,11 +258,11 @@ __global__ __launch_bounds__(64, NP == 16 && FULL ? 3 : 1) void ssm_kernel(SsmAr
     const uint32_t starts = (uint32_t)__ballot(mine && mark.x >= 0), ends = (uint32_t)__ballot(mine && mark.y >= 0);
     if (row0 + T < end) fetch(row0 + T);
     __syncthreads();
-    const E *xt = (const E *)tile[0] + lane, *ut = (const E *)tile[1] + lane, *zt = (const E *)tile[2] + lane;
-    E *y = (E *)a.y + (row0 + lo) * a.ys + d;
+    const E *xt = (const E *)tile[0] + column, *ut = (const E *)tile[1] + column, *zt = (const E *)tile[2] + column;
+    E *y = (E *)a.y + (row0 + lo) * a.ys + dc;
     auto put = [&](int t) {  // the state before row t, for the backward
-      if (a.saved && (t & (kSaved - 1)) == 0 && in) {
-        float *to = a.saved + ((row0 + t) / kSaved * a.dim + d) * NP;
+      if (a.saved && (t & (kSaved - 1)) == 0) {
+        float *to = a.saved + ((row0 + t) / kSaved * a.dim + dc) * NP;
 #pragma unroll
         for (int n = 0; n < NP; n += 4) *(float4 *)(to + n) = make_float4(h[n], h[n + 1], h[n + 2], h[n + 3]);
       }
@@ -271,10 +290,8 @@ __global__ __launch_bounds__(64, NP == 16 && FULL ? 3 : 1) void ssm_kernel(SsmAr
         float v[R];
 #pragma unroll
         for (int i = 0; i < R; ++i) v[i] = go(t + i, xt[(t + i) * 64], ut[(t + i) * 64], zt[(t + i) * 64]);
-        if (in) {
 #pragma unroll
-          for (int i = 0; i < R; ++i) y[i * a.ys] = (E)v[i];
-        }
+        for (int i = 0; i < R; ++i) y[i * a.ys] = (E)v[i];
         y += R * a.ys;
         t += R;
         continue;
@@ -299,11 +316,11 @@ __global__ __launch_bounds__(64, NP == 16 && FULL ? 3 : 1) void ssm_kernel(SsmAr
       }
       put(t);
       const float v = go(t, xe, ue, ze);
-      if (in) *y = (E)v;
+      *y = (E)v;
       y += a.ys;
-      if ((ends >> t & 1) && a.last && in) {
+      if ((ends >> t & 1) && a.last) {
         const int64_t bag = __builtin_amdgcn_readlane(bag_of.y, t);
-        float *to = a.last + (bag * a.dim + d) * N;
+        float *to = a.last + (bag * a.dim + dc) * N;
 #pragma unroll
         for (int n = 0; n < NP; n += 4) {
           const float v[4] = {h[n], h[n + 1], h[n + 2], h[n + 3]};
@@ -332,18 +349,18 @@ __global__ __launch_bounds__(64) void ssm_ends_kernel(SsmArgs a) {
   const int64_t begin = BACK ? u.begin : max(u.begin, a.off[next.bag]);
   const int64_t end = BACK && !whole ? min(next.begin, max(a.off[u.bag + 1], begin)) : next.begin;
   const int wave = (int)(blockIdx.x % a.waves), lane = threadIdx.x, N = a.states;
-  const int d = wave * 64 + lane, dc = min(d, a.dim - 1), group = a.groups > 1 ? wave * 64 / (a.dim / a.groups) : 0;
+  const int column = min(lane, a.dim - 1 - wave * 64), dc = wave * 64 + column, group = a.groups > 1 ? wave * 64 / (a.dim / a.groups) : 0;
   Words<E, V> raw[3][2];
   constexpr int NUMBERS = T * NP / 64;
   E shared[NUMBERS];
   auto fetch = [&](int64_t row0) {
-    const int me = lane_again(), pack = wave * 64 + me % PACKS * V, have = a.dim - pack;
+    const int me = lane_again(), pack = wave * 64 + me % PACKS * V;
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       const int64_t r = min(max(row0 + i * V + me / PACKS, begin), end - 1);
-      load_words<E, V>(BACK ? (const E *)a.dy + r * a.dys + pack : (const E *)a.x + r * a.xs + pack, have, raw[0][i]);
-      load_words<E, V>((const E *)a.delta + r * a.ts + pack, have, raw[1][i]);
-      if (gated) load_words<E, V>((const E *)a.z + r * a.zs + pack, have, raw[2][i]);
+      load_pack_of<E, V>(BACK ? (const E *)a.dy + r * a.dys : (const E *)a.x + r * a.xs, a.dim, pack, raw[0][i]);
+      load_pack_of<E, V>((const E *)a.delta + r * a.ts, a.dim, pack, raw[1][i]);
+      if (gated) load_pack_of<E, V>((const E *)a.z + r * a.zs, a.dim, pack, raw[2][i]);
     }
 #pragma unroll
     for (int i = 0; i < NUMBERS; ++i) {
@@ -376,7 +393,7 @@ __global__ __launch_bounds__(64) void ssm_ends_kernel(SsmArgs a) {
     for (int i = 0; i < NUMBERS; ++i) (&bc[0][0])[lane + i * 64] = (lane + i * 64) % NP < N ? (float)shared[i] : 0.0f;
     if (BACK ? row0 > begin : row0 + T < end) fetch(row0 + (BACK ? -T : T));
     __syncthreads();
-    const E *xt = (const E *)tile[0] + lane, *ut = (const E *)tile[1] + lane, *zt = (const E *)tile[2] + lane;
+    const E *xt = (const E *)tile[0] + column, *ut = (const E *)tile[1] + column, *zt = (const E *)tile[2] + column;
     auto go = [&](int t) {
       const float step = soft((float)ut[t * 64] + bias), x = (float)xt[t * 64];
       const float s = BACK ? before_gate(x, gated, gated ? (float)zt[t * 64] : 0.0f) : step * x;
@@ -399,11 +416,10 @@ __global__ __launch_bounds__(64) void ssm_ends_kernel(SsmArgs a) {
       }
     }
   }
-  if (d >= a.dim) return;
-  float *to = a.ends + (k * a.dim + d) * NP;
+  float *to = a.ends + (k * a.dim + dc) * NP;
 #pragma unroll
   for (int n = 0; n < NP; n += 4) *(float4 *)(to + n) = make_float4(h[n], h[n + 1], h[n + 2], h[n + 3]);
-  a.spans[k * a.dim + d] = span;
+  a.spans[k * a.dim + dc] = span;
 }
 
 // Whether unit k says something to the next one (BACK: the one before), and whether that has a part of what it has heard itself
@@ -640,9 +656,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void ssm_grad_kernel(SsmArgs a) {
       const int n = me + i * THREADS, kind = n / (S * PACKS) & 3, t = n / PACKS % S, at = block * CH + n % PACKS * V;
       const E *from = (const E *)(kind == 0 || (kind == 3 && !GATED) ? a.x : kind == 1 ? a.delta : kind == 2 ? a.dy : a.z);
       const int64_t stride = kind == 0 || (kind == 3 && !GATED) ? a.xs : kind == 1 ? a.ts : kind == 2 ? a.dys : a.zs;
-      const E *r = from + min(max(p.row0 + t, p.begin), p.end - 1) * stride;
-      if (a.dim % V == 0) __builtin_memcpy(&raw[i], r + min(at, a.dim - V), sizeof raw[i]);
-      else load_words<E, V>(r + at, a.dim - at, raw[i]);
+      load_pack_of<E, V>(from + min(max(p.row0 + t, p.begin), p.end - 1) * stride, a.dim, at, raw[i]);
     }
 #pragma unroll
     for (int i = 0; i < NUMBERS; ++i) {
