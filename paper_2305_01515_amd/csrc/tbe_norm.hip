@@ -63,10 +63,10 @@ __device__ inline uint32_t row_max(uint32_t v, int lanes, uint32_t *lds) {
   return v;
 }
 
-// Codes of V numbers whose group has the largest magnitude `top`, at scale top / 448.  Where the scale is zero, so are the codes.  A
+// Codes of V numbers whose group has the largest magnitude `top`, as 448ths of it.  Where the scale is zero (`zero`), so are the codes.  A
 // group with an infinity or a NaN has such a scale and reads back as NaN: its finite numbers' codes are zero, and zero times that is NaN.
 template <int V>
-__device__ inline void store_codes(uint8_t *p, int n, const float (&v)[V], float top) {
+__device__ inline void store_codes(uint8_t *p, int n, const float (&v)[V], float top, bool zero) {
   uint32_t w[V / 4];
   auto codes = [&](float up, float f) {
 #pragma unroll
@@ -78,11 +78,12 @@ __device__ inline void store_codes(uint8_t *p, int n, const float (&v)[V], float
   };
   if (top < 0x1p-100f) {  // 448 over a very small number would be infinite
     codes(0x1p100f, top > 0.0f ? 448.0f / (top * 0x1p100f) : 0.0f);
-    if (top / 448.0f == 0.0f)
-#pragma unroll
-      for (int i = 0; i < V / 4; ++i) w[i] = 0;
   } else {
     codes(1.0f, 448.0f / top);
+  }
+  if (zero) {
+#pragma unroll
+    for (int i = 0; i < V / 4; ++i) w[i] = 0;
   }
   if (n >= V) {
     __builtin_memcpy(p, w, V);
@@ -132,13 +133,16 @@ __global__ __launch_bounds__(ROW_THREADS > 64 ? ROW_THREADS : kThreads) void nor
   sum = row_sum<ROW_THREADS>(sum, L, lds);
   const float rstd = 1.0f / sqrtf(sum / (float)a.dim + a.eps);
   if (there && lane == 0 && a.rstd) a.rstd[row] = rstd;
+  // Codes do not depend on rstd but for their scale: they are found from s w times the power of two in rstd, which rounds nothing.
+  const float power = __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, rstd) & 0x7F800000u), times = BITS8 ? power : rstd;
+  const float rest = power > 0.0f ? rstd / power : 1.0f;
 #pragma unroll
   for (int i = 0; i < P; ++i) {
     const int at = (lane + i * L) * V;
     float w[V];
     load_params<V>(a.weight, a.weight_dtype, at, a.dim - at, w);
 #pragma unroll
-    for (int j = 0; j < V; ++j) v[i][j] = v[i][j] * rstd * w[j];
+    for (int j = 0; j < V; ++j) v[i][j] = v[i][j] * times * w[j];
     if (at + V > a.dim) {
 #pragma unroll
       for (int j = 0; j < V; ++j) v[i][j] = at + j < a.dim ? v[i][j] : 0.0f;  // (an infinite rstd has no part beyond the row)
@@ -175,8 +179,9 @@ __global__ __launch_bounds__(ROW_THREADS > 64 ? ROW_THREADS : kThreads) void nor
       const int at = (lane + i * L) * V;
       const float t = __builtin_bit_cast(float, top[i]);
       if (!there || at >= a.dim) continue;
-      if (at % a.group == 0) a.scales[row * a.groups + at / a.group] = t / 448.0f;
-      store_codes<V>((uint8_t *)a.out + row * a.os + at, a.dim - at, v[i], t);
+      const float scale = t * rest / 448.0f;
+      if (at % a.group == 0) a.scales[row * a.groups + at / a.group] = scale;
+      store_codes<V>((uint8_t *)a.out + row * a.os + at, a.dim - at, v[i], t, scale == 0.0f);
     }
   }
 }
