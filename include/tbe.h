@@ -495,10 +495,10 @@ int tbe_plan_placement(const tbe_place_table *tables, int32_t num_tables, const 
  * ---- Operators beside the embedding path ----
  *
  * What a model needs that trains on histories of looked-up rows: a pooling that keeps the order of a bag's rows
- * (tbe_scan_*), a learned table looked up by the bucket of a distance between two rows of a history (tbe_bias_*), and
- * the step of the dense weights (tbe_adamw_*).  The conventions above hold: pointers d_* are device memory of the
+ * (tbe_scan_*), a learned table looked up by the bucket of a distance between two rows of a history (tbe_bias_*),
+ * the step of the dense weights (tbe_adamw_*), and the parts of layers on histories (tbe_norm_*, tbe_conv_*, tbe_ssm_*).  The conventions above hold: pointers d_* are device memory of the
  * caller's, h_* host memory; a call enqueues on the stream it is given (which may be capturing a graph) and returns
- * without waiting (the *_create, *_destroy and tbe_scan_check calls wait); scratch memory is the handle's, allocated in
+ * without waiting (the *_create, *_destroy and *_check calls wait); scratch memory is the handle's, allocated in
  * *_create, so calls of one handle on several streams, and replays of graphs that hold some, have to be ordered by the caller;
  * errors are returned as codes, their text is tbe_last_error(NULL).  A handle is used from one host thread at a time and on
  * the GPU it was created on (TBE_EORDER).  Rows and scores may be TBE_FP32, TBE_FP16 or TBE_BF16; sums, states and
@@ -732,7 +732,7 @@ typedef struct {
   const float *d_h0;                /* [dim, states] of each bag, h0_stride apart (0: one for all), or null */
   int64_t h0_stride;
 } tbe_ssm_batch;
-/* fp32 numbers that tbe_ssm_forward leaves in d_saved for the backward of `rows` rows: the states before every 8th row */
+/* fp32 numbers that tbe_ssm_forward leaves in d_saved (from a multiple of 16 bytes on) for the backward of `rows` rows: the states before every 8th row */
 int64_t tbe_ssm_saved_floats(tbe_ssm_handle s, int64_t rows);
 /* Writes d_y and, each unless null, d_last (fp32 [bags, dim, states], h after a bag's last row) and d_saved. */
 int tbe_ssm_forward(tbe_ssm_handle s, const tbe_ssm_batch *batch, void *d_y, int64_t y_stride, float *d_last, float *d_saved, void *stream);

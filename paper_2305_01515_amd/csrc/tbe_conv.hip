@@ -35,22 +35,8 @@ struct ConvArgs {
   bool silu;
 };
 
-template <class E> constexpr int kPack = 16 / sizeof(E);
+template <class E> constexpr int kPack = 8 / sizeof(E);
 template <class E> constexpr int kGradPack = 8 / sizeof(E);
-
-// how many of the ascending offsets[0 .. n) are at most `row`, the same in all lanes of a wavefront: 64 places are looked at at once
-__device__ inline int64_t count_up_to(const int64_t *off, int64_t n, int64_t row) {
-  int64_t lo = 0, hi = n;  // off[i] <= row for i < lo, not for i >= hi
-  while (lo < hi) {
-    const int64_t step = (hi - lo + 63) / 64, at = lo + (int64_t)(threadIdx.x & 63) * step;
-    const uint64_t m = __ballot(at < hi && off[at] <= row);
-    const int c = __popcll(m);  // the first c places are
-    if (c == 0) return lo;
-    lo += (int64_t)(c - 1) * step + 1;
-    hi = min(hi, lo + step - 1);
-  }
-  return lo;
-}
 
 // Bags that start in rows [r0, r1): marks[row - r0] = bag, -1 elsewhere; head: the bag that row r0 belongs to and its first row
 struct Head {
@@ -101,15 +87,18 @@ __device__ inline void young(const ConvArgs &a, int age, int64_t bag, int at, in
     }
 }
 
+// The weights of V elements lie one behind another: one look at their type, wide loads.  (A look for each was a wait for each, 20 of them.)
 template <int W, int V>
 __device__ inline void load_weights(const ConvArgs &a, int at, float (&w)[W][V], float (&bias)[V]) {
+  float all[V * W];
+  load_params<V * W>(a.weight, a.weight_dtype, (int64_t)at * W, (a.dim - at) * W, all);
 #pragma unroll
   for (int j = 0; j < V; ++j) {
-    const bool in = at + j < a.dim;
-    bias[j] = in && a.bias ? load_param(a.bias, a.weight_dtype, at + j) : 0.0f;
+    bias[j] = 0.0f;
 #pragma unroll
-    for (int k = 0; k < W; ++k) w[k][j] = in ? load_param(a.weight, a.weight_dtype, (int64_t)(at + j) * W + k) : 0.0f;
+    for (int k = 0; k < W; ++k) w[k][j] = all[j * W + k];
   }
+  if (a.bias) load_params<V>(a.bias, a.weight_dtype, at, a.dim - at, bias);
 }
 
 template <int W, int V, class R>

@@ -9,10 +9,10 @@ namespace tbe {
 template <class E, int V>
 __device__ inline void load_floats(const E *p, int n, float (&to)[V]) {
   if (n >= V) {
-    Pack<E, V> r;
-    __builtin_memcpy(&r, p, sizeof r);
+    E r[V];
+    __builtin_memcpy(r, p, sizeof r);
 #pragma unroll
-    for (int i = 0; i < V; ++i) to[i] = (float)r.e[i];
+    for (int i = 0; i < V; ++i) to[i] = (float)r[i];
   } else {
 #pragma unroll
     for (int i = 0; i < V; ++i) to[i] = i < n ? (float)p[i] : 0.0f;
@@ -87,6 +87,19 @@ __device__ inline void load_params(const void *p, int dtype, int64_t at, int n, 
   if (dtype == TBE_FP32) load_floats<float, V>((const float *)p + at, n, to);
   else if (dtype == TBE_FP16) load_floats<_Float16, V>((const _Float16 *)p + at, n, to);
   else load_floats<__bf16, V>((const __bf16 *)p + at, n, to);
+}
+
+// how many of the ascending offsets[0 .. n) are at most `row`, the same in all lanes of a wavefront: 64 places are looked at at once
+__device__ inline int64_t count_up_to(const int64_t *off, int64_t n, int64_t row) {
+  int64_t lo = 0, hi = n;  // off[i] <= row for i < lo, not for i >= hi
+  while (lo < hi) {
+    const int64_t step = (hi - lo + 63) / 64, at = lo + (int64_t)(threadIdx.x & 63) * step;
+    const int c = __popcll(__ballot(at < hi && off[at] <= row));  // the first c places are
+    if (c == 0) return lo;
+    lo += (int64_t)(c - 1) * step + 1;
+    hi = min(hi, lo + step - 1);
+  }
+  return lo;
 }
 
 constexpr float kLog2e = 1.44269504f, kLn2 = 0.693147181f;

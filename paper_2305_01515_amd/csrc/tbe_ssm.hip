@@ -66,19 +66,6 @@ struct SsmArgs {
   int blocks;       // workgroups that a row has in the backward
 };
 
-// how many of the ascending offsets[0 .. n) are at most `row`, the same in all lanes of a wavefront: 64 places are looked at at once
-__device__ inline int64_t count_up_to(const int64_t *off, int64_t n, int64_t row) {
-  int64_t lo = 0, hi = n;  // off[i] <= row for i < lo, not for i >= hi
-  while (lo < hi) {
-    const int64_t step = (hi - lo + 63) / 64, at = lo + (int64_t)(threadIdx.x & 63) * step;
-    const int c = __popcll(__ballot(at < hi && off[at] <= row));  // the first c places are
-    if (c == 0) return lo;
-    lo += (int64_t)(c - 1) * step + 1;
-    hi = min(hi, lo + step - 1);
-  }
-  return lo;
-}
-
 // The units and the marks of their rows, what empty bags have; offsets that do not ascend from 0 to rows are reported.
 // empty_to (or null): [bags, dim, states] that an empty bag has of empty_from (null: zero).
 constexpr int kMostUnit = 128;
@@ -169,8 +156,8 @@ __device__ inline int lane_again() {
   return me;
 }
 
-// Elements at .. at + V - 1 of a row, those beyond its end being other ones of it.  All lanes go one way: with registers as scarce as here, branches that part them
-// gave results of other registers (64 states of rows that end within a wavefront, ROCm 7.2).
+// Elements at .. at + V - 1 of a row, those beyond its end being other ones of it.  All lanes go one way: where a branch parted them, 64 states of rows that
+// end within a wavefront came out wrong, with registers all in use (ROCm 7.2).
 template <class E, int V>
 __device__ inline void load_pack_of(const E *row, int dim, int at, Words<E, V> &to) {
   if (dim % V == 0) {
@@ -1158,6 +1145,7 @@ int tbe_ssm_forward(tbe_ssm_handle s, const tbe_ssm_batch *b, void *d_y, int64_t
   for (const void *in : {b->d_x, b->d_delta, b->d_z, b->d_b, b->d_c})
     if (b->rows > 0 && in && d_y == in) return report(TBE_EINVAL, "the output is one of the inputs");
   if (d_last && d_last == b->d_h0) return report(TBE_EINVAL, "the output is one of the inputs");
+  if ((uintptr_t)d_saved & 15) return report(TBE_EINVAL, "what is saved begins at no multiple of 16 bytes");
   if (b->bags == 0) return TBE_OK;
   SsmArgs a = args_of(s, b);
   a.y = d_y, a.ys = y_stride, a.last = d_last, a.saved = d_saved;
@@ -1169,6 +1157,7 @@ int tbe_ssm_backward(tbe_ssm_handle s, const tbe_ssm_batch *b, const float *d_sa
   if (!g || !g->d_da) return report(TBE_EINVAL, "null gradients");
   if (b->rows > 0 && (!d_saved || !g->d_dy || !g->d_dx || !g->d_ddelta || !g->d_db || !g->d_dc || (b->d_z && !g->d_dz)))
     return report(TBE_EINVAL, "null pointer for what the forward saved or for a gradient");
+  if ((uintptr_t)d_saved & 15) return report(TBE_EINVAL, "what is saved begins at no multiple of 16 bytes");
   if (b->rows > 0 && g->dy_stride < s->dim) return report(TBE_EINVAL, "a stride below the length of a row");
   for (const void *in : {b->d_x, b->d_delta, b->d_z, b->d_b, b->d_c, g->d_dy})
     for (const void *out : {(const void *)g->d_dx, (const void *)g->d_ddelta, (const void *)(b->d_z ? g->d_dz : nullptr), (const void *)g->d_db, (const void *)g->d_dc})

@@ -9,7 +9,7 @@ RMSNorm       a root-mean-square norm with the residual's addition, with its gra
 
 Argument marshalling only: every step runs in the HIP kernels of the library.  A call enqueues on the current stream, behind
 this object's last call or its constructor if that was on another one (an object's calls share its scratch memory; replays of a captured graph
-are the caller's to order; graphs need the objects whose calls they hold).  No call waits for the GPU, apart from `Scan.check` and a
+are the caller's to order; graphs need the objects whose calls they hold).  No call waits for the GPU, apart from `check` and a
 step of `AdamW` that makes its plan anew, which no capture can hold.
 What a call writes into a tensor that it was given counts for autograd as changed in place.
 """
@@ -161,11 +161,13 @@ class _Handle:
 
     def _rows_of(self, name: str, t: torch.Tensor, n: int, dim: int, dtype: torch.dtype) -> Tuple[int, int]:
         """address of rows of `dim` elements that lie side by side, and how far apart the rows are"""
-        p = self._tensor(name, t, dtype, (n, dim))
-        stride = t.stride()
-        if dim > 1 and n and stride[1] != 1:
+        if _dtype(t) is not dtype or _shape(t) != (n, dim) or _gpu(t) != self.device.index:
+            self._tensor(name, t, dtype, (n, dim))
+        if _dense(t):
+            return _address(t), dim
+        if dim > 1 and n and t.stride(1) != 1:
             raise ValueError(f"{name}: the elements of a row lie side by side")
-        return p, (stride[0] if n > 1 else dim)
+        return _address(t), (t.stride(0) if n > 1 else dim)
 
     def _offsets(self, offsets: torch.Tensor) -> Tuple[int, int]:
         """number of bags, address"""
@@ -178,7 +180,11 @@ class _Handle:
         return self._whole("slots", slots, torch.int64, (n,)) if slots is not None else None
 
     def _empty(self, *shape, dtype: torch.dtype = torch.float32) -> torch.Tensor:
-        return torch.empty(shape, dtype=dtype, device=self.device)
+        return torch.empty(*shape, dtype=dtype, device=self.device)
+
+    def _empty_as(self, x: torch.Tensor) -> torch.Tensor:
+        """rows of x's number and type, one behind another"""
+        return torch.empty_like(x) if _dense(x) else torch.empty(x.shape, dtype=x.dtype, device=self.device)
 
     def close(self):
         if self._h:
@@ -600,8 +606,7 @@ class RMSNorm(_Handle):
             if self.residual_dtype is None:
                 raise ValueError("residual: the object was made without one (residual_dtype)")
             rp, rs = self._rows_of("residual", residual, n, self.dim, self.residual_dtype)
-            given = summed
-            summed = self._empty(n, self.dim, dtype=self.residual_dtype) if given is None else given
+            summed = self._empty_as(residual) if summed is None else summed
             sp, ss = self._rows_of("summed", summed, n, self.dim, self.residual_dtype)
         elif summed is not None:
             raise ValueError("summed: there is no residual")
@@ -613,7 +618,7 @@ class RMSNorm(_Handle):
         """(out, summed, rstd): summed is the stored sum (x without a residual; `summed` may be `residual`), rstd fp32 [rows] what `backward` needs"""
         b, s = self._batch(x, weight, residual, summed)
         written = [t for t in (out, summed) if t is not None]
-        out = self._empty(b.rows, self.dim, dtype=self.dtype) if out is None else out
+        out = self._empty_as(x) if out is None else out
         rstd = self._empty(b.rows)
         self._check(_lib().tbe_norm_forward(self._h, C.byref(b), *self._rows_of("out", out, b.rows, self.dim, self.dtype), rstd.data_ptr(), self._stream()),
                     "tbe_norm_forward")
@@ -706,7 +711,7 @@ class ShortConv(_Handle):
         """(y, last); last is None without want_last"""
         b = self._batch(x, offsets, weight, bias, before)
         given = y
-        y = self._empty(b.rows, self.dim, dtype=self.dtype) if y is None else y
+        y = self._empty_as(x) if y is None else y
         last = self._empty(b.bags, self.width - 1, self.dim, dtype=self.dtype) if want_last else None
         self._check(_lib().tbe_conv_forward(self._h, C.byref(b), *self._rows_of("y", y, b.rows, self.dim, self.dtype),
                                             last.data_ptr() if want_last else None, self._stream()), "tbe_conv_forward")
@@ -734,7 +739,7 @@ class ShortConv(_Handle):
         n = x.shape[0]
         b = ConvBatch(*self._rows_of("x", x, n, self.dim, self.dtype), None, 0, n, *self._weights(weight, bias), None, DTYPES[weight.dtype])
         written = (state,) if y is None else (state, y)
-        y = self._empty(n, self.dim, dtype=self.dtype) if y is None else y
+        y = self._empty_as(x) if y is None else y
         sp = self._whole("state", state, self.dtype, (state.shape[0], self.width - 1, self.dim))
         self._check(_lib().tbe_conv_step(self._h, C.byref(b), sp, state.shape[0], self._slots(slots, n), *self._rows_of("y", y, n, self.dim, self.dtype),
                                          self._stream()), "tbe_conv_step")
@@ -800,7 +805,7 @@ class SelectiveScan(_Handle):
         """(y, last, saved): last fp32 [bags, dim, states] after the last rows (None without want_last), what `backward` needs"""
         t = self._batch(x, delta, a, b, c, skip, delta_bias, z, offsets, h0)
         given = y
-        y = self._empty(t.rows, self.dim, dtype=self.dtype) if y is None else y
+        y = self._empty_as(x) if y is None else y
         last = self._empty(t.bags, self.dim, self.states) if want_last else None
         saved = self._empty(self._check(_lib().tbe_ssm_saved_floats(self._h, t.rows), "tbe_ssm_saved_floats")) if save else None
         self._check(_lib().tbe_ssm_forward(self._h, C.byref(t), *self._rows_of("y", y, t.rows, self.dim, self.dtype), last.data_ptr() if want_last else None,
@@ -842,7 +847,7 @@ class SelectiveScan(_Handle):
         if count and not state[0].is_contiguous():
             raise ValueError("state: the states of a slot lie one behind another")
         written = (state,) if y is None else (state, y)
-        y = self._empty(n, self.dim, dtype=self.dtype) if y is None else y
+        y = self._empty_as(x) if y is None else y
         self._check(_lib().tbe_ssm_step(self._h, C.byref(t), sp, state.stride(0) if count > 1 else self.dim * self.states, count, self._slots(slots, n),
                                         *self._rows_of("y", y, n, self.dim, self.dtype), self._stream()), "tbe_ssm_step")
         _written(written)
