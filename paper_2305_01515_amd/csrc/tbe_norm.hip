@@ -6,7 +6,9 @@
 //   with d = dout w:  ds = rstd (d - s rstd mean(d s rstd)) + what comes from the next layers,  dw = sum over rows of dout s rstd.
 //
 // Bound by memory: each row is read once, into registers.  A row lies on lanes of V elements (16 bytes of x) a pack, P packs a lane:
-// a part of a wavefront or a whole one (ROW_THREADS 64), or a workgroup of ROW_THREADS lanes.
+// a part of a wavefront or a whole one (ROW_THREADS 64), or a workgroup of ROW_THREADS lanes.  245760 rows of 128 in bfloat16 with an fp32 residual:
+// forward 64 us (5.9 TB/s), backward 97 us (5.2 TB/s); 16384 rows of 4096 to 8 bits 95 us (5.0 TB/s; with 32 elements a lane instead of 16, half of
+// them beyond the row, 134 us of vector instructions).
 #include <algorithm>
 #include <new>
 #include <type_traits>

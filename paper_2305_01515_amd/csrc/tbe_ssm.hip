@@ -5,8 +5,8 @@
 //   Backward, with dv = dy silu(z):  g_t = c_t dv_t + exp(D_{t+1} a) g_{t+1} (a bag's last row: + dlast),  w_t = exp(D_t a) h_{t-1},
 //   dx = skip dv + D sum_n g b,  dD = sum_n g w a + x sum_n g b,  da = sum_t g w D,  db = sum over elements of g D x,  dc = sum of dv h.
 //
-// Bound by vector instructions: an element and a state take an exponential (as long as four others) and four more, 16 states 128 of them,
-// for 8 to 14 bytes of rows in 16 bits.  So the rows are gone through once where that can be, and no lane idles:
+// Bound by vector instructions: an element and a state take an exponential (two turns of the vector unit) and four more, 16 states 96 turns, for 8 to
+// 14 bytes of rows in 16 bits.  So the rows are gone through once where that can be, and no lane idles:
 //   units    The rows are cut every `unit` rows.  A bag of up to two units is not cut: the unit it starts in goes on to its end.
 //   ends     Units whose end cuts a bag find the state there from a zero one (or the bag's start), and the sum of the D: the
 //            product of the decays is the exponential of a times that                          (ssm_ends_kernel)
@@ -15,6 +15,8 @@
 // Where no bag is longer than two units, `ends` and `join` find nothing to do.
 // Forward: a lane has an element with all of its states in registers, b and c come from LDS.  Backward: a lane has four states of an
 // element, so that 8 rows' w and decays stay in registers on the way back; states before every 8th row were saved by the forward.
+// 245760 rows of 128 in bags of 30, bfloat16, 16 states, gated: forward 200 us (0.86 of it vector instructions), backward 880 us (0.6 of it); three bags of 100 k
+// rows of 64 in fp32: forward 125 us and 86 for the ends, backward 510 and 91, joins 34 + 17 us each way.
 #include <algorithm>
 #include <new>
 #include <type_traits>
