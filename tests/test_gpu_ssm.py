@@ -325,6 +325,9 @@ def test_what_is_refused():
         plan.forward(*args, offsets([3, 3, 3]).cuda())  # three bags
     with pytest.raises(ValueError):
         plan.backward(*args, off, torch.zeros(1, device="cuda"), t["dy"])
+    saved = plan.forward(*args, off, save=True)[2]
+    with pytest.raises(TbeError):  # not from a multiple of 16 bytes on
+        plan.backward(*args, off, torch.empty(saved.numel() + 1, device="cuda")[1:], t["dy"])
     plan.forward(*args, torch.tensor([0, 6, 4]).cuda())
     with pytest.raises(TbeError):
         plan.check()
@@ -340,3 +343,17 @@ def test_what_is_refused():
     assert (got[1] == 0).all() and (state[[0, 2]] == 0).all() and (state[1] != 0).any()
     with pytest.raises(TbeError):
         plan.step(state[:1], *(v[:2] if i != 2 else v for i, v in enumerate(args)))
+
+
+def test_what_is_not_wanted_is_not_found():
+    from paper_2305_01515_amd.dense import SelectiveScan
+    t = {k: v.cuda() for k, v in inputs(300, 3, 40, 16, 1, "bf16", 6).items()}
+    plan, off = SelectiveScan(40, 16, torch.bfloat16, 3, 300), offsets([200, 0, 100]).cuda()
+    args = [t[k] for k in ("x", "delta", "a", "b", "c")] + [off]
+    y, last, saved = plan.forward(*args, z=t["z"], save=True)
+    given = torch.full((300, 50), 5.0, dtype=torch.bfloat16, device="cuda")
+    y2, none, nothing = plan.forward(*args, z=t["z"], y=given[:, 3:43], want_last=False)
+    assert none is None and nothing is None and torch.equal(y, y2) and (given[:, :3] == 5).all() and (given[:, 43:] == 5).all()
+    with_zero = plan.backward(*args, saved, t["dy"], torch.zeros_like(last), z=t["z"])
+    for k, v in plan.backward(*args, saved, t["dy"], z=t["z"]).items():
+        assert torch.equal(v, with_zero[k])
