@@ -158,8 +158,8 @@ __device__ inline int lane_again() {
   return me;
 }
 
-// Elements at .. at + V - 1 of a row, those beyond its end being other ones of it.  All lanes go one way: where a branch parted them, 64 states of rows that
-// end within a wavefront came out wrong, with registers all in use (ROCm 7.2).
+// Elements at .. at + V - 1 of a row, those beyond its end being other ones of it.  All lanes go one way, and no v_readlane stands where lanes are masked off:
+// a register that has been kept elsewhere comes back in the active lanes only, and what is then read of another lane is something else.
 template <class E, int V>
 __device__ inline void load_pack_of(const E *row, int dim, int at, Words<E, V> &to) {
   if (dim % V == 0) {
@@ -833,9 +833,9 @@ __global__ __launch_bounds__(64 * WAVES, 2) void ssm_grad_kernel(SsmArgs a) {
         };
         if (from == 0 && to == S) walk(std::true_type{});
         else walk(std::false_type{});
-        if (rows.starts && args_again()->dh0 && in) {
-          float *p = args_again()->dh0 + ((int64_t)__builtin_amdgcn_readlane(bag_of.x, from) * args_again()->dim + d) * N + 4 * q;
-          store_floats<float, 4>(p, N - 4 * q, carry);
+        if (rows.starts && args_again()->dh0) {
+          const int64_t first_bag = __builtin_amdgcn_readlane(bag_of.x, from);  // by all lanes, as everywhere: the lane that knows may be beyond the row
+          if (in) store_floats<float, 4>(args_again()->dh0 + (first_bag * args_again()->dim + d) * N + 4 * q, N - 4 * q, carry);
         }
         to = from;
       }

@@ -179,6 +179,13 @@ def test_many_units_a_segment_and_wide_rows():
             assert (v - w).abs().max() <= 1000 * EPS * w.abs().max()
 
 
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("dim,states,leave", [(17, 16, ()), (65, 3, ("z",)), (129, 16, ()), (41, 64, ()), (70, 64, ("z",)), (130, 64, ()), (65, 32, ()), (129, 33, ("skip",)), (67, 50, ())])
+def test_rows_that_end_within_a_wavefront_of_the_backward(dim, states, leave, dtype):
+    """a wavefront there has 16, 8 or 4 elements: rows that leave one of them, or some, and whole wavefronts of a workgroup; bags that start in any row of 8, cut ones too"""
+    run_and_compare([1, 2, 3, 4, 5, 0, 6, 7, 70, 1, 300], dim, states, dtype=dtype, leave=leave, seed=dim + states)
+
+
 def test_groups_see_their_own():
     """groups = two scans beside each other"""
     from paper_2305_01515_amd.dense import SelectiveScan
