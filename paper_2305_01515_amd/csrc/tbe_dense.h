@@ -10,7 +10,9 @@ namespace tbe {
 // Error without a handle of the embedding path: the text is what tbe_last_error(NULL) returns (tbe_api.hip).
 int report(int code, const char *text) noexcept;
 
+// HIP keeps an error until it is read: the next call's look after its launch must not find it again.
 inline int report_hip(hipError_t e) noexcept {
+  (void)hipGetLastError();
   return report(e == hipErrorOutOfMemory ? TBE_ENOMEM : TBE_EHIP, hipGetErrorString(e));
 }
 

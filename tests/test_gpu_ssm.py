@@ -306,6 +306,18 @@ def test_gradients_through_autograd():
         (g ** 2).sum().backward()
 
 
+def test_a_failed_allocation_is_not_the_next_calls():
+    """a handle for 2^26 rows of 4096 with 64 states would take more than 4 TB; other operators go on"""
+    from paper_2305_01515_amd.dense import RMSNorm, SelectiveScan, ShortConv
+    from paper_2305_01515_amd.tbe import TbeError
+    conv, norm = ShortConv(8, 2, torch.float32, 1, 4), RMSNorm(8, torch.float32, 4)
+    x, w, off = torch.ones(4, 8, device="cuda"), torch.ones(8, 2, device="cuda"), offsets([4]).cuda()
+    for call in (lambda: conv.forward(x, off, w), lambda: norm.forward(x, w[:, 0].contiguous()), lambda: ShortConv(8, 2, torch.float32, 1, 4)):
+        with pytest.raises(TbeError, match="TBE_ENOMEM"):
+            SelectiveScan(4096, 64, torch.bfloat16, 1, 1 << 26)
+        call()
+
+
 def test_what_is_refused():
     from paper_2305_01515_amd.dense import SelectiveScan
     from paper_2305_01515_amd.tbe import TbeError
