@@ -238,14 +238,15 @@ template <class E, int W>
 __global__ __launch_bounds__(kThreads) void conv_grad_kernel(ConvArgs a, int64_t workers) {
   constexpr int V = kGradPack<E>, R = grad_rows(W), K = W + 1;  // sums of an element: W of dw, one of dbias
   extern __shared__ int marks[];                             // tile_rows + W - 1 of them, and then the sums of the walks
-  if ((int64_t)blockIdx.x >= workers * a.passes) {
-    const int64_t i = ((int64_t)blockIdx.x - workers * a.passes) * kThreads + threadIdx.x;
+  const int64_t group = a.first_group + blockIdx.x;
+  if (group >= workers * a.passes) {
+    const int64_t i = (group - workers * a.passes) * kThreads + threadIdx.x;
     if (W > 1 && a.dbefore) earlier_rows<E, W>(a, i);
     else look_over(a, i);
     return;
   }
   const int lane = threadIdx.x & (a.lanes - 1), walk = threadIdx.x / a.lanes, walks = kThreads / a.lanes, tile_rows = walks * R;
-  const int64_t worker = blockIdx.x / a.passes;
+  const int64_t worker = blockIdx.x / a.passes;  // (they are all in the first launch)
   const int at = ((int)(blockIdx.x % a.passes) * a.lanes + lane) * V, n = a.dim - at;
   float w[W][V], bias[V], dw[K][V];
   if (n > 0) load_weights<W, V>(a, at, w, bias);
@@ -443,9 +444,11 @@ template <class E, int W>
 int backward(ConvArgs a, float *dweight, float *dbias, hipStream_t st) {
   lanes_of(a, kGradPack<E>, grad_rows(W));
   const int64_t workers = workers_of(a), groups = workers * a.passes + tail_groups(a, W, 1);
-  if (groups > most_groups(kThreads)) return report(TBE_ELIMIT, "more bags than one launch can take");
   const size_t lds = std::max((size_t)(kThreads / a.lanes * grad_rows(W) + W - 1) * sizeof(int), (size_t)kThreads * kGradPack<E> * (W + 1) * sizeof(float));
-  conv_grad_kernel<E, W><<<dim3((unsigned)groups), kThreads, lds, st>>>(a, workers);
+  for (int64_t done = 0; done < groups; done += most_groups(kThreads)) {  // one launch, unless the earlier rows are of 2^32 elements
+    a.first_group = done;
+    conv_grad_kernel<E, W><<<dim3((unsigned)std::min(groups - done, most_groups(kThreads))), kThreads, lds, st>>>(a, workers);
+  }
   if (a.parts) sum_parts(a.parts, workers, (int64_t)a.dim * (W + 1), W + 1, W, dweight, dbias, nullptr, st);
   return check_launch();
 }

@@ -136,6 +136,29 @@ def test_step_goes_on_where_bags_end(dim, width, dtype):
     assert (store[untouched] == 3).all()
 
 
+def test_more_elements_of_earlier_rows_than_a_launch_has_lanes():
+    """2^32 of them and more: the gradient of an empty bag's earlier rows is that of its last ones, the others' what a call of these bags alone gives"""
+    from paper_2305_01515_amd.dense import ShortConv
+    bags, width, dim, rows = 9400, 8, 65536, 5
+    assert bags * (width - 1) * dim > 1 << 32
+    if torch.cuda.mem_get_info()[0] < 5 * bags * (width - 1) * dim * 2:
+        pytest.skip("takes 35 GB")
+    t = {k: v.cuda() for k, v in inputs(rows, 2, dim, width, "bf16", "f32", 21).items()}
+    before, dlast = (torch.zeros(bags, width - 1, dim, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    dlast += torch.arange(bags, device="cuda")[:, None, None] % 251
+    ends = torch.tensor([0, bags - 1], device="cuda")
+    before[ends], dlast[ends] = t["before"], t["dlast"]
+    few, many = ShortConv(dim, width, torch.bfloat16, 2, rows), ShortConv(dim, width, torch.bfloat16, bags, rows)
+    want = few.backward(t["x"], offsets([2, 3]).cuda(), t["weight"], t["dy"], t["bias"], t["before"], t["dlast"])
+    got = many.backward(t["x"], offsets([2] + [0] * (bags - 2) + [3]).cuda(), t["weight"], t["dy"], t["bias"], before, dlast)
+    many.check()
+    for v, w in zip(got[:3], want[:3]):
+        assert torch.equal(v, w)
+    assert torch.equal(got[3][ends], want[3])
+    for k in range(1, bags - 1, 1000):
+        assert torch.equal(got[3][k:min(k + 1000, bags - 1)], dlast[k:min(k + 1000, bags - 1)])
+
+
 def test_an_infinity_stays_in_its_bag():
     from paper_2305_01515_amd.dense import ShortConv
     t = {k: v.cuda() for k, v in inputs(60, 3, 8, 4, "f32", "f32", 3).items()}
