@@ -583,12 +583,11 @@ int tbe_conv_backward(tbe_conv_handle s, const tbe_conv_batch *b, const void *d_
   if (b->rows > 0 && (dy_stride < s->dim || dx_stride < s->dim)) return report(TBE_EINVAL, "a stride below dim");
   if (b->rows > 0 && (d_dx == b->d_x || d_dx == d_dy)) return report(TBE_EINVAL, "an output is one of the inputs");
   if (d_dbefore && (d_dbefore == b->d_before || d_dbefore == d_dlast)) return report(TBE_EINVAL, "an output is one of the inputs");
-  if (d_dbias && !d_dweight) return report(TBE_EINVAL, "the gradient of the bias comes with that of the weights");
-  if (b->bags == 0 && !d_dweight) return TBE_OK;
+  if (b->bags == 0 && !d_dweight && !d_dbias) return TBE_OK;
   ConvArgs a = args_of(s, b);
   a.dy = d_dy, a.dys = dy_stride, a.dx = d_dx, a.dxs = dx_stride;
   a.dlast = s->width > 1 ? d_dlast : nullptr, a.dbefore = s->width > 1 ? d_dbefore : nullptr;
-  a.parts = d_dweight ? s->parts : nullptr;
+  a.parts = d_dweight || d_dbias ? s->parts : nullptr;
   return of_handle(s, Backward{a, d_dweight, d_dbias, (hipStream_t)stream});
 }
 

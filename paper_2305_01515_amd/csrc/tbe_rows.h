@@ -128,9 +128,8 @@ __global__ __launch_bounds__(1024) static void sum_parts_kernel(const float *par
   if (s == 0 && at < n) {
     const int64_t r = at / width;
     const int k = (int)(at % width);
-    float *p = k < cut ? to + r * cut + k : k == cut ? next : other;
-    if (k >= cut && p) p += r;
-    if (p) *p = lds[0][c];
+    float *p = k < cut ? to : k == cut ? next : other;
+    if (p) p[k < cut ? r * cut + k : r] = lds[0][c];
   }
 }
 

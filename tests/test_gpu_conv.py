@@ -159,6 +159,29 @@ def test_more_elements_of_earlier_rows_than_a_launch_has_lanes():
         assert torch.equal(got[3][k:min(k + 1000, bags - 1)], dlast[k:min(k + 1000, bags - 1)])
 
 
+@pytest.mark.parametrize("lengths", [[17, 0, 40], []])
+def test_each_gradient_of_the_weights_alone(lengths):
+    """the C entry point takes null for either: the other one has the same bits as with it"""
+    import ctypes as C
+
+    from paper_2305_01515_amd import dense
+    rows, bags = sum(lengths), len(lengths)
+    t = {k: v.cuda() for k, v in inputs(rows, bags, 70, 4, "f32", "f32", 4).items()}
+    plan, off = dense.ShortConv(70, 4, torch.float32, bags, rows), offsets(lengths).cuda()
+    batch = plan._batch(t["x"], off, t["weight"], t["bias"], None)
+
+    def grads(weight, bias):
+        dx, dw, db = torch.empty_like(t["x"]), torch.full((70, 4), 7.0, device="cuda"), torch.full((70,), 7.0, device="cuda")
+        assert dense._lib().tbe_conv_backward(plan._h, C.byref(batch), t["dy"].data_ptr(), 70, None, dx.data_ptr(), 70, dw.data_ptr() if weight else None,
+                                              db.data_ptr() if bias else None, None, plan._stream()) == 0
+        return dx, dw, db
+    want = grads(True, True)
+    assert rows or not (want[1].any() or want[2].any())
+    for weight, bias in ((True, False), (False, True), (False, False)):
+        dx, dw, db = grads(weight, bias)
+        assert torch.equal(dx, want[0]) and torch.equal(dw, want[1] if weight else torch.full_like(dw, 7.0)) and torch.equal(db, want[2] if bias else torch.full_like(db, 7.0))
+
+
 def test_an_infinity_stays_in_its_bag():
     from paper_2305_01515_amd.dense import ShortConv
     t = {k: v.cuda() for k, v in inputs(60, 3, 8, 4, "f32", "f32", 3).items()}
