@@ -837,6 +837,8 @@ class SelectiveScan(_Handle):
         return g
 
     def __call__(self, x, delta, a, b, c, offsets, skip=None, delta_bias=None, z=None, h0=None):
+        if not torch.is_grad_enabled() or not any(t is not None and t.requires_grad for t in (x, delta, a, b, c, skip, delta_bias, z, h0)):
+            return self.forward(x, delta, a, b, c, offsets, skip, delta_bias, z, h0)[:2]  # nothing saved
         return _SsmFunction.apply(self, x, delta, a, b, c, offsets, skip, delta_bias, z, h0)
 
     def step(self, state, x, delta, a, b, c, skip=None, delta_bias=None, z=None, slots=None, y=None):

@@ -306,6 +306,33 @@ def test_gradients_through_autograd():
         (g ** 2).sum().backward()
 
 
+def test_states_are_saved_where_a_gradient_is_asked_for():
+    """called for its results alone (without gradients, or with inputs that want none) the object takes the memory of its results"""
+    from paper_2305_01515_amd.dense import SelectiveScan
+    rows, dim, states = 4096, 64, 64
+    t = {k: v.cuda() for k, v in inputs(rows, 2, dim, states, 1, "bf16", 12).items()}
+    off, plan = offsets([rows - 9, 9]).cuda(), SelectiveScan(dim, states, torch.bfloat16, 2, rows)
+    results = (rows * dim * 2 + 2 * dim * states * 4) + 4096
+    saved = rows // 8 * dim * states * 4
+
+    def call():
+        torch.cuda.synchronize()
+        torch.cuda.reset_peak_memory_stats()
+        before = torch.cuda.memory_allocated()
+        out = plan(*(t[k] for k in ("x", "delta", "a", "b", "c")), off, **{k: t[k] for k in ("skip", "delta_bias", "z", "h0")})
+        return torch.cuda.max_memory_allocated() - before, out
+    took, want = call()
+    assert took <= results
+    t["h0"].requires_grad_()
+    with torch.no_grad():
+        took, got = call()
+    assert took <= results and not got[0].requires_grad
+    took, got_grad = call()
+    assert took >= saved and got_grad[0].requires_grad
+    for v, w, u in zip(want, got, got_grad):
+        assert torch.equal(v, w) and torch.equal(v, u)
+
+
 def test_a_failed_allocation_is_not_the_next_calls():
     """a handle for 2^26 rows of 4096 with 64 states would take more than 4 TB; other operators go on"""
     from paper_2305_01515_amd.dense import RMSNorm, SelectiveScan, ShortConv
