@@ -510,7 +510,7 @@ int tbe_plan_placement(const tbe_place_table *tables, int32_t num_tables, const 
  * Gated linear recurrence over the rows of every bag.  With f = 1 / (1 + exp(-u)), element by element,
  *   h_t = f_t h_{t-1} + (1 - f_t) x_t   (coupled = 1)   or   h_t = f_t h_{t-1} + x_t   (coupled = 0)
  * for the rows t = offsets[b] .. offsets[b+1]-1 of bag b in turn, from h = d_h0[b] (null: zero).
- * f and 1 - f are off by up to (|u| + 8) 2^-24 of themselves.  Bits are the same from call to call, but for the last ones where a workgroup
+ * f and 1 - f are off by up to (1.25 |u| + 8) 2^-24 of themselves.  Bits are the same from call to call, but for the last ones where a workgroup
  * has heard nothing of another one for a millisecond or so (work of other streams in between) and finds a state by itself, in another order.
  * dim: elements of a row, 1 .. 65536; max_bags, max_rows: what a call may bring at most (scratch memory: 16 bytes
  * for each of max_rows and 28 * dim for each chunk of them, which has 8192 elements, or somewhat fewer where dim is no power of two).  A call
@@ -715,8 +715,9 @@ int tbe_conv_check(tbe_conv_handle s, void *stream);
  * dim / groups elements of a group.
  * dim: 1 .. 65536; states: 1 .. 64; groups: 1, or such that dim / groups is a multiple of 64; dtype: of x, delta, z, b, c, y and their gradients.
  * max_bags, max_rows: what a call may bring at most.  What a call writes may not overlap what it reads.
- * The decays are found as powers of two of D_t (a log2(e)), so they are off by up to (|D_t a| + 8) 2^-23 of themselves; a decay's product
- * over many rows is found from the sum of their D.  A decay below 2^-126 is zero.
+ * With u = delta + delta_bias rounded to fp32, D is off by up to (1.25 |u| + 8) 2^-24 of itself.  The decays are found as powers of two of D_t (a log2(e)), so
+ * they are off by up to (1.25 |D_t a| + 8) 2^-23 of exp(D_t a) of that D; a decay's product over many rows is found from the sum of their D.
+ * A decay below 2^-126 is zero.
  */
 typedef struct tbe_ssm_t *tbe_ssm_handle;
 int tbe_ssm_create(tbe_ssm_handle *out, int32_t dim, int32_t states, int32_t groups, int32_t dtype, int64_t max_bags, int64_t max_rows);

@@ -70,8 +70,8 @@ __device__ inline void join(float pa, float ph, float &a, float &h) {  // (pa, p
 __device__ inline float go(float a, float h, float s) { return signbit(a) ? h : a * s + h; }
 
 // The two gates f = 1 / (1 + exp(-u)) and 1 - f in one number: the smaller one, negative where that is 1 - f.  Each then keeps
-// its own bits (1 - f from a rounded f near one would not).  The exponential is the hardware's power of two of the rounded u log2(e), so a gate is
-// off by up to (|u| + 8) 2^-24 of itself: 5e-7 at |u| = 8, 2e-6 at 30, where the gate is below 1e-13.  Carrying the product's rounding on
+// its own bits (1 - f from a rounded f near one would not).  The exponential is the hardware's power of two of the rounded u log2(e), the constant
+// itself in 32 bits, so a gate is off by up to (1.25 |u| + 8) 2^-24 of itself: 1.1e-6 at |u| = 8, 2.7e-6 at 30, where the gate is below 1e-13.  Carrying the product's rounding on
 // would take 4 of some 32 (forward) and 83 (gradient) instructions an element more.
 __device__ inline float gate(float u) {
   const float e = __builtin_amdgcn_exp2f(fabsf(u) * -1.44269504f), s = e * __builtin_amdgcn_rcpf(1.0f + e);

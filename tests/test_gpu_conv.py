@@ -136,6 +136,17 @@ def test_step_goes_on_where_bags_end(dim, width, dtype):
     assert (store[untouched] == 3).all()
 
 
+def test_silu_over_its_range():
+    """What the header says of a sigmoid, to the end of its range: v log2(e) is rounded (|v| eps of the exponential), log2(e) in 32 bits is 0.224 eps of itself too small
+    (0.224 |v| eps); exponential, sum, quotient and product round to within some eps each.  So (1.25 |v| + 8) eps of the sigmoid and one of the product."""
+    from paper_2305_01515_amd.dense import ShortConv
+    v = torch.linspace(-86, 86, 1 << 22, dtype=torch.float64).float().view(-1, 64)
+    plan = ShortConv(64, 1, torch.float32, 1, len(v))
+    y, _ = plan.forward(v.cuda(), offsets([len(v)]).cuda(), torch.ones(64, 1, device="cuda"))
+    d = f64(v)
+    near("silu", y, d * sigmoid(d), (1.25 * np.abs(d) + 9) * EPS * np.abs(d * sigmoid(d)))
+
+
 def test_more_elements_of_earlier_rows_than_a_launch_has_lanes():
     """2^32 of them and more: the gradient of an empty bag's earlier rows is that of its last ones, the others' what a call of these bags alone gives"""
     from paper_2305_01515_amd.dense import ShortConv

@@ -160,6 +160,26 @@ def test_small_and_large_steps(step):
     run_and_compare([3000, 17, 200], 20, 16, seed=5, step=step)
 
 
+def test_steps_and_decays_over_their_range():
+    """What the header says of D and of the decays.  D = log(1 + exp(u)): u log2(e) is rounded, log2(e) in 32 bits is 0.224 eps of itself too small, together 1.224 |u| eps of
+    the exponential, and no more of D; the other steps round to within some eps each.  A decay's exponent is rounded twice: 2.224 |D a| eps of the decay."""
+    from paper_2305_01515_amd.dense import SelectiveScan
+    u = torch.cat([torch.linspace(-85, 85, 1 << 18, dtype=torch.float64), torch.linspace(-18, -14, 1 << 16, dtype=torch.float64)]).float().view(-1, 64)
+    rows = len(u)
+    plan, off, ones = SelectiveScan(64, 1, torch.float32, rows, rows), torch.arange(rows + 1, device="cuda"), torch.ones(rows, 64, device="cuda")
+    one, two = torch.ones(rows, 1, device="cuda"), torch.tensor([0, 1], device="cuda")
+    _, last, _ = plan.forward(ones, u.cuda(), -ones[:1].view(64, 1), one, one, off)  # a row's state from zero with b = x = 1 is D
+    d = f64(u)
+    near("D", last.view(rows, 64), np.logaddexp(0, d), (1.25 * np.abs(d) + 8) * EPS * np.logaddexp(0, d))
+    a = -torch.linspace(1e-3, 86, 1 << 16, dtype=torch.float64).float().view(1024, 64)
+    step = [SelectiveScan(1024, n, torch.float32, 1, 1) for n in (1, 64)]
+    x, delta, h0 = torch.zeros(1, 1024, device="cuda"), torch.full((1, 1024), 0.5413, device="cuda"), torch.ones(1, 1024, 64, device="cuda")
+    _, D, _ = step[0].forward(x + 1, delta, a[:, :1].contiguous().cuda(), one[:1], one[:1], two)
+    _, last, _ = step[1].forward(x, delta, a.cuda(), x[:, :64].contiguous(), x[:, :64].contiguous(), two, h0=h0)
+    p = f64(D).reshape(1024, 1) * f64(a)
+    near("decay", last[0], np.exp(p), (1.25 * np.abs(p) + 8) * 2 * EPS * np.exp(p))
+
+
 def test_many_units_a_segment_and_wide_rows():
     """units of 64 rows (many elements) and of 128: the same numbers as rows of fewer elements have, which units of 32 rows go through"""
     from paper_2305_01515_amd.dense import SelectiveScan
