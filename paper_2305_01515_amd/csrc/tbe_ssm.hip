@@ -1092,8 +1092,9 @@ int tbe_ssm_create(tbe_ssm_handle *out, int32_t dim, int32_t states, int32_t gro
     return report(TBE_ELIMIT, "more than 2^38 elements or states of bags, or 2^31 bags");
   const int np = padded(states);
   const int64_t units = most_units(max_rows, dim), segments = divide_up(units, kSegment), waves = divide_up(dim, 64);
-  if (units * waves > most_groups(64) || segments * divide_up((int64_t)dim * np, kThreads) > most_groups(kThreads))
-    return report(TBE_ELIMIT, "more rows than one launch can take");
+  if (units * waves > most_groups(64) || segments * divide_up((int64_t)dim * np, kThreads) > most_groups(kThreads) ||
+      divide_up(max_bags, kThreads) + divide_up(units + 1, kThreads / 64) > most_groups(kThreads))
+    return report(TBE_ELIMIT, "more rows or bags than one launch can take");
   tbe_ssm_t *s = new (std::nothrow) tbe_ssm_t;
   if (!s) return report(TBE_ENOMEM, "no memory for the handle");
   s->dim = dim, s->states = states, s->groups = groups, s->dtype = dtype, s->np = np, s->max_bags = max_bags, s->max_rows = max_rows;

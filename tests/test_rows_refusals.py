@@ -49,3 +49,10 @@ def test_ssm():
     assert l.tbe_ssm_backward(None, C.byref(b), None, C.byref(g), None) == -1
     assert l.tbe_ssm_step(None, C.byref(b), None, 8, 1, None, None, 8, None) == -1
     assert b"null handle" in l.tbe_last_error(None)
+
+
+def test_ssm_grids():
+    """rows and bags whose units and offsets would take a launch of 2^32 lanes"""
+    l, h = lib(), C.c_void_p()
+    for dim, bags, rows in ((1, 1, 67108863 * 128), (1, 1 << 30, 60 * (1 << 20) * 128), (64, (1 << 31) - 2, 1 << 32)):
+        assert l.tbe_ssm_create(C.byref(h), dim, 1, 1, 0, bags, rows) == -5 and not h
