@@ -644,7 +644,9 @@ int tbe_adamw_step_counted(tbe_adamw_handle s, const void *const *h_grads, int64
  * Root-mean-square norm of rows, with the addition of a residual in front of it.  s = x + residual, rounded to the residual's type and stored
  * (without a residual s = x, and nothing is stored);  out = s rstd weight,  rstd = 1 / sqrt(mean(s s) + eps), of the stored s.
  * dim: 1 .. 32768.  dtype: of x and out; residual_dtype: dtype or TBE_FP32, -1 for a handle that has none.  max_rows: rows of a call
- * at most.  d_summed may be d_residual, or d_x where they have one type, with the same strides; d_out may be neither of the inputs.
+ * at most.  d_summed may be d_residual, or d_x where they have one type, with the same strides; apart from
+ * that what a call of tbe_norm_*, tbe_conv_* or tbe_ssm_* writes may not overlap what it reads.  Such calls are refused (TBE_EINVAL), but for rows of two
+ * different strides both wider than a row, of which it is not found out.
  */
 typedef struct tbe_norm_t *tbe_norm_handle;
 int tbe_norm_create(tbe_norm_handle *out, int32_t dim, int32_t dtype, int32_t residual_dtype, double eps, int64_t max_rows);
@@ -681,7 +683,7 @@ int tbe_norm_backward(tbe_norm_handle s, const tbe_norm_grad *gradients, void *s
  * and behind them its rows,
  *   v_t = bias + sum over j < width of weight[j] e_{t+j},   y_t = v_t, or v_t / (1 + exp(-v_t)) with silu.
  * dim: 1 .. 65536; width: 1 .. 8; dtype: of rows, earlier rows and results; weights (d_weight [dim, width], d_bias [dim] or null) are of
- * weight_dtype.  max_bags, max_rows: what a call may bring at most.  What a call writes may not overlap what it reads.
+ * weight_dtype.  max_bags, max_rows: what a call may bring at most.
  */
 typedef struct tbe_conv_t *tbe_conv_handle;
 int tbe_conv_create(tbe_conv_handle *out, int32_t dim, int32_t width, int32_t dtype, int32_t silu, int64_t max_bags, int64_t max_rows);
@@ -702,7 +704,8 @@ int tbe_conv_forward(tbe_conv_handle s, const tbe_conv_batch *batch, void *d_y, 
 int tbe_conv_backward(tbe_conv_handle s, const tbe_conv_batch *batch, const void *d_dy, int64_t dy_stride, const void *d_dlast, void *d_dx,
                       int64_t dx_stride, float *d_dweight, float *d_dbias, void *d_dbefore, void *stream);
 /* One more row for `rows` of the `slots` states d_state [slots, width - 1, dim] of dtype, in place.  d_slots null: row i belongs to state i.
- * A negative slot leaves its row out (y = 0).  A slot twice in one call: undefined.  Of the batch: d_x, x_stride, rows, the weights. */
+ * A negative slot leaves its row out (y = 0).  A slot twice in one call: undefined.  d_y may be d_x with the same stride.  Of the batch: d_x, x_stride,
+ * rows, the weights. */
 int tbe_conv_step(tbe_conv_handle s, const tbe_conv_batch *batch, void *d_state, int64_t slots, const int64_t *d_slots, void *d_y,
                   int64_t y_stride, void *stream);
 /* as tbe_scan_check */
@@ -714,7 +717,7 @@ int tbe_conv_check(tbe_conv_handle s, void *stream);
  * times z_t / (1 + exp(-z_t)) where d_z is given; h = d_h0[bag] (null: zero) before a bag's first row.  b_t and c_t are a row's own and shared by the
  * dim / groups elements of a group.
  * dim: 1 .. 65536; states: 1 .. 64; groups: 1, or such that dim / groups is a multiple of 64; dtype: of x, delta, z, b, c, y and their gradients.
- * max_bags, max_rows: what a call may bring at most.  What a call writes may not overlap what it reads.
+ * max_bags, max_rows: what a call may bring at most.
  * With u = delta + delta_bias rounded to fp32, D is off by up to (1.25 |u| + 8) 2^-24 of itself.  The decays are found as powers of two of D_t (a log2(e)), so
  * they are off by up to (1.25 |D_t a| + 8) 2^-23 of exp(D_t a) of that D; a decay's product over many rows is found from the sum of their D.
  * A decay below 2^-126 is zero.
@@ -748,7 +751,7 @@ typedef struct {
 } tbe_ssm_grads;
 int tbe_ssm_backward(tbe_ssm_handle s, const tbe_ssm_batch *batch, const float *d_saved, const tbe_ssm_grads *gradients, void *stream);
 /* One more row for `rows` of the `slots` states d_state (fp32 [dim, states] each, state_stride apart), in place; slots as in tbe_conv_step.
- * Of the batch: everything but offsets, bags and h0. */
+ * d_y may be d_x, d_delta or d_z with the same stride.  Of the batch: everything but offsets, bags and h0. */
 int tbe_ssm_step(tbe_ssm_handle s, const tbe_ssm_batch *batch, float *d_state, int64_t state_stride, int64_t slots, const int64_t *d_slots, void *d_y,
                  int64_t y_stride, void *stream);
 /* as tbe_scan_check */

@@ -514,6 +514,18 @@ int check_batch(tbe_conv_handle s, const tbe_conv_batch *b, bool bags) {
   if (b->rows > 0 && b->x_stride < s->dim) return report(TBE_EINVAL, "a stride below dim");
   return TBE_OK;
 }
+// what a batch's bags share, or have beside their rows
+struct Shared {
+  Span weight, bias, before, offsets;
+  int64_t bag_bytes;
+  Shared(tbe_conv_handle s, const tbe_conv_batch *b, bool with_bags = true) {
+    const int each = elem_bytes(b->weight_dtype);
+    bag_bytes = (with_bags ? b->bags : 0) * (s->width - 1) * s->dim * elem_bytes(s->dtype);
+    weight = span(b->d_weight, (int64_t)s->dim * s->width * each), bias = span(b->d_bias, (int64_t)s->dim * each);
+    before = of_bags(b->d_before), offsets = with_bags ? span(b->d_offsets, (b->bags + 1) * 8) : Span{};
+  }
+  Span of_bags(const void *p) const { return span(p, bag_bytes); }
+};
 ConvArgs args_of(tbe_conv_handle s, const tbe_conv_batch *b) {
   ConvArgs a{};
   a.x = b->d_x, a.xs = b->x_stride, a.weight = b->d_weight, a.bias = b->d_bias, a.weight_dtype = b->weight_dtype;
@@ -568,8 +580,9 @@ int tbe_conv_forward(tbe_conv_handle s, const tbe_conv_batch *b, void *d_y, int6
   if (int rc = check_batch(s, b, true)) return rc;
   if (b->rows > 0 && !d_y) return report(TBE_EINVAL, "null results");
   if (b->rows > 0 && y_stride < s->dim) return report(TBE_EINVAL, "a stride below dim");
-  if (b->rows > 0 && d_y == b->d_x) return report(TBE_EINVAL, "the output is one of the inputs");
-  if (d_last && d_last == b->d_before) return report(TBE_EINVAL, "the output is one of the inputs");
+  const Span x = span(b->d_x, s->dim, b->x_stride, b->rows, elem_bytes(s->dtype)), y = span(d_y, s->dim, y_stride, b->rows, elem_bytes(s->dtype));
+  const Shared shared(s, b);
+  if (int rc = check_apart({y, shared.of_bags(d_last)}, {x, shared.before, shared.weight, shared.bias, shared.offsets})) return rc;
   if (b->bags == 0) return TBE_OK;
   ConvArgs a = args_of(s, b);
   a.y = d_y, a.ys = y_stride, a.last = d_last;
@@ -581,8 +594,12 @@ int tbe_conv_backward(tbe_conv_handle s, const tbe_conv_batch *b, const void *d_
   if (int rc = check_batch(s, b, true)) return rc;
   if (b->rows > 0 && (!d_dy || !d_dx)) return report(TBE_EINVAL, "null gradients");
   if (b->rows > 0 && (dy_stride < s->dim || dx_stride < s->dim)) return report(TBE_EINVAL, "a stride below dim");
-  if (b->rows > 0 && (d_dx == b->d_x || d_dx == d_dy)) return report(TBE_EINVAL, "an output is one of the inputs");
-  if (d_dbefore && (d_dbefore == b->d_before || d_dbefore == d_dlast)) return report(TBE_EINVAL, "an output is one of the inputs");
+  const int bytes = elem_bytes(s->dtype);
+  const Shared shared(s, b);
+  if (int rc = check_apart({span(d_dx, s->dim, dx_stride, b->rows, bytes), shared.of_bags(d_dbefore), span(d_dweight, (int64_t)s->dim * s->width * 4), span(d_dbias, (int64_t)s->dim * 4)},
+                           {span(b->d_x, s->dim, b->x_stride, b->rows, bytes), span(d_dy, s->dim, dy_stride, b->rows, bytes), shared.of_bags(d_dlast), shared.before,
+                            shared.weight, shared.bias, shared.offsets}))
+    return rc;
   if (b->bags == 0 && !d_dweight && !d_dbias) return TBE_OK;
   ConvArgs a = args_of(s, b);
   a.dy = d_dy, a.dys = dy_stride, a.dx = d_dx, a.dxs = dx_stride;
@@ -600,6 +617,14 @@ int tbe_conv_step(tbe_conv_handle s, const tbe_conv_batch *b, void *d_state, int
   if (s->width > 1 && !d_state) return report(TBE_EINVAL, "null states");
   if (!d_slots && b->rows > slots) return report(TBE_EINVAL, "more rows than states");
   if (d_y && y_stride < s->dim) return report(TBE_EINVAL, "a stride below dim");
+  const int bytes = elem_bytes(s->dtype);
+  const Span x = span(b->d_x, s->dim, b->x_stride, b->rows, bytes), y = span(d_y, s->dim, y_stride, b->rows, bytes);
+  const Span state = span(d_state, slots * (s->width - 1) * s->dim * bytes), of_rows = span(d_slots, b->rows * 8);
+  const Shared shared(s, b, false);
+  if (int rc = check_apart({y, state}, {shared.weight, shared.bias, of_rows})) return rc;
+  if (int rc = check_apart({state}, {x, y})) return rc;
+  if (!same_span(x, y))  // (a lane reads a row's elements before it writes them)
+    if (int rc = check_apart({y}, {x})) return rc;
   ConvArgs a = args_of(s, b);
   a.y = d_y, a.ys = y_stride;
   return of_handle(s, Step{a, d_state, slots, d_slots, (hipStream_t)stream});

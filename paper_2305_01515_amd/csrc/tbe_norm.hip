@@ -419,10 +419,15 @@ int forward(tbe_norm_handle s, const tbe_norm_batch *b, void *out, int64_t os, f
   if (!b->d_x || !b->d_weight || !out || (residual && !b->d_summed) || (bits8 && !scales)) return report(TBE_EINVAL, "null rows, weights or results");
   if (b->x_stride < s->dim || os < s->dim || (residual && (b->residual_stride < s->dim || b->summed_stride < s->dim)))
     return report(TBE_EINVAL, "a stride below dim");
-  if (out == b->d_x || (residual && (out == b->d_residual || out == b->d_summed))) return report(TBE_EINVAL, "the result is one of the inputs, or the sum");
   if (residual && ((b->d_summed == b->d_residual && b->summed_stride != b->residual_stride) ||
                    (b->d_summed == b->d_x && (b->summed_stride != b->x_stride || s->dtype != s->residual_dtype))))
     return report(TBE_EINVAL, "a sum in place of an input has its type and strides");
+  const int bytes = elem_bytes(s->dtype), res_bytes = residual ? elem_bytes(s->residual_dtype) : 0;
+  const int64_t groups = group && group < s->dim ? divide_up(s->dim, group) : 1;
+  const Span x = span(b->d_x, s->dim, b->x_stride, b->rows, bytes), res = span(residual ? b->d_residual : nullptr, s->dim, b->residual_stride, b->rows, res_bytes);
+  const Span sum = span(residual ? b->d_summed : nullptr, s->dim, b->summed_stride, b->rows, res_bytes), weight = span(b->d_weight, (int64_t)s->dim * elem_bytes(b->weight_dtype));
+  if (int rc = check_apart({span(out, s->dim, os, b->rows, bits8 ? 1 : bytes), span(rstd, b->rows * 4), span(scales, b->rows * groups * 4)}, {x, res, sum, weight})) return rc;
+  if (int rc = check_apart({sum}, {same_span(sum, x) ? Span{} : x, same_span(sum, res) ? Span{} : res, weight})) return rc;
   NormArgs a{};
   a.x = b->d_x, a.residual = b->d_residual, a.weight = b->d_weight;
   a.xs = b->x_stride, a.rs = b->residual_stride, a.rows = b->rows;
@@ -492,8 +497,11 @@ int tbe_norm_backward(tbe_norm_handle s, const tbe_norm_grad *g, void *stream) {
   if (g->rows > 0 && (g->summed_stride < s->dim || g->dout_stride < s->dim || (g->d_dsummed && g->dsummed_stride < s->dim) ||
                       (g->d_dx && g->dx_stride < s->dim) || (g->d_dresidual && g->dresidual_stride < s->dim)))
     return report(TBE_EINVAL, "a stride below dim");
-  for (const void *in : {g->d_summed, g->d_dout, g->d_dsummed})
-    if (g->rows > 0 && in && (in == g->d_dx || in == g->d_dresidual)) return report(TBE_EINVAL, "an output is one of the inputs");
+  const int bytes = elem_bytes(s->dtype), sum_bytes = residual ? elem_bytes(s->residual_dtype) : bytes;
+  if (int rc = check_apart({span(g->d_dx, s->dim, g->dx_stride, g->rows, bytes), span(g->d_dresidual, s->dim, g->dresidual_stride, g->rows, sum_bytes), span(g->d_dweight, (int64_t)s->dim * 4)},
+                           {span(g->d_summed, s->dim, g->summed_stride, g->rows, sum_bytes), span(g->d_dout, s->dim, g->dout_stride, g->rows, bytes),
+                            span(g->d_dsummed, s->dim, g->dsummed_stride, g->rows, sum_bytes), span(g->d_weight, (int64_t)s->dim * elem_bytes(g->weight_dtype)), span(g->d_rstd, g->rows * 4)}))
+    return rc;
   NormGrad a{};
   a.s = g->d_summed, a.dout = g->d_dout, a.ds = g->d_dsummed, a.weight = g->d_weight;
   a.ss = g->summed_stride, a.dos = g->dout_stride, a.dss = g->dsummed_stride, a.rows = g->rows;

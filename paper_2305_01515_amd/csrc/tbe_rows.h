@@ -1,9 +1,49 @@
 // Shared by the operators on rows (norm, short convolution, selective scan): packs at any address, parameters of any type, small
 // functions, sums of partial results.
 #pragma once
+#include <algorithm>
+#include <initializer_list>
+
 #include "tbe_dense.h"
 
 namespace tbe {
+
+// Memory of a call: `rows` pieces of `row` bytes, `stride` apart (0: all the same one)
+struct Span {
+  const void *p;
+  int64_t row, stride, rows;
+};
+inline Span span(const void *p, int64_t bytes) { return {p, bytes, bytes, 1}; }
+inline Span span(const void *p, int64_t elems, int64_t stride, int64_t rows, int bytes) { return {p, elems * bytes, stride * bytes, rows}; }
+inline bool same_span(const Span &a, const Span &b) { return a.p == b.p && a.row == b.row && (a.stride == b.stride || (a.rows <= 1 && b.rows <= 1)) && a.rows == b.rows; }
+
+// Whether two have a byte in common.  Of rows that lie apart by two different strides it is not found out: columns of one piece of memory may be meant.
+inline bool overlap(Span a, Span b) {
+  for (Span *s : {&a, &b}) {
+    if (!s->p || s->row <= 0 || s->rows <= 0) return false;
+    if (s->rows > 1 && s->stride == s->row) s->row *= s->rows, s->rows = 1;
+    if (s->rows == 1 || s->stride == 0) s->stride = s->row, s->rows = 1;
+  }
+  const int64_t at = (int64_t)((uintptr_t)b.p - (uintptr_t)a.p);  // of b from a's first byte
+  if (at >= (a.rows - 1) * a.stride + a.row || at + (b.rows - 1) * b.stride + b.row <= 0) return false;
+  if (b.rows == 1) {
+    // the first row of a that ends behind b's first byte
+    const int64_t i = at < a.row ? 0 : (at - a.row) / a.stride + 1;
+    return i < a.rows && i * a.stride < at + b.row;
+  }
+  if (a.rows == 1) return overlap(b, a);
+  if (a.stride != b.stride) return false;
+  int64_t k = at / a.stride, rest = at % a.stride;  // b's first row begins `rest` bytes behind where a's row k does
+  if (rest < 0) --k, rest += a.stride;
+  auto meet = [&](int64_t k) { return k < a.rows && k + b.rows > 0; };  // some row j of b and row j + k of a are both there
+  return (rest < a.row && meet(k)) || (rest + b.row > a.stride && meet(k + 1));
+}
+inline int check_apart(std::initializer_list<Span> written, std::initializer_list<Span> read) {
+  for (const Span &w : written)
+    for (const Span &r : read)
+      if (overlap(w, r)) return report(TBE_EINVAL, "what the call writes overlaps what it reads");
+  return TBE_OK;
+}
 
 // V elements (the first `n` of them, if fewer) at any address that an element may have, as fp32; what is beyond n reads as zero
 template <class E, int V>

@@ -1063,6 +1063,23 @@ int check_batch(tbe_ssm_handle s, const tbe_ssm_batch *b, bool bags) {
   if (bags && b->d_h0 && b->h0_stride != 0 && b->h0_stride < (int64_t)s->dim * s->states) return report(TBE_EINVAL, "a stride below the states of a bag");
   return TBE_OK;
 }
+// where a batch's inputs lie
+struct Inputs {
+  int64_t dim, states, rows, bags;
+  int bytes;
+  Span x, delta, z, b, c, a, skip, bias, offsets, h0;
+  Inputs(tbe_ssm_handle s, const tbe_ssm_batch *t, bool with_bags = true)
+      : dim(s->dim), states(s->states), rows(t->rows), bags(with_bags ? t->bags : 0), bytes(elem_bytes(s->dtype)) {
+    const int64_t k = states * s->groups;
+    x = rows_of(t->d_x, t->x_stride), delta = rows_of(t->d_delta, t->delta_stride), z = rows_of(t->d_z, t->z_stride);
+    b = span(t->d_b, k, t->b_stride, rows, bytes), c = span(t->d_c, k, t->c_stride, rows, bytes);
+    a = span(t->d_a, dim * states * 4), skip = span(t->d_skip, dim * 4), bias = span(t->d_delta_bias, dim * 4);
+    offsets = with_bags ? span(t->d_offsets, (bags + 1) * 8) : Span{}, h0 = span(t->d_h0, dim * states, t->h0_stride, bags, 4);
+  }
+  Span rows_of(const void *p, int64_t stride) const { return span(p, dim, stride, rows, bytes); }
+  Span of_bags(const void *p) const { return span(p, bags * dim * states * 4); }
+  int apart(std::initializer_list<Span> written) const { return check_apart(written, {x, delta, z, b, c, a, skip, bias, offsets, h0}); }
+};
 SsmArgs args_of(tbe_ssm_handle s, const tbe_ssm_batch *b) {
   SsmArgs a = s->scratch;
   a.x = b->d_x, a.delta = b->d_delta, a.z = b->d_z, a.b = b->d_b, a.c = b->d_c;
@@ -1145,10 +1162,9 @@ int tbe_ssm_forward(tbe_ssm_handle s, const tbe_ssm_batch *b, void *d_y, int64_t
   if (int rc = check_batch(s, b, true)) return rc;
   if (b->rows > 0 && !d_y) return report(TBE_EINVAL, "null results");
   if (b->rows > 0 && y_stride < s->dim) return report(TBE_EINVAL, "a stride below the length of a row");
-  for (const void *in : {b->d_x, b->d_delta, b->d_z, b->d_b, b->d_c})
-    if (b->rows > 0 && in && d_y == in) return report(TBE_EINVAL, "the output is one of the inputs");
-  if (d_last && d_last == b->d_h0) return report(TBE_EINVAL, "the output is one of the inputs");
   if ((uintptr_t)d_saved & 15) return report(TBE_EINVAL, "what is saved begins at no multiple of 16 bytes");
+  const Inputs in(s, b);
+  if (int rc = in.apart({in.rows_of(d_y, y_stride), in.of_bags(d_last), span(d_saved, tbe_ssm_saved_floats(s, b->rows) * 4)})) return rc;
   if (b->bags == 0) return TBE_OK;
   SsmArgs a = args_of(s, b);
   a.y = d_y, a.ys = y_stride, a.last = d_last, a.saved = d_saved;
@@ -1162,10 +1178,12 @@ int tbe_ssm_backward(tbe_ssm_handle s, const tbe_ssm_batch *b, const float *d_sa
     return report(TBE_EINVAL, "null pointer for what the forward saved or for a gradient");
   if ((uintptr_t)d_saved & 15) return report(TBE_EINVAL, "what is saved begins at no multiple of 16 bytes");
   if (b->rows > 0 && g->dy_stride < s->dim) return report(TBE_EINVAL, "a stride below the length of a row");
-  for (const void *in : {b->d_x, b->d_delta, b->d_z, b->d_b, b->d_c, g->d_dy})
-    for (const void *out : {(const void *)g->d_dx, (const void *)g->d_ddelta, (const void *)(b->d_z ? g->d_dz : nullptr), (const void *)g->d_db, (const void *)g->d_dc})
-      if (b->rows > 0 && in && in == out) return report(TBE_EINVAL, "an output is one of the inputs");
-  if (g->d_dh0 && (g->d_dh0 == b->d_h0 || g->d_dh0 == g->d_dlast)) return report(TBE_EINVAL, "an output is one of the inputs");
+  const Inputs in(s, b);
+  const int64_t shared = b->rows * s->groups * s->states * elem_bytes(s->dtype), each = (int64_t)s->dim * 4;
+  const std::initializer_list<Span> written = {in.rows_of(g->d_dx, s->dim), in.rows_of(g->d_ddelta, s->dim), in.rows_of(b->d_z ? g->d_dz : nullptr, s->dim), span(g->d_db, shared),
+                                               span(g->d_dc, shared), span(g->d_da, each * s->states), span(g->d_dskip, each), span(g->d_ddelta_bias, each), in.of_bags(g->d_dh0)};
+  if (int rc = in.apart(written)) return rc;
+  if (int rc = check_apart(written, {in.rows_of(g->d_dy, g->dy_stride), in.of_bags(g->d_dlast), span(d_saved, tbe_ssm_saved_floats(s, b->rows) * 4)})) return rc;
   SsmArgs a = args_of(s, b);
   a.saved = const_cast<float *>(d_saved), a.dy = g->d_dy, a.dys = g->dy_stride, a.dlast = g->d_dlast;
   a.dx = g->d_dx, a.ddelta = g->d_ddelta, a.dz = g->d_dz, a.db = g->d_db, a.dc = g->d_dc, a.dh0 = g->d_dh0;
@@ -1181,6 +1199,14 @@ int tbe_ssm_step(tbe_ssm_handle s, const tbe_ssm_batch *b, float *d_state, int64
   if (!d_state) return report(TBE_EINVAL, "null states");
   if (!d_slots && b->rows > slots) return report(TBE_EINVAL, "more rows than states");
   if (state_stride < (int64_t)s->dim * s->states || (d_y && y_stride < s->dim)) return report(TBE_EINVAL, "a stride below the length of a row or of a state");
+  Inputs in(s, b, false);
+  const Span y = in.rows_of(d_y, y_stride), state = span(d_state, (int64_t)s->dim * s->states, state_stride, slots, 4), of_rows = span(d_slots, b->rows * 8);
+  if (int rc = in.apart({state})) return rc;
+  if (int rc = check_apart({state, y}, {of_rows})) return rc;
+  if (int rc = check_apart({state}, {y})) return rc;
+  for (Span *r : {&in.x, &in.delta, &in.z})  // (an element's lanes read it before one of them writes there)
+    if (same_span(*r, y)) *r = Span{};
+  if (int rc = in.apart({y})) return rc;
   SsmArgs a = args_of(s, b);
   a.y = d_y, a.ys = y_stride;
   return of_handle(s, Step{a, d_state, state_stride, slots, d_slots, (hipStream_t)stream});

@@ -11,7 +11,7 @@ Argument marshalling only: every step runs in the HIP kernels of the library.  A
 this object's last call or its constructor if that was on another one (an object's calls share its scratch memory; replays of a captured graph
 are the caller's to order; graphs need the objects whose calls they hold).  No call waits for the GPU, apart from `check` and a
 step of `AdamW` that makes its plan anew, which no capture can hold.
-What a call writes into a tensor that it was given counts for autograd as changed in place.
+What a call writes into a tensor that it was given counts for autograd as changed in place.  It may not overlap what the call reads, but for what is said to be in place.
 """
 from __future__ import annotations
 
