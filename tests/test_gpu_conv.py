@@ -136,6 +136,14 @@ def test_step_goes_on_where_bags_end(dim, width, dtype):
     assert (store[untouched] == 3).all()
 
 
+@pytest.mark.parametrize("dim,width,dtype", [(4096, 4, "f32"), (4096, 8, "f32"), (1024, 4, "bf16"), (8190, 3, "f16")])
+def test_more_tiles_than_workgroups_of_the_backward(dim, width, dtype):
+    """each walks a second tile, with the marks and the sums of the first one behind it"""
+    rows = {1024: 9000, 4096: 1300, 8190: 1400}[dim]
+    lengths = [rows - 320, 0, 1, 2, 7, 9, 300, 1]
+    run_and_compare(lengths, dim, width, dtype, seed=dim + width)
+
+
 def test_silu_over_its_range():
     """What the header says of a sigmoid, to the end of its range: v log2(e) is rounded (|v| eps of the exponential), log2(e) in 32 bits is 0.224 eps of itself too small
     (0.224 |v| eps); exponential, sum, quotient and product round to within some eps each.  So (1.25 |v| + 8) eps of the sigmoid and one of the product."""

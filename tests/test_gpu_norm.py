@@ -69,6 +69,14 @@ def test_sizes(rows, dim, layout, dtype, residual, weights):
     run_and_compare(rows, dim, dtype, residual, weights, layout, seed=dim)
 
 
+@pytest.mark.parametrize("dtype,residual,weights", [KINDS[1], KINDS[2], KINDS[7]])
+@pytest.mark.parametrize("rows,dim", [(12000, 130), (9000, 200), (2500, 1001), (2500, 3000), (2300, 8000), (2100, 8200)])
+def test_more_rows_than_workgroups_of_the_backward(rows, dim, dtype, residual, weights):
+    """each has a second group of rows, whose part of the weights' gradient is added to the first one's, in registers or (8200 elements) in memory; without it the
+    gradient of a weight would be off by the root of the rows left out, several times the bar"""
+    run_and_compare(rows, dim, dtype, residual, weights, seed=rows)
+
+
 def test_no_rows():
     from paper_2305_01515_amd.dense import RMSNorm
     plan, w = RMSNorm(64, torch.bfloat16, 8, residual_dtype=torch.float32), torch.ones(64, device="cuda")

@@ -160,6 +160,11 @@ def test_small_and_large_steps(step):
     run_and_compare([3000, 17, 200], 20, 16, seed=5, step=step)
 
 
+def test_more_segments_than_are_read_at_once():
+    """33500 rows are 1047 units in 17 segments, in both directions; with steps of 1e-4 the first segment's states are still there in the last one"""
+    run_and_compare([33500, 0, 700], 3, 4, seed=8, step=-10.0)
+
+
 def test_steps_and_decays_over_their_range():
     """What the header says of D and of the decays.  D = log(1 + exp(u)): u log2(e) is rounded, log2(e) in 32 bits is 0.224 eps of itself too small, together 1.224 |u| eps of
     the exponential, and no more of D; the other steps round to within some eps each.  A decay's exponent is rounded twice: 2.224 |D a| eps of the decay."""
