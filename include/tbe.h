@@ -643,6 +643,7 @@ int tbe_adamw_step_counted(tbe_adamw_handle s, const void *const *h_grads, int64
 /*
  * Root-mean-square norm of rows, with the addition of a residual in front of it.  s = x + residual, rounded to the residual's type and stored
  * (without a residual s = x, and nothing is stored);  out = s rstd weight,  rstd = 1 / sqrt(mean(s s) + eps), of the stored s.
+ * Squares are summed in fp32: a row of finite numbers whose sum is 2^128 or more has rstd 0 and comes out as zeros, as do its gradients.
  * dim: 1 .. 32768.  dtype: of x and out; residual_dtype: dtype or TBE_FP32, -1 for a handle that has none.  max_rows: rows of a call
  * at most.  d_summed may be d_residual, or d_x where they have one type, with the same strides; apart from
  * that what a call of tbe_norm_*, tbe_conv_* or tbe_ssm_* writes may not overlap what it reads.  Such calls are refused (TBE_EINVAL), but for rows of two

@@ -148,6 +148,20 @@ def test_small_results_in_8_bits():
     assert (codes.float() == 0).all() and (scales == 0).all()
 
 
+def test_squares_beyond_32_bits():
+    """sums of squares up to 2^128 are found; a row beyond that is zeros, and so are its gradients, apart from what comes to the stored sum"""
+    from paper_2305_01515_amd.dense import RMSNorm
+    plan, w = RMSNorm(64, torch.float32, 3, residual_dtype=torch.float32), torch.full((64,), 2.0, device="cuda")
+    x = torch.tensor([2.0 ** 60, 2.0 ** 61, 1.0]).view(3, 1).expand(3, 64).contiguous().cuda()  # 64 squares: 2^126, 2^128, 64
+    zero = torch.zeros_like(x)
+    out, summed, rstd = plan.forward(x, w, zero)
+    assert torch.equal(summed, x) and (out[[0, 2]] - 2).abs().max() <= 1e-6 and not out[1].any() and rstd[1] == 0
+    codes, scales, _ = plan.quantise(x, w, zero)
+    assert not codes[1].float().any() and scales[1] == 0 and (codes[[0, 2]].float() * scales[[0, 2]] - 2).abs().max() <= 1e-6
+    dx, _, dw = plan.backward(zero + 3, summed, rstd, w, zero + 5)
+    assert (dx[1] == 5).all() and torch.isfinite(dx).all() and torch.isfinite(dw).all()
+
+
 def test_sum_in_place_of_its_inputs():
     from paper_2305_01515_amd.dense import RMSNorm
     for dtype, residual in (("f32", "f32"), ("bf16", "bf16"), ("bf16", "f32")):
