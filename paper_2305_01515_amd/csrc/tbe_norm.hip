@@ -66,23 +66,28 @@ __device__ inline uint32_t row_max(uint32_t v, int lanes, uint32_t *lds) {
 }
 
 // Codes of V numbers whose group has the largest magnitude `top`, as 448ths of it.  Where the scale is zero (`zero`), so are the codes.  A
-// group with an infinity or a NaN has such a scale and reads back as NaN: its finite numbers' codes are zero, and zero times that is NaN.
+// group with an infinity or a NaN has such a scale, and codes of NaN.  A code is the even one of two where 448 v / top lies half way between them, which
+// happens: rows and weights of 16 bits have few products (2 in 10000 codes of bfloat16).  So the quotient is found to its last bit: what is left of 448 v behind
+// the first quotient times top is found exactly, and divided once more.
 template <int V>
 __device__ inline void store_codes(uint8_t *p, int n, const float (&v)[V], float top, bool zero) {
   uint32_t w[V / 4];
-  auto codes = [&](float up, float f) {
+  auto codes = [&](float up) {
+    const float t = top * up, r = t > 0.0f ? 1.0f / t : 0.0f, f = 448.0f * r;
+    auto quotient = [&](float v) {
+      const float x = v * up, q = x * f, p = q * t;
+      return __builtin_fmaf(__builtin_fmaf(x, 448.0f, -p) - __builtin_fmaf(q, t, -p), r, q);
+    };
 #pragma unroll
     for (int i = 0; i < V; i += 4) {
-      int c = __builtin_amdgcn_cvt_pk_fp8_f32(v[i] * up * f, v[i + 1] * up * f, 0, false);
-      c = __builtin_amdgcn_cvt_pk_fp8_f32(v[i + 2] * up * f, v[i + 3] * up * f, c, true);
+      int c = __builtin_amdgcn_cvt_pk_fp8_f32(quotient(v[i]), quotient(v[i + 1]), 0, false);
+      c = __builtin_amdgcn_cvt_pk_fp8_f32(quotient(v[i + 2]), quotient(v[i + 3]), c, true);
       w[i / 4] = (uint32_t)c;
     }
   };
-  if (top < 0x1p-100f) {  // 448 over a very small number would be infinite
-    codes(0x1p100f, top > 0.0f ? 448.0f / (top * 0x1p100f) : 0.0f);
-  } else {
-    codes(1.0f, 448.0f / top);
-  }
+  // (one over a very small number would be infinite, 448 of a very large one too)
+  if (top < 0x1p-100f || top > 0x1p100f) codes(top < 1.0f ? 0x1p100f : 0x1p-100f);
+  else codes(1.0f);
   if (zero) {
 #pragma unroll
     for (int i = 0; i < V / 4; ++i) w[i] = 0;

@@ -148,6 +148,26 @@ def test_small_results_in_8_bits():
     assert (codes.float() == 0).all() and (scales == 0).all()
 
 
+@pytest.mark.parametrize("dtype,dim,group,power", [(*case, power) for case in (("bf16", 4096, 0), ("bf16", 1000, 32)) for power in (0, -110, 110)] +
+                         [("f16", 4096, 0, 0), ("f16", 256, 64, 0)])
+def test_codes_half_way_are_even(dtype, dim, group, power):
+    """Rows and weights of 16 bits: their products s w, and 448 s w over the largest one, are exact in 64 bits or far enough from half way between two codes (22 bits by 22, so
+    2^-27 of it) that rounding to 53 bits says which side: every code is the nearest, the even one of two.  Weights times 2^power: results near both ends of fp32 (bfloat16)."""
+    from paper_2305_01515_amd.dense import RMSNorm
+    t = inputs(500, dim, dtype, None, dtype, dim + group)
+    t["weight"] = t["weight"] * 2.0 ** power
+    plan = RMSNorm(dim, TYPES[dtype][0], 500)
+    codes, scales, _ = plan.quantise(t["x"].cuda(), t["weight"].cuda(), group=group)
+    v = np.zeros((500, -(-dim // (group or dim)) * (group or dim)))
+    v[:, :dim] = f64(t["x"]) * f64(t["weight"])
+    v = v.reshape(500, -1, group or dim)
+    q = 448 * v / np.abs(v).max(2, keepdims=True)
+    step = 2.0 ** (np.maximum(np.floor(np.log2(np.maximum(np.abs(q), 1e-30))), -6) - 3)
+    assert (np.rint(q / step) != np.floor(q / step + 0.5)).any() or dtype == "f16"  # some do lie half way, below an even code
+    want = (np.rint(q / step) * step).reshape(500, -1)[:, :dim]
+    assert np.array_equal(f64(codes.float()), want)
+
+
 def test_squares_beyond_32_bits():
     """sums of squares up to 2^128 are found; a row beyond that is zeros, and so are its gradients, apart from what comes to the stored sum"""
     from paper_2305_01515_amd.dense import RMSNorm
