@@ -718,7 +718,9 @@ int tbe_conv_check(tbe_conv_handle s, void *stream);
  * times z_t / (1 + exp(-z_t)) where d_z is given; h = d_h0[bag] (null: zero) before a bag's first row.  b_t and c_t are a row's own and shared by the
  * dim / groups elements of a group.
  * dim: 1 .. 65536; states: 1 .. 64; groups: 1, or such that dim / groups is a multiple of 64; dtype: of x, delta, z, b, c, y and their gradients.
- * max_bags, max_rows: what a call may bring at most.
+ * max_bags, max_rows: what a call may bring at most.  (Scratch memory: 8 bytes for each of max_rows, 4 dim (states padded to 16, 32 or 64, and 2) for each unit
+ * of 32 to 128 of them; and where a group's elements take more than one workgroup of the backward, which has up to 128, 64 or 32 elements, 8 * states for each
+ * of these workgroups and each of max_rows.)
  * With u = delta + delta_bias rounded to fp32, D is off by up to (1.25 |u| + 8) 2^-24 of itself.  The decays are found as powers of two of D_t (a log2(e)), so
  * they are off by up to (1.25 |D_t a| + 8) 2^-23 of exp(D_t a) of that D; a decay's product over many rows is found from the sum of their D.
  * A decay below 2^-126 is zero.

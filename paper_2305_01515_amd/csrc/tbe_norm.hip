@@ -7,8 +7,9 @@
 //
 // Bound by memory: each row is read once, into registers.  A row lies on lanes of V elements (16 bytes of x) a pack, P packs a lane:
 // a part of a wavefront or a whole one (ROW_THREADS 64), or a workgroup of ROW_THREADS lanes.  245760 rows of 128 in bfloat16 with an fp32 residual:
-// forward 64 us (5.9 TB/s), backward 97 us (5.2 TB/s); 16384 rows of 4096 to 8 bits 95 us (5.0 TB/s; with 32 elements a lane instead of 16, half of
-// them beyond the row, 134 us of vector instructions).
+// forward 64 us (5.9 TB/s, more than a copy of 1 GB, 5.2: rows of this size stay in the last-level cache in part), backward 97 us (5.2 TB/s); 16384 rows of 4096 to 8 bits 95 us (5.0 TB/s; with 32 elements a lane instead of 16, half of
+// them beyond the row, 134 us of vector instructions).  The backward of long rows has few wavefronts a SIMD (two for 8192 elements), and beyond that reads its inputs
+// twice: 8192 rows of 8192 in bfloat16 147 us (2.7 TB/s), 4096 of 16384 210 (1.9), in fp32 163 (4.9) and 286 (2.8).
 #include <algorithm>
 #include <new>
 #include <type_traits>
